@@ -205,7 +205,10 @@ enum {
   RO_K_ASM_COPY = 8, RO_K_RETRY_CLAIM = 9, RO_K_RETRY_SCATTER = 10, RO_K_PB_KEYS = 11,
   RO_K_PB_HIST = 12, RO_K_PB_ROWSCAN = 13, RO_K_PB_SORT = 14, RO_K_PB_BOUNDS = 15,
   RO_K_PB_HEADS = 16, RO_K_PB_MARK = 17, RO_K_PB_SCAN = 18, RO_K_PB_EMIT = 19,
-  RO_K_COMMIT_FIX = 20, RO_K_READY_FUSED = 21, RO_K_COUNT = 22
+  RO_K_COMMIT_FIX = 20, RO_K_READY_FUSED = 21,
+  /* rayorch_cache.h */
+  RO_K_ROTARY = 22, RO_K_ATTEND_ROWS = 23, RO_K_ATTEND_TILES = 24, RO_K_WEIGH = 25,
+  RO_K_WEIGH_TILES = 26, RO_K_EVICT_SELECT = 27, RO_K_EVICT_MOVE = 28, RO_K_COUNT = 29
 };
 /* Tracing (no counterpart in the paper; it instruments the path).  Every
  * kernel launch is counted; kernels whose bit (1 << RO_K_*) is set in

@@ -1,4 +1,4 @@
-"""Thin ctypes binding of the C ABI in include/rayorch_gpu.h.
+"""Thin ctypes binding of the C ABI in include/rayorch_gpu.h and rayorch_cache.h.
 
 Function names and argument order follow the C entry points.  Pointer
 arguments accept a torch tensor (its data_ptr), a raw integer address or
@@ -26,19 +26,23 @@ RO_GROUP_FAILURE = 5
 # report verdicts (Eq. 3)
 RO_ACCEPT, RO_REJ_INVALID, RO_REJ_NOT_INFLIGHT, RO_REJ_STALE_GEN, RO_REJ_DUPLICATE, RO_REJ_BARRIER = range(6)
 
+# element types of the model-step operators
+RO_BF16, RO_F16, RO_F32 = range(3)
+
 STATUS_NAMES = {0: "RO_OK", 1: "RO_E_INVAL", 2: "RO_E_CAPACITY", 3: "RO_E_OVERFLOW",
                 4: "RO_E_STATE", 5: "RO_E_OOM", 6: "RO_E_CUDA", 7: "RO_E_TIMEOUT"}
 
 EXPORTS = ("ro_ctx_create", "ro_ctx_destroy", "ro_ctx_reset", "ro_ctx_sync", "ro_ctx_stats",
            "ro_ctx_set_streams", "ro_ctx_set_call_streams", "ro_ctx_join", "ro_ctx_selftest_timeout", "ro_last_error", "ro_ctx_profile", "ro_ctx_profile_read", "ro_expand", "ro_batch_ready",
            "ro_batch_ready_calls", "ro_retry", "ro_batch_ready_parent", "ro_gather_commit", "ro_assemble", "ro_assemble_list", "ro_filter_reports",
-           "ro_expand_noalloc")
+           "ro_expand_noalloc", "ro_rotary", "ro_cache_append", "ro_cache_attend", "ro_cache_weigh", "ro_cache_evict")
 
 # kernel ids (RO_K_*), in launch order of the path
 KERNELS = ("expand_scan", "expand_fill", "ready_count", "ready_scatter", "commit_scatter",
            "commit_plan", "asm_parents", "asm_members", "asm_copy", "retry_claim", "retry_scatter",
            "pb_keys", "pb_hist", "pb_rowscan", "pb_sort", "pb_bounds", "pb_heads", "pb_mark",
-           "pb_scan", "pb_emit", "commit_fix", "ready_fused")
+           "pb_scan", "pb_emit", "commit_fix", "ready_fused", "rotary", "attend_rows", "attend_tiles",
+           "weigh", "weigh_tiles", "evict_select", "evict_move")
 
 
 class RoError(RuntimeError):
@@ -52,6 +56,36 @@ class _Stats(C.Structure):
         "accepted", "rej_invalid", "rej_not_inflight", "rej_stale_gen", "rej_duplicate",
         "ready_bad_candidates", "assemble_incomplete", "rej_barrier", "barrier_not_dispatched",
         "barrier_in_flight", "queue_dropped", "retried", "retry_skipped")]
+
+
+class ro_rope(C.Structure):
+    """Rotary positions: the pairs each axis turns, the base, how pairs lie (see the header)."""
+    _fields_ = [("n_axes", C.c_uint32), ("pairs", C.c_uint32 * 4), ("interleaved", C.c_uint32), ("base", C.c_double)]
+
+    def __init__(self, pairs, base: float = 10_000.0, interleaved: bool = False):
+        if not 1 <= len(pairs) <= 4:
+            raise ValueError("ro_rope: 1 to 4 axes")
+        super().__init__(len(pairs), (C.c_uint32 * 4)(*pairs), int(interleaved), float(base))
+
+
+class ro_cache(C.Structure):
+    """A paged cache: pools d_k, d_v [pages, heads, slots, head_dim] (alike in
+    shape and strides), page lists d_page_base (64-bit, one more than there are
+    sequences) and d_pages (32-bit).  Keeps the tensors alive."""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("n_pages", C.c_uint32),
+                ("page_size", C.c_uint32), ("n_heads", C.c_uint32), ("head_dim", C.c_uint32), ("n_seqs", C.c_uint32),
+                ("page_stride", C.c_uint64), ("head_stride", C.c_uint64), ("slot_stride", C.c_uint64),
+                ("d_page_base", C.c_void_p), ("d_pages", C.c_void_p)]
+
+    def __init__(self, d_k, d_v, d_page_base, d_pages):
+        if d_k.dim() != 4 or d_k.shape != d_v.shape or d_k.stride() != d_v.stride() or d_k.dtype != d_v.dtype:
+            raise ValueError("ro_cache: k and v must be alike, [pages, heads, slots, head_dim]")
+        if d_k.stride(3) != 1:
+            raise ValueError("ro_cache: the last dimension must be contiguous")
+        n_pages, heads, slots, dim = d_k.shape
+        super().__init__(_ptr(d_k), _ptr(d_v), _dtype(d_k), n_pages, slots, heads, dim, d_page_base.numel() - 1,
+                         d_k.stride(0), d_k.stride(1), d_k.stride(2), _list(d_page_base, 8), _list(d_pages, 4))
+        self._tensors = (d_k, d_v, d_page_base, d_pages)
 
 
 _lib = None
@@ -101,6 +135,14 @@ def load(path: Optional[str] = None):
     L.ro_batch_ready_parent.argtypes = [_vp, _i32, C.c_uint32, _vp, _u64, C.c_uint32, _i32, _vp,
                                         _u64, _vp, _u64, _vp, _vp, _pu64, _pu64]
     L.ro_expand_noalloc.argtypes = [_vp, _u64, _vp, _vp, _vp, _u64, _vp, _vp, _pu64, _pu64]
+    rope, cache, f32 = C.POINTER(ro_rope), C.POINTER(ro_cache), C.c_float
+    rows = [_vp, _u64, _u64, _u32]   # a [tokens, heads, head_dim] tensor: pointer, strides, heads
+    L.ro_rotary.argtypes = [_vp, _i32, _vp, _u64, _u64, _vp, _u64, _u64, _u64, _u32, _u32, _vp, rope, _i32]
+    L.ro_cache_append.argtypes = [_vp, cache, _vp, _vp, _u64, _vp, _vp, rope] + rows + [_vp, _u64, _u64] * 3
+    L.ro_cache_attend.argtypes = [_vp, cache, _vp, _u64, _u32, _vp, _u32] + rows + [f32, _u32, _u32, _vp, _u64, _u64,
+                                                                                 _vp]
+    L.ro_cache_weigh.argtypes = [_vp, cache, _vp, _u64, _u32, _vp] + rows + [f32, _u32, _u32, _vp, f32, _vp, _vp, _u64]
+    L.ro_cache_evict.argtypes = [_vp, cache, _vp, _vp, _u64, _u32, _u32, _u32, _vp, _vp, _vp, _vp, _vp]
     for f in EXPORTS:
         if f != "ro_last_error":
             getattr(L, f).restype = C.c_int32
@@ -119,6 +161,30 @@ def _ptr(x):
     if not getattr(x, "is_cuda", True) and not x.is_pinned():
         raise ValueError("argument is a pageable CPU tensor (pin it or move it to the GPU)")
     return data_ptr()
+
+
+def _dtype(x) -> int:
+    name = str(x.dtype)
+    try:
+        return {"torch.bfloat16": RO_BF16, "torch.float16": RO_F16, "torch.float32": RO_F32}[name]
+    except KeyError:
+        raise ValueError(f"{name} is not a type of the model-step operators") from None
+
+
+def _list(x, size):
+    """A dense integer or float array of elements of `size` bytes."""
+    if x is not None and not isinstance(x, int) and (x.element_size() != size or not x.is_contiguous()):
+        raise ValueError(f"argument must be contiguous, {size} bytes an element")
+    return _ptr(x)
+
+
+def _rows(x, like=None):
+    """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
+    if x.dim() != 3 or x.stride(2) != 1:
+        raise ValueError("argument must be [tokens, heads, head_dim], contiguous in the last dimension")
+    if like is not None and (x.dtype != like.dtype or x.shape[2] != like.shape[-1]):
+        raise ValueError("argument differs from the cache in type or head_dim")
+    return _ptr(x), x.stride(0), x.stride(1)
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -322,3 +388,65 @@ def ro_expand_noalloc(d_counts, n_parents, d_offsets, d_child_parent, d_child_or
                                   _ptr(d_child_ordinal), child_cap, _ptr(d_empty_parents),
                                   _stream_handle(stream), C.byref(n), C.byref(ne))
     return st, n.value, ne.value
+
+
+# ---- model-step operators (rayorch_cache.h) -----------------------------------
+# Tensors stand for their pointer and strides ([tokens, heads, head_dim]), the
+# cache and the rotary for their structs; the order of the rest is the C order.
+def ro_rotary(ctx, d_x, d_out, d_pos, rope, inverse: bool = False) -> int:
+    """Turn d_x by its positions into d_out (which may be d_x)."""
+    if d_x.shape != d_out.shape or d_x.dtype != d_out.dtype or d_pos.numel() != d_x.shape[0] * rope.n_axes:
+        raise ValueError("ro_rotary: x, out and positions do not fit one another")
+    return load().ro_rotary(ctx, _dtype(d_x), *_rows(d_x), *_rows(d_out), *d_x.shape, _list(d_pos, 4), C.byref(rope),
+                            int(inverse))
+
+
+def ro_cache_append(ctx, cache, d_tok_base, d_tok_seq, d_len, d_pos, rope, d_q, d_q_out, d_k, d_v) -> int:
+    """Put a step's tokens into the cache, k and q turned (rope None: as they
+    are; d_q None: keys and values alone)."""
+    pool = cache._tensors[0]
+    n = d_k.shape[0]
+    if d_k.shape != d_v.shape or d_k.shape[1] != cache.n_heads or (d_q is not None and (
+            d_q.shape != d_q_out.shape or d_q.shape[0] != n)) or (rope is not None and d_pos.numel() != n * rope.n_axes) \
+            or d_tok_seq.numel() < n:
+        raise ValueError("ro_cache_append: tensors do not fit one another")
+    q = _rows(d_q, pool) + (d_q.shape[1],) + _rows(d_q_out, pool) if d_q is not None else (None, 0, 0, 0, None, 0, 0)
+    return load().ro_cache_append(ctx, C.byref(cache), _list(d_tok_base, 8), _list(d_tok_seq, 4), n, _list(d_len, 4),
+                                  _list(d_pos, 4), None if rope is None else C.byref(rope), *q, *_rows(d_k, pool),
+                                  *_rows(d_v, pool))
+
+
+def ro_cache_attend(ctx, cache, d_tok_base, max_new, d_len, max_len, d_q, scale, window, sinks, d_out,
+                    d_lse=None) -> int:
+    """Attention of a step's tokens over the cache that holds them."""
+    pool = cache._tensors[0]
+    if d_out.shape != d_q.shape or (d_lse is not None and d_lse.shape != d_q.shape[:2]):
+        raise ValueError("ro_cache_attend: q, out and lse do not fit one another")
+    return load().ro_cache_attend(ctx, C.byref(cache), _list(d_tok_base, 8), d_q.shape[0], max_new, _list(d_len, 4),
+                                  max_len, *_rows(d_q, pool), d_q.shape[1], scale, window, sinks,
+                                  *_rows(d_out, pool), _list(d_lse, 4))
+
+
+def ro_cache_weigh(ctx, cache, d_tok_base, max_new, d_len, d_q, scale, window, sinks, d_lse, decay, d_past,
+                   d_score) -> int:
+    """Attention weight per cached token, d_score [sequences, heads, slots] from
+    d_past (None: nothing yet; may be d_score)."""
+    if d_lse.shape != d_q.shape[:2] or d_score.shape[:2] != (cache.n_seqs, cache.n_heads) or (
+            d_past is not None and d_past.shape != d_score.shape):
+        raise ValueError("ro_cache_weigh: q, lse and scores do not fit one another")
+    return load().ro_cache_weigh(ctx, C.byref(cache), _list(d_tok_base, 8), d_q.shape[0], max_new, _list(d_len, 4),
+                                 *_rows(d_q, cache._tensors[0]), d_q.shape[1], scale, window, sinks, _list(d_lse, 4),
+                                 decay, _list(d_past, 4), _list(d_score, 4), d_score.shape[2])
+
+
+def ro_cache_evict(ctx, cache, d_len, d_score, budget, sinks, recent, d_dst_base, d_dst_pages, d_keep, d_len_out,
+                   d_score_out=None) -> int:
+    """Cut every sequence back to its `budget` heaviest tokens, in new pages;
+    d_keep [sequences, heads, budget]."""
+    units = (cache.n_seqs, cache.n_heads)
+    if d_score.shape[:2] != units or d_keep.shape != units + (budget,) or d_dst_base.numel() != cache.n_seqs + 1 or (
+            d_score_out is not None and d_score_out.shape != d_score.shape):
+        raise ValueError("ro_cache_evict: scores, kept slots or page lists do not fit the cache")
+    return load().ro_cache_evict(ctx, C.byref(cache), _list(d_len, 4), _list(d_score, 4), d_score.shape[2], budget,
+                                 sinks, recent, _list(d_dst_base, 8), _list(d_dst_pages, 4), _list(d_keep, 4),
+                                 _list(d_len_out, 4), _list(d_score_out, 4))

@@ -37,7 +37,7 @@ def _sources():
 
 def _deps():
     return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) \
-        + [os.path.join(ROOT, "include", "rayorch_gpu.h")]
+        + glob.glob(os.path.join(ROOT, "include", "*.h"))
 
 
 def _compile(src: str, extra) -> str:

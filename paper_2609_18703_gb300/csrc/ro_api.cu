@@ -19,6 +19,7 @@
 
 #include "../../include/rayorch_gpu.h"
 #include "ro_internal.h"
+#include "ro_step.h"
 
 namespace ro {
 cudaError_t prepare_assemble_kernels();
@@ -184,6 +185,7 @@ struct ro_ctx {
   TsBuf ts[N_TS];
   DevBuf code;
   DevBuf selftest;                      // ro_ctx_selftest_timeout scratch
+  DevBuf step[SS_COUNT];                // model-step workspaces (ro_step.h)
   DevBuf x_mb, x_coff, x_mtfp, x_hdr;   // explicit-list assembly scratch
   // parent-bound reservation scratch (see ParentArgs)
   DevBuf pb_key[2], pb_val[2], pb_child, pb_hist, pb_dtot, pb_first, pb_endp, pb_hsz, pb_left,
@@ -599,7 +601,7 @@ ro_status ro_ctx_create(ro_ctx** out, int32_t device, void* stream, uint32_t n_c
   c->call_join.resize(n_calls);
   c->call_pending.assign(n_calls, 0);
   c->ts_call.resize(n_calls);
-  if (prepare_assemble_kernels() != cudaSuccess) {
+  if (prepare_assemble_kernels() != cudaSuccess || prepare_attend_kernels() != cudaSuccess) {
     cudaGetLastError();
     free_scalars(c);
     delete c;
@@ -673,6 +675,7 @@ ro_status ro_ctx_destroy(ro_ctx* c) {
   for (auto& t : c->ts) {
     free_buf(t.flag); free_buf(t.agg); free_buf(t.inc);
   }
+  for (DevBuf& b : c->step) free_buf(b);
   free_buf(c->code); free_buf(c->selftest); free_buf(c->x_mb); free_buf(c->x_coff); free_buf(c->x_mtfp); free_buf(c->x_hdr);
   for (DevBuf* b : {&c->pb_key[0], &c->pb_key[1], &c->pb_val[0], &c->pb_val[1], &c->pb_child,
                     &c->pb_hist, &c->pb_dtot, &c->pb_first, &c->pb_endp, &c->pb_hsz, &c->pb_left,
@@ -1581,3 +1584,36 @@ ro_status assemble_impl(ro_ctx* c, int32_t xid, const uint8_t* d_arena, uint64_t
   return RO_OK;
 }
 }  // namespace
+
+// ---- model-step calls (ro_step.h) ---------------------------------------------------
+namespace ro {
+StepCall::StepCall(ro_ctx* c) : status(enter(c)), c_(c) {
+  if (status != RO_OK) return;
+  int cur = -1;
+  if (cudaGetDevice(&cur) == cudaSuccess && cur != c->device) {
+    prev_ = cur;
+    cudaSetDevice(c->device);
+  }
+}
+StepCall::~StepCall() {
+  if (prev_ >= 0) cudaSetDevice(prev_);
+}
+ro_status StepCall::begin() { return settle_calls(c_); }
+ro_status StepCall::refuse(ro_status st, const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(c_, st, "%s", buf);
+}
+ro_status StepCall::launched(const char* what) { return check_launch(c_, what); }
+ro_status StepCall::scratch(int which, size_t bytes, void** p) {
+  const ro_status st = ensure(c_, c_->step[which], bytes, "a model-step workspace");
+  *p = c_->step[which].p;
+  return st;
+}
+const LaunchCfg& StepCall::launch() const { return c_->L; }
+uint32_t* StepCall::err() const { return &c_->ds->err; }
+int StepCall::sms() const { return c_->num_sms; }
+}  // namespace ro

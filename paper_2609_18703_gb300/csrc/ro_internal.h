@@ -51,7 +51,8 @@ constexpr uint64_t AC_SMALL_CHUNKS = 256;
 enum KernelId { K_EXPAND_SCAN, K_FILL, K_RB_COUNT, K_RB_SCATTER, K_COMMIT, K_CPLAN, K_APARENTS,
                 K_AMEMBERS, K_ACOPY, K_RT_CLAIM, K_RT_SCATTER, K_PB_KEYS, K_PB_HIST,
                 K_PB_ROWSCAN, K_PB_SORT, K_PB_BOUNDS, K_PB_HEADS, K_PB_MARK, K_PB_SCAN, K_PB_EMIT,
-                K_CFIX, K_RB_FUSED, K_COUNT,
+                K_CFIX, K_RB_FUSED, K_ROTARY, K_ATTEND_ROWS, K_ATTEND_TILES, K_WEIGH, K_WEIGH_TILES,
+                K_EVICT_SELECT, K_EVICT_MOVE, K_COUNT,
                 K_RB_FUSED_CALLS = 100 };   // occupancy query only (profiled as K_RB_FUSED)
 
 
@@ -77,11 +78,11 @@ struct LaunchCfg {
 // stream drains, and waits (griddepcontrol.wait, first statement of every
 // kernel here) until the predecessor has finished and its writes are visible.
 template <typename Arg>
-inline void launch_k(const LaunchCfg& L, int kid, void (*kern)(Arg), int grid, int block,
+inline void launch_k(const LaunchCfg& L, int kid, void (*kern)(Arg), dim3 grid, int block,
                      size_t smem, const Arg& a) {
   prof_begin(L.prof, L.stream, kid);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = L.stream;

@@ -1,0 +1,178 @@
+// ro_step.cuh — device helpers shared by the model-step kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ro_step.h"
+
+namespace ro {
+
+constexpr float LN2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ uint32_t step_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void record(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
+
+// 16 bytes to shared memory, zeros instead when !ok (src is then not read)
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+
+// c += a (16 x 16) * b (16 x 8), 32-bit accumulation
+template <typename T>
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                                     uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ float to_f32(T x) { return (float)x; }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+// One sequence's rows and pages, read once per CTA.
+struct SeqInfo {
+  uint64_t tok0;             // first of its new tokens
+  uint32_t n;                // new tokens
+  uint32_t len;              // cached tokens, at most what its pages hold
+  uint64_t page0;            // first entry of its page list
+  int64_t first;             // slot of its first new token (negative: before the cache)
+  bool ok;
+};
+// Checks what the GPU alone can see; a sequence that fails is left out (ok false).
+__device__ __forceinline__ SeqInfo seq_info(const PagedArgs& c, const RowsArgs& r, uint32_t s, uint32_t* err) {
+  SeqInfo q;
+  const uint64_t t0 = r.tok_base[s], t1 = r.tok_base[s + 1], p0 = c.page_base[s], p1 = c.page_base[s + 1];
+  const uint32_t len = r.len[s];
+  q.tok0 = t0;
+  q.n = (uint32_t)(t1 - t0);
+  q.len = len;
+  q.page0 = p0;
+  q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && len < 0x80000000u;
+  if (!q.ok) {
+    if (threadIdx.x == 0) record(err, ERR_INVAL);
+    q.n = 0;
+    q.len = 0;
+  } else if ((uint64_t)len > (p1 - p0) * c.page_size) {
+    if (threadIdx.x == 0) record(err, ERR_CAPACITY);
+    q.len = (uint32_t)((p1 - p0) * c.page_size);
+  }
+  q.first = (int64_t)len - (int64_t)q.n;
+  return q;
+}
+__device__ __forceinline__ void split_slot(const PagedArgs& c, uint32_t j, uint32_t* page, uint32_t* slot) {
+  if (c.page_shift >= 0) {
+    *page = j >> c.page_shift;
+    *slot = j & (c.page_size - 1u);
+  } else {
+    *page = j / c.page_size;
+    *slot = j - *page * c.page_size;
+  }
+}
+
+// The keys that the tokens [i0, i1) of a sequence see, numbered without the
+// gap between the sinks and the window: u < s_hi is slot u, then slot
+// lo + (u - s_hi).
+struct KeySpan {
+  uint32_t s_hi, lo, total;
+  __device__ __forceinline__ uint32_t slot(uint32_t u) const { return u < s_hi ? u : lo + (u - s_hi); }
+};
+__device__ __forceinline__ KeySpan key_span(const SeqInfo& q, const RowsArgs& r, uint32_t i0, uint32_t i1) {
+  KeySpan k;
+  const int64_t a0 = q.first + i0, a1 = q.first + i1 - 1;
+  int64_t hi = a1 + 1 < (int64_t)q.len ? a1 + 1 : (int64_t)q.len;
+  if (hi < 0 || i1 <= i0) hi = 0;
+  int64_t lo = r.window ? a0 - (int64_t)r.window + 1 : 0;
+  if (lo < 0) lo = 0;
+  if (lo > hi) lo = hi;
+  k.lo = (uint32_t)lo;
+  k.s_hi = (uint32_t)((int64_t)r.sinks < lo ? (int64_t)r.sinks : lo);
+  k.total = k.s_hi + (uint32_t)(hi - lo);
+  return k;
+}
+__device__ __forceinline__ bool sees(const RowsArgs& r, int64_t a, uint32_t j) {
+  return (int64_t)j <= a && (r.window == 0u || (int64_t)j > a - (int64_t)r.window || j < r.sinks);
+}
+
+// Row tile `tile` (of toks_per_tile tokens): its sequence and its place among
+// that sequence's tiles.  A whole warp calls it; with one tile per sequence
+// (max_new tokens fit a tile) it is the sequence itself.  The host launches
+// one tile more than there can be, so that some CTA walks the whole list and
+// records a range that has no tiles because it is out of bounds.
+__device__ __forceinline__ bool find_tile(const RowsArgs& r, uint32_t n_seqs, uint32_t tile, uint32_t toks_per_tile,
+                                          uint32_t* seq, uint32_t* part, uint32_t* err) {
+  if (r.max_new <= toks_per_tile) {
+    *seq = tile;
+    *part = 0;
+    return tile < n_seqs;
+  }
+  const uint32_t lane = threadIdx.x & 31u;
+  uint64_t before = 0;
+  for (uint32_t s0 = 0; s0 < n_seqs; s0 += 32) {
+    const uint32_t s = s0 + lane;
+    uint32_t t = 0;
+    if (s < n_seqs) {
+      const uint64_t b0 = r.tok_base[s], b1 = r.tok_base[s + 1];
+      if (b1 >= b0 && b1 - b0 <= r.max_new && b1 <= r.n_tokens)
+        t = (uint32_t)((b1 - b0 + toks_per_tile - 1) / toks_per_tile);
+      else
+        record(err, ERR_INVAL);
+    }
+    const uint32_t inc = warp_incl_scan(t);
+    const uint32_t total = __shfl_sync(0xffffffffu, inc, 31);
+    if (tile < before + total) {
+      const uint32_t want = (uint32_t)(tile - before);
+      const uint32_t hit = __ballot_sync(0xffffffffu, inc > want);
+      const int l = __ffs(hit) - 1;
+      *seq = s0 + l;
+      *part = want - (__shfl_sync(0xffffffffu, inc, l) - __shfl_sync(0xffffffffu, t, l));
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+
+}  // namespace ro
