@@ -1,0 +1,508 @@
+// k_attend_tiles.cu — attention of chunks over a paged cache (ro_cache_attend)
+// on the fifth-generation tensor cores.
+//
+//   S = Q K^T, P = exp2(scale log2(e) S - m), O = P V, l = row sums of P,
+// per 128-row tile of (token, head of the group) and 128 slots at a time, with
+// a running m.  Bound by the tensor cores: 4 D operations for each pair of a
+// row and a slot it sees.
+//
+// A CTA holds two row tiles, so that one tile's exponentials run while the
+// tensor cores work for the other: a warp of TMA loads (page by page, swizzled)
+// into a ring of key and value tiles, a warp that issues the products, and for
+// each row tile four warps of softmax, a thread a row.  S and O live in TMEM;
+// P replaces S there and is the left operand of the second product.  m only
+// moves when a row's maximum grew by more than 2^8, so O is seldom rescaled.
+// Slots that no row of the CTA sees are never loaded or are zeroed in shared
+// memory first (a weight of 0 does not silence a NaN in a matrix product).
+// When there are fewer row tiles than places, the slots are split over CTAs
+// and the last CTA of a tile to finish joins the runs' (m, l, O) in order.
+#include <algorithm>
+
+#include "ro_tcgen05.cuh"
+
+namespace ro {
+
+constexpr int AT_THREADS = 384, AT_ROWS = 128, AT_KEYS = 128;
+constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then one warp of products, one of loads, two idle
+// Registers: 168 a thread at launch (3 warps in each quarter of the SM); the
+// last warpgroup gives up what the softmax threads need, 2 x 208 + 80 <= 3 x 168.
+#define AT_REGS_SOFTMAX 208
+#define AT_REGS_OTHERS 80
+constexpr uint32_t AT_TMEM_COLS = 512;
+constexpr float AT_SLACK = 8.f;   // log2 of what a row's maximum may grow before O is rescaled
+
+template <int DP>
+struct TileShape {
+  static constexpr uint32_t BLOCKS = DP / 64;                    // 64-column blocks of a row
+  static constexpr uint32_t BLOCK_BYTES = 128 * 128;             // 128 rows of 128 bytes
+  static constexpr uint32_t TILE_BYTES = BLOCKS * BLOCK_BYTES;
+  static constexpr uint32_t SLOTS = DP == 128 ? 5 : 8;           // key / value tiles in the ring
+  static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE_BYTES;
+};
+
+struct AttendTileArgs {
+  AttendArgs a;
+  CUtensorMap q, k, v;
+  uint32_t toks;             // tokens of a row tile
+  uint32_t box;              // slots of a TMA box
+};
+
+// A tile of slots: first slot, and the slots [lo, hi) of it that count.
+struct SlotTile {
+  uint32_t t0, lo, hi;
+  bool sink;
+};
+__device__ __forceinline__ SlotTile slot_tile(const KeySpan& ks, uint32_t hi, uint32_t sink_tiles, uint32_t first,
+                                              uint32_t t) {
+  SlotTile s;
+  s.sink = t < sink_tiles;
+  if (s.sink) {
+    s.t0 = t * AT_KEYS;
+    s.lo = s.t0;
+    s.hi = min(s.t0 + AT_KEYS, ks.s_hi);
+  } else {
+    s.t0 = first + (t - sink_tiles) * AT_KEYS;
+    s.lo = max(s.t0, ks.lo);
+    s.hi = min(s.t0 + AT_KEYS, hi);
+  }
+  return s;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
+  using S = TileShape<DP>;
+  const AttendArgs& a = g.a;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t s_bar[1 + 2 * S::SLOTS + 6];
+  __shared__ uint32_t s_tmem, s_seq, s_part, s_found, s_last;
+  __shared__ uint32_t s_gave_up;
+  wait_predecessor();
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // the last tiles of a sequence see the most slots: they go first
+  const uint32_t rt = blockIdx.x / a.c.n_heads, kh = blockIdx.x - rt * a.c.n_heads, tile = a.tiles - 1 - rt;
+  if (warp == 0) {
+    uint32_t s = 0, p = 0;
+    const bool f = find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
+    if (lane == 0) {
+      s_seq = s;
+      s_part = p;
+      s_found = f;
+      s_gave_up = 0;
+    }
+  }
+  __syncthreads();
+  if (!s_found) return;
+  const SeqInfo q = seq_info(a.c, a.r, s_seq, a.err);
+  const uint32_t G = a.r.group;
+  const uint32_t i0 = s_part * 2 * g.toks, i1 = min(q.n, i0 + 2 * g.toks);
+  if (i0 >= i1) return;
+  const KeySpan ks = key_span(q, a.r, i0, i1);
+  const uint32_t hi = ks.lo + (ks.total - ks.s_hi);
+  const uint32_t first = ks.lo & ~(g.box - 1u);
+  const uint32_t sink_tiles = (ks.s_hi + AT_KEYS - 1) / AT_KEYS;
+  const uint32_t n_tiles = sink_tiles + (hi > ks.lo ? (hi - first + AT_KEYS - 1) / AT_KEYS : 0);
+  const uint32_t per = max(a.chunk, n_tiles / a.max_chunks + 1);   // slot tiles of a run
+  const uint32_t n_chunks = max(1u, (n_tiles + per - 1) / per);
+  if (blockIdx.y >= n_chunks) return;
+  const uint32_t c0 = blockIdx.y * per, n = min(per, n_tiles - min(n_tiles, c0));   // this run's tiles
+
+  const uint32_t sm = (step_smem(smem_raw) + 1023u) & ~1023u;
+  const uint32_t sm_ring = sm + 2 * S::TILE_BYTES;
+  const uint32_t bar0 = step_smem(s_bar);
+  const uint32_t b_q = bar0, b_full = bar0 + 8, b_empty = b_full + 8 * S::SLOTS, b_s = b_empty + 8 * S::SLOTS,
+                 b_p = b_s + 16, b_o = b_p + 16;
+  if (tid == 0) {
+    bar_init(b_q, 1);
+    for (uint32_t i = 0; i < S::SLOTS; ++i) {
+      bar_init(b_full + 8 * i, 1);
+      bar_init(b_empty + 8 * i, 1);
+    }
+    for (uint32_t i = 0; i < 2; ++i) {
+      bar_init(b_s + 8 * i, 1);
+      bar_init(b_p + 8 * i, 4);
+      bar_init(b_o + 8 * i, 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 8) tmem_alloc(step_smem(&s_tmem), AT_TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = s_tmem;
+  const uint32_t tm_s = tm, tm_o = tm + 256;   // 128 columns for each row tile
+
+  if (warp >= AT_SOFTMAX / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AT_REGS_OTHERS));
+  }
+  if (warp == 9) {
+    // ---- loads ----
+    if (n > 0) {
+      if (lane == 0) {
+        bar_expect(b_q, 2 * S::BLOCKS * g.toks * G * 128);
+        for (uint32_t w = 0; w < 2; ++w)
+          for (uint32_t b = 0; b < S::BLOCKS; ++b)
+            tma3(sm + w * S::TILE_BYTES + b * S::BLOCK_BYTES, &g.q, b * 64, kh * G, (int)(q.tok0 + i0 + w * g.toks), b_q);
+      }
+      const uint32_t boxes = AT_KEYS / g.box;
+      // this lane's box of a tile: its page (all ones: not loaded)
+      auto page_of = [&](uint32_t t) -> uint32_t {
+        if (t >= n || lane >= boxes) return ~0u;
+        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+        const uint32_t j = st.t0 + lane * g.box;
+        if (j >= st.hi || j + g.box <= st.lo) return ~0u;
+        const uint32_t page = a.c.pages[q.page0 + (j >> a.c.page_shift)];
+        if (page >= a.c.n_pages) {
+          record(a.err, ERR_INVAL);
+          return ~0u;
+        }
+        return page;
+      };
+      uint32_t page = page_of(0);
+      for (uint32_t t = 0; t < n; ++t) {
+        const uint32_t next = page_of(t + 1);
+        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+        const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
+        const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, page != ~0u));
+        for (uint32_t kv = 0; kv < 2; ++kv) {
+          const uint32_t use = 2 * t + kv, slot = use % S::SLOTS, round = use / S::SLOTS;
+          if (round > 0) bar_wait(b_empty + 8 * slot, (round - 1) & 1, &s_gave_up, a.err);
+          if (*(volatile uint32_t*)&s_gave_up) break;
+          const uint32_t full = b_full + 8 * slot, dst = sm_ring + slot * S::TILE_BYTES + lane * g.box * 128;
+          if (lane == 0) bar_expect(full, loaded * S::BLOCKS * g.box * 128);
+          __syncwarp();
+          if (page != ~0u)
+            for (uint32_t b = 0; b < S::BLOCKS; ++b)
+              tma4(dst + b * S::BLOCK_BYTES, kv ? &g.v : &g.k, b * 64, (int)y, (int)kh, (int)page, full);
+        }
+        page = next;
+        if (*(volatile uint32_t*)&s_gave_up) break;
+      }
+    }
+  } else if (warp == 8) {
+    // ---- products ----
+    const uint32_t shape_s = mma_shape<T>(AT_KEYS, false), shape_o = mma_shape<T>(DP, true);
+    auto product_s = [&](uint32_t w, uint32_t slot) {
+      const uint32_t qa = sm + w * S::TILE_BYTES, ka = sm_ring + slot * S::TILE_BYTES;
+#pragma unroll
+      for (uint32_t k = 0; k < DP / 16; ++k) {
+        const uint32_t off = (k / 4) * S::BLOCK_BYTES + (k % 4) * 32;
+        mma_ss(tm_s + w * 128, smem_operand(qa + off, 16, 1024), smem_operand(ka + off, 16, 1024), shape_s, k > 0);
+      }
+    };
+    auto product_o = [&](uint32_t w, uint32_t slot, bool add) {
+      const uint32_t va = sm_ring + slot * S::TILE_BYTES;
+#pragma unroll
+      for (uint32_t k = 0; k < AT_KEYS / 16; ++k)
+        mma_ts(tm_o + w * 128, tm_s + w * 128 + k * 8, smem_operand(va + k * 2048, S::BLOCK_BYTES, 1024), shape_o, add || k > 0);
+    };
+    if (n > 0) {
+      bar_wait(b_q, 0, &s_gave_up, a.err);
+      bar_wait(b_full, 0, &s_gave_up, a.err);
+      tc_fence_after();
+      if (lane == 0) {
+        product_s(0, 0);
+        tc_commit(b_s);
+        product_s(1, 0);
+        tc_commit(b_s + 8);
+        tc_commit(b_empty);
+      }
+      for (uint32_t t = 0; t < n; ++t) {
+        const bool more = t + 1 < n;
+        const uint32_t vu = 2 * t + 1, ku = 2 * t + 2, vs = vu % S::SLOTS, kslot = ku % S::SLOTS;
+        bar_wait(b_full + 8 * vs, (vu / S::SLOTS) & 1, &s_gave_up, a.err);
+        if (more) bar_wait(b_full + 8 * kslot, (ku / S::SLOTS) & 1, &s_gave_up, a.err);
+        for (uint32_t w = 0; w < 2; ++w) {
+          bar_wait(b_p + 8 * w, t & 1, &s_gave_up, a.err);
+          tc_fence_after();
+          if (lane == 0) {
+            product_o(w, vs, t > 0);
+            if (w == 1) tc_commit(b_empty + 8 * vs);
+            if (more) {
+              product_s(w, kslot);
+              tc_commit(b_s + 8 * w);
+              if (w == 1) tc_commit(b_empty + 8 * kslot);
+            } else {
+              tc_commit(b_o + 8 * w);
+            }
+          }
+          __syncwarp();
+        }
+        if (*(volatile uint32_t*)&s_gave_up) break;
+      }
+    }
+  }
+  if (warp >= AT_SOFTMAX / 32) {
+    __syncwarp();
+    asm volatile("bar.sync 0;" ::: "memory");   // O is read
+    if (*(volatile uint32_t*)&s_gave_up) __nanosleep(1000000);   // copies and products in flight end by themselves
+    if (warp == 8) {
+      tc_fence_after();
+      tmem_free(tm, AT_TMEM_COLS);
+    }
+    return;
+  }
+  // ---- softmax: a thread a row ----
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AT_REGS_SOFTMAX));
+  {
+    const uint32_t w = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (warp & 3) << 21;                 // this warp's TMEM lanes
+    const uint32_t ts = tm_s + w * 128 + lanes, to = tm_o + w * 128 + lanes;
+    const uint32_t j0 = i0 + w * g.toks, j1 = min(i1, j0 + g.toks);   // the row tile's tokens
+    const bool live = j0 < i1;
+    const uint32_t tok = j0 + row / G, head = kh * G + row % G;
+    const bool mine = row < g.toks * G && tok < j1;
+    const int64_t pos = q.first + tok;                       // the row's slot
+    const int64_t a_lo = q.first + j0, a_hi = q.first + (live ? j1 : j0 + 1) - 1;
+    float m = -INFINITY, l = 0.f;
+    const float scale = a.r.scale_log2;
+    for (uint32_t t = 0; t < n; ++t) {
+      const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+      bar_wait(b_s + 8 * w, t & 1, &s_gave_up, a.err);
+      tc_fence_after();
+      uint32_t x[AT_KEYS];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
+      tc_wait_ld();
+      const bool whole = st.lo == st.t0 && st.hi == st.t0 + AT_KEYS;
+      const bool all = whole && (st.sink || ((int64_t)st.t0 + AT_KEYS - 1 <= a_lo &&
+                                             (a.r.window == 0u || (int64_t)st.t0 > a_hi - (int64_t)a.r.window)));
+      if (!all) {
+        // columns [b, e) count; of those the ones below `sinks` or from the window's first on
+        const int64_t t0 = st.t0;
+        const int e = (int)max((int64_t)0, min((int64_t)st.hi, pos + 1) - t0), b = (int)(st.lo - st.t0);
+        int s_end = AT_KEYS, w_from = 0;
+        if (a.r.window != 0u && !st.sink) {
+          s_end = (int)max((int64_t)0, min((int64_t)AT_KEYS, (int64_t)a.r.sinks - t0));
+          w_from = (int)max((int64_t)0, min((int64_t)AT_KEYS, pos - (int64_t)a.r.window + 1 - t0));
+        }
+#pragma unroll
+        for (int i = 0; i < AT_KEYS; ++i) {
+          const bool in = i >= b && i < e && (i < s_end || i >= w_from);
+          if (!in) x[i] = 0xff800000u;
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < AT_KEYS; ++i) mx = fmaxf(mx, __uint_as_float(x[i]));
+      const float mn = fmaxf(m, mx * scale);
+      if (__any_sync(0xffffffffu, mn > m + AT_SLACK)) {
+        // the maximum moves for the whole warp: rescale what was summed so far
+        const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
+        m = mn;
+        l *= f;
+        if (t > 0) {
+          uint32_t o[16];
+#pragma unroll 1
+          for (int i = 0; i < DP / 16; ++i) {
+            tc_ld16(to + i * 16, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tc_st16(to + i * 16, o);
+          }
+        }
+      }
+      const float sub = m == -INFINITY ? 0.f : m;   // a row that has seen nothing yet
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float e0 = ex2(fmaf(__uint_as_float(x[i * 32 + 2 * k]), scale, -sub));
+          const float e1 = ex2(fmaf(__uint_as_float(x[i * 32 + 2 * k + 1]), scale, -sub));
+          sum[k & 3] += e0 + e1;
+          p[k] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
+        }
+        tc_st16(ts + i * 16, p);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      // Values no row sees must not reach the product: zero them where the
+      // tile is not whole (the products of both row tiles come after this).
+      if (w == 0 && !whole) {
+        const uint32_t vu = 2 * t + 1, slot = vu % S::SLOTS;
+        bar_wait(b_full + 8 * slot, (vu / S::SLOTS) & 1, &s_gave_up, a.err);
+        const uint32_t j = st.t0 + row;
+        if (j < st.lo || j >= st.hi) {
+#pragma unroll
+          for (uint32_t b = 0; b < S::BLOCKS; ++b)
+#pragma unroll
+            for (uint32_t z = 0; z < 8; ++z)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + slot * S::TILE_BYTES +
+                                                                        b * S::BLOCK_BYTES + row * 128 + z * 16),
+                           "r"(0u)
+                           : "memory");
+        }
+        fence_async_smem();
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_p + 8 * w);
+      if (*(volatile uint32_t*)&s_gave_up) break;
+    }
+    if (n > 0) {
+      bar_wait(b_o + 8 * w, 0, &s_gave_up, a.err);
+      tc_fence_after();
+    }
+    T* out = (T*)a.out + (q.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
+    const float inv = n_chunks > 1 ? 1.f : (l > 0.f || l != l ? 1.f / l : 0.f);
+    const uint64_t run = (uint64_t)blockIdx.x * a.max_chunks + blockIdx.y;
+    float* part = a.partial + (run * 2 * AT_ROWS + w * AT_ROWS + row) * DP;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+      uint32_t o[32];
+      if (n > 0) {
+        tc_ld32(to + i * 32, o);
+        tc_wait_ld();
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = 0u;
+      }
+      if (!mine) continue;
+      if (n_chunks > 1) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4)
+          __stcg((float4*)(part + i * 32 + k), make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]),
+                                                           __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          uint4 v;
+          v.x = pack2<T>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+          v.y = pack2<T>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
+          v.z = pack2<T>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
+          v.w = pack2<T>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
+          if ((uint32_t)(i * 32 + k) < a.c.head_dim) *(uint4*)(out + i * 32 + k) = v;
+        }
+      }
+    }
+    if (mine) {
+      if (n_chunks > 1)
+        __stcg((float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * 2 * AT_ROWS * DP) + run * 2 * AT_ROWS +
+                   w * AT_ROWS + row,
+               make_float2(m, l));
+      else if (a.lse)
+        a.lse[(q.tok0 + tok) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    }
+    tc_fence_before();
+  }
+  if (n_chunks > 1) __threadfence();
+  asm volatile("bar.sync 0;" ::: "memory");
+  if (n_chunks == 1) return;
+  if (tid == 0) s_last = ticket(a.counter + blockIdx.x) == n_chunks - 1;
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+  if (!s_last) return;
+  __threadfence();
+  // the runs of this tile in order: rows x 4-column pieces over the threads
+  const float* p0 = a.partial + (uint64_t)blockIdx.x * a.max_chunks * 2 * AT_ROWS * DP;
+  const float2* ml = (const float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * 2 * AT_ROWS * DP) +
+                     (uint64_t)blockIdx.x * a.max_chunks * 2 * AT_ROWS;
+  for (uint32_t x = tid; x < 2 * AT_ROWS * (DP / 4); x += AT_SOFTMAX) {
+    const uint32_t r = x / (DP / 4), d = (x - r * (DP / 4)) * 4, w = r / AT_ROWS, row = r % AT_ROWS;
+    const uint32_t tok = i0 + w * g.toks + row / G, head = kh * G + row % G;
+    if (row >= g.toks * G || tok >= i1) continue;
+    float M = -INFINITY;
+    for (uint32_t k = 0; k < n_chunks; ++k) M = fmaxf(M, __ldcg(&ml[k * 2 * AT_ROWS + r].x));
+    const float sub = M == -INFINITY ? 0.f : M;
+    float L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t k = 0; k < n_chunks; ++k) {
+      const float2 z = __ldcg(&ml[k * 2 * AT_ROWS + r]);
+      const float4 v = __ldcg((const float4*)(p0 + ((uint64_t)k * 2 * AT_ROWS + r) * DP + d));
+      const float f = ex2(z.x - sub);
+      L += f * z.y;
+      acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+    }
+    const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
+    T* out = (T*)a.out + (q.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
+    if (d < a.c.head_dim)
+      *(uint2*)(out + d) = make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
+    if (d == 0 && a.lse)
+      a.lse[(q.tok0 + tok) * a.n_q_heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+  }
+  if (tid == 0) a.counter[blockIdx.x] = 0u;   // for the next call
+}
+
+// ---- host ------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+  static EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return (EncodeTiled)p;
+  }();
+  return f;
+}
+bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t* size, const uint64_t* stride,
+              const uint32_t* box) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  cuuint64_t sz[5], st[5];
+  cuuint32_t bx[5], el[5];
+  for (int i = 0; i < dims; ++i) {
+    sz[i] = size[i];
+    bx[i] = box[i];
+    el[i] = 1;
+    if (i) st[i - 1] = stride[i] * 2;
+  }
+  return f(m, dtype == RO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)dims,
+           const_cast<void*>(p), sz, st, bx, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool attend_tiles_fits(const AttendArgs& a) {
+  return a.c.page_shift >= 3 && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
+}
+uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
+size_t attend_tiles_partial(const AttendArgs& a) {
+  const size_t dp = a.c.head_dim <= 64 ? 64 : 128;
+  return (size_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * (dp + 2) * sizeof(float);
+}
+
+template <typename T, int DP>
+static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g) {
+  launch_k(L, K_ATTEND_TILES, attend_tiles_kernel<T, DP>, dim3(g.a.tiles * g.a.c.n_heads, g.a.max_chunks), AT_THREADS,
+           TileShape<DP>::SMEM, g);
+}
+bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype) {
+  AttendTileArgs g;
+  g.a = a;
+  g.toks = AT_ROWS / a.r.group;
+  g.box = std::min<uint32_t>(a.c.page_size, AT_KEYS);
+  const uint64_t qs[3] = {a.c.head_dim, a.n_q_heads, a.r.n_tokens}, qt[3] = {1, a.r.q_head, a.r.q_tok};
+  const uint32_t qb[3] = {64, a.r.group, g.toks};
+  const uint64_t ps[4] = {a.c.head_dim, a.c.page_size, a.c.n_heads, a.c.n_pages};
+  const uint64_t pt[4] = {1, a.c.slot_stride, a.c.head_stride, a.c.page_stride};
+  const uint32_t pb[4] = {64, g.box, 1, 1};
+  if (!tile_map(&g.q, dtype, a.r.q, 3, qs, qt, qb) || !tile_map(&g.k, dtype, a.c.k, 4, ps, pt, pb) ||
+      !tile_map(&g.v, dtype, a.c.v, 4, ps, pt, pb))
+    return false;
+  const bool narrow = a.c.head_dim <= 64;
+  if (dtype == RO_BF16)
+    narrow ? launch_tiles<__nv_bfloat16, 64>(L, g) : launch_tiles<__nv_bfloat16, 128>(L, g);
+  else
+    narrow ? launch_tiles<__half, 64>(L, g) : launch_tiles<__half, 128>(L, g);
+  return true;
+}
+
+template <typename T, int DP>
+static cudaError_t allow() {
+  return cudaFuncSetAttribute(attend_tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)TileShape<DP>::SMEM);
+}
+cudaError_t prepare_attend_tiles_kernels() {
+  for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
+}
+
+}  // namespace ro

@@ -96,7 +96,8 @@ struct AttendArgs {
   PagedArgs c;
   RowsArgs r;
   uint32_t tiles;            // row tiles per cache head, at most
-  uint32_t chunk;            // keys of one CTA (more where max_chunks would not reach)
+  uint32_t chunk;            // keys (tensor-core kernel: tiles of 128) of one CTA, more where
+                             // max_chunks would not reach
   uint32_t max_chunks;
   void* out;
   uint64_t out_tok, out_head;
@@ -109,6 +110,13 @@ struct AttendArgs {
 // rows of a tile: 16 or 64
 void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype, int rows);
 cudaError_t prepare_attend_kernels();
+// the tensor-core kernel: whether it takes these sizes, tokens of its CTA,
+// bytes of its runs' partial results; false: the tensors cannot be mapped
+bool attend_tiles_fits(const AttendArgs& a);
+uint32_t attend_tile_tokens(uint32_t group);
+size_t attend_tiles_partial(const AttendArgs& a);
+bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype);
+cudaError_t prepare_attend_tiles_kernels();
 
 constexpr int WG_THREADS = 128;
 constexpr uint32_t WG_KEYS = 64, WG_ROWS = 64;

@@ -235,28 +235,48 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
   a.lse = d_lse;
   a.n_q_heads = n_q_heads;
   a.err = c.err();
-  // Rows of a tile: 16 while a sequence's rows fit them (the warps then split
-  // the keys), else 64.
-  const uint64_t max_rows = (uint64_t)a.r.max_new * group;
-  const uint32_t rows = max_rows <= 16 ? 16 : 64;
-  const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);
-  const uint64_t tiles =
-      (a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1) * row_tiles;
-  if (tiles * cache->n_heads > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
-  a.tiles = (uint32_t)tiles;
-  // Keys of one CTA: about four CTAs' worth of work per place of the GPU, in
-  // steps of 64 keys and at least 128 (a shorter run costs more in its join
-  // than it saves).
   uint64_t keys = max_len ? max_len : 0x7FFFFFFFu;
   keys = std::min<uint64_t>(keys, (uint64_t)cache->n_pages * cache->page_size);
   if (window) keys = std::min<uint64_t>(keys, (uint64_t)window + sinks + a.r.max_new);
   keys = std::max<uint64_t>(keys, 1);
-  const uint64_t places = (uint64_t)c.sms() * 2 * 4, work = tiles * cache->n_heads;
-  const uint64_t split = std::max<uint64_t>(1, places / std::max<uint64_t>(work, 1));
+  const uint64_t max_rows = (uint64_t)a.r.max_new * group;
+  void* p = nullptr;
+  // More rows a sequence than the small tiles hold: the tensor-core kernel, if
+  // the pages and the group fit its tiles.
+  if (max_rows > 64 && attend_tiles_fits(a)) {
+    const uint32_t toks = attend_tile_tokens(group);
+    const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
+    const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
+    if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
+    a.tiles = (uint32_t)tiles;
+    // one CTA an SM; split the slots where that leaves places free, at least 1,024 slots a run
+    const uint64_t split = std::max<uint64_t>(1, (uint64_t)c.sms() * 2 / work);
+    a.chunk = (uint32_t)std::max<uint64_t>(8, ceil_div(slots, split));
+    a.max_chunks = split == 1 ? 1u : (uint32_t)std::min<uint64_t>(ceil_div(slots, a.chunk), 256);
+    if (a.max_chunks > 1) {
+      RO_TRY(c.scratch(SS_PARTIAL, attend_tiles_partial(a), &p));
+      a.partial = (float*)p;
+      RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
+      a.counter = (uint32_t*)p;
+    }
+    if (launch_attend_tiles(c.launch(), a, cache->dtype)) return c.launched(fn);
+  }
+  // Rows of a tile: 16 while a sequence's rows fit them (the warps then split
+  // the keys), else 64.
+  const uint32_t rows = max_rows <= 16 ? 16 : 64;
+  const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);
+  const uint64_t tiles =
+      (a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1) * row_tiles;
+  const uint64_t work = tiles * cache->n_heads;
+  if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
+  a.tiles = (uint32_t)tiles;
+  // Keys of one CTA: about four CTAs' worth of work per place of the GPU, in
+  // steps of 64 keys and at least 128 (a shorter run costs more in its join
+  // than it saves).
+  const uint64_t split = std::max<uint64_t>(1, (uint64_t)c.sms() * 2 * 4 / work);
   a.chunk = (uint32_t)std::min<uint64_t>(0x40000000u, std::max<uint64_t>(128, ceil_div(ceil_div(keys, split), 64) * 64));
   a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(keys, a.chunk), 1024);
   if (a.max_chunks > 1) {
-    void* p = nullptr;
     RO_TRY(c.scratch(SS_PARTIAL, (size_t)work * a.max_chunks * rows * ((cache->head_dim <= 64 ? 64 : 128) + 2) * 4, &p));
     a.partial = (float*)p;
     RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
