@@ -78,11 +78,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   __shared__ uint32_t s_gave_up;
   wait_predecessor();
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // the last tiles of a sequence see the most slots: they go first
-  const uint32_t rt = blockIdx.x / a.c.n_heads, kh = blockIdx.x - rt * a.c.n_heads, tile = a.tiles - 1 - rt;
+  const uint32_t tile = blockIdx.x / a.c.n_heads, kh = blockIdx.x - tile * a.c.n_heads;
   if (warp == 0) {
     uint32_t s = 0, p = 0;
-    const bool f = find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
+    const bool f = a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
+                       ? find_tile_heavy(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err)
+                       : find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
     if (lane == 0) {
       s_seq = s;
       s_part = p;
@@ -282,10 +283,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           if (!in) x[i] = 0xff800000u;
         }
       }
-      float mx = -INFINITY;
+      float mx[8];   // eight chains: one of 128 would cost its latency 128 times
 #pragma unroll
-      for (int i = 0; i < AT_KEYS; ++i) mx = fmaxf(mx, __uint_as_float(x[i]));
-      const float mn = fmaxf(m, mx * scale);
+      for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+#pragma unroll
+      for (int i = 16; i < AT_KEYS; i += 2)
+        mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
+      const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
+                                      fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * scale);
       if (__any_sync(0xffffffffu, mn > m + AT_SLACK)) {
         // the maximum moves for the whole warp: rescale what was summed so far
         const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
@@ -304,20 +309,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
       }
       const float sub = m == -INFINITY ? 0.f : m;   // a row that has seen nothing yet
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint64_t scale2 = pair(scale, scale), sub2 = pair(-sub, -sub);
+      uint64_t sum[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t p[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-          const float e0 = ex2(fmaf(__uint_as_float(x[i * 32 + 2 * k]), scale, -sub));
-          const float e1 = ex2(fmaf(__uint_as_float(x[i * 32 + 2 * k + 1]), scale, -sub));
-          sum[k & 3] += e0 + e1;
+          const uint64_t y = fma_pair(pair_bits(x[i * 32 + 2 * k], x[i * 32 + 2 * k + 1]), scale2, sub2);
+          const float e0 = ex2(pair_lo(y)), e1 = ex2(pair_hi(y));
+          sum[k & 3] = add_pair(sum[k & 3], pair(e0, e1));
           p[k] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
         }
         tc_st16(ts + i * 16, p);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const uint64_t all4 = add_pair(add_pair(sum[0], sum[1]), add_pair(sum[2], sum[3]));
+      l += pair_lo(all4) + pair_hi(all4);
       // Values no row sees must not reach the product: zero them where the
       // tile is not whole (the products of both row tiles come after this).
       if (w == 0 && !whole) {

@@ -175,4 +175,82 @@ __device__ __forceinline__ bool find_tile(const RowsArgs& r, uint32_t n_seqs, ui
   return false;
 }
 
+// The same with the tiles that see the most slots first (without a window a
+// tile's work is the slot after its last token, `hi`), so that the last CTAs
+// to start are short ones.  The tile of rank r has the largest hi = w with at
+// least r + 1 tiles at or above w, found by bisection: a sequence's tiles at
+// or above w are counted in closed form.  At most 32 * FT_SEQS sequences.
+constexpr uint32_t FT_SEQS = 4;
+__device__ __forceinline__ bool find_tile_heavy(const RowsArgs& r, uint32_t n_seqs, uint32_t rank,
+                                                uint32_t toks_per_tile, uint32_t* seq, uint32_t* part, uint32_t* err) {
+  const uint32_t lane = threadIdx.x & 31u, nk = (n_seqs + 31) / 32;
+  const uint32_t recip = 0xFFFFFFFFu / toks_per_tile + 1u;   // a division by product: the order may err by a slot
+  int32_t first[FT_SEQS], len[FT_SEQS], top = 0;
+  uint32_t tiles[FT_SEQS];
+#pragma unroll
+  for (uint32_t k = 0; k < FT_SEQS; ++k) {
+    const uint32_t s = lane * nk + k;   // a lane's sequences are neighbours: ranks follow their order
+    first[k] = len[k] = 0;
+    tiles[k] = 0;
+    if (k < nk && s < n_seqs) {
+      const uint64_t b0 = r.tok_base[s], b1 = r.tok_base[s + 1];
+      if (b1 >= b0 && b1 - b0 <= r.max_new && b1 <= r.n_tokens) {
+        len[k] = (int32_t)(r.len[s] & 0x7FFFFFFFu);
+        first[k] = len[k] - (int32_t)(b1 - b0);
+        top = max(top, len[k]);
+        tiles[k] = (uint32_t)((b1 - b0 + toks_per_tile - 1) / toks_per_tile);
+      } else {
+        record(err, ERR_INVAL);
+      }
+    }
+  }
+  auto at_least = [&](uint32_t k, uint32_t w) -> uint32_t {   // sequence k's tiles with hi >= w
+    if (w == 0) return tiles[k];
+    if (w > (uint32_t)len[k]) return 0;
+    const int32_t d = (int32_t)w - first[k];   // at most its new tokens
+    return tiles[k] - (d <= 0 ? 0u : min(tiles[k], __umulhi((uint32_t)d - 1u, recip)));
+  };
+  auto count = [&](uint32_t w) -> uint32_t {
+    uint32_t c = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < FT_SEQS; ++k)
+      if (k < nk) c += at_least(k, w);
+    return __reduce_add_sync(0xffffffffu, c);
+  };
+  if (count(0) <= rank) return false;
+  uint32_t lo = 0, hi = (uint32_t)__reduce_max_sync(0xffffffffu, top) + 1u;   // count(lo) > rank >= count(hi)
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (count(mid) > rank)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  // of the tiles with hi == lo (0: or below), the one of what rank is left
+  uint32_t left = rank - count(lo + 1), mine = 0;
+  uint32_t eq[FT_SEQS];
+#pragma unroll
+  for (uint32_t k = 0; k < FT_SEQS; ++k) {
+    eq[k] = at_least(k, lo) - at_least(k, lo + 1);
+    mine += eq[k];
+  }
+  const uint32_t inc = warp_incl_scan(mine);
+  const int l = __ffs(__ballot_sync(0xffffffffu, inc > left)) - 1;
+  uint32_t s = 0, p = 0;
+  left -= inc - mine;   // (of use in lane l)
+#pragma unroll
+  for (uint32_t k = 0; k < FT_SEQS; ++k) {
+    if (left < eq[k]) {
+      s = lane * nk + k;
+      p = tiles[k] - at_least(k, lo) + left;
+      left = 0xFFFFFFFFu;
+    } else if (left != 0xFFFFFFFFu) {
+      left -= eq[k];
+    }
+  }
+  *seq = __shfl_sync(0xffffffffu, s, l);
+  *part = __shfl_sync(0xffffffffu, p, l);
+  return true;
+}
+
 }  // namespace ro
