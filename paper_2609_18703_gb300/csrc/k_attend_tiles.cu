@@ -26,8 +26,8 @@ constexpr int AT_THREADS = 384, AT_ROWS = 128, AT_KEYS = 128;
 constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then one warp of products, one of loads, two idle
 // Registers: 168 a thread at launch (3 warps in each quarter of the SM); the
 // last warpgroup gives up what the softmax threads need, 2 x 208 + 80 <= 3 x 168.
-#define AT_REGS_SOFTMAX 208
-#define AT_REGS_OTHERS 80
+#define AT_REGS_SOFTMAX 216
+#define AT_REGS_OTHERS 72
 constexpr uint32_t AT_TMEM_COLS = 512;
 constexpr float AT_SLACK = 8.f;   // log2 of what a row's maximum may grow before O is rescaled
 
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   __shared__ uint32_t s_tmem, s_seq, s_part, s_found, s_last;
   __shared__ uint32_t s_gave_up;
   wait_predecessor();
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t tile = blockIdx.x / a.c.n_heads, kh = blockIdx.x - tile * a.c.n_heads;
   if (warp == 0) {
     uint32_t s = 0, p = 0;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tm = s_tmem;
+  const uint32_t tm = __shfl_sync(0xffffffffu, s_tmem, 0);
   const uint32_t tm_s = tm, tm_o = tm + 256;   // 128 columns for each row tile
 
   if (warp >= AT_SOFTMAX / 32) {
@@ -146,90 +146,98 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
             tma3(sm + w * S::TILE_BYTES + b * S::BLOCK_BYTES, &g.q, b * 64, kh * G, (int)(q.tok0 + i0 + w * g.toks), b_q);
       }
       const uint32_t boxes = AT_KEYS / g.box;
-      // this lane's box of a tile: its page (all ones: not loaded)
-      auto page_of = [&](uint32_t t) -> uint32_t {
-        if (t >= n || lane >= boxes) return ~0u;
-        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+      // boxes without a slot that counts are not loaded
+      auto has_box = [&](const SlotTile& st) {
         const uint32_t j = st.t0 + lane * g.box;
-        if (j >= st.hi || j + g.box <= st.lo) return ~0u;
-        const uint32_t page = a.c.pages[q.page0 + (j >> a.c.page_shift)];
-        if (page >= a.c.n_pages) {
-          record(a.err, ERR_INVAL);
-          return ~0u;
-        }
-        return page;
+        return lane < boxes && j < st.hi && j + g.box > st.lo;
       };
-      uint32_t page = page_of(0);
+      // The page of this lane's box of a tile, looked up two tiles ahead and
+      // not touched before then, so that a tile's loads never wait for it.
+      auto page_of = [&](uint32_t t) -> uint32_t {
+        if (t >= n) return 0u;
+        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+        return has_box(st) ? a.c.pages[q.page0 + ((st.t0 + lane * g.box) >> a.c.page_shift)] : 0u;
+      };
+      uint32_t page = page_of(0), next = page_of(1), slot = 0, parity = 1;   // parity of the round before
       for (uint32_t t = 0; t < n; ++t) {
-        const uint32_t next = page_of(t + 1);
+        const uint32_t after = page_of(t + 2);
         const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
         const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
-        const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, page != ~0u));
+        bool load = has_box(st);
+        if (load && page >= a.c.n_pages) {
+          record(a.err, ERR_INVAL);
+          load = false;
+        }
+        const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
+#pragma unroll
         for (uint32_t kv = 0; kv < 2; ++kv) {
-          const uint32_t use = 2 * t + kv, slot = use % S::SLOTS, round = use / S::SLOTS;
-          if (round > 0) bar_wait(b_empty + 8 * slot, (round - 1) & 1, &s_gave_up, a.err);
+          if (2 * t + kv >= S::SLOTS) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
           if (*(volatile uint32_t*)&s_gave_up) break;
           const uint32_t full = b_full + 8 * slot, dst = sm_ring + slot * S::TILE_BYTES + lane * g.box * 128;
           if (lane == 0) bar_expect(full, loaded * S::BLOCKS * g.box * 128);
           __syncwarp();
-          if (page != ~0u)
+          if (load)
             for (uint32_t b = 0; b < S::BLOCKS; ++b)
               tma4(dst + b * S::BLOCK_BYTES, kv ? &g.v : &g.k, b * 64, (int)y, (int)kh, (int)page, full);
+          if (++slot == S::SLOTS) slot = 0, parity ^= 1;
         }
         page = next;
+        next = after;
         if (*(volatile uint32_t*)&s_gave_up) break;
       }
     }
   } else if (warp == 8) {
     // ---- products ----
     const uint32_t shape_s = mma_shape<T>(AT_KEYS, false), shape_o = mma_shape<T>(DP, true);
+    const uint32_t one = elect_lane();
+    const uint32_t q_lo = operand_lo(sm, 16), k_lo = operand_lo(sm_ring, 16), v_lo = operand_lo(sm_ring, S::BLOCK_BYTES);
     auto product_s = [&](uint32_t w, uint32_t slot) {
-      const uint32_t qa = sm + w * S::TILE_BYTES, ka = sm_ring + slot * S::TILE_BYTES;
+      const uint32_t qa = q_lo + w * (S::TILE_BYTES / 16), ka = k_lo + slot * (S::TILE_BYTES / 16);
 #pragma unroll
       for (uint32_t k = 0; k < DP / 16; ++k) {
-        const uint32_t off = (k / 4) * S::BLOCK_BYTES + (k % 4) * 32;
-        mma_ss(tm_s + w * 128, smem_operand(qa + off, 16, 1024), smem_operand(ka + off, 16, 1024), shape_s, k > 0);
+        const uint32_t off = ((k / 4) * S::BLOCK_BYTES + (k % 4) * 32) / 16;
+        mma_ss(one, tm_s + w * 128, qa + off, ka + off, shape_s, k > 0);
       }
     };
     auto product_o = [&](uint32_t w, uint32_t slot, bool add) {
-      const uint32_t va = sm_ring + slot * S::TILE_BYTES;
+      const uint32_t va = v_lo + slot * (S::TILE_BYTES / 16);
 #pragma unroll
       for (uint32_t k = 0; k < AT_KEYS / 16; ++k)
-        mma_ts(tm_o + w * 128, tm_s + w * 128 + k * 8, smem_operand(va + k * 2048, S::BLOCK_BYTES, 1024), shape_o, add || k > 0);
+        mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8, va + k * (2048 / 16), shape_o, add || k > 0);
     };
     if (n > 0) {
       bar_wait(b_q, 0, &s_gave_up, a.err);
       bar_wait(b_full, 0, &s_gave_up, a.err);
       tc_fence_after();
-      if (lane == 0) {
-        product_s(0, 0);
-        tc_commit(b_s);
-        product_s(1, 0);
-        tc_commit(b_s + 8);
-        tc_commit(b_empty);
-      }
+      product_s(0, 0);
+      tc_commit(one, b_s);
+      product_s(1, 0);
+      tc_commit(one, b_s + 8);
+      tc_commit(one, b_empty);
+      uint32_t vs = 1, v_par = 0, kslot = 2 % S::SLOTS, k_par = 0;   // ring places of V(t), K(t + 1) and their rounds' parity
       for (uint32_t t = 0; t < n; ++t) {
         const bool more = t + 1 < n;
-        const uint32_t vu = 2 * t + 1, ku = 2 * t + 2, vs = vu % S::SLOTS, kslot = ku % S::SLOTS;
-        bar_wait(b_full + 8 * vs, (vu / S::SLOTS) & 1, &s_gave_up, a.err);
-        if (more) bar_wait(b_full + 8 * kslot, (ku / S::SLOTS) & 1, &s_gave_up, a.err);
+        bar_wait(b_full + 8 * vs, v_par, &s_gave_up, a.err);
+#pragma unroll
         for (uint32_t w = 0; w < 2; ++w) {
           bar_wait(b_p + 8 * w, t & 1, &s_gave_up, a.err);
           tc_fence_after();
-          if (lane == 0) {
-            product_o(w, vs, t > 0);
-            if (w == 1) tc_commit(b_empty + 8 * vs);
-            if (more) {
-              product_s(w, kslot);
-              tc_commit(b_s + 8 * w);
-              if (w == 1) tc_commit(b_empty + 8 * kslot);
-            } else {
-              tc_commit(b_o + 8 * w);
-            }
+          product_o(w, vs, t > 0);
+          if (w == 1) tc_commit(one, b_empty + 8 * vs);
+          if (more) {
+            if (w == 0) bar_wait(b_full + 8 * kslot, k_par, &s_gave_up, a.err);
+            product_s(w, kslot);
+            tc_commit(one, b_s + 8 * w);
+            if (w == 1) tc_commit(one, b_empty + 8 * kslot);
+          } else {
+            tc_commit(one, b_o + 8 * w);
           }
-          __syncwarp();
         }
         if (*(volatile uint32_t*)&s_gave_up) break;
+        vs += 2;
+        if (vs >= S::SLOTS) vs -= S::SLOTS, v_par ^= 1;
+        kslot += 2;
+        if (kslot >= S::SLOTS) kslot -= S::SLOTS, k_par ^= 1;
       }
     }
   }

@@ -82,9 +82,13 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// the barrier is arrived at when every MMA issued by this thread so far is done
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// the barrier is arrived at when every product issued by the elected lane so far is done
+__device__ __forceinline__ void tc_commit(uint32_t one, uint32_t bar) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.u32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+      "r"(one)
+      : "memory");
 }
 // 32 columns of this warp's 32 lanes: thread = lane, register = column
 __device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t* r) {
@@ -114,14 +118,15 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r) {
 }
 
 // ---- matrix products -------------------------------------------------------------------------
-// Shared-memory operand with the 128-byte swizzle.  K-major (rows of 64
-// consecutive k): stride = bytes between 8-row groups, lead unused.  MN-major
-// (rows of 64 consecutive m or n, one row per k): stride = bytes between
-// 8-row groups, lead = bytes between blocks of 64 m or n.
-__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t lead, uint32_t stride) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);
+// Shared-memory operand with the 128-byte swizzle, in two 32-bit halves: the
+// low one holds the address (advance it by bytes / 16) and the distance of
+// blocks of 64 m or n; the high one the distance of 8-row groups, 1,024 bytes.
+// K-major (rows of 64 consecutive k): `lead` unused.  MN-major (rows of 64
+// consecutive m or n, one row per k): lead = bytes between blocks.
+__device__ __forceinline__ uint32_t operand_lo(uint32_t addr, uint32_t lead) {
+  return ((addr & 0x3FFFFu) >> 4) | ((lead >> 4) << 16);
 }
+constexpr uint32_t OPERAND_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
 // 16-bit operands, 32-bit accumulators, M = 128
 template <typename T>
 __host__ __device__ constexpr uint32_t mma_shape(uint32_t n, bool b_mn_major);
@@ -133,18 +138,31 @@ template <>
 __host__ __device__ constexpr uint32_t mma_shape<__half>(uint32_t n, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
-// d (+)= a b, a and b in shared memory; one thread
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+// One lane of the warp, the same every time.  The products are issued under
+// this predicate by a warp that has not diverged, so that their operands stay
+// in uniform registers; moved there from a divergent branch each product cost
+// 80 cycles of issue, more than it takes.
+__device__ __forceinline__ uint32_t elect_lane() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p;
+}
+// d (+)= a b, a and b in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "{\n .reg .pred p, q;\n .reg .b64 a, b;\n setp.ne.u32 p, %5, 0;\n setp.ne.u32 q, %6, 0;\n"
+      " mov.b64 a, {%1, %4};\n mov.b64 b, {%2, %4};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"(OPERAND_HI), "r"((uint32_t)add), "r"(one)
       : "memory");
 }
 // the same with a in TMEM
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "{\n .reg .pred p, q;\n .reg .b64 b;\n setp.ne.u32 p, %5, 0;\n setp.ne.u32 q, %6, 0;\n"
+      " mov.b64 b, {%2, %4};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(shape), "r"(OPERAND_HI), "r"((uint32_t)add), "r"(one)
       : "memory");
 }
 
