@@ -1,4 +1,5 @@
-// k_attend.cu — attention of few rows over a paged cache (ro_cache_attend).
+// k_attend.cu — attention over a paged cache whose pages or groups fit no tensor
+// tile (ro_cache_attend): any page size, any number of heads in a group.
 //
 //   o_r = sum_j p_rj v_j,  p_rj = exp2(x_rj - m_r) / l_r,
 //   x_rj = scale log2(e) q_r.k_j over the slots j that row r sees,
@@ -6,35 +7,32 @@
 // The rows of a tile are the tokens of one sequence times the query heads that
 // share a cache head, so a key is read once for all of them.
 //
-// Bound by the bytes of K and V: a single token with G shared heads does 4 G
-// operations per pair of bytes.  A CTA of four warps takes a run of keys,
-// staged by cp.async three deep (pages looked up a stage ahead); with up to 16
-// rows the warps split the keys of a stage, with up to 64 the rows.  A long
-// sequence is cut into runs of `chunk` keys; the last CTA of a tile to finish
-// joins the runs' (m, l, o) in the order of the keys, so the result does not
-// depend on which CTA that is.
+// A CTA of four warps takes 64 rows (a token's heads, tokens of one sequence)
+// and a run of keys, staged by cp.async three deep with pages looked up a
+// stage ahead; each warp has 16 rows.  A long sequence is cut into runs of
+// `chunk` keys; the last CTA of a tile to finish joins the runs' (m, l, o) in
+// the order of the keys, so the result does not depend on which CTA that is.
+// mma.sync bounds it, at about a fifth of what the tensor-core tiles reach.
 #include <algorithm>
 
 #include "ro_step.cuh"
 
 namespace ro {
 
-constexpr int AR_THREADS = 128, AR_STAGES = 3, AR_KEYS = 64;
+constexpr int AR_THREADS = 128, AR_STAGES = 3, AR_KEYS = 64, AR_ROWS = 64;
 
 template <int DP>
 constexpr size_t attend_rows_smem() {
   return (size_t)AR_STAGES * 2 * AR_KEYS * DP * 2;
 }
 
-// WR: 16-row groups (warps split the rows); 4 / WR warps share a group's keys.
-template <typename T, int DP, int WR>
+template <typename T, int DP>
 __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int WK = 4 / WR, KW = AR_KEYS / WK, ROWS = 16 * WR;
+  constexpr int KW = AR_KEYS, ROWS = AR_ROWS;
   constexpr int CH = DP / 8;                         // 16-byte pieces of a row
   constexpr int RPP = AR_THREADS / CH, PASSES = AR_KEYS / RPP;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint32_t s_seq, s_part, s_found, s_last;
-  __shared__ float s_m[4][16], s_l[4][16];
   wait_predecessor();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t G = a.r.group, D = a.c.head_dim;
@@ -110,14 +108,13 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
   }
 
   // queries as matrix fragments; rows past the tile's are zero
-  const int wr = warp % WR, wk = warp / WR;
   uint32_t qf[DP / 16][4];
   int64_t row_a[2];
   {
     const T* qp[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const uint32_t r = wr * 16 + lane / 4 + 8 * z;
+      const uint32_t r = warp * 16 + lane / 4 + 8 * z;
       qp[z] = nullptr;
       row_a[z] = INT64_MIN / 2;
       if (r < rows) {
@@ -153,7 +150,6 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     }
     cp_async_commit();
     const uint32_t kb = sm + (step % AR_STAGES) * stage_bytes, vb = kb + AR_KEYS * DP * 2;
-    const uint32_t key0 = wk * KW;
     float s[KW / 8][4];
 #pragma unroll
     for (int i = 0; i < KW / 8; ++i)
@@ -163,7 +159,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     for (int k = 0; k < DP / 16; ++k) {
 #pragma unroll
       for (int n = 0; n < KW / 16; ++n) {
-        const uint32_t r = key0 + n * 16 + (lane & 7) + ((lane >> 4) << 3), c = k * 2 + ((lane >> 3) & 1);
+        const uint32_t r = n * 16 + (lane & 7) + ((lane >> 4) << 3), c = k * 2 + ((lane >> 3) & 1);
         uint32_t b[4];
         ldsm4(b, kb + r * DP * 2 + ((c ^ (r & 7)) * 16));
         mma16<T>(s[2 * n], qf[k], b[0], b[1]);
@@ -181,7 +177,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
       for (int z = 0; z < 4; ++z) {
         float x = s[n][z] * a.r.scale_log2;
         if (!all) {
-          const uint32_t u = ub + key0 + n * 8 + (lane & 3) * 2 + (z & 1);
+          const uint32_t u = ub + n * 8 + (lane & 3) * 2 + (z & 1);
           if (u >= u1 || !sees(a.r, row_a[z >> 1], ks.slot(u))) x = -INFINITY;
         }
         s[n][z] = x;
@@ -222,7 +218,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     for (int n = 0; n < KW / 16; ++n) {
 #pragma unroll
       for (int d = 0; d < DP / 16; ++d) {
-        const uint32_t r = key0 + n * 16 + (lane & 15), c = d * 2 + (lane >> 4);
+        const uint32_t r = n * 16 + (lane & 15), c = d * 2 + (lane >> 4);
         uint32_t b[4];
         ldsm4_t(b, vb + r * DP * 2 + ((c ^ (r & 7)) * 16));
         mma16<T>(o[2 * d], p[n], b[0], b[1]);
@@ -237,62 +233,39 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     l[z] += __shfl_xor_sync(0xffffffffu, l[z], 2);
   }
   __syncthreads();
-  // the warps that shared a row group join theirs: o in shared memory, [warp][16][DP]
-  float* so = (float*)smem;
+  // each warp's rows are its own: to the output, or to this run's partial result
+  float* part = a.partial + (((uint64_t)blockIdx.x * a.max_chunks + blockIdx.y) * ROWS) * (uint64_t)(DP + 2);
+  T* out = (T*)a.out;
 #pragma unroll
   for (int z = 0; z < 2; ++z) {
-    const int r = lane / 4 + 8 * z;
-    if ((lane & 3) == 0) {
-      s_m[warp][r] = m[z];
-      s_l[warp][r] = l[z];
-    }
-#pragma unroll
-    for (int i = 0; i < DP / 8; ++i)
-      *(float2*)(so + (warp * 16 + r) * DP + i * 8 + (lane & 3) * 2) = make_float2(o[i][z * 2], o[i][z * 2 + 1]);
-  }
-  __syncthreads();
-  const uint64_t tile_id = blockIdx.x;
-  float* part = a.partial + ((tile_id * a.max_chunks + blockIdx.y) * ROWS) * (uint64_t)(DP + 2);
-  T* out = (T*)a.out;
-  for (uint32_t x = tid; x < rows * (DP / 4); x += AR_THREADS) {
-    const uint32_t r = x / (DP / 4), d = (x - r * (DP / 4)) * 4;
-    const uint32_t w0 = r / 16, rr = r % 16;
-    float M = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < WK; ++k) M = fmaxf(M, s_m[w0 + k * WR][rr]);
-    const float sub = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < WK; ++k) {
-      const float f = exp2f(s_m[w0 + k * WR][rr] - sub);
-      L += f * s_l[w0 + k * WR][rr];
-      const float4 v = *(const float4*)(so + ((w0 + k * WR) * 16 + rr) * DP + d);
-      acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-    }
+    const uint32_t r = warp * 16 + lane / 4 + 8 * z;
+    if (r >= rows) continue;
+    const uint64_t t = q.tok0 + i0 + r / gn;
+    const uint32_t h = kh * G + g0 + r % gn;
+    const float inv = l[z] > 0.f || l[z] != l[z] ? 1.f / l[z] : 0.f;
+    float* pp = part + r * (DP + 2);
     if (n_chunks > 1) {
-      float* pp = part + r * (DP + 2);
-      __stcg((float2*)(pp + d), make_float2(acc.x, acc.y));
-      __stcg((float2*)(pp + d + 2), make_float2(acc.z, acc.w));
-      if (d == 0) __stcg((float2*)(pp + DP), make_float2(M, L));
-    } else {
-      const uint64_t t = q.tok0 + i0 + r / gn;
-      const uint32_t h = kh * G + g0 + r % gn;
-      const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
-      if (d < D)
-        *(uint2*)(out + t * a.out_tok + h * a.out_head + d) =
-            make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-      if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+      if ((lane & 3) == 0) __stcg((float2*)(pp + DP), make_float2(m[z], l[z]));
+    } else if ((lane & 3) == 0 && a.lse) {
+      a.lse[t * a.n_q_heads + h] = l[z] == 0.f ? -INFINITY : (m[z] + log2f(l[z])) * LN2;
+    }
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+      const uint32_t d = i * 8 + (lane & 3) * 2;
+      if (n_chunks > 1)
+        __stcg((float2*)(pp + d), make_float2(o[i][z * 2], o[i][z * 2 + 1]));
+      else if (d < D)
+        *(uint32_t*)(out + t * a.out_tok + h * a.out_head + d) = pack2<T>(o[i][z * 2] * inv, o[i][z * 2 + 1] * inv);
     }
   }
   if (n_chunks == 1) return;
   __threadfence();
   __syncthreads();
-  if (tid == 0) s_last = ticket(a.counter + tile_id) == n_chunks - 1;
+  if (tid == 0) s_last = ticket(a.counter + blockIdx.x) == n_chunks - 1;
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  const float* p0 = a.partial + (tile_id * a.max_chunks * ROWS) * (uint64_t)(DP + 2);
+  const float* p0 = a.partial + ((uint64_t)blockIdx.x * a.max_chunks * ROWS) * (uint64_t)(DP + 2);
   const uint64_t step = (uint64_t)ROWS * (DP + 2);
   for (uint32_t x = tid; x < rows * (DP / 2); x += AR_THREADS) {
     const uint32_t r = x / (DP / 2), d = (x - r * (DP / 2)) * 2;
@@ -317,44 +290,31 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
       *(uint32_t*)(out + t * a.out_tok + h * a.out_head + d) = pack2<T>(acc.x * inv, acc.y * inv);
     if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
   }
-  if (tid == 0) a.counter[tile_id] = 0u;   // for the next call
+  if (tid == 0) a.counter[blockIdx.x] = 0u;   // for the next call
 }
 
-template <typename T, int DP, int WR>
+template <typename T, int DP>
 static void launch_rows(const LaunchCfg& L, const AttendArgs& a) {
-  static_assert(attend_rows_smem<DP>() >= 4 * 16 * DP * sizeof(float), "the join fits the stages");
-  launch_k(L, K_ATTEND_ROWS, attend_rows_kernel<T, DP, WR>, dim3(a.tiles * a.c.n_heads, a.max_chunks), AR_THREADS,
+  launch_k(L, K_ATTEND_ROWS, attend_rows_kernel<T, DP>, dim3(a.tiles * a.c.n_heads, a.max_chunks), AR_THREADS,
            attend_rows_smem<DP>(), a);
 }
-template <typename T>
-static void launch_rows(const LaunchCfg& L, const AttendArgs& a, int rows) {
-  if (a.c.head_dim <= 64)
-    rows == 16 ? launch_rows<T, 64, 1>(L, a) : launch_rows<T, 64, 4>(L, a);
-  else
-    rows == 16 ? launch_rows<T, 128, 1>(L, a) : launch_rows<T, 128, 4>(L, a);
-}
-
-void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype, int rows) {
+void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype) {
+  const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)
-    launch_rows<__nv_bfloat16>(L, a, rows);
+    narrow ? launch_rows<__nv_bfloat16, 64>(L, a) : launch_rows<__nv_bfloat16, 128>(L, a);
   else
-    launch_rows<__half>(L, a, rows);
+    narrow ? launch_rows<__half, 64>(L, a) : launch_rows<__half, 128>(L, a);
 }
 
-template <typename T, int DP, int WR>
-static cudaError_t allow_smem() {
-  return cudaFuncSetAttribute(attend_rows_kernel<T, DP, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+template <typename T, int DP>
+static cudaError_t allow() {
+  return cudaFuncSetAttribute(attend_rows_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               (int)attend_rows_smem<DP>());
 }
-template <typename T>
-static cudaError_t allow_smem() {
-  for (cudaError_t e : {allow_smem<T, 64, 1>(), allow_smem<T, 64, 4>(), allow_smem<T, 128, 1>(), allow_smem<T, 128, 4>()})
+cudaError_t prepare_attend_kernels() {
+  for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
-}
-cudaError_t prepare_attend_kernels() {
-  const cudaError_t e = allow_smem<__nv_bfloat16>();
-  return e != cudaSuccess ? e : allow_smem<__half>();
 }
 
 }  // namespace ro

@@ -40,34 +40,6 @@ struct TileShape {
   static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE_BYTES;
 };
 
-struct AttendTileArgs {
-  AttendArgs a;
-  CUtensorMap q, k, v;
-  uint32_t toks;             // tokens of a row tile
-  uint32_t box;              // slots of a TMA box
-};
-
-// A tile of slots: first slot, and the slots [lo, hi) of it that count.
-struct SlotTile {
-  uint32_t t0, lo, hi;
-  bool sink;
-};
-__device__ __forceinline__ SlotTile slot_tile(const KeySpan& ks, uint32_t hi, uint32_t sink_tiles, uint32_t first,
-                                              uint32_t t) {
-  SlotTile s;
-  s.sink = t < sink_tiles;
-  if (s.sink) {
-    s.t0 = t * AT_KEYS;
-    s.lo = s.t0;
-    s.hi = min(s.t0 + AT_KEYS, ks.s_hi);
-  } else {
-    s.t0 = first + (t - sink_tiles) * AT_KEYS;
-    s.lo = max(s.t0, ks.lo);
-    s.hi = min(s.t0 + AT_KEYS, hi);
-  }
-  return s;
-}
-
 template <typename T, int DP>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
   using S = TileShape<DP>;
@@ -98,14 +70,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   const uint32_t i0 = s_part * 2 * g.toks, i1 = min(q.n, i0 + 2 * g.toks);
   if (i0 >= i1) return;
   const KeySpan ks = key_span(q, a.r, i0, i1);
-  const uint32_t hi = ks.lo + (ks.total - ks.s_hi);
-  const uint32_t first = ks.lo & ~(g.box - 1u);
-  const uint32_t sink_tiles = (ks.s_hi + AT_KEYS - 1) / AT_KEYS;
-  const uint32_t n_tiles = sink_tiles + (hi > ks.lo ? (hi - first + AT_KEYS - 1) / AT_KEYS : 0);
-  const uint32_t per = max(a.chunk, n_tiles / a.max_chunks + 1);   // slot tiles of a run
-  const uint32_t n_chunks = max(1u, (n_tiles + per - 1) / per);
+  const SlotTiles<AT_KEYS> slots(ks, g.box);
+  const uint32_t per = max(a.chunk, slots.n / a.max_chunks + 1);   // slot tiles of a run
+  const uint32_t n_chunks = max(1u, (slots.n + per - 1) / per);
   if (blockIdx.y >= n_chunks) return;
-  const uint32_t c0 = blockIdx.y * per, n = min(per, n_tiles - min(n_tiles, c0));   // this run's tiles
+  const uint32_t c0 = blockIdx.y * per, n = min(per, slots.n - min(slots.n, c0));   // this run's tiles
 
   const uint32_t sm = (step_smem(smem_raw) + 1023u) & ~1023u;
   const uint32_t sm_ring = sm + 2 * S::TILE_BYTES;
@@ -155,13 +124,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       // not touched before then, so that a tile's loads never wait for it.
       auto page_of = [&](uint32_t t) -> uint32_t {
         if (t >= n) return 0u;
-        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+        const SlotTile st = slots.at(c0 + t);
         return has_box(st) ? a.c.pages[q.page0 + ((st.t0 + lane * g.box) >> a.c.page_shift)] : 0u;
       };
       uint32_t page = page_of(0), next = page_of(1), slot = 0, parity = 1;   // parity of the round before
       for (uint32_t t = 0; t < n; ++t) {
         const uint32_t after = page_of(t + 2);
-        const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+        const SlotTile st = slots.at(c0 + t);
         const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
         bool load = has_box(st);
         if (load && page >= a.c.n_pages) {
@@ -172,7 +141,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 #pragma unroll
         for (uint32_t kv = 0; kv < 2; ++kv) {
           if (2 * t + kv >= S::SLOTS) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
-          if (*(volatile uint32_t*)&s_gave_up) break;
+          if (has_given_up(&s_gave_up)) break;
           const uint32_t full = b_full + 8 * slot, dst = sm_ring + slot * S::TILE_BYTES + lane * g.box * 128;
           if (lane == 0) bar_expect(full, loaded * S::BLOCKS * g.box * 128);
           __syncwarp();
@@ -183,7 +152,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
         page = next;
         next = after;
-        if (*(volatile uint32_t*)&s_gave_up) break;
+        if (has_given_up(&s_gave_up)) break;
       }
     }
   } else if (warp == 8) {
@@ -233,7 +202,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
             tc_commit(one, b_o + 8 * w);
           }
         }
-        if (*(volatile uint32_t*)&s_gave_up) break;
+        if (has_given_up(&s_gave_up)) break;
         vs += 2;
         if (vs >= S::SLOTS) vs -= S::SLOTS, v_par ^= 1;
         kslot += 2;
@@ -266,7 +235,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     float m = -INFINITY, l = 0.f;
     const float scale = a.r.scale_log2;
     for (uint32_t t = 0; t < n; ++t) {
-      const SlotTile st = slot_tile(ks, hi, sink_tiles, first, c0 + t);
+      const SlotTile st = slots.at(c0 + t);
       bar_wait(b_s + 8 * w, t & 1, &s_gave_up, a.err);
       tc_fence_after();
       uint32_t x[AT_KEYS];
@@ -355,7 +324,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       tc_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive(b_p + 8 * w);
-      if (*(volatile uint32_t*)&s_gave_up) break;
+      if (has_given_up(&s_gave_up)) break;
     }
     if (n > 0) {
       bar_wait(b_o + 8 * w, 0, &s_gave_up, a.err);
@@ -441,39 +410,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 }
 
 // ---- host ------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiled encode_tiled() {
-  static EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-        r != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      p = nullptr;
-    }
-    return (EncodeTiled)p;
-  }();
-  return f;
-}
-bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t* size, const uint64_t* stride,
-              const uint32_t* box) {
-  const EncodeTiled f = encode_tiled();
-  if (!f) return false;
-  cuuint64_t sz[5], st[5];
-  cuuint32_t bx[5], el[5];
-  for (int i = 0; i < dims; ++i) {
-    sz[i] = size[i];
-    bx[i] = box[i];
-    el[i] = 1;
-    if (i) st[i - 1] = stride[i] * 2;
-  }
-  return f(m, dtype == RO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)dims,
-           const_cast<void*>(p), sz, st, bx, el, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 bool attend_tiles_fits(const AttendArgs& a) {
   return a.c.page_shift >= 3 && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
 }
@@ -495,11 +431,8 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype) {
   g.box = std::min<uint32_t>(a.c.page_size, AT_KEYS);
   const uint64_t qs[3] = {a.c.head_dim, a.n_q_heads, a.r.n_tokens}, qt[3] = {1, a.r.q_head, a.r.q_tok};
   const uint32_t qb[3] = {64, a.r.group, g.toks};
-  const uint64_t ps[4] = {a.c.head_dim, a.c.page_size, a.c.n_heads, a.c.n_pages};
-  const uint64_t pt[4] = {1, a.c.slot_stride, a.c.head_stride, a.c.page_stride};
-  const uint32_t pb[4] = {64, g.box, 1, 1};
-  if (!tile_map(&g.q, dtype, a.r.q, 3, qs, qt, qb) || !tile_map(&g.k, dtype, a.c.k, 4, ps, pt, pb) ||
-      !tile_map(&g.v, dtype, a.c.v, 4, ps, pt, pb))
+  if (!tile_map(&g.q, dtype, a.r.q, 3, qs, qt, qb) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
+      !pool_map(&g.v, a.c, a.c.v, dtype, g.box))
     return false;
   const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)

@@ -136,6 +136,35 @@ __device__ __forceinline__ bool sees(const RowsArgs& r, int64_t a, uint32_t j) {
   return (int64_t)j <= a && (r.window == 0u || (int64_t)j > a - (int64_t)r.window || j < r.sinks);
 }
 
+// The slots that a CTA's rows see, cut into tiles of KEYS: tiles over the
+// sinks, then tiles from the window's first slot (rounded down to `box`, the
+// slots that are loaded together) on.  [lo, hi) of a tile are the slots that
+// count.
+struct SlotTile {
+  uint32_t t0, lo, hi;
+  bool sink;
+};
+template <int KEYS>
+struct SlotTiles {
+  uint32_t s_hi, lo, hi, first, sink_tiles, n;
+  __device__ __forceinline__ SlotTiles(const KeySpan& ks, uint32_t box) {
+    s_hi = ks.s_hi;
+    lo = ks.lo;
+    hi = ks.lo + (ks.total - ks.s_hi);
+    first = lo & ~(box - 1u);
+    sink_tiles = (s_hi + KEYS - 1) / KEYS;
+    n = sink_tiles + (hi > lo ? (hi - first + KEYS - 1) / KEYS : 0);
+  }
+  __device__ __forceinline__ SlotTile at(uint32_t t) const {
+    SlotTile s;
+    s.sink = t < sink_tiles;
+    s.t0 = s.sink ? t * KEYS : first + (t - sink_tiles) * KEYS;
+    s.lo = s.sink ? s.t0 : max(s.t0, lo);
+    s.hi = min(s.t0 + KEYS, s.sink ? s_hi : hi);
+    return s;
+  }
+};
+
 // Row tile `tile` (of toks_per_tile tokens): its sequence and its place among
 // that sequence's tiles.  A whole warp calls it; with one tile per sequence
 // (max_new tokens fit a tile) it is the sequence itself.  The host launches

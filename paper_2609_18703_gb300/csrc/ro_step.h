@@ -96,8 +96,8 @@ struct AttendArgs {
   PagedArgs c;
   RowsArgs r;
   uint32_t tiles;            // row tiles per cache head, at most
-  uint32_t chunk;            // keys (tensor-core kernel: tiles of 128) of one CTA, more where
-                             // max_chunks would not reach
+  uint32_t chunk;            // of one CTA, more where max_chunks would not reach: keys
+                             // (attend_rows), stages (attend_few), tiles (attend_tiles)
   uint32_t max_chunks;
   void* out;
   uint64_t out_tok, out_head;
@@ -107,8 +107,13 @@ struct AttendArgs {
   uint32_t* counter;         // [tile], zero between calls
   uint32_t* err;
 };
-// rows of a tile: 16 or 64
-void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype, int rows);
+// at most 16 rows a sequence; slots of a stage, bytes of its runs' partial results
+void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype);
+uint32_t attend_few_keys(uint32_t head_dim);
+size_t attend_few_partial(const AttendArgs& a);
+cudaError_t prepare_attend_few_kernels();
+// tiles of 64 rows, any page size
+void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype);
 cudaError_t prepare_attend_kernels();
 // the tensor-core kernel: whether it takes these sizes, tokens of its CTA,
 // bytes of its runs' partial results; false: the tensors cannot be mapped

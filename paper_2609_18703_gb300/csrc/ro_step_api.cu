@@ -241,9 +241,32 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
   keys = std::max<uint64_t>(keys, 1);
   const uint64_t max_rows = (uint64_t)a.r.max_new * group;
   void* p = nullptr;
-  // More rows a sequence than the small tiles hold: the tensor-core kernel, if
-  // the pages and the group fit its tiles.
-  if (max_rows > 64 && attend_tiles_fits(a)) {
+  // At most 16 rows a sequence: bound by the cache's bytes.
+  if (max_rows <= 16) {
+    const uint64_t work = (uint64_t)cache->n_seqs * cache->n_heads, stage = attend_few_keys(cache->head_dim);
+    if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many sequences and heads", fn);
+    a.tiles = cache->n_seqs;
+    // Runs that fill two CTAs an SM in whole rounds, of at most 96 stages of
+    // 16 KB (longer ones leave SMs idle at the end where lengths differ) and
+    // at least 8 (shorter ones cost more in their start and join than they
+    // save).  One sequence of 100,000 slots, 8 heads of 128: 68 us in one round
+    // of 83 stages, 85 in two of 64; 64 ragged ones of up to 32,000: 432 us at
+    // 96, 476 at 32, 565 at 16.
+    const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
+    const uint64_t each = ceil_div(stages * work, places);
+    a.chunk = (uint32_t)std::max<uint64_t>(8, ceil_div(each, ceil_div(each, 96)));
+    a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 1024);
+    if (a.max_chunks > 1) {
+      RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));
+      a.partial = (float*)p;
+      RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
+      a.counter = (uint32_t*)p;
+    }
+    launch_attend_few(c.launch(), a, cache->dtype);
+    return c.launched(fn);
+  }
+  // More: the tensor-core kernel, if the pages and the group fit its tiles.
+  if (attend_tiles_fits(a)) {
     const uint32_t toks = attend_tile_tokens(group);
     const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
     const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
@@ -261,9 +284,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     }
     if (launch_attend_tiles(c.launch(), a, cache->dtype)) return c.launched(fn);
   }
-  // Rows of a tile: 16 while a sequence's rows fit them (the warps then split
-  // the keys), else 64.
-  const uint32_t rows = max_rows <= 16 ? 16 : 64;
+  const uint32_t rows = 64;
   const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);
   const uint64_t tiles =
       (a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1) * row_tiles;
@@ -282,7 +303,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
     a.counter = (uint32_t*)p;
   }
-  launch_attend_rows(c.launch(), a, cache->dtype, (int)rows);
+  launch_attend_rows(c.launch(), a, cache->dtype);
   return c.launched(fn);
 }
 

@@ -51,6 +51,10 @@ __device__ __forceinline__ void bar_wait_slow(uint32_t bar, uint32_t parity, vol
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* err) {
   if (!bar_try(bar, parity)) bar_wait_slow(bar, parity, gave_up, err);
 }
+// a whole warp, so that it leaves a loop together
+__device__ __forceinline__ bool has_given_up(volatile uint32_t* gave_up) {
+  return __any_sync(0xffffffffu, *gave_up != 0u);
+}
 
 // ---- TMA ----------------------------------------------------------------------------------
 __device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
@@ -192,5 +196,25 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// ---- host: tensor maps -----------------------------------------------------------------------
+// 64-column blocks with the 128-byte swizzle; false: the tensor cannot be mapped
+bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t* size, const uint64_t* stride,
+              const uint32_t* box);
+// a cache's pool, boxes of `box` slots of one page and head
+bool pool_map(CUtensorMap* m, const PagedArgs& c, const void* pool, int dtype, uint32_t box);
+
+struct AttendTileArgs {
+  AttendArgs a;
+  CUtensorMap q, k, v;
+  uint32_t toks;             // tokens of a row tile
+  uint32_t box;              // slots of a TMA box
+};
+struct AttendFewArgs {
+  AttendArgs a;
+  CUtensorMap k, v;
+  uint32_t box;              // slots loaded together
+  uint32_t tma;              // 0: row by row
+};
 
 }  // namespace ro
