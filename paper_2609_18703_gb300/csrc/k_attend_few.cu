@@ -71,80 +71,8 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
   __syncthreads();
 
   if (warp == AF_WARPS) {
-    // ---- loads ----
-    uint32_t slot = 0, parity = 1;
-    if (g.tma) {
-      const uint32_t boxes = KEYS / g.box;          // of a stage, a lane each
-      const uint32_t ahead = 32 / boxes;            // stages whose pages the lanes hold
-      // the page of this lane's box among the boxes of stages t .. t + ahead - 1
-      auto page_of = [&](uint32_t t) -> uint32_t {
-        const uint32_t u = t + lane / boxes;
-        if (u >= n) return 0u;
-        const SlotTile st = slots.at(c0 + u);
-        const uint32_t j = st.t0 + (lane % boxes) * g.box;
-        return j < st.hi && j + g.box > st.lo ? a.c.pages[q.page0 + (j >> a.c.page_shift)] : 0u;
-      };
-      uint32_t next = page_of(0), page = 0;
-      for (uint32_t t = 0; t < n; ++t) {
-        if (t % ahead == 0) {
-          page = next;
-          next = page_of(t + ahead);
-        }
-        const SlotTile st = slots.at(c0 + t);
-        const uint32_t b = lane % boxes, j = st.t0 + b * g.box;
-        bool load = lane / boxes == t % ahead && j < st.hi && j + g.box > st.lo;
-        if (load && page >= a.c.n_pages) {
-          record(a.err, ERR_INVAL);
-          load = false;
-        }
-        const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
-        if (t >= AF_STAGES) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
-        if (has_given_up(&s_gave_up)) break;
-        const uint32_t full = b_full + 8 * slot, dst = sm + slot * AF_STAGE + b * g.box * 128;
-        if (lane == 0) bar_expect(full, 2 * loaded * S::BLOCKS * g.box * 128);
-        __syncwarp();
-        if (load) {
-          const int y = (int)(j & (a.c.page_size - 1u));
-#pragma unroll
-          for (uint32_t x = 0; x < S::BLOCKS; ++x) {
-            tma4(dst + x * S::BLOCK_BYTES, &g.k, x * 64, y, (int)kh, (int)page, full);
-            tma4(dst + S::SIDE + x * S::BLOCK_BYTES, &g.v, x * 64, y, (int)kh, (int)page, full);
-          }
-        }
-        if (++slot == AF_STAGES) slot = 0, parity ^= 1;
-      }
-    } else {
-      constexpr uint32_t CH = DP / 8, PER = 32 / CH;   // 16-byte pieces of a row; rows at a time
-      const uint32_t pc = lane % CH;
-      for (uint32_t t = 0; t < n; ++t) {
-        const SlotTile st = slots.at(c0 + t);
-        if (t >= AF_STAGES) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
-        if (has_given_up(&s_gave_up)) break;
-        for (uint32_t r = lane / CH; r < (uint32_t)KEYS; r += PER) {
-          const uint32_t j = st.t0 + r;
-          bool ok = j >= st.lo && j < st.hi && pc * 8 < D;
-          uint64_t e = 0;
-          if (ok) {
-            uint32_t pi, at;
-            split_slot(a.c, j, &pi, &at);
-            const uint32_t page = a.c.pages[q.page0 + pi];
-            if (page < a.c.n_pages) {
-              e = page * a.c.page_stride + kh * a.c.head_stride + at * a.c.slot_stride + pc * 8;
-            } else {
-              record(a.err, ERR_INVAL);
-              ok = false;
-            }
-          }
-          const uint32_t dst = sm + slot * AF_STAGE + (pc / 8) * S::BLOCK_BYTES + r * 128 + (((pc & 7) ^ (r & 7)) * 16);
-          cp_async16_or_zero(dst, (const T*)a.c.k + e, ok);
-          cp_async16_or_zero(dst + S::SIDE, (const T*)a.c.v + e, ok);
-        }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(b_full + 8 * slot) : "memory");
-        if (++slot == AF_STAGES) slot = 0, parity ^= 1;
-      }
-      cp_async_commit();
-      cp_async_wait<0>();
-    }
+    load_stages<T, DP, KEYS, AF_STAGES, true>(a.c, &g.k, &g.v, g.tma != 0, g.box, slots, c0, n, kh, q.page0, sm, b_full,
+                                              b_empty, &s_gave_up, a.err, [](const SlotTile&) { return true; });
   }
 
   // queries as matrix fragments; rows past the tile's are zero

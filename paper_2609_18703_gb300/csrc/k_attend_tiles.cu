@@ -429,9 +429,7 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype) {
   g.a = a;
   g.toks = AT_ROWS / a.r.group;
   g.box = std::min<uint32_t>(a.c.page_size, AT_KEYS);
-  const uint64_t qs[3] = {a.c.head_dim, a.n_q_heads, a.r.n_tokens}, qt[3] = {1, a.r.q_head, a.r.q_tok};
-  const uint32_t qb[3] = {64, a.r.group, g.toks};
-  if (!tile_map(&g.q, dtype, a.r.q, 3, qs, qt, qb) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
+  if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
       !pool_map(&g.v, a.c, a.c.v, dtype, g.box))
     return false;
   const bool narrow = a.c.head_dim <= 64;

@@ -1,4 +1,5 @@
-// k_weigh.cu — the attention weight cached tokens gathered (ro_cache_weigh).
+// k_weigh.cu — the attention weight cached tokens gathered (ro_cache_weigh),
+// where pages or groups fit no tensor tile.
 //
 //   score_j = decay past_j + sum_r exp2(x_rj - lse_r log2(e)) over the rows r
 //   that see slot j; x_rj = scale log2(e) q_r.k_j.
@@ -6,8 +7,8 @@
 // A CTA takes 64 slots of one cache head of one sequence and runs over the
 // query rows that can see one of them: keys are the rows of the matrix
 // product and stay in registers, query rows its columns, so a key's sum stays
-// in the four lanes that hold its row and is added in a fixed order.  With
-// single tokens it is bound by reading K, with chunks by the exponentials.
+// in the four lanes that hold its row and is added in a fixed order.  Bound by
+// mma.sync and the exponentials between its products.
 #include <algorithm>
 
 #include "ro_step.cuh"
@@ -34,16 +35,8 @@ __global__ void __launch_bounds__(WG_THREADS) weigh_kernel(const __grid_constant
   }
   if (j0 >= len) return;
   const uint32_t jn = min((uint32_t)WG_KEYS, len - (uint32_t)j0), j_lo = (uint32_t)j0, j_hi = j_lo + jn - 1;
-  // the tokens that can see one of these slots
-  uint32_t i0 = 0, i1 = q.n;
-  {
-    const int64_t f = (int64_t)j_lo - q.first;
-    if (f > 0) i0 = (uint32_t)min((int64_t)q.n, f);
-    if (a.r.window && j_lo >= a.r.sinks) {
-      const int64_t e = (int64_t)j_hi + a.r.window - q.first;   // a < j + window
-      i1 = (uint32_t)max((int64_t)i0, min((int64_t)q.n, e));
-    }
-  }
+  uint32_t i0, i1;
+  seeing_tokens(q, a.r, j_lo, j_hi, &i0, &i1);
   const uint32_t G = a.r.group, D = a.c.head_dim;
   const uint32_t rows = (i1 - i0) * G;
   const uint32_t sm = step_smem(s_tile);

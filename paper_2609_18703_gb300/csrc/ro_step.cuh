@@ -165,6 +165,20 @@ struct SlotTiles {
   }
 };
 
+// The new tokens [i0, i1) of a sequence that can see one of the slots
+// [j_lo, j_hi].
+__device__ __forceinline__ void seeing_tokens(const SeqInfo& q, const RowsArgs& r, uint32_t j_lo, uint32_t j_hi,
+                                              uint32_t* i0, uint32_t* i1) {
+  *i0 = 0;
+  *i1 = q.n;
+  const int64_t f = (int64_t)j_lo - q.first;
+  if (f > 0) *i0 = (uint32_t)min((int64_t)q.n, f);
+  if (r.window && j_lo >= r.sinks) {
+    const int64_t e = (int64_t)j_hi + r.window - q.first;   // a < j + window
+    *i1 = (uint32_t)max((int64_t)*i0, min((int64_t)q.n, e));
+  }
+}
+
 // Row tile `tile` (of toks_per_tile tokens): its sequence and its place among
 // that sequence's tiles.  A whole warp calls it; with one tile per sequence
 // (max_new tokens fit a tile) it is the sequence itself.  The host launches

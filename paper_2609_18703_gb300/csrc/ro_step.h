@@ -123,20 +123,32 @@ size_t attend_tiles_partial(const AttendArgs& a);
 bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype);
 cudaError_t prepare_attend_tiles_kernels();
 
-constexpr int WG_THREADS = 128;
-constexpr uint32_t WG_KEYS = 64, WG_ROWS = 64;
 struct WeighArgs {
   PagedArgs c;
   RowsArgs r;
   const float* lse;
   uint32_t n_q_heads;
   float decay;
-  const float* past;
+  const float* past;         // optional
   float* score;
   uint64_t score_cap;
-  uint32_t tiles;            // of WG_KEYS slots up to score_cap
+  uint32_t tiles;            // CTAs along score_cap for each sequence and head, at most
+  uint32_t chunk;            // weigh_few: stages of a CTA
   uint32_t* err;
 };
+// at most 16 rows a sequence; slots of a stage
+void launch_weigh_few(const LaunchCfg& L, const WeighArgs& a, int dtype);
+uint32_t weigh_few_keys(uint32_t head_dim);
+cudaError_t prepare_weigh_few_kernels();
+// the tensor-core kernel: whether it takes these sizes, slots of its CTA;
+// false: the tensors cannot be mapped
+constexpr uint32_t WT_KEYS = 128;
+bool weigh_tiles_fits(const WeighArgs& a);
+bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype);
+cudaError_t prepare_weigh_tiles_kernels();
+// any page size and group
+constexpr int WG_THREADS = 128;
+constexpr uint32_t WG_KEYS = 64, WG_ROWS = 64;
 void launch_weigh(const LaunchCfg& L, const WeighArgs& a, int dtype);
 
 // ---- evict ------------------------------------------------------------------------------

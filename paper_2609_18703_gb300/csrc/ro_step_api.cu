@@ -319,8 +319,9 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   if ((n_tokens && !d_lse) || (score_cap && !d_score)) return c.refuse(RO_E_INVAL, "%s: NULL argument", fn);
   if (!std::isfinite(decay)) return c.refuse(RO_E_INVAL, "%s: decay must be finite", fn);
   if (score_cap >= 0x80000000ull) return c.refuse(RO_E_OVERFLOW, "%s: 2^31 scores a head or more", fn);
-  const uint64_t tiles = ceil_div(score_cap, WG_KEYS);
-  if (tiles * cache->n_seqs > MAX_GRID / cache->n_heads) return c.refuse(RO_E_OVERFLOW, "%s: too many scores", fn);
+  const uint64_t units = (uint64_t)cache->n_seqs * cache->n_heads;
+  if (units > MAX_GRID || ceil_div(score_cap, WG_KEYS) > MAX_GRID / units)
+    return c.refuse(RO_E_OVERFLOW, "%s: too many scores", fn);
   if (score_cap == 0) return RO_OK;
   RO_TRY(c.begin());
   WeighArgs a = {};
@@ -333,8 +334,19 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   a.past = d_past;
   a.score = d_score;
   a.score_cap = score_cap;
-  a.tiles = (uint32_t)tiles;
   a.err = c.err();
+  if ((uint64_t)a.r.max_new * a.r.group <= 16) {
+    // bound by the keys' bytes: runs of stages as in the attention of few rows
+    const uint64_t stages = ceil_div(score_cap, weigh_few_keys(cache->head_dim));
+    const uint64_t each = ceil_div(stages * units, (uint64_t)c.sms() * 2);
+    a.chunk = (uint32_t)std::max<uint64_t>(6, ceil_div(each, ceil_div(each, 48)));
+    a.tiles = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 65535);
+    launch_weigh_few(c.launch(), a, cache->dtype);
+    return c.launched(fn);
+  }
+  a.tiles = (uint32_t)ceil_div(score_cap, WT_KEYS);
+  if (n_tokens && weigh_tiles_fits(a) && launch_weigh_tiles(c.launch(), a, cache->dtype)) return c.launched(fn);
+  a.tiles = (uint32_t)ceil_div(score_cap, WG_KEYS);
   launch_weigh(c.launch(), a, cache->dtype);
   return c.launched(fn);
 }

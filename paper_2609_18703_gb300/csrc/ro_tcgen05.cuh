@@ -197,18 +197,121 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// ---- a ring of stages of slots -----------------------------------------------------------------
+// One warp's work: keep a ring of STAGES stages full with the tiles
+// [c0, c0 + n) of one sequence and head, KEYS slots of DP dimensions each, keys
+// (and values behind them).  want(tile): false leaves a tile unloaded.  By TMA
+// a box (part of a page) a lane; without, row by row with cp.async, 32 arrivals
+// on a full stage instead of one.
+template <typename T, int DP, int KEYS, uint32_t STAGES, bool VALUES, class Want>
+__device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMap* km, const CUtensorMap* vm, bool tma,
+                                            uint32_t box, const SlotTiles<KEYS>& slots, uint32_t c0, uint32_t n,
+                                            uint32_t kh, uint64_t page0, uint32_t sm, uint32_t b_full, uint32_t b_empty,
+                                            uint32_t* gave_up, uint32_t* err, Want want) {
+  constexpr uint32_t BLOCKS = DP / 64, BLOCK_BYTES = KEYS * 128, SIDE = BLOCKS * BLOCK_BYTES;
+  constexpr uint32_t STAGE = VALUES ? 2 * SIDE : SIDE;
+  const uint32_t lane = threadIdx.x & 31u;
+  uint32_t slot = 0, parity = 1;
+  if (tma) {
+    const uint32_t boxes = KEYS / box;            // of a stage, a lane each
+    const uint32_t ahead = 32 / boxes;            // stages whose pages the lanes hold
+    auto has_box = [&](const SlotTile& st, uint32_t j) { return j < st.hi && j + box > st.lo && want(st); };
+    // the page of this lane's box among the boxes of stages t .. t + ahead - 1
+    auto page_of = [&](uint32_t t) -> uint32_t {
+      const uint32_t u = t + lane / boxes;
+      if (u >= n) return 0u;
+      const SlotTile st = slots.at(c0 + u);
+      const uint32_t j = st.t0 + (lane % boxes) * box;
+      return has_box(st, j) ? c.pages[page0 + (j >> c.page_shift)] : 0u;
+    };
+    uint32_t next = page_of(0), page = 0;
+    for (uint32_t t = 0; t < n; ++t) {
+      if (t % ahead == 0) {
+        page = next;
+        next = page_of(t + ahead);
+      }
+      const SlotTile st = slots.at(c0 + t);
+      const uint32_t b = lane % boxes, j = st.t0 + b * box;
+      bool load = lane / boxes == t % ahead && has_box(st, j);
+      if (load && page >= c.n_pages) {
+        record(err, ERR_INVAL);
+        load = false;
+      }
+      const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
+      if (t >= STAGES) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
+      if (has_given_up(gave_up)) break;
+      const uint32_t full = b_full + 8 * slot, dst = sm + slot * STAGE + b * box * 128;
+      if (lane == 0) bar_expect(full, (VALUES ? 2 : 1) * loaded * BLOCKS * box * 128);
+      __syncwarp();
+      if (load) {
+        const int y = (int)(j & (c.page_size - 1u));
+#pragma unroll
+        for (uint32_t x = 0; x < BLOCKS; ++x) {
+          tma4(dst + x * BLOCK_BYTES, km, x * 64, y, (int)kh, (int)page, full);
+          if (VALUES) tma4(dst + SIDE + x * BLOCK_BYTES, vm, x * 64, y, (int)kh, (int)page, full);
+        }
+      }
+      if (++slot == STAGES) slot = 0, parity ^= 1;
+    }
+  } else {
+    constexpr uint32_t CH = DP / 8, PER = 32 / CH;   // 16-byte pieces of a row; rows at a time
+    const uint32_t pc = lane % CH;
+    for (uint32_t t = 0; t < n; ++t) {
+      const SlotTile st = slots.at(c0 + t);
+      const bool wanted = want(st);
+      if (t >= STAGES) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
+      if (has_given_up(gave_up)) break;
+      for (uint32_t r = lane / CH; r < (uint32_t)KEYS; r += PER) {
+        const uint32_t j = st.t0 + r;
+        bool ok = wanted && j >= st.lo && j < st.hi && pc * 8 < c.head_dim;
+        uint64_t e = 0;
+        if (ok) {
+          uint32_t pi, at;
+          split_slot(c, j, &pi, &at);
+          const uint32_t page = c.pages[page0 + pi];
+          if (page < c.n_pages) {
+            e = page * c.page_stride + kh * c.head_stride + at * c.slot_stride + pc * 8;
+          } else {
+            record(err, ERR_INVAL);
+            ok = false;
+          }
+        }
+        const uint32_t dst = sm + slot * STAGE + (pc / 8) * BLOCK_BYTES + r * 128 + (((pc & 7) ^ (r & 7)) * 16);
+        cp_async16_or_zero(dst, (const T*)c.k + e, ok);
+        if (VALUES) cp_async16_or_zero(dst + SIDE, (const T*)c.v + e, ok);
+      }
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(b_full + 8 * slot) : "memory");
+      if (++slot == STAGES) slot = 0, parity ^= 1;
+    }
+    cp_async_commit();
+    cp_async_wait<0>();
+  }
+}
+
 // ---- host: tensor maps -----------------------------------------------------------------------
 // 64-column blocks with the 128-byte swizzle; false: the tensor cannot be mapped
 bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t* size, const uint64_t* stride,
               const uint32_t* box);
 // a cache's pool, boxes of `box` slots of one page and head
 bool pool_map(CUtensorMap* m, const PagedArgs& c, const void* pool, int dtype, uint32_t box);
+// the query rows, boxes of `toks` tokens times one group of heads
+bool rows_map(CUtensorMap* m, const RowsArgs& r, uint32_t head_dim, uint32_t n_q_heads, int dtype, uint32_t toks);
 
 struct AttendTileArgs {
   AttendArgs a;
   CUtensorMap q, k, v;
   uint32_t toks;             // tokens of a row tile
   uint32_t box;              // slots of a TMA box
+};
+struct WeighFewArgs {
+  WeighArgs a;
+  CUtensorMap k;
+  uint32_t box, tma;
+};
+struct WeighTileArgs {
+  WeighArgs a;
+  CUtensorMap q, k;
+  uint32_t toks, box;
 };
 struct AttendFewArgs {
   AttendArgs a;

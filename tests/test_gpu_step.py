@@ -384,9 +384,10 @@ def test_weigh(ctx, dtype, dim, heads, kv, page, news, window, sinks):
     base = i64(starts(news))
     ok(ctx, ro.ro_cache_weigh(ctx, cache, base, max(news), i32(lens), dq, scale, window, sinks, lse, 0.75, past, score))
     in_place = past.clone()
-    ok(ctx, ro.ro_cache_weigh(ctx, cache, base, 0, i32(lens), dq, scale, window, sinks, lse, 0.75, in_place, in_place))
+    ok(ctx, ro.ro_cache_weigh(ctx, cache, base, max(news), i32(lens), dq, scale, window, sinks, lse, 0.75, in_place,
+                              in_place))
     fresh = torch.full((4, kv, cap), -5.0, device="cuda")
-    ok(ctx, ro.ro_cache_weigh(ctx, cache, base, max(news), i32(lens), dq, scale, window, sinks, lse, 1.0, None, fresh))
+    ok(ctx, ro.ro_cache_weigh(ctx, cache, base, 0, i32(lens), dq, scale, window, sinks, lse, 1.0, None, fresh))
     sync_ok(ctx)
     t = starts(news)
     for s, L in enumerate(lens):
