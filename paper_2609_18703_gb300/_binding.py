@@ -66,6 +66,8 @@ class ro_rope(C.Structure):
         if not 1 <= len(pairs) <= 4:
             raise ValueError("ro_rope: 1 to 4 axes")
         super().__init__(len(pairs), (C.c_uint32 * 4)(*pairs), int(interleaved), float(base))
+        self._axes = len(pairs)
+        self._ref = C.byref(self)
 
 
 class ro_cache(C.Structure):
@@ -86,6 +88,9 @@ class ro_cache(C.Structure):
         super().__init__(_ptr(d_k), _ptr(d_v), _dtype(d_k), n_pages, slots, heads, dim, d_page_base.numel() - 1,
                          d_k.stride(0), d_k.stride(1), d_k.stride(2), _list(d_page_base, 8), _list(d_pages, 4))
         self._tensors = (d_k, d_v, d_page_base, d_pages)
+        self._kind = (d_k.dtype, dim)             # what rows beside the cache must be
+        self._units = (d_page_base.numel() - 1, heads)
+        self._ref = C.byref(self)
 
 
 _lib = None
@@ -153,6 +158,8 @@ def load(path: Optional[str] = None):
 def _ptr(x):
     if x is None or isinstance(x, int):
         return x
+    if getattr(x, "is_cuda", False):
+        return x.data_ptr()
     data_ptr = getattr(x, "data_ptr", None)
     if data_ptr is None:
         raise TypeError(f"cannot pass {type(x)!r} as a pointer")
@@ -163,28 +170,36 @@ def _ptr(x):
     return data_ptr()
 
 
+_DTYPES = {}   # torch dtype -> RO_*, filled as they come up (torch is not imported here)
+
+
 def _dtype(x) -> int:
-    name = str(x.dtype)
-    try:
-        return {"torch.bfloat16": RO_BF16, "torch.float16": RO_F16, "torch.float32": RO_F32}[name]
-    except KeyError:
-        raise ValueError(f"{name} is not a type of the model-step operators") from None
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        name = str(x.dtype)
+        code = {"torch.bfloat16": RO_BF16, "torch.float16": RO_F16, "torch.float32": RO_F32}.get(name)
+        if code is None:
+            raise ValueError(f"{name} is not a type of the model-step operators")
+        _DTYPES[x.dtype] = code
+    return code
 
 
 def _list(x, size):
     """A dense integer or float array of elements of `size` bytes."""
-    if x is not None and not isinstance(x, int) and (x.element_size() != size or not x.is_contiguous()):
+    if x is None or isinstance(x, int):
+        return x
+    if x.itemsize != size or not x.is_contiguous():
         raise ValueError(f"argument must be contiguous, {size} bytes an element")
-    return _ptr(x)
+    return x.data_ptr() if x.is_cuda else _ptr(x)
 
 
-def _rows(x, like=None):
-    """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
-    if x.dim() != 3 or x.stride(2) != 1:
-        raise ValueError("argument must be [tokens, heads, head_dim], contiguous in the last dimension")
-    if like is not None and (x.dtype != like.dtype or x.shape[2] != like.shape[-1]):
-        raise ValueError("argument differs from the cache in type or head_dim")
-    return _ptr(x), x.stride(0), x.stride(1)
+def _rows(x, dtype, dim):
+    """(pointer, token stride, head stride) of a [tokens, heads, dim] tensor of the type."""
+    tok, head, one = x.stride()
+    if one != 1 or x.dtype is not dtype or x.shape[2] != dim:
+        raise ValueError("argument must be [tokens, heads, head_dim], contiguous in the last dimension, of the others' "
+                         "type and head_dim")
+    return x.data_ptr() if x.is_cuda else _ptr(x), tok, head
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -395,58 +410,66 @@ def ro_expand_noalloc(d_counts, n_parents, d_offsets, d_child_parent, d_child_or
 # cache and the rotary for their structs; the order of the rest is the C order.
 def ro_rotary(ctx, d_x, d_out, d_pos, rope, inverse: bool = False) -> int:
     """Turn d_x by its positions into d_out (which may be d_x)."""
-    if d_x.shape != d_out.shape or d_x.dtype != d_out.dtype or d_pos.numel() != d_x.shape[0] * rope.n_axes:
+    shape, dtype = d_x.shape, d_x.dtype
+    n, heads, dim = shape
+    if shape != d_out.shape or d_pos.numel() != n * rope._axes:
         raise ValueError("ro_rotary: x, out and positions do not fit one another")
-    return load().ro_rotary(ctx, _dtype(d_x), *_rows(d_x), *_rows(d_out), *d_x.shape, _list(d_pos, 4), C.byref(rope),
-                            int(inverse))
+    return (_lib or load()).ro_rotary(ctx, _DTYPES.get(dtype) or _dtype(d_x), *_rows(d_x, dtype, dim),
+                                      *_rows(d_out, dtype, dim), n, heads, dim, _list(d_pos, 4), rope._ref, inverse)
 
 
 def ro_cache_append(ctx, cache, d_tok_base, d_tok_seq, d_len, d_pos, rope, d_q, d_q_out, d_k, d_v) -> int:
     """Put a step's tokens into the cache, k and q turned (rope None: as they
     are; d_q None: keys and values alone)."""
-    pool = cache._tensors[0]
-    n = d_k.shape[0]
-    if d_k.shape != d_v.shape or d_k.shape[1] != cache.n_heads or (d_q is not None and (
-            d_q.shape != d_q_out.shape or d_q.shape[0] != n)) or (rope is not None and d_pos.numel() != n * rope.n_axes) \
-            or d_tok_seq.numel() < n:
+    kind = cache._kind
+    shape = d_k.shape
+    n = shape[0]
+    if d_v.shape != shape or shape[1] != cache._units[1] or d_tok_seq.numel() < n or (
+            rope is not None and d_pos.numel() != n * rope._axes):
         raise ValueError("ro_cache_append: tensors do not fit one another")
-    q = _rows(d_q, pool) + (d_q.shape[1],) + _rows(d_q_out, pool) if d_q is not None else (None, 0, 0, 0, None, 0, 0)
-    return load().ro_cache_append(ctx, C.byref(cache), _list(d_tok_base, 8), _list(d_tok_seq, 4), n, _list(d_len, 4),
-                                  _list(d_pos, 4), None if rope is None else C.byref(rope), *q, *_rows(d_k, pool),
-                                  *_rows(d_v, pool))
+    if d_q is None:
+        q = (None, 0, 0, 0, None, 0, 0)
+    else:
+        shape = d_q.shape
+        if shape != d_q_out.shape or shape[0] != n:
+            raise ValueError("ro_cache_append: tensors do not fit one another")
+        q = (*_rows(d_q, *kind), shape[1], *_rows(d_q_out, *kind))
+    return (_lib or load()).ro_cache_append(ctx, cache._ref, _list(d_tok_base, 8), _list(d_tok_seq, 4), n,
+                                            _list(d_len, 4), _list(d_pos, 4), None if rope is None else rope._ref, *q,
+                                            *_rows(d_k, *kind), *_rows(d_v, *kind))
 
 
 def ro_cache_attend(ctx, cache, d_tok_base, max_new, d_len, max_len, d_q, scale, window, sinks, d_out,
                     d_lse=None) -> int:
     """Attention of a step's tokens over the cache that holds them."""
-    pool = cache._tensors[0]
-    if d_out.shape != d_q.shape or (d_lse is not None and d_lse.shape != d_q.shape[:2]):
+    kind, shape = cache._kind, d_q.shape
+    if d_out.shape != shape or (d_lse is not None and d_lse.shape != shape[:2]):
         raise ValueError("ro_cache_attend: q, out and lse do not fit one another")
-    return load().ro_cache_attend(ctx, C.byref(cache), _list(d_tok_base, 8), d_q.shape[0], max_new, _list(d_len, 4),
-                                  max_len, *_rows(d_q, pool), d_q.shape[1], scale, window, sinks,
-                                  *_rows(d_out, pool), _list(d_lse, 4))
+    return (_lib or load()).ro_cache_attend(ctx, cache._ref, _list(d_tok_base, 8), shape[0], max_new, _list(d_len, 4),
+                                            max_len, *_rows(d_q, *kind), shape[1], scale, window, sinks,
+                                            *_rows(d_out, *kind), _list(d_lse, 4))
 
 
 def ro_cache_weigh(ctx, cache, d_tok_base, max_new, d_len, d_q, scale, window, sinks, d_lse, decay, d_past,
                    d_score) -> int:
     """Attention weight per cached token, d_score [sequences, heads, slots] from
     d_past (None: nothing yet; may be d_score)."""
-    if d_lse.shape != d_q.shape[:2] or d_score.shape[:2] != (cache.n_seqs, cache.n_heads) or (
-            d_past is not None and d_past.shape != d_score.shape):
+    shape, slots = d_q.shape, d_score.shape
+    if d_lse.shape != shape[:2] or slots[:2] != cache._units or (d_past is not None and d_past.shape != slots):
         raise ValueError("ro_cache_weigh: q, lse and scores do not fit one another")
-    return load().ro_cache_weigh(ctx, C.byref(cache), _list(d_tok_base, 8), d_q.shape[0], max_new, _list(d_len, 4),
-                                 *_rows(d_q, cache._tensors[0]), d_q.shape[1], scale, window, sinks, _list(d_lse, 4),
-                                 decay, _list(d_past, 4), _list(d_score, 4), d_score.shape[2])
+    return (_lib or load()).ro_cache_weigh(ctx, cache._ref, _list(d_tok_base, 8), shape[0], max_new, _list(d_len, 4),
+                                           *_rows(d_q, *cache._kind), shape[1], scale, window, sinks, _list(d_lse, 4),
+                                           decay, _list(d_past, 4), _list(d_score, 4), slots[2])
 
 
 def ro_cache_evict(ctx, cache, d_len, d_score, budget, sinks, recent, d_dst_base, d_dst_pages, d_keep, d_len_out,
                    d_score_out=None) -> int:
     """Cut every sequence back to its `budget` heaviest tokens, in new pages;
     d_keep [sequences, heads, budget]."""
-    units = (cache.n_seqs, cache.n_heads)
-    if d_score.shape[:2] != units or d_keep.shape != units + (budget,) or d_dst_base.numel() != cache.n_seqs + 1 or (
-            d_score_out is not None and d_score_out.shape != d_score.shape):
+    units, slots = cache._units, d_score.shape
+    if slots[:2] != units or d_keep.shape != units + (budget,) or d_dst_base.numel() != units[0] + 1 or (
+            d_score_out is not None and d_score_out.shape != slots):
         raise ValueError("ro_cache_evict: scores, kept slots or page lists do not fit the cache")
-    return load().ro_cache_evict(ctx, C.byref(cache), _list(d_len, 4), _list(d_score, 4), d_score.shape[2], budget,
-                                 sinks, recent, _list(d_dst_base, 8), _list(d_dst_pages, 4), _list(d_keep, 4),
-                                 _list(d_len_out, 4), _list(d_score_out, 4))
+    return (_lib or load()).ro_cache_evict(ctx, cache._ref, _list(d_len, 4), _list(d_score, 4), slots[2], budget,
+                                           sinks, recent, _list(d_dst_base, 8), _list(d_dst_pages, 4), _list(d_keep, 4),
+                                           _list(d_len_out, 4), _list(d_score_out, 4))

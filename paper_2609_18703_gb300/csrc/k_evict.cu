@@ -1,11 +1,13 @@
 // k_evict.cu — cut a cache back to its heaviest tokens (ro_cache_evict).
 //
-// evict_select  One CTA per sequence and cache head.  Of the slots between the
-//               sinks and the recent ones the k largest scores stay: scores map
-//               to 32-bit keys that order alike (NaN lowest, -0 as 0), four
-//               passes of 8 bits find the k-th largest key T, and a last pass
-//               in slot order writes the slots with a key above T and the first
-//               ones equal to it.  Reads each score five times, from L2.
+// evict_select  A cluster of 1 to 8 CTAs per sequence and cache head, a run of
+//               slots each.  Of the slots between the sinks and the recent ones
+//               the k largest scores stay: scores map to 32-bit keys that order
+//               alike (NaN lowest, -0 as 0), read once into shared memory where
+//               they fit; three passes of 11, 11 and 10 bits find the k-th
+//               largest key T (histograms summed over the cluster), and a last
+//               pass in slot order writes the slots with a key above T and the
+//               first ones equal to it.  Bound by the latency of its steps.
 // evict_move    Kept rows of K and V to the new pages: bound by reading and
 //               writing them once; 16 bytes a thread.
 #include <algorithm>
@@ -37,90 +39,177 @@ __device__ __forceinline__ uint32_t cached(const EvictArgs& a, uint32_t s, bool 
   return len;
 }
 
+// ---- clusters ------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// every thread of the cluster; shared memory written before it is seen after it
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of `p` of this CTA's shared memory in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t cluster_at(const uint32_t* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(step_smem(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ uint32_t cluster_load(const uint32_t* p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_at(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_add(const uint32_t* p, uint32_t rank, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(cluster_at(p, rank)), "r"(v) : "memory");
+}
+// Exclusive prefix of one value per thread over 1,024 threads, and the total;
+// one barrier (every warp scans the warps' totals for itself).  smem: 32 words
+// that no earlier call of this kernel used.
+template <class T>
+__device__ __forceinline__ T select_scan(T v, T* smem, T* total) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const T inc = warp_incl_scan(v);
+  if (lane == 31) smem[wid] = inc;
+  __syncthreads();
+  const T all = warp_incl_scan(smem[lane]);
+  const T before = __shfl_sync(0xffffffffu, all, wid > 0 ? wid - 1 : 0);
+  *total = __shfl_sync(0xffffffffu, all, 31);
+  return (wid > 0 ? before : T(0)) + inc - v;
+}
+
+constexpr uint32_t ES_BINS = 2048;
+
 __global__ void __launch_bounds__(ES_THREADS) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ uint32_t s_hist[256];
-  __shared__ uint32_t s_scan[33];
-  __shared__ uint32_t s_digit, s_left;
+  extern __shared__ uint32_t s_keys[];          // [cached]
+  __shared__ uint32_t s_hist[ES_BINS];          // this CTA's counts of a pass
+  __shared__ uint32_t s_sum[3][ES_BINS];        // the cluster's, a pass each
+  __shared__ uint32_t s_scan[3][32];
+  __shared__ unsigned long long s_scan2[32];
+  __shared__ uint32_t s_digit[3], s_left[3], s_total[2];
   wait_predecessor();
-  const uint32_t tid = threadIdx.x;
-  const uint32_t s = blockIdx.x / a.c.n_heads, h = blockIdx.x - s * a.c.n_heads;
-  const uint32_t len = cached(a, s, tid == 0 && h == 0);
-  const uint64_t row = (uint64_t)blockIdx.x * a.score_cap;
+  const uint32_t tid = threadIdx.x, nc = a.cluster, rank = nc > 1 ? cluster_rank() : 0;
+  const uint32_t unit = blockIdx.x / nc;
+  const uint32_t s = unit / a.c.n_heads, h = unit - s * a.c.n_heads;
+  const uint32_t len = cached(a, s, tid == 0 && h == 0 && rank == 0);
+  const uint64_t row = (uint64_t)unit * a.score_cap;
   const float* score = a.score + row;
-  uint32_t* keep = a.keep + (uint64_t)blockIdx.x * a.budget;
+  uint32_t* keep = a.keep + (uint64_t)unit * a.budget;
   float* out = a.score_out ? a.score_out + row : nullptr;
-  const uint32_t kept = min(len, a.budget);
-  if (h == 0 && tid == 0) a.len_out[s] = kept;
-  if (len <= a.budget) {
-    for (uint32_t j = tid; j < len; j += ES_THREADS) {
+  const uint32_t t0 = rank * ES_THREADS + tid, step = nc * ES_THREADS;   // this thread among the cluster's
+  if (h == 0 && t0 == 0) a.len_out[s] = min(len, a.budget);
+  if (len <= a.budget) {                        // (the whole cluster)
+    for (uint32_t j = t0; j < len; j += step) {
       keep[j] = j;
       if (out) out[j] = score[j];
     }
     return;
   }
   const uint32_t lo = a.sinks, hi = len - a.recent;
-  uint32_t left = a.budget - a.sinks - a.recent;   // still to choose among equal prefixes
-  uint32_t prefix = 0, mask = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) s_hist[tid] = 0;
-    __syncthreads();
-    for (uint32_t j = lo + tid; j < hi; j += ES_THREADS) {
-      const uint32_t k = score_key(score[j]);
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    // the digit whose keys, counted from the largest, reach `left`
-    uint32_t c = 0, total;
-    if (tid < 256) c = s_hist[255 - tid];
-    const uint32_t above = block_excl_scan(c, s_scan, &total);
-    if (left > 0 && tid < 256 && above < left && above + c >= left) {
-      s_digit = 255 - tid;
-      s_left = left - above;
-    }
-    if (left == 0 && tid == 0) {   // nothing to choose: a threshold above every key
-      s_digit = 255;
-      s_left = 0;
-    }
-    __syncthreads();
-    prefix |= s_digit << shift;
-    mask |= 255u << shift;
-    left = s_left;
-    __syncthreads();
-  }
-  // keys above prefix, and the first `left` equal to it, in slot order
-  for (uint32_t j = tid; j < a.sinks; j += ES_THREADS) {
+  for (uint32_t j = t0; j < a.sinks; j += step) {
     keep[j] = j;
     if (out) out[j] = score[j];
   }
-  uint32_t done = 0, ties = 0;
-  for (uint32_t j0 = lo; j0 < hi; j0 += ES_THREADS) {
-    const uint32_t j = j0 + tid;
-    uint32_t gt = 0, eq = 0;
-    float x = 0.f;
-    if (j < hi) {
-      x = score[j];
-      const uint32_t k = score_key(x);
-      gt = k > prefix;
-      eq = k == prefix;
-    }
-    uint32_t total;
-    // both counts in one scan: at most 1,024 each
-    const uint32_t e = block_excl_scan(gt | (eq << 16), s_scan, &total);
-    const uint32_t eq_before = ties + (e >> 16), gt_before = done + (e & 0xFFFFu);
-    const uint32_t eq_taken = min(eq_before, left);
-    if (gt || (eq && eq_before < left)) {
-      const uint32_t at = a.sinks + gt_before + eq_taken;
-      keep[at] = j;
-      if (out) out[at] = x;
-    }
-    done += total & 0xFFFFu;
-    ties += total >> 16;
-  }
-  for (uint32_t j = tid; j < a.recent; j += ES_THREADS) {
+  for (uint32_t j = t0; j < a.recent; j += step) {
     const uint32_t at = a.budget - a.recent + j;
     keep[at] = hi + j;
     if (out) out[at] = score[hi + j];
   }
+  // this CTA's run of the slots between, [j0, j0 + n)
+  const uint32_t each = (hi - lo + nc - 1) / nc, j0 = min(hi, lo + rank * each), n = min(each, hi - j0);
+  const uint32_t held = min(n, a.cached);       // of them in shared memory, the rest read again
+#pragma unroll 4
+  for (uint32_t i = tid; i < held; i += ES_THREADS) s_keys[i] = score_key(score[j0 + i]);
+  for (uint32_t i = tid; i < ES_BINS; i += ES_THREADS) s_hist[i] = s_sum[0][i] = s_sum[1][i] = s_sum[2][i] = 0;
+  if (tid < 3) {                                // nothing to choose: a threshold above every key
+    s_digit[tid] = tid == 2 ? 1023u : ES_BINS - 1;
+    s_left[tid] = 0;
+  }
+  if (nc > 1)
+    cluster_sync();                             // every CTA's sums are zero
+  else
+    __syncthreads();
+  auto key = [&](uint32_t i) { return i < held ? s_keys[i] : score_key(score[j0 + i]); };
+  uint32_t left = a.budget - a.sinks - a.recent;   // still to choose among equal prefixes
+  uint32_t prefix = 0, mask = 0;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int bits = pass == 2 ? 10 : 11, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t bins = 1u << bits;
+    uint32_t* hist = nc > 1 ? s_hist : s_sum[pass];
+    for (uint32_t i = tid; i < n; i += ES_THREADS) {
+      const uint32_t k = key(i);
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+    }
+    if (nc > 1) {                               // bins that hold something go to every CTA's sums
+      __syncthreads();
+      for (uint32_t i = tid; i < bins; i += ES_THREADS) {
+        const uint32_t c = s_hist[i];
+        if (c == 0) continue;
+        for (uint32_t r = 0; r < nc; ++r) cluster_add(&s_sum[pass][i], r, c);
+        s_hist[i] = 0;
+      }
+      cluster_sync();
+    } else {
+      __syncthreads();
+    }
+    // the digit whose keys, counted from the largest, reach `left`: two bins a thread, largest first
+    const uint32_t b1 = bins - 1 - 2 * tid, b0 = b1 - 1;
+    uint32_t c1 = 0, c0 = 0, total;
+    if (2 * tid < bins) {
+      c1 = s_sum[pass][b1];
+      c0 = s_sum[pass][b0];
+    }
+    const uint32_t above = select_scan(c1 + c0, s_scan[pass], &total);
+    if (left > 0 && above < left && above + c1 + c0 >= left) {
+      const bool first = above + c1 >= left;
+      s_digit[pass] = first ? b1 : b0;
+      s_left[pass] = left - above - (first ? 0 : c1);
+    }
+    __syncthreads();
+    prefix |= s_digit[pass] << shift;
+    mask |= (bins - 1) << shift;
+    left = s_left[pass];
+  }
+  // Keys above prefix, and the first `left` equal to it, in slot order: a
+  // thread takes neighbouring slots, an odd number of them (the banks of
+  // shared memory), and counts before it writes.
+  const uint32_t own = ((n + ES_THREADS - 1) / ES_THREADS) | 1u, f0 = min(n, tid * own), f1 = min(n, f0 + own);
+  uint32_t gt = 0, eq = 0;
+  for (uint32_t i = f0; i < f1; ++i) {
+    const uint32_t k = key(i);
+    gt += k > prefix;
+    eq += k == prefix;
+  }
+  unsigned long long all;                       // counts of both kinds in one scan
+  const unsigned long long before = select_scan(((unsigned long long)eq << 32) | gt, s_scan2, &all);
+  uint32_t gt_before = (uint32_t)before, eq_before = (uint32_t)(before >> 32);
+  if (nc > 1) {
+    if (tid == 0) {
+      s_total[0] = (uint32_t)all;
+      s_total[1] = (uint32_t)(all >> 32);
+    }
+    cluster_sync();
+    for (uint32_t r = 0; r < rank; ++r) {
+      gt_before += cluster_load(s_total, r);
+      eq_before += cluster_load(s_total + 1, r);
+    }
+  }
+  for (uint32_t i = f0; i < f1; ++i) {
+    const uint32_t k = key(i);
+    const bool tie = k == prefix;
+    if (k > prefix || (tie && eq_before < left)) {
+      const uint32_t at = a.sinks + gt_before + min(eq_before, left);
+      keep[at] = j0 + i;
+      // a key gives its score back, but for NaN and the sign of 0
+      if (out)
+        out[at] = k == 0u || k == 0x80000000u ? score[j0 + i]
+                                              : __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+    }
+    gt_before += k > prefix;
+    eq_before += tie;
+  }
+  if (nc > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
 }
 
 constexpr int EM_THREADS = 256;
@@ -160,11 +249,39 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
 void launch_evict(const LaunchCfg& L, const EvictArgs& in, int sms) {
   EvictArgs a = in;
   const unsigned units = a.c.n_seqs * a.c.n_heads;
-  launch_k(L, K_EVICT_SELECT, evict_select_kernel, units, ES_THREADS, 0, a);
+  // CTAs of a unit: up to 8 while that gives each at least 4,096 slots and the
+  // GPU has places (one unit of 100,000 slots: 8 CTAs measured below)
+  a.cluster = 1;
+  while (a.cluster < 8 && (uint64_t)units * a.cluster * 2 <= (uint64_t)sms * 2 && a.score_cap / (a.cluster * 2) >= 4096)
+    a.cluster *= 2;
+  // keys in shared memory: a run's, as far as two CTAs an SM have room for them
+  a.cached = (uint32_t)std::min<uint64_t>(ceil_div(a.score_cap, a.cluster), ES_CACHED);
+  prof_begin(L.prof, L.stream, K_EVICT_SELECT);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(units * a.cluster);
+  cfg.blockDim = dim3(ES_THREADS);
+  cfg.dynamicSmemBytes = a.cached * sizeof(uint32_t);
+  cfg.stream = L.stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+  cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
+  prof_end(L.prof, L.stream, K_EVICT_SELECT);
   // eight CTAs an SM over all units, at most one per 4 items of a thread
   const uint64_t most = ceil_div((uint64_t)a.budget * (a.c.head_dim / 8), EM_THREADS * 4);
   a.parts = (uint32_t)std::max<uint64_t>(1, std::min(most, ceil_div((uint64_t)sms * 8, units)));
   launch_k(L, K_EVICT_MOVE, evict_move_kernel, a.parts * units, EM_THREADS, 0, a);
+}
+
+cudaError_t prepare_evict_kernels() {
+  return cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)(ES_CACHED * sizeof(uint32_t)));
 }
 
 }  // namespace ro

@@ -149,18 +149,19 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
                                ? INT32_MAX
                                : (int32_t)max((int64_t)0, min(d + (int64_t)a.r.window, (int64_t)INT32_MAX));
     uint64_t acc[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
+    // this thread's row of a tile, fetched a turn ahead: minus its lse, -inf for
+    // rows past the end and rows that see nothing (they add 0)
+    auto row_lse = [&](uint32_t t) -> float {
+      const uint32_t i = i0 + t * g.toks + row / G;
+      if (t >= n || row >= g.toks * G || i >= i1) return INFINITY;
+      return a.lse[(q.tok0 + i) * a.n_q_heads + kh * G + row % G];
+    };
+    float next = row_lse(w);
     for (uint32_t t = w; t < n; t += 2) {
       const uint32_t t0 = i0 + t * g.toks, buf = (t >> 1) & 1;
-      {   // this row of the tile; rows past the end, and rows that see nothing, add 0
-        float z = -INFINITY;
-        const uint32_t i = t0 + row / G;
-        s_tok[w][buf][row] = row < g.toks * G && i < i1 ? (int32_t)i : -1;
-        if (row < g.toks * G && i < i1) {
-          z = -a.lse[(q.tok0 + i) * a.n_q_heads + kh * G + row % G] * 1.44269504088896340736f;
-          if (z == INFINITY) z = -INFINITY;
-        }
-        s_lse[w][buf][row] = z;
-      }
+      s_lse[w][buf][row] = next == -INFINITY ? -INFINITY : next * -1.44269504088896340736f;
+      s_tok[w][buf][row] = row < g.toks * G && t0 + row / G < i1 ? (int32_t)(t0 + row / G) : -1;
+      next = row_lse(t + 2);
       if (w == 0)
         asm volatile("bar.sync 1, 128;" ::: "memory");
       else

@@ -603,7 +603,8 @@ ro_status ro_ctx_create(ro_ctx** out, int32_t device, void* stream, uint32_t n_c
   c->ts_call.resize(n_calls);
   if (prepare_assemble_kernels() != cudaSuccess || prepare_attend_kernels() != cudaSuccess ||
       prepare_attend_tiles_kernels() != cudaSuccess || prepare_attend_few_kernels() != cudaSuccess ||
-      prepare_weigh_tiles_kernels() != cudaSuccess || prepare_weigh_few_kernels() != cudaSuccess) {
+      prepare_weigh_tiles_kernels() != cudaSuccess || prepare_weigh_few_kernels() != cudaSuccess ||
+      prepare_evict_kernels() != cudaSuccess) {
     cudaGetLastError();
     free_scalars(c);
     delete c;

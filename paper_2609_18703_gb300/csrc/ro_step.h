@@ -153,6 +153,7 @@ void launch_weigh(const LaunchCfg& L, const WeighArgs& a, int dtype);
 
 // ---- evict ------------------------------------------------------------------------------
 constexpr int ES_THREADS = 1024;
+constexpr uint32_t ES_CACHED = 18432;   // keys a CTA of evict_select holds: 72 KB, two CTAs an SM
 struct EvictArgs {
   PagedArgs c;
   const uint32_t* len;
@@ -164,9 +165,11 @@ struct EvictArgs {
   uint32_t* keep;
   uint32_t* len_out;
   float* score_out;          // optional
-  uint32_t parts;            // CTAs of the move for each (sequence, head)
+  uint32_t cluster, cached;  // evict_select: CTAs and keys in shared memory
+  uint32_t parts;            // evict_move: CTAs for each (sequence, head)
   uint32_t* err;
 };
 void launch_evict(const LaunchCfg& L, const EvictArgs& a, int sms);
+cudaError_t prepare_evict_kernels();
 
 }  // namespace ro

@@ -248,13 +248,13 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     a.tiles = cache->n_seqs;
     // Runs that fill two CTAs an SM in whole rounds, of at most 96 stages of
     // 16 KB (longer ones leave SMs idle at the end where lengths differ) and
-    // at least 8 (shorter ones cost more in their start and join than they
-    // save).  One sequence of 100,000 slots, 8 heads of 128: 68 us in one round
+    // at least 4 (shorter ones cost more in their start and join than they
+    // save: one sequence of 777 slots, 4 heads of 64, 8.4 us at 4, 9.4 at 8, 9.7 at 2).  One sequence of 100,000 slots, 8 heads of 128: 68 us in one round
     // of 83 stages, 85 in two of 64; 64 ragged ones of up to 32,000: 432 us at
     // 96, 476 at 32, 565 at 16.
     const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
     const uint64_t each = ceil_div(stages * work, places);
-    a.chunk = (uint32_t)std::max<uint64_t>(8, ceil_div(each, ceil_div(each, 96)));
+    a.chunk = (uint32_t)std::max<uint64_t>(4, ceil_div(each, ceil_div(each, 96)));
     a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 1024);
     if (a.max_chunks > 1) {
       RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));

@@ -278,6 +278,33 @@ def test_attend_splits_and_joins(ctx):
     assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
+@pytest.mark.parametrize("page", [16, 20, 256])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_long_runs(ctx, dim, page):
+    """Enough sequences that a CTA goes round its ring of stages many times."""
+    g = np.random.default_rng(page)
+    lens = [int(x) for x in g.integers(3000, 6000, 44)]
+    check_attend(ctx, ref.Cache(lens, 7, dim, page, BF16, page), [1] * 44, 7)
+
+
+@pytest.mark.parametrize("heads,kv", [(4, 4), (14, 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 5)])
+def test_attend_many_row_tiles(ctx, heads, kv, window, sinks):
+    """Chunks of more row tiles than the GPU has places for, of uneven sequences."""
+    lens, news = [900, 2100, 300, 1500], [900, 600, 1, 1100]
+    c = ref.Cache(lens, kv, 64, 32, F16, 31)
+    scale = 0.125
+    q, _, out, lse = run_attend(ctx, c, news, heads, scale, window, sinks)
+    t = starts(news)
+    for s in range(4):
+        for i in sorted({0, news[s] // 2, news[s] - 1}):   # some rows of each chunk
+            c.lens = list(lens)
+            c.lens[s] = lens[s] - news[s] + i + 1          # the row is the last of its cache
+            w_out, w_lse, tol, lse_tol = ref.attend(c, s, q[t[s] + i:t[s] + i + 1], scale, window, sinks)
+            within(out[t[s] + i:t[s] + i + 1], w_out, tol)
+            within(lse[t[s] + i:t[s] + i + 1], w_lse, lse_tol)
+
+
 @pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf"), 6e4])
 @pytest.mark.parametrize("news", [[1, 1], [64, 30]])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
@@ -400,6 +427,32 @@ def test_weigh(ctx, dtype, dim, heads, kv, page, news, window, sinks):
         assert torch.equal(in_place[s, :, L:], past[s, :, L:])
 
 
+@pytest.mark.parametrize("page", [64, 20])
+@pytest.mark.parametrize("heads,kv,news,window,sinks", [(4, 4, 1, 0, 0), (16, 2, 2, 1000, 9), (6, 2, 300, 0, 0),
+                                                        (14, 2, 130, 900, 0)])
+def test_weigh_long_runs(ctx, page, heads, kv, news, window, sinks):
+    """Many stages and row tiles a CTA; the weights of a row add up to one."""
+    g = np.random.default_rng(heads)
+    lens = [int(x) for x in g.integers(2000, 5000, 70 if news < 3 else 3)]
+    c = ref.Cache(lens, kv, 128, page, BF16, page)
+    n = [news] * len(lens)
+    q, dq, _, lse = run_attend(ctx, c, n, heads, 0.088, window, sinks)
+    cache, _, _ = on_gpu(c)
+    score = torch.zeros(len(lens), kv, max(lens), device="cuda")
+    ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(starts(n)), news, i32(lens), dq, 0.088, window, sinks, lse, 1.0, None, score))
+    sync_ok(ctx)
+    # each of news * heads / kv rows gives 1 in all; a weight errs by its exponent's 32 bits (|x| < 64: 2^-18) and the lse's
+    total = score.double().sum(2).cpu()
+    want = torch.full_like(total, news * heads / kv)
+    assert bool(((total - want).abs() <= want * 2.0 ** -16).all())
+    for s in (0, len(lens) - 1):
+        if news > 2:
+            continue
+        w, tol = ref.weigh(c, s, q[s * news:(s + 1) * news], 0.088, window, sinks,
+                           lse[s * news:(s + 1) * news].double().cpu(), 1.0, torch.zeros(kv, max(lens)))
+        within(score[s, :, :lens[s]], w, tol + 1e-30)
+
+
 def test_weigh_rows_that_see_nothing_and_short_scores(ctx):
     c = ref.Cache([7], 1, 64, 16, BF16, 13)
     q, dq, _, lse = run_attend(ctx, c, [30], 2, 0.125, 0, 0)
@@ -455,6 +508,40 @@ def test_evict(ctx, budget, sinks, recent, kind):
             want_k[at, h, d % page] = before_k[page_of, h, j % page]
             want_v[at, h, d % page] = before_v[page_of, h, j % page]
     assert total == k.shape[0] and torch.equal(k.cpu(), want_k) and torch.equal(v.cpu(), want_v)
+
+
+@pytest.mark.parametrize("lens,kv,budget,sinks,recent", [([40_000, 9_000], 2, 700, 4, 100), ([200_000], 1, 20_000, 0, 0),
+                                                         ([30_000, 0, 12_000, 8_200], 1, 8_192, 16, 8_000),
+                                                         ([33_333], 3, 33_332, 1, 5), ([20_000] * 3, 2, 50, 20, 30)])
+@pytest.mark.parametrize("kind", ["tail", "ties", "same"])
+def test_evict_long_sequences(ctx, lens, kv, budget, sinks, recent, kind):
+    """Sequences that several CTAs share: kept slots and scores (rows of 8 dimensions stand for the rest)."""
+    g = torch.Generator().manual_seed(len(lens))
+    page, cap = 128, max(lens) + 3
+    x = torch.randn(len(lens), kv, cap, generator=g)
+    score = {"tail": (3 * x).exp(), "ties": (x.abs() * 4).floor(), "same": x * 0 + 1.5}[kind]
+    held = [-(-L // page) for L in lens]
+    need = [-(-min(L, budget) // page) for L in lens]
+    k = torch.arange((sum(held) + sum(need)) * kv * page * 8, device="cuda").view(-1, kv, page, 8).to(BF16)
+    v = -k
+    cache = ro.ro_cache(k, v, i64(starts(held)), i32(np.arange(sum(held))))
+    before = k.clone()
+    keep = torch.full((len(lens), kv, budget), -1, dtype=torch.int32, device="cuda")
+    n_out = torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+    out = torch.full_like(score, -7.0).cuda()
+    ok(ctx, ro.ro_cache_evict(ctx, cache, i32(lens), score.cuda(), budget, sinks, recent, i64(starts(need)),
+                              i32(sum(held) + np.arange(sum(need))), keep, n_out, out))
+    sync_ok(ctx)
+    for s, L in enumerate(lens):
+        for h in range(kv):
+            idx = ref.evict(L, score[s, h].numpy(), budget, sinks, recent)
+            n = len(idx)
+            assert np.array_equal(keep[s, h, :n].cpu().numpy(), idx)
+            assert np.array_equal(out[s, h, :n].cpu().numpy(), score[s, h].numpy()[idx])
+            j, d = torch.as_tensor(idx).cuda(), torch.arange(n, device="cuda")
+            at = sum(held) + starts(need)[s] + d // page
+            assert torch.equal(k[at, h, d % page], before[starts(held)[s] + j // page, h, j % page])
+            assert torch.equal(v[at, h, d % page], -before[starts(held)[s] + j // page, h, j % page])
 
 
 def test_evict_records_what_does_not_fit(ctx):
