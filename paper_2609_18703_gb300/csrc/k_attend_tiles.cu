@@ -14,8 +14,11 @@
 // moves when a row's maximum grew by more than 2^8, so O is seldom rescaled.
 // Slots that no row of the CTA sees are never loaded or are zeroed in shared
 // memory first (a weight of 0 does not silence a NaN in a matrix product).
-// When there are fewer row tiles than places, the slots are split over CTAs
-// and the last CTA of a tile to finish joins the runs' (m, l, O) in order.
+// A CTA stays on its SM and takes pairs of row tiles as it gets free, heavy ones
+// first: the next pair's queries, keys and first products are under way while
+// the last one's output is written.  When there are fewer pairs than places,
+// the slots are split into runs and the last warp to finish its rows joins the
+// runs' (m, l, O) in order.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -23,7 +26,7 @@
 namespace ro {
 
 constexpr int AT_THREADS = 384, AT_ROWS = 128, AT_KEYS = 128;
-constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then one warp of products, one of loads, two idle
+constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then a warp each of products, loads, work
 // Registers: 168 a thread at launch (3 warps in each quarter of the SM); the
 // last warpgroup gives up what the softmax threads need, 2 x 208 + 80 <= 3 x 168.
 #define AT_REGS_SOFTMAX 216
@@ -40,49 +43,46 @@ struct TileShape {
   static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE_BYTES;
 };
 
+// A piece of work: a pair of row tiles of one sequence and head, and a run of
+// the slots they see.
+struct TileItem {
+  uint64_t tok0, page0;
+  int64_t first;             // slot of the chunk's first token
+  KeySpan span;
+  uint32_t i0, i1;           // the chunk's tokens in the row tiles
+  uint32_t kh, unit;         // head; (tile, head) for the runs' tickets
+  uint32_t c0, n;            // the run's slot tiles
+  uint32_t run, n_runs;
+  uint32_t last;             // no work: the end
+};
+constexpr uint32_t AT_ITEMS = 2;
+// The next item is taken this many slot tiles before the loads of the present
+// one end: early enough to decode it, late enough not to hold work that a CTA
+// which runs dry could do.
+constexpr uint32_t AT_AHEAD = 5;
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
   using S = TileShape<DP>;
   const AttendArgs& a = g.a;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t s_bar[1 + 2 * S::SLOTS + 6];
-  __shared__ uint32_t s_tmem, s_seq, s_part, s_found, s_last;
-  __shared__ uint32_t s_gave_up;
+  __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 8 + 2 * AT_ITEMS + 1];
+  __shared__ TileItem s_item[AT_ITEMS];
+  __shared__ uint32_t s_tmem, s_gave_up;
   wait_predecessor();
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const uint32_t tile = blockIdx.x / a.c.n_heads, kh = blockIdx.x - tile * a.c.n_heads;
-  if (warp == 0) {
-    uint32_t s = 0, p = 0;
-    const bool f = a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
-                       ? find_tile_heavy(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err)
-                       : find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
-    if (lane == 0) {
-      s_seq = s;
-      s_part = p;
-      s_found = f;
-      s_gave_up = 0;
-    }
-  }
-  __syncthreads();
-  if (!s_found) return;
-  const SeqInfo q = seq_info(a.c, a.r, s_seq, a.err);
   const uint32_t G = a.r.group;
-  const uint32_t i0 = s_part * 2 * g.toks, i1 = min(q.n, i0 + 2 * g.toks);
-  if (i0 >= i1) return;
-  const KeySpan ks = key_span(q, a.r, i0, i1);
-  const SlotTiles<AT_KEYS> slots(ks, g.box);
-  const uint32_t per = max(a.chunk, slots.n / a.max_chunks + 1);   // slot tiles of a run
-  const uint32_t n_chunks = max(1u, (slots.n + per - 1) / per);
-  if (blockIdx.y >= n_chunks) return;
-  const uint32_t c0 = blockIdx.y * per, n = min(per, slots.n - min(slots.n, c0));   // this run's tiles
-
   const uint32_t sm = (step_smem(smem_raw) + 1023u) & ~1023u;
   const uint32_t sm_ring = sm + 2 * S::TILE_BYTES;
-  const uint32_t bar0 = step_smem(s_bar);
-  const uint32_t b_q = bar0, b_full = bar0 + 8, b_empty = b_full + 8 * S::SLOTS, b_s = b_empty + 8 * S::SLOTS,
-                 b_p = b_s + 16, b_o = b_p + 16;
+  // full / empty: queries, the ring, S, P, O, items
+  const uint32_t b_q = step_smem(s_bar), b_qe = b_q + 8, b_full = b_qe + 8, b_empty = b_full + 8 * S::SLOTS,
+                 b_s = b_empty + 8 * S::SLOTS, b_p = b_s + 16, b_o = b_p + 16, b_oe = b_o + 16, b_item = b_oe + 16,
+                 b_item_free = b_item + 8 * AT_ITEMS, b_want = b_item_free + 8 * AT_ITEMS;
   if (tid == 0) {
+    s_gave_up = 0;
     bar_init(b_q, 1);
+    bar_init(b_qe, 1);
+    bar_init(b_want, 1);
     for (uint32_t i = 0; i < S::SLOTS; ++i) {
       bar_init(b_full + 8 * i, 1);
       bar_init(b_empty + 8 * i, 1);
@@ -91,6 +91,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       bar_init(b_s + 8 * i, 1);
       bar_init(b_p + 8 * i, 4);
       bar_init(b_o + 8 * i, 1);
+      bar_init(b_oe + 8 * i, 4);
+    }
+    for (uint32_t i = 0; i < AT_ITEMS; ++i) {
+      bar_init(b_item + 8 * i, 1);
+      bar_init(b_item_free + 8 * i, 10);   // 8 warps of softmax, loads, products
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -104,115 +109,205 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 
   if (warp >= AT_SOFTMAX / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AT_REGS_OTHERS));
-  }
-  if (warp == 9) {
-    // ---- loads ----
-    if (n > 0) {
-      if (lane == 0) {
-        bar_expect(b_q, 2 * S::BLOCKS * g.toks * G * 128);
-        for (uint32_t w = 0; w < 2; ++w)
-          for (uint32_t b = 0; b < S::BLOCKS; ++b)
-            tma3(sm + w * S::TILE_BYTES + b * S::BLOCK_BYTES, &g.q, b * 64, kh * G, (int)(q.tok0 + i0 + w * g.toks), b_q);
-      }
-      const uint32_t boxes = AT_KEYS / g.box;
-      // boxes without a slot that counts are not loaded
-      auto has_box = [&](const SlotTile& st) {
-        const uint32_t j = st.t0 + lane * g.box;
-        return lane < boxes && j < st.hi && j + g.box > st.lo;
-      };
-      // The page of this lane's box of a tile, looked up two tiles ahead and
-      // not touched before then, so that a tile's loads never wait for it.
-      auto page_of = [&](uint32_t t) -> uint32_t {
-        if (t >= n) return 0u;
-        const SlotTile st = slots.at(c0 + t);
-        return has_box(st) ? a.c.pages[q.page0 + ((st.t0 + lane * g.box) >> a.c.page_shift)] : 0u;
-      };
-      uint32_t page = page_of(0), next = page_of(1), slot = 0, parity = 1;   // parity of the round before
-      for (uint32_t t = 0; t < n; ++t) {
-        const uint32_t after = page_of(t + 2);
-        const SlotTile st = slots.at(c0 + t);
-        const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
-        bool load = has_box(st);
-        if (load && page >= a.c.n_pages) {
-          record(a.err, ERR_INVAL);
-          load = false;
-        }
-        const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
-#pragma unroll
-        for (uint32_t kv = 0; kv < 2; ++kv) {
-          if (2 * t + kv >= S::SLOTS) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
-          if (has_given_up(&s_gave_up)) break;
-          const uint32_t full = b_full + 8 * slot, dst = sm_ring + slot * S::TILE_BYTES + lane * g.box * 128;
-          if (lane == 0) bar_expect(full, loaded * S::BLOCKS * g.box * 128);
-          __syncwarp();
-          if (load)
-            for (uint32_t b = 0; b < S::BLOCKS; ++b)
-              tma4(dst + b * S::BLOCK_BYTES, kv ? &g.v : &g.k, b * 64, (int)y, (int)kh, (int)page, full);
-          if (++slot == S::SLOTS) slot = 0, parity ^= 1;
-        }
-        page = next;
-        next = after;
-        if (has_given_up(&s_gave_up)) break;
-      }
-    }
-  } else if (warp == 8) {
-    // ---- products ----
-    const uint32_t shape_s = mma_shape<T>(AT_KEYS, false), shape_o = mma_shape<T>(DP, true);
-    const uint32_t one = elect_lane();
-    const uint32_t q_lo = operand_lo(sm, 16), k_lo = operand_lo(sm_ring, 16), v_lo = operand_lo(sm_ring, S::BLOCK_BYTES);
-    auto product_s = [&](uint32_t w, uint32_t slot) {
-      const uint32_t qa = q_lo + w * (S::TILE_BYTES / 16), ka = k_lo + slot * (S::TILE_BYTES / 16);
-#pragma unroll
-      for (uint32_t k = 0; k < DP / 16; ++k) {
-        const uint32_t off = ((k / 4) * S::BLOCK_BYTES + (k % 4) * 32) / 16;
-        mma_ss(one, tm_s + w * 128, qa + off, ka + off, shape_s, k > 0);
-      }
+    // the k-th item, to a whole warp; released once its reader is done with it
+    auto item = [&](uint32_t k) -> const TileItem& {
+      bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
+      return s_item[k % AT_ITEMS];
     };
-    auto product_o = [&](uint32_t w, uint32_t slot, bool add) {
-      const uint32_t va = v_lo + slot * (S::TILE_BYTES / 16);
-#pragma unroll
-      for (uint32_t k = 0; k < AT_KEYS / 16; ++k)
-        mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8, va + k * (2048 / 16), shape_o, add || k > 0);
+    auto release = [&](uint32_t k) {
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
     };
-    if (n > 0) {
-      bar_wait(b_q, 0, &s_gave_up, a.err);
-      bar_wait(b_full, 0, &s_gave_up, a.err);
-      tc_fence_after();
-      product_s(0, 0);
-      tc_commit(one, b_s);
-      product_s(1, 0);
-      tc_commit(one, b_s + 8);
-      tc_commit(one, b_empty);
-      uint32_t vs = 1, v_par = 0, kslot = 2 % S::SLOTS, k_par = 0;   // ring places of V(t), K(t + 1) and their rounds' parity
-      for (uint32_t t = 0; t < n; ++t) {
-        const bool more = t + 1 < n;
-        bar_wait(b_full + 8 * vs, v_par, &s_gave_up, a.err);
-#pragma unroll
-        for (uint32_t w = 0; w < 2; ++w) {
-          bar_wait(b_p + 8 * w, t & 1, &s_gave_up, a.err);
-          tc_fence_after();
-          product_o(w, vs, t > 0);
-          if (w == 1) tc_commit(one, b_empty + 8 * vs);
-          if (more) {
-            if (w == 0) bar_wait(b_full + 8 * kslot, k_par, &s_gave_up, a.err);
-            product_s(w, kslot);
-            tc_commit(one, b_s + 8 * w);
-            if (w == 1) tc_commit(one, b_empty + 8 * kslot);
-          } else {
-            tc_commit(one, b_o + 8 * w);
+    if (warp == 10) {
+      // ---- work ----
+      // The first item by the CTA's number, the others as they are asked for;
+      // items are in falling order of work where that is known.
+      const uint32_t items = a.tiles * a.c.n_heads * a.max_chunks;
+      uint32_t k = 0;
+      for (uint32_t id = blockIdx.x;;) {
+        TileItem it = {};
+        it.last = id >= items;
+        bool some = true;
+        if (!it.last) {
+          const uint32_t x = id / a.c.n_heads, tile = x / a.max_chunks;
+          it.kh = id - x * a.c.n_heads;
+          it.run = x - tile * a.max_chunks;
+          it.unit = tile * a.c.n_heads + it.kh;
+          uint32_t s = 0, p = 0;
+          some = a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
+                     ? find_tile_heavy(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err)
+                     : find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
+          if (some) {
+            const SeqInfo q = seq_info(a.c, a.r, s, a.err);
+            it.tok0 = q.tok0;
+            it.page0 = q.page0;
+            it.first = q.first;
+            it.i0 = p * 2 * g.toks;
+            it.i1 = min(q.n, it.i0 + 2 * g.toks);
+            some = it.i0 < it.i1;
+            it.span = key_span(q, a.r, it.i0, max(it.i1, it.i0));
+            const uint32_t n = SlotTiles<AT_KEYS>(it.span, g.box).n;
+            const uint32_t per = max(a.chunk, n / a.max_chunks + 1);   // slot tiles of a run
+            it.n_runs = max(1u, (n + per - 1) / per);
+            it.c0 = it.run * per;
+            it.n = min(per, n - min(n, it.c0));
+            some = some && it.run < it.n_runs;
           }
         }
-        if (has_given_up(&s_gave_up)) break;
-        vs += 2;
-        if (vs >= S::SLOTS) vs -= S::SLOTS, v_par ^= 1;
-        kslot += 2;
-        if (kslot >= S::SLOTS) kslot -= S::SLOTS, k_par ^= 1;
+        if (some) {
+          const uint32_t slot = k % AT_ITEMS;
+          if (k >= AT_ITEMS) bar_wait_idle(b_item_free + 8 * slot, (k / AT_ITEMS - 1) & 1, &s_gave_up, a.err);
+          if (lane == 0) s_item[slot] = it;
+          __syncwarp();
+          if (lane == 0) bar_arrive(b_item + 8 * slot);
+          if (!it.last) bar_wait_idle(b_want, k & 1, &s_gave_up, a.err);
+          ++k;
+        }
+        if (it.last || has_given_up(&s_gave_up)) break;
+        if (lane == 0) id = gridDim.x + atomicAdd(a.counter, 1u);
+        id = __shfl_sync(0xffffffffu, id, 0);
+      }
+      // the last CTA to leave sets the count back for the next call
+      if (lane == 0 && ticket(a.counter + 1) == gridDim.x - 1) {
+        a.counter[0] = 0u;
+        a.counter[1] = 0u;
+      }
+    } else if (warp == 9) {
+      // ---- loads ----
+      const uint32_t boxes = AT_KEYS / g.box;
+      uint32_t slot = 0, parity = 1, uses = 0, qi = 0;   // parity of the ring's round before
+      for (uint32_t k = 0;; ++k) {
+        const TileItem& it = item(k);
+        if (it.last || has_given_up(&s_gave_up)) break;
+        const uint32_t n = it.n, c0 = it.c0, kh = it.kh;
+        const uint64_t page0 = it.page0;
+        const SlotTiles<AT_KEYS> slots(it.span, g.box);
+        if (n > 0) {
+          if (qi > 0) bar_wait(b_qe, (qi - 1) & 1, &s_gave_up, a.err);
+          if (lane == 0) {
+            bar_expect(b_q, 2 * S::BLOCKS * g.toks * G * 128);
+            for (uint32_t w = 0; w < 2; ++w)
+              for (uint32_t b = 0; b < S::BLOCKS; ++b)
+                tma3(sm + w * S::TILE_BYTES + b * S::BLOCK_BYTES, &g.q, b * 64, kh * G,
+                     (int)(it.tok0 + it.i0 + w * g.toks), b_q);
+          }
+          __syncwarp();
+          ++qi;
+        }
+        // boxes without a slot that counts are not loaded
+        auto has_box = [&](const SlotTile& st) {
+          const uint32_t j = st.t0 + lane * g.box;
+          return lane < boxes && j < st.hi && j + g.box > st.lo;
+        };
+        // The page of this lane's box of a tile, looked up two tiles ahead and
+        // not touched before then, so that a tile's loads never wait for it.
+        auto page_of = [&](uint32_t t) -> uint32_t {
+          if (t >= n) return 0u;
+          const SlotTile st = slots.at(c0 + t);
+          return has_box(st) ? a.c.pages[page0 + ((st.t0 + lane * g.box) >> a.c.page_shift)] : 0u;
+        };
+        uint32_t page = page_of(0), next = page_of(1);
+        const uint32_t want = n > AT_AHEAD ? n - AT_AHEAD : 0;
+        if (n == 0 && lane == 0) bar_arrive(b_want);
+        for (uint32_t t = 0; t < n; ++t) {
+          if (t == want && lane == 0) bar_arrive(b_want);
+          const uint32_t after = page_of(t + 2);
+          const SlotTile st = slots.at(c0 + t);
+          const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
+          bool load = has_box(st);
+          if (load && page >= a.c.n_pages) {
+            record(a.err, ERR_INVAL);
+            load = false;
+          }
+          const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
+#pragma unroll
+          for (uint32_t kv = 0; kv < 2; ++kv) {
+            if (uses >= S::SLOTS) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
+            if (has_given_up(&s_gave_up)) break;
+            const uint32_t full = b_full + 8 * slot, dst = sm_ring + slot * S::TILE_BYTES + lane * g.box * 128;
+            if (lane == 0) bar_expect(full, loaded * S::BLOCKS * g.box * 128);
+            __syncwarp();
+            if (load)
+              for (uint32_t b = 0; b < S::BLOCKS; ++b)
+                tma4(dst + b * S::BLOCK_BYTES, kv ? &g.v : &g.k, b * 64, (int)y, (int)kh, (int)page, full);
+            uses = min(uses + 1, S::SLOTS);
+            if (++slot == S::SLOTS) slot = 0, parity ^= 1;
+          }
+          page = next;
+          next = after;
+          if (has_given_up(&s_gave_up)) break;
+        }
+        release(k);
+      }
+    } else if (warp == 8) {
+      // ---- products ----
+      const uint32_t shape_s = mma_shape<T>(AT_KEYS, false), shape_o = mma_shape<T>(DP, true);
+      const uint32_t one = elect_lane();
+      const uint32_t q_lo = operand_lo(sm, 16), k_lo = operand_lo(sm_ring, 16), v_lo = operand_lo(sm_ring, S::BLOCK_BYTES);
+      auto product_s = [&](uint32_t w, uint32_t slot) {
+        const uint32_t qa = q_lo + w * (S::TILE_BYTES / 16), ka = k_lo + slot * (S::TILE_BYTES / 16);
+#pragma unroll
+        for (uint32_t k = 0; k < DP / 16; ++k) {
+          const uint32_t off = ((k / 4) * S::BLOCK_BYTES + (k % 4) * 32) / 16;
+          mma_ss(one, tm_s + w * 128, qa + off, ka + off, shape_s, k > 0);
+        }
+        tc_commit(one, b_s + 8 * w);
+      };
+      auto product_o = [&](uint32_t w, uint32_t slot, bool add) {
+        const uint32_t va = v_lo + slot * (S::TILE_BYTES / 16);
+#pragma unroll
+        for (uint32_t k = 0; k < AT_KEYS / 16; ++k)
+          mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8, va + k * (2048 / 16), shape_o, add || k > 0);
+      };
+      uint32_t slot = 0, parity = 0, tiles = 0, qi = 0;   // place in the ring of the next tile used, its round's parity
+      auto advance = [&] {
+        if (++slot == S::SLOTS) slot = 0, parity ^= 1;
+      };
+      for (uint32_t k = 0;; ++k) {
+        const TileItem& it = item(k);
+        if (it.last || has_given_up(&s_gave_up)) break;
+        const uint32_t n = it.n;
+        release(k);
+        if (n == 0) continue;
+        bar_wait(b_q, qi & 1, &s_gave_up, a.err);
+        bar_wait(b_full + 8 * slot, parity, &s_gave_up, a.err);
+        tc_fence_after();
+        product_s(0, slot);
+        product_s(1, slot);
+        tc_commit(one, b_empty + 8 * slot);
+        if (n == 1) tc_commit(one, b_qe);
+        advance();
+        for (uint32_t t = 0; t < n; ++t, ++tiles) {
+          const bool more = t + 1 < n;
+          const uint32_t vs = slot;
+          bar_wait(b_full + 8 * vs, parity, &s_gave_up, a.err);
+          advance();
+#pragma unroll
+          for (uint32_t w = 0; w < 2; ++w) {
+            bar_wait(b_p + 8 * w, tiles & 1, &s_gave_up, a.err);
+            if (t == 0 && qi > 0) bar_wait(b_oe + 8 * w, (qi - 1) & 1, &s_gave_up, a.err);   // the last item's O is read
+            tc_fence_after();
+            product_o(w, vs, t > 0);
+            if (w == 1) tc_commit(one, b_empty + 8 * vs);
+            if (more) {
+              if (w == 0) bar_wait(b_full + 8 * slot, parity, &s_gave_up, a.err);
+              product_s(w, slot);
+              if (w == 1) {
+                tc_commit(one, b_empty + 8 * slot);
+                if (t + 2 == n) tc_commit(one, b_qe);
+              }
+            } else {
+              tc_commit(one, b_o + 8 * w);
+            }
+          }
+          if (more) advance();
+          if (has_given_up(&s_gave_up)) break;
+        }
+        ++qi;
       }
     }
-  }
-  if (warp >= AT_SOFTMAX / 32) {
     __syncwarp();
-    asm volatile("bar.sync 0;" ::: "memory");   // O is read
+    asm volatile("bar.sync 0;" ::: "memory");   // every product is read
     if (*(volatile uint32_t*)&s_gave_up) __nanosleep(1000000);   // copies and products in flight end by themselves
     if (warp == 8) {
       tc_fence_after();
@@ -222,21 +317,32 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   }
   // ---- softmax: a thread a row ----
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AT_REGS_SOFTMAX));
-  {
-    const uint32_t w = warp >> 2, row = tid & 127;
-    const uint32_t lanes = (warp & 3) << 21;                 // this warp's TMEM lanes
-    const uint32_t ts = tm_s + w * 128 + lanes, to = tm_o + w * 128 + lanes;
-    const uint32_t j0 = i0 + w * g.toks, j1 = min(i1, j0 + g.toks);   // the row tile's tokens
+  const uint32_t w = warp >> 2, row = tid & 127;
+  const uint32_t lanes = (warp & 3) << 21;                 // this warp's TMEM lanes
+  const uint32_t ts = tm_s + w * 128 + lanes, to = tm_o + w * 128 + lanes;
+  const float scale = a.r.scale_log2;
+  uint32_t tiles = 0, vslot = 1, vpar = 0, done = 0;       // tiles so far; the ring's place of V; items with slots so far
+  for (uint32_t k = 0;; ++k) {
+    bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
+    const TileItem& it = s_item[k % AT_ITEMS];
+    if (it.last || has_given_up(&s_gave_up)) break;
+    const uint32_t n = it.n, c0 = it.c0, i1 = it.i1, n_runs = it.n_runs;
+    const SlotTiles<AT_KEYS> slots(it.span, g.box);
+    const uint32_t j0 = it.i0 + w * g.toks, j1 = min(i1, j0 + g.toks);   // the row tile's tokens
     const bool live = j0 < i1;
-    const uint32_t tok = j0 + row / G, head = kh * G + row % G;
+    const uint32_t tok = j0 + row / G, head = it.kh * G + row % G;
     const bool mine = row < g.toks * G && tok < j1;
-    const int64_t pos = q.first + tok;                       // the row's slot
-    const int64_t a_lo = q.first + j0, a_hi = q.first + (live ? j1 : j0 + 1) - 1;
+    const int64_t pos = it.first + tok;                    // the row's slot
+    const int64_t a_lo = it.first + j0, a_hi = it.first + (live ? j1 : j0 + 1) - 1;
+    const uint64_t out_at = (it.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
+    const uint64_t lse_at = (it.tok0 + tok) * a.n_q_heads + head;
+    const uint32_t unit = it.unit, run = it.run;
+    __syncwarp();
+    if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
     float m = -INFINITY, l = 0.f;
-    const float scale = a.r.scale_log2;
-    for (uint32_t t = 0; t < n; ++t) {
+    for (uint32_t t = 0; t < n; ++t, ++tiles) {
       const SlotTile st = slots.at(c0 + t);
-      bar_wait(b_s + 8 * w, t & 1, &s_gave_up, a.err);
+      bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
       uint32_t x[AT_KEYS];
 #pragma unroll
@@ -280,7 +386,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
             tc_ld16(to + i * 16, o);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
             tc_st16(to + i * 16, o);
           }
         }
@@ -292,11 +398,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       for (int i = 0; i < 4; ++i) {
         uint32_t p[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const uint64_t y = fma_pair(pair_bits(x[i * 32 + 2 * k], x[i * 32 + 2 * k + 1]), scale2, sub2);
+        for (int z = 0; z < 16; ++z) {
+          const uint64_t y = fma_pair(pair_bits(x[i * 32 + 2 * z], x[i * 32 + 2 * z + 1]), scale2, sub2);
           const float e0 = ex2(pair_lo(y)), e1 = ex2(pair_hi(y));
-          sum[k & 3] = add_pair(sum[k & 3], pair(e0, e1));
-          p[k] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
+          sum[z & 3] = add_pair(sum[z & 3], pair(e0, e1));
+          p[z] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
         }
         tc_st16(ts + i * 16, p);
       }
@@ -305,15 +411,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       // Values no row sees must not reach the product: zero them where the
       // tile is not whole (the products of both row tiles come after this).
       if (w == 0 && !whole) {
-        const uint32_t vu = 2 * t + 1, slot = vu % S::SLOTS;
-        bar_wait(b_full + 8 * slot, (vu / S::SLOTS) & 1, &s_gave_up, a.err);
+        bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
         const uint32_t j = st.t0 + row;
         if (j < st.lo || j >= st.hi) {
 #pragma unroll
           for (uint32_t b = 0; b < S::BLOCKS; ++b)
 #pragma unroll
             for (uint32_t z = 0; z < 8; ++z)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + slot * S::TILE_BYTES +
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
                                                                         b * S::BLOCK_BYTES + row * 128 + z * 16),
                            "r"(0u)
                            : "memory");
@@ -324,89 +429,88 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       tc_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive(b_p + 8 * w);
+      vslot += 2;
+      if (vslot >= S::SLOTS) vslot -= S::SLOTS, vpar ^= 1;
       if (has_given_up(&s_gave_up)) break;
     }
+    // ---- to the output, or to this run's partial result ----
+    uint32_t o[DP];
     if (n > 0) {
-      bar_wait(b_o + 8 * w, 0, &s_gave_up, a.err);
+      bar_wait(b_o + 8 * w, done & 1, &s_gave_up, a.err);
       tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) tc_ld32(to + i * 32, o + i * 32);
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_oe + 8 * w);
+      ++done;
+    } else {
+#pragma unroll
+      for (int i = 0; i < DP; ++i) o[i] = 0u;
     }
-    T* out = (T*)a.out + (q.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
-    const float inv = n_chunks > 1 ? 1.f : (l > 0.f || l != l ? 1.f / l : 0.f);
-    const uint64_t run = (uint64_t)blockIdx.x * a.max_chunks + blockIdx.y;
-    float* part = a.partial + (run * 2 * AT_ROWS + w * AT_ROWS + row) * DP;
+    const uint32_t prow = w * AT_ROWS + row;               // the row among the pair's 256
+    float* part = a.partial + ((uint64_t)unit * a.max_chunks * 2 * AT_ROWS + prow) * DP;
+    float2* ml = (float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * DP) +
+                 (uint64_t)unit * a.max_chunks * 2 * AT_ROWS + prow;
+    constexpr uint32_t STEP = 2 * AT_ROWS;                 // rows of a run
+    if (n_runs > 1) {
+      if (mine) {
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-      uint32_t o[32];
-      if (n > 0) {
-        tc_ld32(to + i * 32, o);
-        tc_wait_ld();
-      } else {
-#pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = 0u;
+        for (int i = 0; i < DP; i += 4)
+          __stcg((float4*)(part + (uint64_t)run * STEP * DP + i),
+                 make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]),
+                             __uint_as_float(o[i + 3])));
+        __stcg(ml + run * STEP, make_float2(m, l));
       }
-      if (!mine) continue;
-      if (n_chunks > 1) {
+      // the last of the runs' warps to hold these 32 rows joins them, in order
+      __threadfence();
+      __syncwarp();
+      uint32_t* count = a.counter + 2 + unit * 8 + warp;
+      uint32_t last = 0;
+      if (lane == 0) last = ticket(count) == n_runs - 1;
+      if (!__shfl_sync(0xffffffffu, last, 0)) continue;
+      __threadfence();
+      if (lane == 0) *count = 0u;   // for the next call
+      m = -INFINITY;
+      l = 0.f;
 #pragma unroll
-        for (int k = 0; k < 32; k += 4)
-          __stcg((float4*)(part + i * 32 + k), make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]),
-                                                           __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])));
-      } else {
+      for (int i = 0; i < DP; ++i) o[i] = 0u;
+      if (mine) {
+        for (uint32_t r = 0; r < n_runs; ++r) m = fmaxf(m, __ldcg(ml + r * STEP).x);
+        const float sub = m == -INFINITY ? 0.f : m;
+        for (uint32_t r = 0; r < n_runs; ++r) {
+          const float2 z = __ldcg(ml + r * STEP);
+          const float f = ex2(z.x - sub);
+          l += f * z.y;
 #pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-          uint4 v;
-          v.x = pack2<T>(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-          v.y = pack2<T>(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
-          v.z = pack2<T>(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
-          v.w = pack2<T>(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
-          if ((uint32_t)(i * 32 + k) < a.c.head_dim) *(uint4*)(out + i * 32 + k) = v;
+          for (int i = 0; i < DP; i += 4) {
+            const float4 v = __ldcg((const float4*)(part + (uint64_t)r * STEP * DP + i));
+            o[i] = __float_as_uint(__uint_as_float(o[i]) + f * v.x);
+            o[i + 1] = __float_as_uint(__uint_as_float(o[i + 1]) + f * v.y);
+            o[i + 2] = __float_as_uint(__uint_as_float(o[i + 2]) + f * v.z);
+            o[i + 3] = __float_as_uint(__uint_as_float(o[i + 3]) + f * v.w);
+          }
         }
       }
     }
-    if (mine) {
-      if (n_chunks > 1)
-        __stcg((float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * 2 * AT_ROWS * DP) + run * 2 * AT_ROWS +
-                   w * AT_ROWS + row,
-               make_float2(m, l));
-      else if (a.lse)
-        a.lse[(q.tok0 + tok) * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (!mine) continue;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    T* out = (T*)a.out + out_at;
+#pragma unroll
+    for (int i = 0; i < DP; i += 8) {
+      uint4 v;
+      v.x = pack2<T>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+      v.y = pack2<T>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+      v.z = pack2<T>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+      v.w = pack2<T>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+      if ((uint32_t)i < a.c.head_dim) *(uint4*)(out + i) = v;
     }
-    tc_fence_before();
+    if (a.lse) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
   }
-  if (n_chunks > 1) __threadfence();
+  __syncwarp();
+  tc_fence_before();
   asm volatile("bar.sync 0;" ::: "memory");
-  if (n_chunks == 1) return;
-  if (tid == 0) s_last = ticket(a.counter + blockIdx.x) == n_chunks - 1;
-  asm volatile("bar.sync 1, 256;" ::: "memory");
-  if (!s_last) return;
-  __threadfence();
-  // the runs of this tile in order: rows x 4-column pieces over the threads
-  const float* p0 = a.partial + (uint64_t)blockIdx.x * a.max_chunks * 2 * AT_ROWS * DP;
-  const float2* ml = (const float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * 2 * AT_ROWS * DP) +
-                     (uint64_t)blockIdx.x * a.max_chunks * 2 * AT_ROWS;
-  for (uint32_t x = tid; x < 2 * AT_ROWS * (DP / 4); x += AT_SOFTMAX) {
-    const uint32_t r = x / (DP / 4), d = (x - r * (DP / 4)) * 4, w = r / AT_ROWS, row = r % AT_ROWS;
-    const uint32_t tok = i0 + w * g.toks + row / G, head = kh * G + row % G;
-    if (row >= g.toks * G || tok >= i1) continue;
-    float M = -INFINITY;
-    for (uint32_t k = 0; k < n_chunks; ++k) M = fmaxf(M, __ldcg(&ml[k * 2 * AT_ROWS + r].x));
-    const float sub = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t k = 0; k < n_chunks; ++k) {
-      const float2 z = __ldcg(&ml[k * 2 * AT_ROWS + r]);
-      const float4 v = __ldcg((const float4*)(p0 + ((uint64_t)k * 2 * AT_ROWS + r) * DP + d));
-      const float f = ex2(z.x - sub);
-      L += f * z.y;
-      acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-    }
-    const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
-    T* out = (T*)a.out + (q.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
-    if (d < a.c.head_dim)
-      *(uint2*)(out + d) = make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-    if (d == 0 && a.lse)
-      a.lse[(q.tok0 + tok) * a.n_q_heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
-  }
-  if (tid == 0) a.counter[blockIdx.x] = 0u;   // for the next call
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -414,17 +518,21 @@ bool attend_tiles_fits(const AttendArgs& a) {
   return a.c.page_shift >= 3 && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
 }
 uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
+size_t attend_tiles_counters(const AttendArgs& a) {
+  return (2 + (a.max_chunks > 1 ? (size_t)a.tiles * a.c.n_heads * 8 : 0)) * sizeof(uint32_t);
+}
 size_t attend_tiles_partial(const AttendArgs& a) {
   const size_t dp = a.c.head_dim <= 64 ? 64 : 128;
   return (size_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * (dp + 2) * sizeof(float);
 }
 
 template <typename T, int DP>
-static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g) {
-  launch_k(L, K_ATTEND_TILES, attend_tiles_kernel<T, DP>, dim3(g.a.tiles * g.a.c.n_heads, g.a.max_chunks), AT_THREADS,
+static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
+  const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
+  launch_k(L, K_ATTEND_TILES, attend_tiles_kernel<T, DP>, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), AT_THREADS,
            TileShape<DP>::SMEM, g);
 }
-bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype) {
+bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int sms) {
   AttendTileArgs g;
   g.a = a;
   g.toks = AT_ROWS / a.r.group;
@@ -434,9 +542,9 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype) {
     return false;
   const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)
-    narrow ? launch_tiles<__nv_bfloat16, 64>(L, g) : launch_tiles<__nv_bfloat16, 128>(L, g);
+    narrow ? launch_tiles<__nv_bfloat16, 64>(L, g, sms) : launch_tiles<__nv_bfloat16, 128>(L, g, sms);
   else
-    narrow ? launch_tiles<__half, 64>(L, g) : launch_tiles<__half, 128>(L, g);
+    narrow ? launch_tiles<__half, 64>(L, g, sms) : launch_tiles<__half, 128>(L, g, sms);
   return true;
 }
 

@@ -407,6 +407,9 @@ ro_status sync_and_check(ro_ctx* c) {
   const uint32_t err = c->hs->err;
   if (!err) return RO_OK;
   cudaMemsetAsync(&c->ds->err, 0, sizeof(uint32_t), c->stream);
+  // (a model-step kernel that gave up may have left its counters behind)
+  if ((err & ERR_TIMEOUT) && c->step[SS_COUNTER].p)
+    cudaMemsetAsync(c->step[SS_COUNTER].p, 0, c->step[SS_COUNTER].cap, c->stream);
   if (err & ERR_TIMEOUT)
     return fail(c, RO_E_TIMEOUT, (err & ERR_DRAIN)
                                      ? "a device-side wait timed out (a copy CTA exited with bulk "

@@ -92,11 +92,11 @@ __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& c, const RowsArgs& 
   q.page0 = p0;
   q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && len < 0x80000000u;
   if (!q.ok) {
-    if (threadIdx.x == 0) record(err, ERR_INVAL);
+    if ((threadIdx.x & 31u) == 0) record(err, ERR_INVAL);
     q.n = 0;
     q.len = 0;
   } else if ((uint64_t)len > (p1 - p0) * c.page_size) {
-    if (threadIdx.x == 0) record(err, ERR_CAPACITY);
+    if ((threadIdx.x & 31u) == 0) record(err, ERR_CAPACITY);
     q.len = (uint32_t)((p1 - p0) * c.page_size);
   }
   q.first = (int64_t)len - (int64_t)q.n;

@@ -104,7 +104,7 @@ struct AttendArgs {
   float* lse;                // optional
   uint32_t n_q_heads;
   float* partial;            // [tile][chunk][rows][head_dim + 2]
-  uint32_t* counter;         // [tile], zero between calls
+  uint32_t* counter;         // zero between calls
   uint32_t* err;
 };
 // at most 16 rows a sequence; slots of a stage, bytes of its runs' partial results
@@ -116,11 +116,13 @@ cudaError_t prepare_attend_few_kernels();
 void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype);
 cudaError_t prepare_attend_kernels();
 // the tensor-core kernel: whether it takes these sizes, tokens of its CTA,
-// bytes of its runs' partial results; false: the tensors cannot be mapped
+// bytes of its counters and of its runs' partial results; false: the tensors
+// cannot be mapped
 bool attend_tiles_fits(const AttendArgs& a);
 uint32_t attend_tile_tokens(uint32_t group);
+size_t attend_tiles_counters(const AttendArgs& a);
 size_t attend_tiles_partial(const AttendArgs& a);
-bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype);
+bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int sms);
 cudaError_t prepare_attend_tiles_kernels();
 
 struct WeighArgs {

@@ -270,19 +270,20 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     const uint32_t toks = attend_tile_tokens(group);
     const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
     const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
-    if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
+    if (work > MAX_GRID / 256) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
     a.tiles = (uint32_t)tiles;
-    // one CTA an SM; split the slots where that leaves places free, at least 1,024 slots a run
+    // One CTA an SM takes pairs of row tiles in turn.  Fewer pairs than two an
+    // SM: split the slots into runs, at least 1,024 slots each.
     const uint64_t split = std::max<uint64_t>(1, (uint64_t)c.sms() * 2 / work);
     a.chunk = (uint32_t)std::max<uint64_t>(8, ceil_div(slots, split));
     a.max_chunks = split == 1 ? 1u : (uint32_t)std::min<uint64_t>(ceil_div(slots, a.chunk), 256);
+    RO_TRY(c.scratch(SS_COUNTER, attend_tiles_counters(a), &p));
+    a.counter = (uint32_t*)p;
     if (a.max_chunks > 1) {
       RO_TRY(c.scratch(SS_PARTIAL, attend_tiles_partial(a), &p));
       a.partial = (float*)p;
-      RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
-      a.counter = (uint32_t*)p;
     }
-    if (launch_attend_tiles(c.launch(), a, cache->dtype)) return c.launched(fn);
+    if (launch_attend_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
   }
   const uint32_t rows = 64;
   const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);

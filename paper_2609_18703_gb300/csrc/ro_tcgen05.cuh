@@ -51,6 +51,17 @@ __device__ __forceinline__ void bar_wait_slow(uint32_t bar, uint32_t parity, vol
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* err) {
   if (!bar_try(bar, parity)) bar_wait_slow(bar, parity, gave_up, err);
 }
+// A wait that need not end at once: it leaves the issue slots to others.
+__device__ __forceinline__ void bar_wait_idle(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* err) {
+  const unsigned long long t0 = timer_ns();
+  while (!bar_try(bar, parity) && !*gave_up) {
+    if (timer_ns() - t0 > 2000000000ull) {
+      record(err, ERR_TIMEOUT);
+      *gave_up = 1u;
+    }
+    __nanosleep(500);
+  }
+}
 // a whole warp, so that it leaves a loop together
 __device__ __forceinline__ bool has_given_up(volatile uint32_t* gave_up) {
   return __any_sync(0xffffffffu, *gave_up != 0u);
