@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   using S = TileShape<DP>;
   const AttendArgs& a = g.a;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 8 + 2 * AT_ITEMS + 1];
+  __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 10 + 2 * AT_ITEMS + 1];
   __shared__ TileItem s_item[AT_ITEMS];
   __shared__ uint32_t s_tmem, s_gave_up;
   wait_predecessor();
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   const uint32_t sm_ring = sm + 2 * S::TILE_BYTES;
   // full / empty: queries, the ring, S, P, O, items
   const uint32_t b_q = step_smem(s_bar), b_qe = b_q + 8, b_full = b_qe + 8, b_empty = b_full + 8 * S::SLOTS,
-                 b_s = b_empty + 8 * S::SLOTS, b_p = b_s + 16, b_o = b_p + 16, b_oe = b_o + 16, b_item = b_oe + 16,
+                 b_s = b_empty + 8 * S::SLOTS, b_p = b_s + 16, b_o = b_p + 32, b_oe = b_o + 16, b_item = b_oe + 16,
                  b_item_free = b_item + 8 * AT_ITEMS, b_want = b_item_free + 8 * AT_ITEMS;
   if (tid == 0) {
     s_gave_up = 0;
@@ -89,7 +89,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     }
     for (uint32_t i = 0; i < 2; ++i) {
       bar_init(b_s + 8 * i, 1);
-      bar_init(b_p + 8 * i, 4);
+      bar_init(b_p + 16 * i, 4);       // P in two halves of 64 slots
+      bar_init(b_p + 16 * i + 8, 4);
       bar_init(b_o + 8 * i, 1);
       bar_init(b_oe + 8 * i, 4);
     }
@@ -253,10 +254,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
         tc_commit(one, b_s + 8 * w);
       };
-      auto product_o = [&](uint32_t w, uint32_t slot, bool add) {
+      auto product_o = [&](uint32_t w, uint32_t half, uint32_t slot, bool add) {
         const uint32_t va = v_lo + slot * (S::TILE_BYTES / 16);
 #pragma unroll
-        for (uint32_t k = 0; k < AT_KEYS / 16; ++k)
+        for (uint32_t k = half * (AT_KEYS / 32); k < (half + 1) * (AT_KEYS / 32); ++k)
           mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8, va + k * (2048 / 16), shape_o, add || k > 0);
       };
       uint32_t slot = 0, parity = 0, tiles = 0, qi = 0;   // place in the ring of the next tile used, its round's parity
@@ -284,10 +285,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           advance();
 #pragma unroll
           for (uint32_t w = 0; w < 2; ++w) {
-            bar_wait(b_p + 8 * w, tiles & 1, &s_gave_up, a.err);
+            bar_wait(b_p + 16 * w, tiles & 1, &s_gave_up, a.err);
             if (t == 0 && qi > 0) bar_wait(b_oe + 8 * w, (qi - 1) & 1, &s_gave_up, a.err);   // the last item's O is read
             tc_fence_after();
-            product_o(w, vs, t > 0);
+            product_o(w, 0, vs, t > 0);
+            bar_wait(b_p + 16 * w + 8, tiles & 1, &s_gave_up, a.err);
+            tc_fence_after();
+            product_o(w, 1, vs, true);
             if (w == 1) tc_commit(one, b_empty + 8 * vs);
             if (more) {
               if (w == 0) bar_wait(b_full + 8 * slot, parity, &s_gave_up, a.err);
@@ -333,7 +337,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     const uint32_t tok = j0 + row / G, head = it.kh * G + row % G;
     const bool mine = row < g.toks * G && tok < j1;
     const int64_t pos = it.first + tok;                    // the row's slot
-    const int64_t a_lo = it.first + j0, a_hi = it.first + (live ? j1 : j0 + 1) - 1;
+    // The run's tiles whose every slot every row of this row tile sees: those
+    // of the sinks before `sinks_all`, and [all_from, all_to).
+    uint32_t sinks_all, all_from, all_to;
+    {
+      const int64_t a_lo = it.first + j0, a_hi = it.first + (live ? j1 : j0 + 1) - 1;
+      const int64_t from = max((int64_t)slots.lo, a.r.window ? a_hi - (int64_t)a.r.window + 1 : (int64_t)0);
+      const int64_t to = min((int64_t)slots.hi, a_lo + 1);
+      auto tile_of = [&](int64_t x) { return x <= (int64_t)slots.first ? 0u : (uint32_t)(x - slots.first) / AT_KEYS; };
+      sinks_all = slots.s_hi / AT_KEYS;
+      all_from = slots.sink_tiles + tile_of(from + AT_KEYS - 1);
+      all_to = slots.sink_tiles + tile_of(to);
+      sinks_all = sinks_all > c0 ? sinks_all - c0 : 0;
+      all_from = all_from > c0 ? all_from - c0 : 0;
+      all_to = all_to > c0 ? all_to - c0 : 0;
+    }
     const uint64_t out_at = (it.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
     const uint64_t lse_at = (it.tok0 + tok) * a.n_q_heads + head;
     const uint32_t unit = it.unit, run = it.run;
@@ -341,17 +359,15 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
     float m = -INFINITY, l = 0.f;
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
-      const SlotTile st = slots.at(c0 + t);
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
       uint32_t x[AT_KEYS];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
       tc_wait_ld();
-      const bool whole = st.lo == st.t0 && st.hi == st.t0 + AT_KEYS;
-      const bool all = whole && (st.sink || ((int64_t)st.t0 + AT_KEYS - 1 <= a_lo &&
-                                             (a.r.window == 0u || (int64_t)st.t0 > a_hi - (int64_t)a.r.window)));
+      const bool all = t < sinks_all || (t >= all_from && t < all_to);
       if (!all) {
+        const SlotTile st = slots.at(c0 + t);
         // columns [b, e) count; of those the ones below `sinks` or from the window's first on
         const int64_t t0 = st.t0;
         const int e = (int)max((int64_t)0, min((int64_t)st.hi, pos + 1) - t0), b = (int)(st.lo - st.t0);
@@ -364,6 +380,23 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         for (int i = 0; i < AT_KEYS; ++i) {
           const bool in = i >= b && i < e && (i < s_end || i >= w_from);
           if (!in) x[i] = 0xff800000u;
+        }
+        // Values no row sees must not reach the product: zero them where the
+        // tile is not whole (the products of both row tiles come after this).
+        if (w == 0 && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS)) {
+          bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
+          const uint32_t j = st.t0 + row;
+          if (j < st.lo || j >= st.hi) {
+#pragma unroll
+            for (uint32_t i = 0; i < S::BLOCKS; ++i)
+#pragma unroll
+              for (uint32_t z = 0; z < 8; ++z)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
+                                                                          i * S::BLOCK_BYTES + row * 128 + z * 16),
+                             "r"(0u)
+                             : "memory");
+          }
+          fence_async_smem();
         }
       }
       float mx[8];   // eight chains: one of 128 would cost its latency 128 times
@@ -405,30 +438,15 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           p[z] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
         }
         tc_st16(ts + i * 16, p);
+        if (i & 1) {   // the product of a half starts while the other's exponentials run
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(b_p + 16 * w + (i / 2) * 8);
+        }
       }
       const uint64_t all4 = add_pair(add_pair(sum[0], sum[1]), add_pair(sum[2], sum[3]));
       l += pair_lo(all4) + pair_hi(all4);
-      // Values no row sees must not reach the product: zero them where the
-      // tile is not whole (the products of both row tiles come after this).
-      if (w == 0 && !whole) {
-        bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
-        const uint32_t j = st.t0 + row;
-        if (j < st.lo || j >= st.hi) {
-#pragma unroll
-          for (uint32_t b = 0; b < S::BLOCKS; ++b)
-#pragma unroll
-            for (uint32_t z = 0; z < 8; ++z)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
-                                                                        b * S::BLOCK_BYTES + row * 128 + z * 16),
-                           "r"(0u)
-                           : "memory");
-        }
-        fence_async_smem();
-      }
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(b_p + 8 * w);
       vslot += 2;
       if (vslot >= S::SLOTS) vslot -= S::SLOTS, vpar ^= 1;
       if (has_given_up(&s_gave_up)) break;
