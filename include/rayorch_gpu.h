@@ -208,7 +208,8 @@ enum {
   RO_K_COMMIT_FIX = 20, RO_K_READY_FUSED = 21,
   /* rayorch_cache.h */
   RO_K_ROTARY = 22, RO_K_ATTEND_ROWS = 23, RO_K_ATTEND_TILES = 24, RO_K_WEIGH = 25,
-  RO_K_WEIGH_TILES = 26, RO_K_EVICT_SELECT = 27, RO_K_EVICT_MOVE = 28, RO_K_COUNT = 29
+  RO_K_WEIGH_TILES = 26, RO_K_EVICT_SELECT = 27, RO_K_EVICT_MOVE = 28,
+  RO_K_ATTEND_JOIN = 29, RO_K_COUNT = 30
 };
 /* Tracing (no counterpart in the paper; it instruments the path).  Every
  * kernel launch is counted; kernels whose bit (1 << RO_K_*) is set in

@@ -42,7 +42,7 @@ KERNELS = ("expand_scan", "expand_fill", "ready_count", "ready_scatter", "commit
            "commit_plan", "asm_parents", "asm_members", "asm_copy", "retry_claim", "retry_scatter",
            "pb_keys", "pb_hist", "pb_rowscan", "pb_sort", "pb_bounds", "pb_heads", "pb_mark",
            "pb_scan", "pb_emit", "commit_fix", "ready_fused", "rotary", "attend_rows", "attend_tiles",
-           "weigh", "weigh_tiles", "evict_select", "evict_move")
+           "weigh", "weigh_tiles", "evict_select", "evict_move", "attend_join")
 
 
 class RoError(RuntimeError):

@@ -17,8 +17,7 @@
 // A CTA stays on its SM and takes pairs of row tiles as it gets free, heavy ones
 // first: the next pair's queries, keys and first products are under way while
 // the last one's output is written.  When there are fewer pairs than places,
-// the slots are split into runs and the last warp to finish its rows joins the
-// runs' (m, l, O) in order.
+// the slots are split into runs, whose (m, l, O) a second kernel joins in order.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -55,11 +54,16 @@ struct TileItem {
   uint32_t run, n_runs;
   uint32_t last;             // no work: the end
 };
+// A pair of row tiles for the join: its first token, its tokens, its runs.
+struct JoinItem {
+  uint64_t tok;
+  uint32_t n, runs;
+};
 constexpr uint32_t AT_ITEMS = 2;
 // The next item is taken this many slot tiles before the loads of the present
 // one end: early enough to decode it, late enough not to hold work that a CTA
 // which runs dry could do.
-constexpr uint32_t AT_AHEAD = 5;
+constexpr uint32_t AT_AHEAD = 8;
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
@@ -130,9 +134,20 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         it.last = id >= items;
         bool some = true;
         if (!it.last) {
-          const uint32_t x = id / a.c.n_heads, tile = x / a.max_chunks;
-          it.kh = id - x * a.c.n_heads;
-          it.run = x - tile * a.max_chunks;
+          // Unsplit: the heads of a pair of row tiles together, heavy pairs
+          // first.  Split: the pairs that read the same slots together, so
+          // that those come from L2 (one sequence of 64,000 slots, 512 new
+          // tokens: its cache is twice L2).
+          uint32_t tile;
+          if (a.max_chunks == 1) {
+            tile = id / a.c.n_heads;
+            it.kh = id - tile * a.c.n_heads;
+          } else {
+            const uint32_t x = id / a.tiles;
+            tile = id - x * a.tiles;
+            it.run = x / a.c.n_heads;
+            it.kh = x - it.run * a.c.n_heads;
+          }
           it.unit = tile * a.c.n_heads + it.kh;
           uint32_t s = 0, p = 0;
           some = a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
@@ -155,6 +170,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
             some = some && it.run < it.n_runs;
           }
         }
+        if (!it.last && a.max_chunks > 1 && it.run == 0 && lane == 0)   // for the join of the runs
+          ((JoinItem*)a.counter)[1 + it.unit] = {it.tok0 + it.i0, some ? it.i1 - it.i0 : 0u, some ? it.n_runs : 0u};
         if (some) {
           const uint32_t slot = k % AT_ITEMS;
           if (k >= AT_ITEMS) bar_wait_idle(b_item_free + 8 * slot, (k / AT_ITEMS - 1) & 1, &s_gave_up, a.err);
@@ -468,61 +485,42 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       for (int i = 0; i < DP; ++i) o[i] = 0u;
     }
     const uint32_t prow = w * AT_ROWS + row;               // the row among the pair's 256
-    float* part = a.partial + ((uint64_t)unit * a.max_chunks * 2 * AT_ROWS + prow) * DP;
-    float2* ml = (float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * DP) +
-                 (uint64_t)unit * a.max_chunks * 2 * AT_ROWS + prow;
     constexpr uint32_t STEP = 2 * AT_ROWS;                 // rows of a run
-    if (n_runs > 1) {
+    // four columns of a row together, rows next to one another: a warp's
+    // accesses are whole lines
+    float4* part = (float4*)a.partial + (uint64_t)unit * a.max_chunks * (DP / 4) * STEP + prow;
+    float2* ml = (float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * STEP * DP) +
+                 (uint64_t)unit * a.max_chunks * STEP + prow;
+    if (n_runs > 1) {   // joined by attend_join_kernel
       if (mine) {
 #pragma unroll
-        for (int i = 0; i < DP; i += 4)
-          __stcg((float4*)(part + (uint64_t)run * STEP * DP + i),
-                 make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]),
-                             __uint_as_float(o[i + 3])));
+        for (int i = 0; i < DP / 4; ++i)
+          __stcg(part + ((uint64_t)run * (DP / 4) + i) * STEP,
+                 make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
+                             __uint_as_float(o[4 * i + 3])));
         __stcg(ml + run * STEP, make_float2(m, l));
       }
-      // the last of the runs' warps to hold these 32 rows joins them, in order
-      __threadfence();
-      __syncwarp();
-      uint32_t* count = a.counter + 2 + unit * 8 + warp;
-      uint32_t last = 0;
-      if (lane == 0) last = ticket(count) == n_runs - 1;
-      if (!__shfl_sync(0xffffffffu, last, 0)) continue;
-      __threadfence();
-      if (lane == 0) *count = 0u;   // for the next call
-      m = -INFINITY;
-      l = 0.f;
-#pragma unroll
-      for (int i = 0; i < DP; ++i) o[i] = 0u;
-      if (mine) {
-        for (uint32_t r = 0; r < n_runs; ++r) m = fmaxf(m, __ldcg(ml + r * STEP).x);
-        const float sub = m == -INFINITY ? 0.f : m;
-        for (uint32_t r = 0; r < n_runs; ++r) {
-          const float2 z = __ldcg(ml + r * STEP);
-          const float f = ex2(z.x - sub);
-          l += f * z.y;
-#pragma unroll
-          for (int i = 0; i < DP; i += 4) {
-            const float4 v = __ldcg((const float4*)(part + (uint64_t)r * STEP * DP + i));
-            o[i] = __float_as_uint(__uint_as_float(o[i]) + f * v.x);
-            o[i + 1] = __float_as_uint(__uint_as_float(o[i + 1]) + f * v.y);
-            o[i + 2] = __float_as_uint(__uint_as_float(o[i + 2]) + f * v.z);
-            o[i + 3] = __float_as_uint(__uint_as_float(o[i + 3]) + f * v.w);
-          }
-        }
-      }
+      continue;
     }
     if (!mine) continue;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     T* out = (T*)a.out + out_at;
+    uint32_t y[DP / 2];
 #pragma unroll
-    for (int i = 0; i < DP; i += 8) {
-      uint4 v;
-      v.x = pack2<T>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-      v.y = pack2<T>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-      v.z = pack2<T>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-      v.w = pack2<T>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-      if ((uint32_t)i < a.c.head_dim) *(uint4*)(out + i) = v;
+    for (int i = 0; i < DP / 2; ++i) y[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+    // Each row is its thread's: 32 bytes a store where rows are aligned to
+    // them, half as many stores to as many lines.
+    if (g.wide) {
+#pragma unroll
+      for (int i = 0; i < DP / 2; i += 8)
+        if ((uint32_t)i * 2 < a.c.head_dim)
+          asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 2 * i), "r"(y[i]), "r"(y[i + 1]),
+                       "r"(y[i + 2]), "r"(y[i + 3]), "r"(y[i + 4]), "r"(y[i + 5]), "r"(y[i + 6]), "r"(y[i + 7])
+                       : "memory");
+    } else {
+#pragma unroll
+      for (int i = 0; i < DP / 2; i += 4)
+        if ((uint32_t)i * 2 < a.c.head_dim) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
     }
     if (a.lse) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
   }
@@ -531,13 +529,52 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   asm volatile("bar.sync 0;" ::: "memory");
 }
 
+// Joins the runs of split pairs of row tiles, in order: a thread takes four
+// columns of a row, a CTA the 256 rows of a pair.  (A second launch: the last
+// CTA of a pair would have to read all of its runs at one SM's rate, 2 us a run.)
+template <typename T, int DP>
+__global__ void __launch_bounds__(2 * AT_ROWS) attend_join_kernel(const __grid_constant__ AttendTileArgs g) {
+  wait_predecessor();
+  const AttendArgs& a = g.a;
+  constexpr uint32_t STEP = 2 * AT_ROWS;
+  const uint32_t unit = blockIdx.x / (DP / 4), c = blockIdx.x - unit * (DP / 4), prow = threadIdx.x;
+  const JoinItem it = ((const JoinItem*)a.counter)[1 + unit];
+  const uint32_t runs = it.runs, w = prow / AT_ROWS, row = prow % AT_ROWS;
+  const uint32_t i = w * g.toks + row / a.r.group, head = (unit % a.c.n_heads) * a.r.group + row % a.r.group;
+  if (runs < 2 || runs > a.max_chunks || row >= g.toks * a.r.group || i >= it.n || it.tok + i >= a.r.n_tokens) return;
+  const float4* part = (const float4*)a.partial + ((uint64_t)unit * a.max_chunks * (DP / 4) + c) * STEP + prow;
+  const float2* ml = (const float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * STEP * DP) +
+                     (uint64_t)unit * a.max_chunks * STEP + prow;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (uint32_t r = 0; r < runs; ++r) {
+    const float2 z = ml[r * STEP];
+    const float4 v = part[(uint64_t)r * (DP / 4) * STEP];
+    const float nm = fmaxf(m, z.x), sub = nm == -INFINITY ? 0.f : nm;
+    const float f = ex2(m - sub), e = ex2(z.x - sub);
+    m = nm;
+    l = l * f + z.y * e;
+    o.x = o.x * f + v.x * e;
+    o.y = o.y * f + v.y * e;
+    o.z = o.z * f + v.z * e;
+    o.w = o.w * f + v.w * e;
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const uint64_t t = it.tok + i;
+  if (c * 4 < a.c.head_dim)
+    *(uint2*)((T*)a.out + t * a.out_tok + (uint64_t)head * a.out_head + c * 4) =
+        make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+  if (c == 0 && a.lse) a.lse[t * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+}
+
 // ---- host ------------------------------------------------------------------------------------
 bool attend_tiles_fits(const AttendArgs& a) {
   return a.c.page_shift >= 3 && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
 }
 uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
 size_t attend_tiles_counters(const AttendArgs& a) {
-  return (2 + (a.max_chunks > 1 ? (size_t)a.tiles * a.c.n_heads * 8 : 0)) * sizeof(uint32_t);
+  return (1 + (a.max_chunks > 1 ? (size_t)a.tiles * a.c.n_heads : 0)) * sizeof(JoinItem);
 }
 size_t attend_tiles_partial(const AttendArgs& a) {
   const size_t dp = a.c.head_dim <= 64 ? 64 : 128;
@@ -549,12 +586,16 @@ static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
   launch_k(L, K_ATTEND_TILES, attend_tiles_kernel<T, DP>, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), AT_THREADS,
            TileShape<DP>::SMEM, g);
+  if (g.a.max_chunks > 1)
+    launch_k(L, K_ATTEND_JOIN, attend_join_kernel<T, DP>, g.a.tiles * g.a.c.n_heads * (DP / 4), 2 * AT_ROWS, 0, g);
 }
 bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int sms) {
   AttendTileArgs g;
   g.a = a;
   g.toks = AT_ROWS / a.r.group;
   g.box = std::min<uint32_t>(a.c.page_size, AT_KEYS);
+  g.wide = a.c.head_dim % 16 == 0 && a.out_tok % 16 == 0 && a.out_head % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(a.out) % 32 == 0;
   if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
       !pool_map(&g.v, a.c, a.c.v, dtype, g.box))
     return false;

@@ -52,7 +52,7 @@ enum KernelId { K_EXPAND_SCAN, K_FILL, K_RB_COUNT, K_RB_SCATTER, K_COMMIT, K_CPL
                 K_AMEMBERS, K_ACOPY, K_RT_CLAIM, K_RT_SCATTER, K_PB_KEYS, K_PB_HIST,
                 K_PB_ROWSCAN, K_PB_SORT, K_PB_BOUNDS, K_PB_HEADS, K_PB_MARK, K_PB_SCAN, K_PB_EMIT,
                 K_CFIX, K_RB_FUSED, K_ROTARY, K_ATTEND_ROWS, K_ATTEND_TILES, K_WEIGH, K_WEIGH_TILES,
-                K_EVICT_SELECT, K_EVICT_MOVE, K_COUNT,
+                K_EVICT_SELECT, K_EVICT_MOVE, K_ATTEND_JOIN, K_COUNT,
                 K_RB_FUSED_CALLS = 100 };   // occupancy query only (profiled as K_RB_FUSED)
 
 

@@ -59,7 +59,7 @@ __device__ __forceinline__ void bar_wait_idle(uint32_t bar, uint32_t parity, vol
       record(err, ERR_TIMEOUT);
       *gave_up = 1u;
     }
-    __nanosleep(500);
+    __nanosleep(200);
   }
 }
 // a whole warp, so that it leaves a loop together
@@ -313,6 +313,7 @@ struct AttendTileArgs {
   CUtensorMap q, k, v;
   uint32_t toks;             // tokens of a row tile
   uint32_t box;              // slots of a TMA box
+  uint32_t wide;             // output rows are aligned to 32 bytes
 };
 struct WeighFewArgs {
   WeighArgs a;
