@@ -7,8 +7,8 @@
 //
 // Bound by the bytes of K and V, so everything serves keeping loads in flight:
 // a warp of loads keeps a ring of 16 KB stages full (a stage is 32 slots of
-// 128 dimensions or 64 of 64, keys and values; by TMA a page at a time, or row
-// by row where pages are no power of two of at least 8 slots), and three warps
+// 128 dimensions or 64 of 64, keys and values; by TMA a part of a page at a
+// time, or row by row where the page size is no multiple of 4), and three warps
 // take the stages in turn, each with an (m, l, o) of its own, so that no
 // barrier joins them before the end.  A long sequence is cut into runs; the
 // last CTA of a tile to finish joins them in the order of the slots, so the
@@ -308,8 +308,8 @@ static void launch_few(const LaunchCfg& L, const AttendFewArgs& g) {
 void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype) {
   AttendFewArgs g;
   g.a = a;
-  g.box = a.c.page_shift >= 3 ? std::min<uint32_t>(a.c.page_size, attend_few_keys(a.c.head_dim)) : 1u;
-  g.tma = g.box >= 8 && pool_map(&g.k, a.c, a.c.k, dtype, g.box) && pool_map(&g.v, a.c, a.c.v, dtype, g.box);
+  g.box = page_box(a.c.page_size, attend_few_keys(a.c.head_dim));
+  g.tma = g.box >= MIN_BOX && pool_map(&g.k, a.c, a.c.k, dtype, g.box) && pool_map(&g.v, a.c, a.c.v, dtype, g.box);
   if (!g.tma) g.box = 1;
   const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)

@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         auto page_of = [&](uint32_t t) -> uint32_t {
           if (t >= n) return 0u;
           const SlotTile st = slots.at(c0 + t);
-          return has_box(st) ? a.c.pages[page0 + ((st.t0 + lane * g.box) >> a.c.page_shift)] : 0u;
+          return has_box(st) ? a.c.pages[page0 + page_index(a.c, st.t0 + lane * g.box)] : 0u;
         };
         uint32_t page = page_of(0), next = page_of(1);
         const uint32_t want = n > AT_AHEAD ? n - AT_AHEAD : 0;
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           if (t == want && lane == 0) bar_arrive(b_want);
           const uint32_t after = page_of(t + 2);
           const SlotTile st = slots.at(c0 + t);
-          const uint32_t y = (st.t0 + lane * g.box) & (a.c.page_size - 1u);
+          const uint32_t j = st.t0 + lane * g.box, y = j - page_index(a.c, j) * a.c.page_size;
           bool load = has_box(st);
           if (load && page >= a.c.n_pages) {
             record(a.err, ERR_INVAL);
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(2 * AT_ROWS) attend_join_kernel(const __grid_c
 
 // ---- host ------------------------------------------------------------------------------------
 bool attend_tiles_fits(const AttendArgs& a) {
-  return a.c.page_shift >= 3 && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
+  return page_box(a.c.page_size, AT_KEYS) >= MIN_BOX && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
 }
 uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
 size_t attend_tiles_counters(const AttendArgs& a) {
@@ -593,7 +593,7 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int
   AttendTileArgs g;
   g.a = a;
   g.toks = AT_ROWS / a.r.group;
-  g.box = std::min<uint32_t>(a.c.page_size, AT_KEYS);
+  g.box = page_box(a.c.page_size, AT_KEYS);
   g.wide = a.c.head_dim % 16 == 0 && a.out_tok % 16 == 0 && a.out_head % 16 == 0 &&
            reinterpret_cast<uintptr_t>(a.out) % 32 == 0;
   if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||

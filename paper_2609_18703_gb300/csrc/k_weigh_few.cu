@@ -166,8 +166,8 @@ static void launch_few(const LaunchCfg& L, const WeighFewArgs& g) {
 void launch_weigh_few(const LaunchCfg& L, const WeighArgs& a, int dtype) {
   WeighFewArgs g;
   g.a = a;
-  g.box = a.c.page_shift >= 3 ? std::min<uint32_t>(a.c.page_size, weigh_few_keys(a.c.head_dim)) : 1u;
-  g.tma = g.box >= 8 && pool_map(&g.k, a.c, a.c.k, dtype, g.box);
+  g.box = page_box(a.c.page_size, weigh_few_keys(a.c.head_dim));
+  g.tma = g.box >= MIN_BOX && pool_map(&g.k, a.c, a.c.k, dtype, g.box);
   if (!g.tma) g.box = 1;
   const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)

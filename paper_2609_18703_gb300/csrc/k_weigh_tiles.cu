@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
       bool load = lane < WT_KEYS / g.box && j <= j_hi;
       uint32_t page = 0;
       if (load) {
-        page = a.c.pages[q.page0 + (j >> a.c.page_shift)];
+        page = a.c.pages[q.page0 + page_index(a.c, j)];
         if (page >= a.c.n_pages) {
           record(a.err, ERR_INVAL);
           load = false;
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
       __syncwarp();
       if (load)
         for (uint32_t b = 0; b < S::BLOCKS; ++b)
-          tma4(sm + b * S::BLOCK_BYTES + lane * g.box * 128, &g.k, b * 64, (int)(j & (a.c.page_size - 1u)), (int)kh,
+          tma4(sm + b * S::BLOCK_BYTES + lane * g.box * 128, &g.k, b * 64, (int)(j - page_index(a.c, j) * a.c.page_size), (int)kh,
                (int)page, b_k);
       uint32_t slot = 0, parity = 1;
       for (uint32_t t = 0; t < n; ++t) {
@@ -226,7 +226,9 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
   }
 }
 
-bool weigh_tiles_fits(const WeighArgs& a) { return a.c.page_shift >= 3 && a.r.group <= WT_ROWS; }
+bool weigh_tiles_fits(const WeighArgs& a) {
+  return page_box(a.c.page_size, WT_KEYS) >= MIN_BOX && a.r.group <= WT_ROWS;
+}
 
 template <typename T, int DP>
 static void launch_tiles(const LaunchCfg& L, const WeighTileArgs& g) {
@@ -237,7 +239,7 @@ bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype) {
   WeighTileArgs g;
   g.a = a;
   g.toks = WT_ROWS / a.r.group;
-  g.box = std::min<uint32_t>(a.c.page_size, WT_KEYS);
+  g.box = page_box(a.c.page_size, WT_KEYS);
   if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box))
     return false;
   const bool narrow = a.c.head_dim <= 64;

@@ -102,14 +102,12 @@ __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& c, const RowsArgs& 
   q.first = (int64_t)len - (int64_t)q.n;
   return q;
 }
+__device__ __forceinline__ uint32_t page_index(const PagedArgs& c, uint32_t j) {
+  return c.page_shift >= 0 ? j >> c.page_shift : j / c.page_size;
+}
 __device__ __forceinline__ void split_slot(const PagedArgs& c, uint32_t j, uint32_t* page, uint32_t* slot) {
-  if (c.page_shift >= 0) {
-    *page = j >> c.page_shift;
-    *slot = j & (c.page_size - 1u);
-  } else {
-    *page = j / c.page_size;
-    *slot = j - *page * c.page_size;
-  }
+  *page = page_index(c, j);
+  *slot = j - *page * c.page_size;
 }
 
 // The keys that the tokens [i0, i1) of a sequence see, numbered without the

@@ -233,7 +233,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
       if (u >= n) return 0u;
       const SlotTile st = slots.at(c0 + u);
       const uint32_t j = st.t0 + (lane % boxes) * box;
-      return has_box(st, j) ? c.pages[page0 + (j >> c.page_shift)] : 0u;
+      return has_box(st, j) ? c.pages[page0 + page_index(c, j)] : 0u;
     };
     uint32_t next = page_of(0), page = 0;
     for (uint32_t t = 0; t < n; ++t) {
@@ -255,7 +255,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
       if (lane == 0) bar_expect(full, (VALUES ? 2 : 1) * loaded * BLOCKS * box * 128);
       __syncwarp();
       if (load) {
-        const int y = (int)(j & (c.page_size - 1u));
+        const int y = (int)(j - page_index(c, j) * c.page_size);
 #pragma unroll
         for (uint32_t x = 0; x < BLOCKS; ++x) {
           tma4(dst + x * BLOCK_BYTES, km, x * 64, y, (int)kh, (int)page, full);
@@ -300,6 +300,15 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
 }
 
 // ---- host: tensor maps -----------------------------------------------------------------------
+// Slots that one TMA box loads: the largest power of two that divides the
+// pages, at most `most`.  A box starts at any multiple of 128 bytes of a
+// swizzled tile: the swizzle goes by the address.  Below 4 slots a box the
+// loads go row by row.
+constexpr uint32_t MIN_BOX = 4;
+inline uint32_t page_box(uint32_t page_size, uint32_t most) {
+  const uint32_t b = page_size & (0u - page_size);
+  return b < most ? b : most;
+}
 // 64-column blocks with the 128-byte swizzle; false: the tensor cannot be mapped
 bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t* size, const uint64_t* stride,
               const uint32_t* box);
