@@ -20,7 +20,8 @@
 namespace ro {
 
 constexpr int AF_WARPS = 3, AF_THREADS = 32 * (AF_WARPS + 1), AF_ROWS = 16;
-constexpr uint32_t AF_STAGES = 6, AF_STAGE = 16384;   // two CTAs on an SM
+// two CTAs on an SM
+constexpr uint32_t AF_STAGES = 6, AF_STAGE = 16384;
 // A place of the ring always belongs to the same warp.  (Loads land in any
 // order: a warp that waited for a place's next phase while another warp's load
 // there was still in flight would find the parity of the phase before it.)
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
   __syncthreads();
 
   if (warp == AF_WARPS) {
-    load_stages<T, DP, KEYS, AF_STAGES, true>(a.c, &g.k, &g.v, g.tma != 0, g.box, slots, c0, n, kh, q.page0, sm, b_full,
+    load_stages<T, DP, KEYS, true>(a.c, &g.k, &g.v, g.tma != 0, g.box, AF_STAGES, slots, c0, n, kh, q.page0, sm, b_full,
                                               b_empty, &s_gave_up, a.err, [](const SlotTile&) { return true; });
   }
 

@@ -15,8 +15,10 @@
 namespace ro {
 
 constexpr int WF_WARPS = 3, WF_THREADS = 32 * (WF_WARPS + 1);
-constexpr uint32_t WF_STAGES = 6, WF_STAGE = 16384;   // two CTAs on an SM
-static_assert(WF_STAGES % WF_WARPS == 0, "a place of the ring belongs to one warp");
+// Two CTAs on an SM; calls whose CTAs have at most three stages take half the
+// ring, so that more of them fit.
+constexpr uint32_t WF_STAGES = 6, WF_STAGE = 16384;
+static_assert(WF_STAGES == 2 * WF_WARPS, "a place of the ring belongs to one warp");
 constexpr uint32_t WF_SMEM = 1024 + WF_STAGES * WF_STAGE;
 template <int DP>
 constexpr int wf_keys() {
@@ -44,7 +46,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
   }
   const KeySpan every = {0u, 0u, len};
   const SlotTiles<KEYS> slots(every, g.box);
-  const uint32_t per = max(a.chunk, slots.n / a.tiles + 1);
+  const uint32_t per = max(a.chunk, (slots.n + a.tiles - 1) / a.tiles);
   const uint32_t c0 = blockIdx.y * per;
   if (c0 >= slots.n) return;
   const uint32_t n = min(per, slots.n - c0);
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
   }
   __syncthreads();
   if (warp == WF_WARPS) {
-    load_stages<T, DP, KEYS, WF_STAGES, false>(a.c, &g.k, &g.k, g.tma != 0, g.box, slots, c0, n, kh, q.page0, sm, b_full,
+    load_stages<T, DP, KEYS, false>(a.c, &g.k, &g.k, g.tma != 0, g.box, g.stages, slots, c0, n, kh, q.page0, sm, b_full,
                                                b_empty, &s_gave_up, a.err, seen);
   } else {
     // query rows as the right operand, two groups of eight; each row's lse, +inf for rows that add nothing
@@ -103,7 +105,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
     }
     const uint64_t row = ((uint64_t)seq * a.c.n_heads + kh) * a.score_cap;
     for (uint32_t t = warp; t < n; t += WF_WARPS) {
-      const uint32_t slot = t % WF_STAGES;
+      const uint32_t round = t / WF_WARPS, rounds = g.stages / WF_WARPS, slot = warp + WF_WARPS * (round % rounds);
       const SlotTile st = slots.at(c0 + t);
       float past[KEYS / 32];   // under way while the keys arrive
 #pragma unroll
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
         const uint32_t j = st.t0 + i * 32 + lane;
         past[i] = a.past && j < st.hi && (int64_t)j < q.first ? a.past[row + j] : 0.f;
       }
-      bar_wait(b_full + 8 * slot, (t / WF_STAGES) & 1, &s_gave_up, a.err);
+      bar_wait(b_full + 8 * slot, (round / rounds) & 1, &s_gave_up, a.err);
       const bool used = seen(st);
       if (used) {
         const bool all = (int64_t)st.t0 + KEYS - 1 <= q.first && (r.window == 0u || (int64_t)st.t0 > a_max - (int64_t)r.window);
@@ -161,12 +163,14 @@ uint32_t weigh_few_keys(uint32_t head_dim) { return head_dim <= 64 ? wf_keys<64>
 
 template <typename T, int DP>
 static void launch_few(const LaunchCfg& L, const WeighFewArgs& g) {
-  launch_k(L, K_WEIGH, weigh_few_kernel<T, DP>, dim3(g.a.c.n_seqs * g.a.c.n_heads, g.a.tiles), WF_THREADS, WF_SMEM, g);
+  launch_k(L, K_WEIGH, weigh_few_kernel<T, DP>, dim3(g.a.c.n_seqs * g.a.c.n_heads, g.a.tiles), WF_THREADS,
+           1024 + g.stages * WF_STAGE, g);
 }
 void launch_weigh_few(const LaunchCfg& L, const WeighArgs& a, int dtype) {
   WeighFewArgs g;
   g.a = a;
   g.box = page_box(a.c.page_size, weigh_few_keys(a.c.head_dim));
+  g.stages = a.chunk <= WF_WARPS ? WF_WARPS : WF_STAGES;
   g.tma = g.box >= MIN_BOX && pool_map(&g.k, a.c, a.c.k, dtype, g.box);
   if (!g.tma) g.box = 1;
   const bool narrow = a.c.head_dim <= 64;

@@ -25,6 +25,39 @@ struct WeighShape {
   static constexpr uint32_t SMEM = 1024 + (1 + WT_STAGES) * TILE_BYTES;
 };
 
+// Of a sequence whose tokens have a window: the tiles [0, sinks) of the sinks,
+// then from tile `window` on; those between are seen by no token.
+struct SeenTiles {
+  uint32_t sinks, window;
+};
+__device__ __forceinline__ SeenTiles seen_tiles(const SeqInfo& q, const RowsArgs& r) {
+  const int64_t lo = q.first - (int64_t)r.window + 1;   // the first slot of the first token's window
+  SeenTiles s;
+  s.window = lo > 0 ? (uint32_t)(lo / WT_KEYS) : 0u;
+  s.sinks = min((r.sinks + WT_KEYS - 1) / WT_KEYS, s.window);
+  return s;
+}
+__device__ __forceinline__ uint32_t scored(const WeighArgs& a, const SeqInfo& q, bool first) {
+  if (q.len > a.score_cap) {
+    if (first) record(a.err, ERR_CAPACITY);
+    return (uint32_t)a.score_cap;
+  }
+  return q.len;
+}
+
+// decay * past for the slots that no token sees
+constexpr int WP_THREADS = 256;
+__global__ void __launch_bounds__(WP_THREADS) weigh_past_kernel(const __grid_constant__ WeighArgs a) {
+  wait_predecessor();
+  const uint32_t unit = blockIdx.x / a.chunk, part = blockIdx.x - unit * a.chunk;   // a.chunk CTAs for each
+  const SeqInfo q = seq_info(a.c, a.r, unit / a.c.n_heads, a.err);
+  const SeenTiles st = seen_tiles(q, a.r);
+  const uint32_t to = min(scored(a, q, false), st.window * WT_KEYS);
+  const uint64_t row = (uint64_t)unit * a.score_cap;
+  for (uint32_t j = st.sinks * WT_KEYS + part * WP_THREADS + threadIdx.x; j < to; j += a.chunk * WP_THREADS)
+    a.score[row + j] = a.past ? a.decay * a.past[row + j] : 0.f;   // (before the window: no new slot)
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid_constant__ WeighTileArgs g) {
   using S = WeighShape<DP>;
@@ -38,12 +71,13 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
   wait_predecessor();
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t kh = blockIdx.x % a.c.n_heads, rest = blockIdx.x / a.c.n_heads;
-  const uint32_t seq = rest / a.tiles, tile = rest - seq * a.tiles;
+  const uint32_t seq = rest / a.tiles;
+  uint32_t tile = rest - seq * a.tiles;
   const SeqInfo q = seq_info(a.c, a.r, seq, a.err);
-  uint32_t len = q.len;
-  if (len > a.score_cap) {
-    if (tile == 0 && tid == 0) record(a.err, ERR_CAPACITY);
-    len = (uint32_t)a.score_cap;
+  const uint32_t len = scored(a, q, tile == 0 && tid == 0);
+  if (a.unseen) {
+    const SeenTiles st = seen_tiles(q, a.r);
+    if (tile >= st.sinks) tile += st.window - st.sinks;
   }
   const uint64_t j0 = (uint64_t)tile * WT_KEYS;
   if (j0 >= len) return;
@@ -52,6 +86,12 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
   seeing_tokens(q, a.r, j_lo, j_hi, &i0, &i1);
   const uint32_t G = a.r.group;
   const uint32_t n = (i1 - i0 + g.toks - 1) / g.toks;   // row tiles
+  const uint64_t at = ((uint64_t)seq * a.c.n_heads + kh) * a.score_cap + j_lo + tid;   // this thread's slot's score
+  if (n == 0) {
+    if (tid < WT_KEYS && j_lo + tid <= j_hi)
+      a.score[at] = a.past && (int64_t)(j_lo + tid) < q.first ? a.decay * a.past[at] : 0.f;
+    return;
+  }
 
   const uint32_t sm = (step_smem(smem_raw) + 1023u) & ~1023u, sm_q = sm + S::TILE_BYTES;
   const uint32_t b_k = step_smem(s_bar), b_full = b_k + 8, b_empty = b_full + 8 * WT_STAGES, b_s = b_empty + 8 * WT_STAGES,
@@ -84,7 +124,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
   float sum = 0.f;
   if (warp == 9) {
     // ---- loads ----
-    if (n > 0) {
+    {
       const uint32_t j = j_lo + lane * g.box;
       bool load = lane < WT_KEYS / g.box && j <= j_hi;
       uint32_t page = 0;
@@ -120,7 +160,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
     // ---- products ----
     const uint32_t shape = mma_shape<T>(WT_ROWS, false), one = elect_lane();
     const uint32_t k_lo = operand_lo(sm, 16), q_lo = operand_lo(sm_q, 16);
-    if (n > 0) bar_wait(b_k, 0, &s_gave_up, a.err);
+    bar_wait(b_k, 0, &s_gave_up, a.err);
     uint32_t slot = 0, parity = 0;
     for (uint32_t t = 0; t < n; ++t) {
       const uint32_t w = t & 1;
@@ -219,10 +259,8 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
     tmem_free(tm, WT_TMEM_COLS);
   }
   if (tid < WT_KEYS && j_lo + tid <= j_hi) {
-    const uint32_t j = j_lo + tid;
-    const uint64_t e = ((uint64_t)seq * a.c.n_heads + kh) * a.score_cap + j;
-    const float past = a.past && (int64_t)j < q.first ? a.decay * a.past[e] : 0.f;
-    a.score[e] = past + (sum + s_sum[tid]);
+    const float past = a.past && (int64_t)(j_lo + tid) < q.first ? a.decay * a.past[at] : 0.f;
+    a.score[at] = past + (sum + s_sum[tid]);
   }
 }
 
@@ -235,13 +273,20 @@ static void launch_tiles(const LaunchCfg& L, const WeighTileArgs& g) {
   launch_k(L, K_WEIGH_TILES, weigh_tiles_kernel<T, DP>, g.a.tiles * g.a.c.n_seqs * g.a.c.n_heads, WT_THREADS,
            WeighShape<DP>::SMEM, g);
 }
-bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype) {
+bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype, int sms) {
   WeighTileArgs g;
   g.a = a;
   g.toks = WT_ROWS / a.r.group;
   g.box = page_box(a.c.page_size, WT_KEYS);
   if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box))
     return false;
+  if (a.unseen) {
+    WeighArgs p = a;
+    const uint64_t units = (uint64_t)a.c.n_seqs * a.c.n_heads;
+    p.chunk = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(a.score_cap, WP_THREADS * 8),
+                                                                  ceil_div((uint64_t)sms * 8, units)));
+    launch_k(L, K_WEIGH, weigh_past_kernel, (unsigned)(units * p.chunk), WP_THREADS, 0, p);
+  }
   const bool narrow = a.c.head_dim <= 64;
   if (dtype == RO_BF16)
     narrow ? launch_tiles<__nv_bfloat16, 64>(L, g) : launch_tiles<__nv_bfloat16, 128>(L, g);

@@ -136,6 +136,7 @@ struct WeighArgs {
   uint64_t score_cap;
   uint32_t tiles;            // CTAs along score_cap for each sequence and head, at most
   uint32_t chunk;            // weigh_few: stages of a CTA
+  uint32_t unseen;           // weigh_tiles: the tiles before the windows are another kernel's
   uint32_t* err;
 };
 // at most 16 rows a sequence; slots of a stage
@@ -146,7 +147,7 @@ cudaError_t prepare_weigh_few_kernels();
 // false: the tensors cannot be mapped
 constexpr uint32_t WT_KEYS = 128;
 bool weigh_tiles_fits(const WeighArgs& a);
-bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype);
+bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype, int sms);
 cudaError_t prepare_weigh_tiles_kernels();
 // any page size and group
 constexpr int WG_THREADS = 128;

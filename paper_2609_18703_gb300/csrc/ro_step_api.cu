@@ -352,13 +352,20 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
     // bound by the keys' bytes: runs of stages as in the attention of few rows
     const uint64_t stages = ceil_div(score_cap, weigh_few_keys(cache->head_dim));
     const uint64_t each = ceil_div(stages * units, (uint64_t)c.sms() * 2);
-    a.chunk = (uint32_t)std::max<uint64_t>(6, ceil_div(each, ceil_div(each, 48)));
+    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 48)));
+    a.chunk = (uint32_t)std::min<uint64_t>(a.chunk, stages);
     a.tiles = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 65535);
     launch_weigh_few(c.launch(), a, cache->dtype);
     return c.launched(fn);
   }
-  a.tiles = (uint32_t)ceil_div(score_cap, WT_KEYS);
-  if (n_tokens && weigh_tiles_fits(a) && launch_weigh_tiles(c.launch(), a, cache->dtype)) return c.launched(fn);
+  // Behind a window most tiles of slots only have their past scores decayed: a
+  // second kernel's, which leaves the tiles of the sinks and of the window.
+  const uint64_t all = ceil_div(score_cap, WT_KEYS);
+  const uint64_t seen = ceil_div(sinks, WT_KEYS) + ceil_div((uint64_t)window + a.r.max_new, WT_KEYS) + 1;
+  a.unseen = window != 0 && seen < all;
+  a.tiles = (uint32_t)(a.unseen ? seen : all);
+  if (n_tokens && weigh_tiles_fits(a) && launch_weigh_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
+  a.unseen = 0;
   a.tiles = (uint32_t)ceil_div(score_cap, WG_KEYS);
   launch_weigh(c.launch(), a, cache->dtype);
   return c.launched(fn);

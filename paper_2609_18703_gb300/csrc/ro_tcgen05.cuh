@@ -209,15 +209,15 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // ---- a ring of stages of slots -----------------------------------------------------------------
-// One warp's work: keep a ring of STAGES stages full with the tiles
+// One warp's work: keep a ring of `stages` stages full with the tiles
 // [c0, c0 + n) of one sequence and head, KEYS slots of DP dimensions each, keys
 // (and values behind them).  want(tile): false leaves a tile unloaded.  By TMA
 // a box (part of a page) a lane; without, row by row with cp.async, 32 arrivals
 // on a full stage instead of one.
-template <typename T, int DP, int KEYS, uint32_t STAGES, bool VALUES, class Want>
+template <typename T, int DP, int KEYS, bool VALUES, class Want>
 __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMap* km, const CUtensorMap* vm, bool tma,
-                                            uint32_t box, const SlotTiles<KEYS>& slots, uint32_t c0, uint32_t n,
-                                            uint32_t kh, uint64_t page0, uint32_t sm, uint32_t b_full, uint32_t b_empty,
+                                            uint32_t box, uint32_t stages, const SlotTiles<KEYS>& slots, uint32_t c0,
+                                            uint32_t n, uint32_t kh, uint64_t page0, uint32_t sm, uint32_t b_full, uint32_t b_empty,
                                             uint32_t* gave_up, uint32_t* err, Want want) {
   constexpr uint32_t BLOCKS = DP / 64, BLOCK_BYTES = KEYS * 128, SIDE = BLOCKS * BLOCK_BYTES;
   constexpr uint32_t STAGE = VALUES ? 2 * SIDE : SIDE;
@@ -249,7 +249,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
         load = false;
       }
       const uint32_t loaded = __popc(__ballot_sync(0xffffffffu, load));
-      if (t >= STAGES) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
+      if (t >= stages) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
       if (has_given_up(gave_up)) break;
       const uint32_t full = b_full + 8 * slot, dst = sm + slot * STAGE + b * box * 128;
       if (lane == 0) bar_expect(full, (VALUES ? 2 : 1) * loaded * BLOCKS * box * 128);
@@ -262,7 +262,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
           if (VALUES) tma4(dst + SIDE + x * BLOCK_BYTES, vm, x * 64, y, (int)kh, (int)page, full);
         }
       }
-      if (++slot == STAGES) slot = 0, parity ^= 1;
+      if (++slot == stages) slot = 0, parity ^= 1;
     }
   } else {
     constexpr uint32_t CH = DP / 8, PER = 32 / CH;   // 16-byte pieces of a row; rows at a time
@@ -270,7 +270,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
     for (uint32_t t = 0; t < n; ++t) {
       const SlotTile st = slots.at(c0 + t);
       const bool wanted = want(st);
-      if (t >= STAGES) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
+      if (t >= stages) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
       if (has_given_up(gave_up)) break;
       for (uint32_t r = lane / CH; r < (uint32_t)KEYS; r += PER) {
         const uint32_t j = st.t0 + r;
@@ -292,7 +292,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
         if (VALUES) cp_async16_or_zero(dst + SIDE, (const T*)c.v + e, ok);
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(b_full + 8 * slot) : "memory");
-      if (++slot == STAGES) slot = 0, parity ^= 1;
+      if (++slot == stages) slot = 0, parity ^= 1;
     }
     cp_async_commit();
     cp_async_wait<0>();
@@ -328,6 +328,7 @@ struct WeighFewArgs {
   WeighArgs a;
   CUtensorMap k;
   uint32_t box, tma;
+  uint32_t stages;           // of the ring
 };
 struct WeighTileArgs {
   WeighArgs a;

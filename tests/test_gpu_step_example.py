@@ -1,0 +1,54 @@
+"""The example that runs the model-step operators beside the lineage path: every
+video's assembled records against the same step in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+
+
+def test_every_video_against_64_bits():
+    from examples import stream_frames as ex
+    from tests import step_reference as ref
+    counts, outs, held = ex.run(videos=9, frames=30, wave=7, seed=4)
+    assert held == counts.tolist()
+    _, records, place, weight = ex.inputs(9, 30, 4)
+    qkv = (records @ weight).view(-1, ex.HEADS + 2 * ex.KV_HEADS, ex.DIM).cpu()
+    turned = ref.turn(qkv, place.cpu(), [16, 8, 8], 10_000.0, False)
+    starts = np.concatenate([[0], np.cumsum(counts)])
+    for i, n in enumerate(counts):
+        rows = slice(starts[i], starts[i] + n)
+        k = turned[rows, ex.HEADS:ex.HEADS + ex.KV_HEADS]
+        v = qkv[rows, ex.HEADS + ex.KV_HEADS:].double()
+        for h in range(ex.HEADS):
+            kh = h // (ex.HEADS // ex.KV_HEADS)
+            x = turned[rows, h] @ k[:, kh].T / math.sqrt(ex.DIM)
+            x = x.masked_fill(~torch.ones(n, n, dtype=torch.bool).tril(), -math.inf)
+            p = torch.softmax(x, 1)
+            want = p @ v[:, kh]
+            # q and k are rounded to f16 once turned, a logit errs by their sum's size; weights and output are f16
+            dx = 2 * 2.0 ** -11 * (turned[rows, h].abs() @ k[:, kh].abs().T).amax(1, keepdim=True) / math.sqrt(ex.DIM)
+            tol = (2 * dx + 2.0 ** -10) * (p @ v[:, kh].abs()) + 2.0 ** -11 * want.abs() + 1e-6
+            assert bool(((outs[i][:, h].double().cpu() - want).abs() <= tol).all())
+
+
+def test_caches_stay_within_their_budget():
+    from examples import stream_frames as ex
+    counts, outs, held = ex.run(videos=20, frames=60, wave=16, budget=33, seed=5)
+    assert held == np.minimum(counts, 33).tolist() and max(counts) > 33
+    whole, full, _ = ex.run(videos=20, frames=60, wave=16, seed=5)
+    for i in range(20):
+        assert not bool(torch.isnan(outs[i]).any())
+        n = min(int(counts[i]), 32)   # two waves fit the budget: the same until then
+        assert torch.equal(outs[i][:n], full[i][:n])
