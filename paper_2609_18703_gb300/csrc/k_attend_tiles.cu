@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           }
         }
         if (!it.last && a.max_chunks > 1 && it.run == 0 && lane == 0)   // for the join of the runs
-          ((JoinItem*)a.counter)[1 + it.unit] = {it.tok0 + it.i0, some ? it.i1 - it.i0 : 0u, some ? it.n_runs : 0u};
+          ((JoinItem*)a.join)[it.unit] = {it.tok0 + it.i0, some ? it.i1 - it.i0 : 0u, some ? it.n_runs : 0u};
         if (some) {
           const uint32_t slot = k % AT_ITEMS;
           if (k >= AT_ITEMS) bar_wait_idle(b_item_free + 8 * slot, (k / AT_ITEMS - 1) & 1, &s_gave_up, a.err);
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       uint32_t x[AT_KEYS];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
-      tc_wait_ld();
+      tc_wait_ld(x);
       const bool all = t < sinks_all || (t >= all_from && t < all_to);
       if (!all) {
         const SlotTile st = slots.at(c0 + t);
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 #pragma unroll 1
           for (int i = 0; i < DP / 16; ++i) {
             tc_ld16(to + i * 16, o);
-            tc_wait_ld();
+            tc_wait_ld(o);
 #pragma unroll
             for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
             tc_st16(to + i * 16, o);
@@ -466,8 +466,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       l += pair_lo(all4) + pair_hi(all4);
       vslot += 2;
       if (vslot >= S::SLOTS) vslot -= S::SLOTS, vpar ^= 1;
-      if (has_given_up(&s_gave_up)) break;
-    }
+    }   // (a wait that gave up ends the others at once)
     // ---- to the output, or to this run's partial result ----
     uint32_t o[DP];
     if (n > 0) {
@@ -475,7 +474,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       tc_fence_after();
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i) tc_ld32(to + i * 32, o + i * 32);
-      tc_wait_ld();
+      tc_wait_ld(o);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive(b_oe + 8 * w);
@@ -538,7 +537,7 @@ __global__ void __launch_bounds__(2 * AT_ROWS) attend_join_kernel(const __grid_c
   const AttendArgs& a = g.a;
   constexpr uint32_t STEP = 2 * AT_ROWS;
   const uint32_t unit = blockIdx.x / (DP / 4), c = blockIdx.x - unit * (DP / 4), prow = threadIdx.x;
-  const JoinItem it = ((const JoinItem*)a.counter)[1 + unit];
+  const JoinItem it = ((const JoinItem*)a.join)[unit];
   const uint32_t runs = it.runs, w = prow / AT_ROWS, row = prow % AT_ROWS;
   const uint32_t i = w * g.toks + row / a.r.group, head = (unit % a.c.n_heads) * a.r.group + row % a.r.group;
   if (runs < 2 || runs > a.max_chunks || row >= g.toks * a.r.group || i >= it.n || it.tok + i >= a.r.n_tokens) return;
@@ -573,9 +572,7 @@ bool attend_tiles_fits(const AttendArgs& a) {
   return page_box(a.c.page_size, AT_KEYS) >= MIN_BOX && a.r.group <= AT_ROWS && a.r.scale_log2 > 0.f;
 }
 uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
-size_t attend_tiles_counters(const AttendArgs& a) {
-  return (1 + (a.max_chunks > 1 ? (size_t)a.tiles * a.c.n_heads : 0)) * sizeof(JoinItem);
-}
+size_t attend_tiles_join(const AttendArgs& a) { return (size_t)a.tiles * a.c.n_heads * sizeof(JoinItem); }
 size_t attend_tiles_partial(const AttendArgs& a) {
   const size_t dp = a.c.head_dim <= 64 ? 64 : 128;
   return (size_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * (dp + 2) * sizeof(float);

@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
         for (int i = 0; i < 4; ++i) {
           uint32_t x[32];
           tc_ld32(ts + i * 32, x);
-          tc_wait_ld();
+          tc_wait_ld(x);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const float4 z = z4[i * 8 + k];
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
         for (int i = 0; i < 4; ++i) {
           uint32_t x[32];
           tc_ld32(ts + i * 32, x);
-          tc_wait_ld();
+          tc_wait_ld(x);
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
             const int32_t tok = s_tok[w][buf][i * 32 + k];

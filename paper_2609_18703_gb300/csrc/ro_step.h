@@ -31,7 +31,8 @@ class StepCall {
   ro_ctx* c_;
   int prev_ = -1;
 };
-enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_COUNT };
+// (SS_COUNTER is zero between calls, whichever kernel used it last)
+enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_JOIN = 2, SS_COUNT };
 
 // ---- rotary, append -----------------------------------------------------------------
 constexpr uint32_t ROPE_MAX_PAIRS = 128;
@@ -105,6 +106,7 @@ struct AttendArgs {
   uint32_t n_q_heads;
   float* partial;            // [tile][chunk][rows][head_dim + 2]
   uint32_t* counter;         // zero between calls
+  void* join;                // attend_tiles: what its join kernel needs of each pair of row tiles
   uint32_t* err;
 };
 // at most 16 rows a sequence; slots of a stage, bytes of its runs' partial results
@@ -116,11 +118,11 @@ cudaError_t prepare_attend_few_kernels();
 void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype);
 cudaError_t prepare_attend_kernels();
 // the tensor-core kernel: whether it takes these sizes, tokens of its CTA,
-// bytes of its counters and of its runs' partial results; false: the tensors
-// cannot be mapped
+// bytes of what its join needs and of its runs' partial results; false: the
+// tensors cannot be mapped
 bool attend_tiles_fits(const AttendArgs& a);
 uint32_t attend_tile_tokens(uint32_t group);
-size_t attend_tiles_counters(const AttendArgs& a);
+size_t attend_tiles_join(const AttendArgs& a);
 size_t attend_tiles_partial(const AttendArgs& a);
 bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int sms);
 cudaError_t prepare_attend_tiles_kernels();

@@ -11,6 +11,9 @@ namespace {
 
 constexpr uint32_t MAX_HEADS = 65535;
 constexpr uint64_t MAX_GRID = 0x7FFFFFFFull;
+// Runs whose partial results a call keeps: 1,024 of attend_tiles' 133 KB,
+// 16,384 of attend_few's 8 KB (about 136 MB either way).
+constexpr uint64_t MAX_RUNS = 1024, MAX_FEW_RUNS = 16384;
 
 #define RO_TRY(x)               \
   do {                          \
@@ -127,8 +130,9 @@ RowsArgs rows_of(const uint64_t* tok_base, const uint32_t* len, uint64_t n_token
   r.q = q;
   r.q_tok = q_tok;
   r.q_head = q_head;
-  r.window = window;
-  r.sinks = sinks;
+  // slots are below 2^31: a wider window sees everything
+  r.window = window < 0x80000000u ? window : 0u;
+  r.sinks = std::min(sinks, 0x7FFFFFFFu);
   r.scale_log2 = scale * 1.44269504088896340736f;
   return r;
 }
@@ -237,7 +241,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
   a.err = c.err();
   uint64_t keys = max_len ? max_len : 0x7FFFFFFFu;
   keys = std::min<uint64_t>(keys, (uint64_t)cache->n_pages * cache->page_size);
-  if (window) keys = std::min<uint64_t>(keys, (uint64_t)window + sinks + a.r.max_new);
+  if (a.r.window) keys = std::min<uint64_t>(keys, (uint64_t)a.r.window + a.r.sinks + a.r.max_new);
   keys = std::max<uint64_t>(keys, 1);
   const uint64_t max_rows = (uint64_t)a.r.max_new * group;
   void* p = nullptr;
@@ -255,7 +259,8 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
     const uint64_t each = ceil_div(stages * work, places);
     a.chunk = (uint32_t)std::max<uint64_t>(4, ceil_div(each, ceil_div(each, 96)));
-    a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 1024);
+    a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk),
+                                                std::min<uint64_t>(1024, std::max<uint64_t>(1, MAX_FEW_RUNS / work)));
     if (a.max_chunks > 1) {
       RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));
       a.partial = (float*)p;
@@ -280,7 +285,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     const uint64_t sms = (uint64_t)c.sms();
     const uint64_t pairs = std::min<uint64_t>(work, (uint64_t)cache->n_seqs * ceil_div(a.r.max_new, toks) * cache->n_heads);
     uint64_t runs = 1, least = ~0ull;
-    for (uint64_t k = 1; k <= (pairs < 4 * sms ? 32u : 1u); ++k) {
+    for (uint64_t k = 1; k == 1 || (k <= 32 && pairs < 4 * sms && pairs * k <= MAX_RUNS); ++k) {
       const uint64_t each = ceil_div(slots, k), time = ceil_div(pairs * ceil_div(slots, each), sms) * (each + 6);
       if (time < least) {
         least = time;
@@ -289,9 +294,10 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     }
     a.chunk = runs == 1 ? 0x40000000u : (uint32_t)ceil_div(slots, runs);
     a.max_chunks = runs == 1 ? 1u : (uint32_t)ceil_div(slots, a.chunk);
-    RO_TRY(c.scratch(SS_COUNTER, attend_tiles_counters(a), &p));
+    RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
     a.counter = (uint32_t*)p;
     if (a.max_chunks > 1) {
+      RO_TRY(c.scratch(SS_JOIN, attend_tiles_join(a), &a.join));
       RO_TRY(c.scratch(SS_PARTIAL, attend_tiles_partial(a), &p));
       a.partial = (float*)p;
     }
@@ -361,8 +367,8 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   // Behind a window most tiles of slots only have their past scores decayed: a
   // second kernel's, which leaves the tiles of the sinks and of the window.
   const uint64_t all = ceil_div(score_cap, WT_KEYS);
-  const uint64_t seen = ceil_div(sinks, WT_KEYS) + ceil_div((uint64_t)window + a.r.max_new, WT_KEYS) + 1;
-  a.unseen = window != 0 && seen < all;
+  const uint64_t seen = ceil_div(a.r.sinks, WT_KEYS) + ceil_div((uint64_t)a.r.window + a.r.max_new, WT_KEYS) + 1;
+  a.unseen = a.r.window != 0 && seen < all;
   a.tiles = (uint32_t)(a.unseen ? seen : all);
   if (n_tokens && weigh_tiles_fits(a) && launch_weigh_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
   a.unseen = 0;

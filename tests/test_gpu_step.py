@@ -278,6 +278,46 @@ def test_attend_splits_and_joins(ctx):
     assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
+def test_attend_kernels_share_a_context(ctx):
+    """Calls that split and join in different ways, one after another on one context's workspaces."""
+    few = ref.Cache([3000, 2500, 900], 2, 64, 64, BF16, 41)
+    some = ref.Cache([4000, 60], 2, 64, 64, BF16, 42)
+    odd = ref.Cache([2500, 300], 2, 64, 7, BF16, 43)
+    want = {}
+    for _ in range(2):
+        for name, c, news in (("few", few, [1, 2, 1]), ("some", some, [40, 60]), ("odd", odd, [30, 9]), ("some", some, [40, 60]),
+                              ("few", few, [1, 2, 1])):
+            got = check_attend(ctx, c, news, 4)
+            for a, b in zip(got, want.setdefault(name, got)):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("news", [[1, 1], [50, 90]])
+@pytest.mark.parametrize("window,sinks", [(2 ** 32 - 1, 0), (2 ** 31, 5), (2 ** 31 - 1, 0), (3, 2 ** 32 - 1), (70, 2 ** 31)])
+def test_attend_and_weigh_windows_past_every_slot(ctx, news, window, sinks):
+    """Windows and sinks wider than any cache: the same as none (and as everything)."""
+    lens = [400, 90]
+    c = ref.Cache(lens, 2, 64, 16, BF16, 44)
+    q, dq, out, lse = run_attend(ctx, c, news, 4, 0.125, window, sinks)
+    _, _, want, want_lse = run_attend(ctx, c, news, 4, 0.125, 0, 0)
+    cache, _, _ = on_gpu(c)
+    scores = [torch.zeros(2, 2, 400, device="cuda") for _ in range(2)]
+    for score, w, k in zip(scores, (window, 0), (sinks, 0)):
+        ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(starts(news)), max(news), i32(lens), dq, 0.125, w, k, lse, 1.0, None, score))
+    sync_ok(ctx)
+    if sinks < 2 ** 31:   # the same slots in the same order: the same bits
+        assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(*scores)
+    else:
+        t = starts(news)
+        for s in range(2):
+            w_out, w_lse, tol, lse_tol = ref.attend(c, s, q[t[s]:t[s + 1]], 0.125, 0, 0)
+            within(out[t[s]:t[s + 1]], w_out, tol)
+            within(lse[t[s]:t[s + 1]], w_lse, lse_tol)
+            w, wtol = ref.weigh(c, s, q[t[s]:t[s + 1]], 0.125, 0, 0, lse[t[s]:t[s + 1]].double().cpu(), 1.0,
+                                torch.zeros(2, lens[s]))
+            within(scores[0][s, :, :lens[s]], w, wtol + 1e-30)
+
+
 @pytest.mark.parametrize("page", [16, 20, 256])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_attend_long_runs(ctx, dim, page):
