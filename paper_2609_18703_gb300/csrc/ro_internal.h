@@ -79,18 +79,23 @@ struct LaunchCfg {
 // kernel here) until the predecessor has finished and its writes are visible.
 template <typename Arg>
 inline void launch_k(const LaunchCfg& L, int kid, void (*kern)(Arg), dim3 grid, int block,
-                     size_t smem, const Arg& a) {
+                     size_t smem, const Arg& a, dim3 cluster = dim3(1)) {
   prof_begin(L.prof, L.stream, kid);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = L.stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  const bool clustered = cluster.x * cluster.y * cluster.z > 1;   // CTAs that share their shared memory
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster.x;
+  attr[1].val.clusterDim.y = cluster.y;
+  attr[1].val.clusterDim.z = cluster.z;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = clustered ? 2 : 1;
   cudaLaunchKernelEx(&cfg, kern, a);
   prof_end(L.prof, L.stream, kid);
 }

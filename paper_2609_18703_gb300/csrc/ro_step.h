@@ -110,7 +110,7 @@ struct AttendArgs {
   uint32_t* err;
 };
 // at most 16 rows a sequence; slots of a stage, bytes of its runs' partial results
-void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype);
+void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool cluster);
 uint32_t attend_few_keys(uint32_t head_dim);
 size_t attend_few_partial(const AttendArgs& a);
 cudaError_t prepare_attend_few_kernels();

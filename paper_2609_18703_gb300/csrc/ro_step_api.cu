@@ -252,22 +252,26 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     a.tiles = cache->n_seqs;
     // Runs that fill two CTAs an SM in whole rounds, of at most 96 stages of
     // 16 KB (longer ones leave SMs idle at the end where lengths differ) and
-    // at least 4 (shorter ones cost more in their start and join than they
-    // save: one sequence of 777 slots, 4 heads of 64, 8.4 us at 4, 9.4 at 8, 9.7 at 2).  One sequence of 100,000 slots, 8 heads of 128: 68 us in one round
-    // of 83 stages, 85 in two of 64; 64 ragged ones of up to 32,000: 432 us at
-    // 96, 476 at 32, 565 at 16.
+    // at least 3, one for each warp (shorter ones cost more than they
+    // save).  One sequence of 777 slots, 4 heads of 64: 7.2 us at 3 stages, 9.1
+    // at 8, 7.8 at 2; of 100,000 slots, 8 heads of 128: 70 us in one round, 84 in
+    // two; 64 ragged sequences of up to 32,000 slots: 432 us at 96 stages, 476 at
+    // 32, 565 at 16.
     const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
     const uint64_t each = ceil_div(stages * work, places);
-    a.chunk = (uint32_t)std::max<uint64_t>(4, ceil_div(each, ceil_div(each, 96)));
+    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 96)));
     a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk),
                                                 std::min<uint64_t>(1024, std::max<uint64_t>(1, MAX_FEW_RUNS / work)));
-    if (a.max_chunks > 1) {
+    // Up to eight runs that the GPU holds at once are a cluster and join in
+    // shared memory; more go through L2 and a ticket.
+    const bool cluster = a.max_chunks > 1 && a.max_chunks <= 8 && work * a.max_chunks <= places;
+    if (a.max_chunks > 1 && !cluster) {
       RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));
       a.partial = (float*)p;
       RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
       a.counter = (uint32_t*)p;
     }
-    launch_attend_few(c.launch(), a, cache->dtype);
+    launch_attend_few(c.launch(), a, cache->dtype, cluster);
     return c.launched(fn);
   }
   // More: the tensor-core kernel, if the pages and the group fit its tiles.
@@ -355,7 +359,8 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   a.score_cap = score_cap;
   a.err = c.err();
   if ((uint64_t)a.r.max_new * a.r.group <= 16) {
-    // bound by the keys' bytes: runs of stages as in the attention of few rows
+    // bound by the keys' bytes: runs of stages as in the attention of few rows;
+    // nothing is joined, so short runs cost less
     const uint64_t stages = ceil_div(score_cap, weigh_few_keys(cache->head_dim));
     const uint64_t each = ceil_div(stages * units, (uint64_t)c.sms() * 2);
     a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 48)));

@@ -347,6 +347,7 @@ struct AttendFewArgs {
   CUtensorMap k, v;
   uint32_t box;              // slots loaded together
   uint32_t tma;              // 0: row by row
+  uint32_t cluster;          // a tile's runs are one cluster, which joins them in its shared memory
 };
 
 }  // namespace ro
