@@ -239,10 +239,11 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
 void launch_evict(const LaunchCfg& L, const EvictArgs& in, int sms) {
   EvictArgs a = in;
   const unsigned units = a.c.n_seqs * a.c.n_heads;
-  // CTAs of a unit: up to 8 while that gives each at least 4,096 slots and the
-  // GPU has places
+  // CTAs of a unit: up to 8 while that gives each at least 1,024 slots and the
+  // GPU has places (4 units of 16,000 slots, moved too: 16 us with 8 CTAs, 18 with
+  // 2, 21 with 1; of 100,000: 42 and 315 us with 8 and 1)
   a.cluster = 1;
-  while (a.cluster < 8 && (uint64_t)units * a.cluster * 2 <= (uint64_t)sms * 2 && a.score_cap / (a.cluster * 2) >= 4096)
+  while (a.cluster < 8 && (uint64_t)units * a.cluster * 2 <= (uint64_t)sms * 2 && a.score_cap / (a.cluster * 2) >= 1024)
     a.cluster *= 2;
   // keys in shared memory: a run's, as far as two CTAs an SM have room for them
   a.cached = (uint32_t)std::min<uint64_t>(ceil_div(a.score_cap, a.cluster), ES_CACHED);
