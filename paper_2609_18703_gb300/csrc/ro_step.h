@@ -136,9 +136,10 @@ struct WeighArgs {
   const float* past;         // optional
   float* score;
   uint64_t score_cap;
-  uint32_t tiles;            // CTAs along score_cap for each sequence and head, at most
+  uint32_t tiles;            // along score_cap for each sequence and head, at most
   uint32_t chunk;            // weigh_few: stages of a CTA
   uint32_t unseen;           // weigh_tiles: the tiles before the windows are another kernel's
+  uint32_t* counter;         // weigh_tiles: zero between calls
   uint32_t* err;
 };
 // at most 16 rows a sequence; slots of a stage

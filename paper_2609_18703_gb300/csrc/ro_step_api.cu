@@ -375,7 +375,12 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   const uint64_t seen = ceil_div(a.r.sinks, WT_KEYS) + ceil_div((uint64_t)a.r.window + a.r.max_new, WT_KEYS) + 1;
   a.unseen = a.r.window != 0 && seen < all;
   a.tiles = (uint32_t)(a.unseen ? seen : all);
-  if (n_tokens && weigh_tiles_fits(a) && launch_weigh_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
+  if (n_tokens && weigh_tiles_fits(a)) {
+    void* p = nullptr;
+    RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
+    a.counter = (uint32_t*)p;
+    if (launch_weigh_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
+  }
   a.unseen = 0;
   a.tiles = (uint32_t)ceil_div(score_cap, WG_KEYS);
   launch_weigh(c.launch(), a, cache->dtype);
