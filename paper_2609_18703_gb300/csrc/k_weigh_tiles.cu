@@ -16,10 +16,11 @@
 //
 // Measured: 6 chunks of up to 1,024 tokens over up to 16,384 slots, 16 heads on
 // 4 of 64: 87 us (a CTA an item: 103; mma.sync: 358).  Beside the exponentials
-// (60 us of them are the XU's) the broadcast of the rows' lse from shared memory
+// (the XU needs 50 us for them) the broadcast of the rows' lse from shared memory
 // costs about 10 us and the products' and barriers' latencies the rest.  Row tiles
 // of 64 (with a second S a group, a third group or two slots a thread), S freed in
-// halves, and polynomials for a part of the exponentials measured slower.
+// halves, polynomials for a part of the exponentials and the lse subtracted by a
+product measured slower; more registers for deeper loads of S gave 2 %.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"

@@ -507,6 +507,64 @@ def test_weigh_rows_that_see_nothing_and_short_scores(ctx):
     assert ro.ro_ctx_sync(ctx) == ro.RO_E_CAPACITY
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (48, 3)])
+@pytest.mark.parametrize("dim,heads,kv", [(64, 6, 2), (128, 4, 4)])
+def test_weigh_many_sequences(ctx, window, sinks, dim, heads, kv):
+    """Chunks of 75 sequences, some empty, some without new tokens: CTAs take many of them in turn."""
+    g = np.random.default_rng(dim + window)
+    lens = [int(x) for x in g.integers(0, 900, 75)]
+    news = [min(L, int(x)) for L, x in zip(lens, g.integers(0, 60, 75))]
+    for s in (0, 31, 32, 74):
+        lens[s] = news[s] = 0
+    for s in (5, 40, 73):
+        news[s] = 0
+    c = ref.Cache(lens, kv, dim, 16, BF16, 29)
+    scale = 1 / math.sqrt(dim)
+    q, dq, _, lse = run_attend(ctx, c, news, heads, scale, window, sinks)
+    cache, _, _ = on_gpu(c)
+    cap = max(lens)
+    past = torch.rand(len(lens), kv, cap).cuda()
+    scores = [torch.full((len(lens), kv, cap), -5.0, device="cuda") for _ in range(3)]
+    for score in scores:
+        ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(starts(news)), 60, i32(lens), dq, scale, window, sinks, lse, 0.5, past,
+                                  score))
+    sync_ok(ctx)
+    assert torch.equal(scores[0], scores[1]) and torch.equal(scores[0], scores[2])   # whoever took what
+    t = starts(news)
+    for s, L in enumerate(lens):
+        assert bool((scores[0][s, :, L:] == -5).all())
+        if s % 6 == 0 or news[s] == 0:
+            want, tol = ref.weigh(c, s, q[t[s]:t[s + 1]], scale, window, sinks, lse[t[s]:t[s + 1]].double().cpu(), 0.5,
+                                  past[s].cpu())
+            within(scores[0][s, :, :L], want, tol + 1e-30)
+
+
+def test_weigh_bad_ranges_are_recorded_and_the_next_call_is_whole(ctx):
+    lens, news = [300] * 40, [20] * 40
+    c = ref.Cache(lens, 1, 64, 16, BF16, 31)
+    q, dq, _, lse = run_attend(ctx, c, news, 2, 0.125, 0, 0)
+    cache, _, _ = on_gpu(c)
+    base = starts(news)
+    good = torch.zeros(40, 1, 300, device="cuda")
+    ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(base), 20, i32(lens), dq, 0.125, 0, 0, lse, 1.0, None, good))
+    sync_ok(ctx)
+    bad = base.copy()
+    bad[38] = 10_000                      # the ranges of sequences 37 and 38
+    score = torch.full_like(good, -5.0)
+    ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(bad), 20, i32(lens), dq, 0.125, 0, 0, lse, 1.0, None, score))
+    assert ro.ro_ctx_sync(ctx) == ro.RO_E_INVAL
+    assert bool((score[37:39] == -5).all())
+    assert torch.equal(score[:37], good[:37]) and torch.equal(score[39:], good[39:])
+    other = ro.ro_ctx_create(0, torch.cuda.current_stream(), 1)
+    try:
+        again = torch.zeros_like(good)
+        ok(other, ro.ro_cache_weigh(other, cache, i64(base), 20, i32(lens), dq, 0.125, 0, 0, lse, 1.0, None, again))
+        sync_ok(other)
+        assert torch.equal(again, good)
+    finally:
+        ro.ro_ctx_destroy(other)
+
+
 # ---------------------------------------------------------------------------- evict
 @pytest.mark.parametrize("budget,sinks,recent", [(1, 0, 0), (1, 1, 0), (1, 0, 1), (64, 4, 16), (100, 0, 0), (100, 50, 50),
                                                  (999, 3, 7), (1000, 0, 0), (4000, 4, 100)])
