@@ -20,7 +20,7 @@
 // costs about 10 us and the products' and barriers' latencies the rest.  Row tiles
 // of 64 (with a second S a group, a third group or two slots a thread), S freed in
 // halves, polynomials for a part of the exponentials and the lse subtracted by a
-product measured slower; more registers for deeper loads of S gave 2 %.
+// product measured slower; more registers for deeper loads of S gave 2 %.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
