@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
 
   if (warp == AF_WARPS) {
     load_stages<T, DP, KEYS, true>(a.c, &g.k, &g.v, g.tma != 0, g.box, AF_STAGES, slots, c0, n, kh, q.page0, sm, b_full,
-                                              b_empty, &s_gave_up, a.err, [](const SlotTile&) { return true; });
+                                              b_empty, &s_gave_up, a.err);
   }
 
   // queries as matrix fragments; rows past the tile's are zero

@@ -78,10 +78,10 @@ __global__ void __launch_bounds__(WP_THREADS) weigh_past_kernel(const __grid_con
   const uint32_t unit = blockIdx.x / a.chunk, part = blockIdx.x - unit * a.chunk;   // a.chunk CTAs for each
   const SeqInfo q = seq_info(a.c, a.r, unit / a.c.n_heads, a.err);
   const SeenTiles st = seen_tiles(q, a.r);
-  const uint32_t to = min(scored(a, q, false), st.window * WT_KEYS);
-  const uint64_t row = (uint64_t)unit * a.score_cap;
-  for (uint32_t j = st.sinks * WT_KEYS + part * WP_THREADS + threadIdx.x; j < to; j += a.chunk * WP_THREADS)
-    a.score[row + j] = a.past ? a.decay * a.past[row + j] : 0.f;   // (before the window: no new slot)
+  const uint32_t from = st.sinks * WT_KEYS, to = min(scored(a, q, false), st.window * WT_KEYS);
+  if (from >= to) return;
+  const uint32_t per = ((to - from + a.chunk - 1) / a.chunk + 3) & ~3u, lo = from + min(to - from, part * per);
+  decay_past<WP_THREADS>(a, (uint64_t)unit * a.score_cap, lo, min(to, lo + per), threadIdx.x);   // (no new slot among them)
 }
 
 template <typename T, int DP>

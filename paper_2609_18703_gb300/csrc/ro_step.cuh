@@ -207,6 +207,39 @@ __device__ __forceinline__ void seeing_tokens(const SeqInfo& q, const RowsArgs& 
   }
 }
 
+// score = decay past for the slots [from, to) of a row of scores that no token
+// sees (from a multiple of 4), four at a time where the rows are aligned to it.
+template <int THREADS>
+__device__ __forceinline__ void decay_past(const WeighArgs& a, uint64_t row, uint32_t from, uint32_t to, uint32_t thread) {
+  float* score = a.score + row;
+  const float* past = a.past ? a.past + row : nullptr;
+  uint32_t done = from;
+  if (((reinterpret_cast<uintptr_t>(score) | reinterpret_cast<uintptr_t>(past)) & 15u) == 0u) {
+    const uint32_t end = to & ~3u;
+    for (uint32_t j = from + thread * 4; j < end; j += THREADS * 16) {
+      float4 v[4];
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (j + i * THREADS * 4 < end)
+          v[i] = past ? *(const float4*)(past + j + i * THREADS * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (j + i * THREADS * 4 < end)
+          *(float4*)(score + j + i * THREADS * 4) =
+              past ? make_float4(a.decay * v[i].x, a.decay * v[i].y, a.decay * v[i].z, a.decay * v[i].w) : v[i];
+    }
+    done = max(from, end);
+  }
+  for (uint32_t j = done + thread; j < to; j += THREADS * 4) {
+    float v[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) v[i] = past && j + i * THREADS < to ? past[j + i * THREADS] : 0.f;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+      if (j + i * THREADS < to) score[j + i * THREADS] = past ? a.decay * v[i] : 0.f;
+  }
+}
+
 // Row tile `tile` (of toks_per_tile tokens): its sequence and its place among
 // that sequence's tiles.  A whole warp calls it; with one tile per sequence
 // (max_new tokens fit a tile) it is the sequence itself.  The host launches

@@ -218,14 +218,13 @@ __device__ __forceinline__ float ex2(float x) {
 // ---- a ring of stages of slots -----------------------------------------------------------------
 // One warp's work: keep a ring of `stages` stages full with the tiles
 // [c0, c0 + n) of one sequence and head, KEYS slots of DP dimensions each, keys
-// (and values behind them).  want(tile): false leaves a tile unloaded.  By TMA
-// a box (part of a page) a lane; without, row by row with cp.async, 32 arrivals
-// on a full stage instead of one.
-template <typename T, int DP, int KEYS, bool VALUES, class Want>
+// (and values behind them).  By TMA a box (part of a page) a lane; without, row
+// by row with cp.async, 32 arrivals on a full stage instead of one.
+template <typename T, int DP, int KEYS, bool VALUES, class Slots>
 __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMap* km, const CUtensorMap* vm, bool tma,
-                                            uint32_t box, uint32_t stages, const SlotTiles<KEYS>& slots, uint32_t c0,
+                                            uint32_t box, uint32_t stages, const Slots& slots, uint32_t c0,
                                             uint32_t n, uint32_t kh, uint64_t page0, uint32_t sm, uint32_t b_full, uint32_t b_empty,
-                                            uint32_t* gave_up, uint32_t* err, Want want) {
+                                            uint32_t* gave_up, uint32_t* err) {
   constexpr uint32_t BLOCKS = DP / 64, BLOCK_BYTES = KEYS * 128, SIDE = BLOCKS * BLOCK_BYTES;
   constexpr uint32_t STAGE = VALUES ? 2 * SIDE : SIDE;
   const uint32_t lane = threadIdx.x & 31u;
@@ -233,7 +232,7 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
   if (tma) {
     const uint32_t boxes = KEYS / box;            // of a stage, a lane each
     const uint32_t ahead = 32 / boxes;            // stages whose pages the lanes hold
-    auto has_box = [&](const SlotTile& st, uint32_t j) { return j < st.hi && j + box > st.lo && want(st); };
+    auto has_box = [&](const SlotTile& st, uint32_t j) { return j < st.hi && j + box > st.lo; };
     // the page of this lane's box among the boxes of stages t .. t + ahead - 1
     auto page_of = [&](uint32_t t) -> uint32_t {
       const uint32_t u = t + lane / boxes;
@@ -276,12 +275,11 @@ __device__ __forceinline__ void load_stages(const PagedArgs& c, const CUtensorMa
     const uint32_t pc = lane % CH;
     for (uint32_t t = 0; t < n; ++t) {
       const SlotTile st = slots.at(c0 + t);
-      const bool wanted = want(st);
       if (t >= stages) bar_wait(b_empty + 8 * slot, parity, gave_up, err);
       if (has_given_up(gave_up)) break;
       for (uint32_t r = lane / CH; r < (uint32_t)KEYS; r += PER) {
         const uint32_t j = st.t0 + r;
-        bool ok = wanted && j >= st.lo && j < st.hi && pc * 8 < c.head_dim;
+        bool ok = j >= st.lo && j < st.hi && pc * 8 < c.head_dim;
         uint64_t e = 0;
         if (ok) {
           uint32_t pi, at;

@@ -507,6 +507,31 @@ def test_weigh_rows_that_see_nothing_and_short_scores(ctx):
     assert ro.ro_ctx_sync(ctx) == ro.RO_E_CAPACITY
 
 
+@pytest.mark.parametrize("window,sinks", [(1, 0), (3, 5), (70, 130), (64, 64), (500, 1)])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 20), (40, 5)])
+@pytest.mark.parametrize("cap", [3000, 3001])
+def test_weigh_few_rows_behind_a_window(ctx, window, sinks, dim, page, cap):
+    """What no row sees only has its past decayed, wherever it starts and ends; rows of scores aligned and not."""
+    lens, news = [1000, 513, 64, 3000, 0, 700, 65], [1, 3, 1, 2, 0, 0, 1]
+    c = ref.Cache(lens, 2, dim, page, F16, 41)
+    scale = 1 / math.sqrt(dim)
+    q, dq, _, lse = run_attend(ctx, c, news, 4, scale, window, sinks)
+    cache, _, _ = on_gpu(c)
+    past = torch.rand(7, 2, cap).cuda()
+    score, in_place = torch.full_like(past, -5.0), past.clone()
+    for before, out in ((past, score), (in_place, in_place)):
+        ok(ctx, ro.ro_cache_weigh(ctx, cache, i64(starts(news)), 3, i32(lens), dq, scale, window, sinks, lse, 0.75, before,
+                                  out))
+    sync_ok(ctx)
+    t = starts(news)
+    for s, L in enumerate(lens):
+        want, tol = ref.weigh(c, s, q[t[s]:t[s + 1]], scale, window, sinks, lse[t[s]:t[s + 1]].double().cpu(), 0.75,
+                              past[s].cpu())
+        within(score[s, :, :L], want, tol + 1e-30)
+        assert bool((score[s, :, L:] == -5).all())
+        assert torch.equal(in_place[s, :, :L], score[s, :, :L]) and torch.equal(in_place[s, :, L:], past[s, :, L:])
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (48, 3)])
 @pytest.mark.parametrize("dim,heads,kv", [(64, 6, 2), (128, 4, 4)])
 def test_weigh_many_sequences(ctx, window, sinks, dim, heads, kv):
