@@ -109,9 +109,11 @@ struct AttendArgs {
   void* join;                // attend_tiles: what its join kernel needs of each pair of row tiles
   uint32_t* err;
 };
-// at most 16 rows a sequence; slots of a stage, bytes of its runs' partial results
-void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool cluster);
+// at most 16 rows a sequence (alone: many short ones, a warp each, where the
+// tensors can be mapped); slots of a stage, bytes of its runs' partial results
+void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool cluster, bool alone);
 uint32_t attend_few_keys(uint32_t head_dim);
+uint32_t attend_short_keys(uint32_t head_dim);
 size_t attend_few_partial(const AttendArgs& a);
 cudaError_t prepare_attend_few_kernels();
 // tiles of 64 rows, any page size

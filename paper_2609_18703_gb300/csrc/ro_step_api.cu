@@ -271,7 +271,14 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
       RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
       a.counter = (uint32_t*)p;
     }
-    launch_attend_few(c.launch(), a, cache->dtype, cluster);
+    // Many short sequences: a warp alone for each (sequence, head), where its
+    // stages one after another, about 1 us for 8 KB, take less than the rounds
+    // of larger CTAs, about 6 us each.  2,048 of 40 slots of 128: 13 us against
+    // 41, of 300: 55 against 79; 5,600 of up to 150: 42 against 110.  On either
+    // side of the rule: 1,024 of up to 300 slots 23.4 against 24.4, of up to 600
+    // 44 against 32.
+    const bool alone = a.max_chunks == 1 && work > places && ceil_div(keys, attend_short_keys(cache->head_dim)) * places <= 5 * work;
+    launch_attend_few(c.launch(), a, cache->dtype, cluster, alone);
     return c.launched(fn);
   }
   // More: the tensor-core kernel, if the pages and the group fit its tiles.

@@ -250,6 +250,38 @@ def test_attend_chunks(ctx, dtype, dim, heads, kv, page, window, sinks):
     check_attend(ctx, ref.Cache(lens, kv, dim, page, dtype, page), news, heads, window, sinks)
 
 
+@pytest.mark.parametrize("dtype,dim,heads,kv,page", [(BF16, 128, 8, 4, 64), (F16, 64, 4, 4, 16), (BF16, 80, 12, 4, 4),
+                                                     (F16, 40, 4, 4, 20), (BF16, 96, 4, 4, 5), (F16, 128, 4, 4, 256)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 2), (40, 35)])
+def test_attend_many_short_sequences(ctx, dtype, dim, heads, kv, page, window, sinks):
+    """More sequences and heads than the GPU holds at once: empty ones, one token, ends inside stages and pages."""
+    g = np.random.default_rng(dim + page + window)
+    lens = [int(x) for x in g.integers(0, 140, 260)]
+    lens[:6] = [0, 1, 16, 17, 32, 139]
+    news = [min(L, int(x)) for L, x in zip(lens, g.integers(0, 5, 260))]
+    c = ref.Cache(lens, kv, dim, page, dtype, 50)
+    out, lse = check_attend(ctx, c, news, heads, window, sinks, max_len=139)
+    again = run_attend(ctx, c, news, heads, 1 / math.sqrt(dim), window, sinks, max_len=139)
+    assert torch.equal(out, again[2]) and torch.equal(lse, again[3])
+
+
+def test_attend_short_sequences_bad_pages_and_lengths_are_recorded(ctx):
+    lens = [40] * 400
+    c = ref.Cache(lens, 2, 64, 16, BF16, 3, junk=0.0)
+    good = run_attend(ctx, c, [1] * 400, 2, 0.1, 0, 0)
+    cache, _, _ = on_gpu(c)
+    out = torch.zeros_like(good[2])
+    bad = c.pages.clone()
+    bad[int(c.base[7])] = 10_000
+    wrong = ro.ro_cache(c.k.cuda(), c.v.cuda(), i64(c.base), bad.cuda())
+    ok(ctx, ro.ro_cache_attend(ctx, wrong, i64(range(401)), 1, i32(lens), 40, good[1], 0.1, 0, 0, out))
+    assert ro.ro_ctx_sync(ctx) == ro.RO_E_INVAL
+    rest = [s for s in range(400) if s != 7]
+    assert torch.equal(out[rest], good[2][rest])
+    ok(ctx, ro.ro_cache_attend(ctx, cache, i64(range(401)), 1, i32([500] + lens[1:]), 40, good[1], 0.1, 0, 0, out))
+    assert ro.ro_ctx_sync(ctx) == ro.RO_E_CAPACITY
+
+
 @pytest.mark.parametrize("heads,kv", [(4, 2), (8, 1)])
 @pytest.mark.parametrize("news", [[40, 300], [1, 5]])
 def test_attend_rows_that_see_nothing(ctx, heads, kv, news):
