@@ -9,9 +9,9 @@
 // sum stays in the four lanes that hold its row and is added in a fixed order.
 // Stages that no row sees (behind the sinks, before a window) pass the ring by:
 // their past scores are decayed in one sweep (37 single tokens of up to 23,302
-// slots, 8 heads, window 3: 17 us; stage by stage 48).
+// slots, 8 heads, window 3: 14 us; stage by stage 48).
 //
-// Measured: 32 single tokens, 336 MB of keys and scores: 58 us, 5.8 TB/s; a CTA
+// Measured: 32 single tokens, 336 MB of keys and scores: 56 us, 6.0 TB/s; a CTA
 // for every 64 slots, without a ring: 143 us.
 #include <algorithm>
 
@@ -20,10 +20,12 @@
 namespace ro {
 
 constexpr int WF_WARPS = 3, WF_THREADS = 32 * (WF_WARPS + 1);
-// Two CTAs on an SM; calls whose CTAs have at most three stages take half the
-// ring, so that more of them fit.
-constexpr uint32_t WF_STAGES = 6, WF_STAGE = 16384;
-static_assert(WF_STAGES == 2 * WF_WARPS, "a place of the ring belongs to one warp");
+// A place for each warp and four CTAs on an SM: as many loads in flight as two
+// CTAs with twice the ring, but more starts and ends beside them (1,000 single
+// tokens over up to 200 slots: 59 us against 103; 128 over 1,000 slots 47 against
+// 54; one of 100,000 slots 38 against 37).
+constexpr uint32_t WF_STAGES = 3, WF_STAGE = 16384;
+static_assert(WF_STAGES % WF_WARPS == 0, "a place of the ring belongs to one warp");
 constexpr uint32_t WF_SMEM = 1024 + WF_STAGES * WF_STAGE;
 template <int DP>
 constexpr int wf_keys() {
@@ -39,7 +41,7 @@ struct SeenSlots {
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_constant__ WeighFewArgs g) {
+__global__ void __launch_bounds__(WF_THREADS, 4) weigh_few_kernel(const __grid_constant__ WeighFewArgs g) {
   constexpr int KEYS = wf_keys<DP>();
   constexpr uint32_t BLOCK_BYTES = KEYS * 128;
   const WeighArgs& a = g.a;
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
   }
   __syncthreads();
   if (warp == WF_WARPS) {
-    load_stages<T, DP, KEYS, false>(a.c, &g.k, &g.k, g.tma != 0, g.box, g.stages, slots, c0, n, kh, q.page0, sm, b_full,
+    load_stages<T, DP, KEYS, false>(a.c, &g.k, &g.k, g.tma != 0, g.box, WF_STAGES, slots, c0, n, kh, q.page0, sm, b_full,
                                                b_empty, &s_gave_up, a.err);
   } else {
     // query rows as the right operand, two groups of eight; each row's lse, +inf for rows that add nothing
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(WF_THREADS, 2) weigh_few_kernel(const __grid_c
     if (gap1 > gap0)
       decay_past<32 * WF_WARPS>(a, row, gap0 * KEYS, min(gap1 * KEYS, len), tid);   // (no new slot among them)
     for (uint32_t t = warp; t < n; t += WF_WARPS) {
-      const uint32_t round = t / WF_WARPS, rounds = g.stages / WF_WARPS, slot = warp + WF_WARPS * (round % rounds);
+      const uint32_t round = t / WF_WARPS, rounds = WF_STAGES / WF_WARPS, slot = warp + WF_WARPS * (round % rounds);
       const SlotTile st = slots.at(c0 + t);
       float past[KEYS / 32];   // under way while the keys arrive
 #pragma unroll
@@ -183,13 +185,12 @@ uint32_t weigh_few_keys(uint32_t head_dim) { return head_dim <= 64 ? wf_keys<64>
 template <typename T, int DP>
 static void launch_few(const LaunchCfg& L, const WeighFewArgs& g) {
   launch_k(L, K_WEIGH, weigh_few_kernel<T, DP>, dim3(g.a.c.n_seqs * g.a.c.n_heads, g.a.tiles), WF_THREADS,
-           1024 + g.stages * WF_STAGE, g);
+           WF_SMEM, g);
 }
 void launch_weigh_few(const LaunchCfg& L, const WeighArgs& a, int dtype) {
   WeighFewArgs g;
   g.a = a;
   g.box = page_box(a.c.page_size, weigh_few_keys(a.c.head_dim));
-  g.stages = a.chunk <= WF_WARPS ? WF_WARPS : WF_STAGES;
   g.tma = g.box >= MIN_BOX && pool_map(&g.k, a.c, a.c.k, dtype, g.box);
   if (!g.tma) g.box = 1;
   const bool narrow = a.c.head_dim <= 64;

@@ -370,14 +370,7 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
     // nothing is joined, so short runs cost less
     const uint64_t stages = ceil_div(score_cap, weigh_few_keys(cache->head_dim));
     const uint64_t each = ceil_div(stages * units, (uint64_t)c.sms() * 2);
-    // Stages that no row sees cost little: longer runs where a narrow window
-    // leaves most of them so (12 us against 17 on 17 sequences of up to 34,934
-    // slots, window 14; with windows of more stages runs of 48 balance better:
-    // 46 us against 53 on 8 of 100,000, window 4,096).
-    const uint64_t keys = weigh_few_keys(cache->head_dim);
-    const uint64_t seen = ceil_div(a.r.sinks, keys) + ceil_div((uint64_t)a.r.window + a.r.max_new, keys) + 1;
-    const uint64_t most = a.r.window != 0 && seen <= 12 && seen * 4 <= stages ? 192 : 48;
-    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, most)));
+    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 48)));
     a.chunk = (uint32_t)std::min<uint64_t>(a.chunk, stages);
     a.tiles = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk), 65535);
     launch_weigh_few(c.launch(), a, cache->dtype);

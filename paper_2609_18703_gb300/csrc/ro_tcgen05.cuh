@@ -333,7 +333,6 @@ struct WeighFewArgs {
   WeighArgs a;
   CUtensorMap k;
   uint32_t box, tma;
-  uint32_t stages;           // of the ring
 };
 struct WeighTileArgs {
   WeighArgs a;
