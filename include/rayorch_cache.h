@@ -173,7 +173,8 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
  *               recorded and the tokens past them are not moved.
  *   d_keep      uint32[n_seqs][n_heads][budget] out: kept slots, ascending
  *               (entries past the kept ones are not written).
- *   d_len_out   uint32[n_seqs] out: min(length, budget).
+ *   d_len_out   uint32[n_seqs] out: min(length, budget); may be d_len (but may
+ *               not overlap it otherwise: RO_E_INVAL).
  *   d_score_out float[n_seqs][n_heads][score_cap] out or NULL: kept scores;
  *               not d_score.
  * sinks + recent <= budget, budget >= 1.

@@ -87,7 +87,6 @@ __global__ void __launch_bounds__(ES_THREADS) evict_select_kernel(const __grid_c
   uint32_t* keep = a.keep + (uint64_t)unit * a.budget;
   float* out = a.score_out ? a.score_out + row : nullptr;
   const uint32_t t0 = rank * ES_THREADS + tid, step = nc * ES_THREADS;   // this thread among the cluster's
-  if (h == 0 && t0 == 0) a.len_out[s] = min(len, a.budget);
   if (len <= a.budget) {                        // (the whole cluster)
     for (uint32_t j = t0; j < len; j += step) {
       keep[j] = j;
@@ -210,6 +209,10 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
   const uint32_t s = unit / a.c.n_heads, h = unit - s * a.c.n_heads;
   const uint32_t len = cached(a, s, false);
   const uint32_t kept = min(len, a.budget);
+  // Written here and not by the CTAs that select: len_out may be len, and those
+  // have to read what the sequence held.  Whoever reads a length here after it is
+  // cut keeps as much: a cut of a cut length changes nothing.
+  if (h == 0 && part == 0 && threadIdx.x == 0) a.len_out[s] = kept;
   const uint64_t b0 = a.dst_base[s], b1 = a.dst_base[s + 1], p0 = a.c.page_base[s];
   const uint64_t room = b1 > b0 ? (b1 - b0) * a.c.page_size : 0;
   const uint32_t n = (uint32_t)min((uint64_t)kept, room);

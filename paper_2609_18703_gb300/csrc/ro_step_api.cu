@@ -22,6 +22,11 @@ constexpr uint64_t MAX_RUNS = 1024, MAX_FEW_RUNS = 16384;
   } while (0)
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
+// two arrays of the same number of bytes
+bool overlap(const void* p, const void* q, uint64_t bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return (a < b ? b - a : a - b) < bytes;
+}
 
 ro_status check_rope(StepCall& c, const char* fn, const ro_rope* r, uint32_t head_dim) {
   if (r->n_axes < 1 || r->n_axes > 4) return c.refuse(RO_E_INVAL, "%s: 1 to 4 axes", fn);
@@ -406,6 +411,8 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
     return c.refuse(RO_E_INVAL, "%s: NULL argument", fn);
   if (budget == 0 || (uint64_t)sinks + recent > budget)
     return c.refuse(RO_E_INVAL, "%s: sinks and recent tokens must fit the budget", fn);
+  if (d_len_out != d_len && overlap(d_len, d_len_out, (uint64_t)cache->n_seqs * sizeof(uint32_t)))
+    return c.refuse(RO_E_INVAL, "%s: lengths are cut in place or into another array", fn);
   if (d_score_out && d_score_out == d_score) return c.refuse(RO_E_INVAL, "%s: scores cannot be cut in place", fn);
   if (score_cap >= 0x80000000ull || budget >= 0x80000000u)
     return c.refuse(RO_E_OVERFLOW, "%s: 2^31 scores or a budget of 2^31 or more", fn);

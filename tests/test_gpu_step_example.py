@@ -52,3 +52,28 @@ def test_caches_stay_within_their_budget():
         assert not bool(torch.isnan(outs[i]).any())
         n = min(int(counts[i]), 32)   # two waves fit the budget: the same until then
         assert torch.equal(outs[i][:n], full[i][:n])
+
+
+def test_evictions_keep_the_heaviest(monkeypatch):
+    """The slots that the example's evictions keep, against the definition on the scores that they saw."""
+    from examples import stream_frames as ex
+    from tests import step_reference as ref
+    evict, cuts = ex.ro.ro_cache_evict, []
+
+    def watched(ctx, cache, d_len, d_score, budget, sinks, recent, dst_base, dst_pages, d_keep, d_len_out, d_score_out):
+        lens, score = d_len.cpu(), d_score.cpu()
+        st = evict(ctx, cache, d_len, d_score, budget, sinks, recent, dst_base, dst_pages, d_keep, d_len_out, d_score_out)
+        cuts.append((lens, score, budget, sinks, recent, d_keep.cpu(), d_len_out.cpu(), d_score_out.cpu()))
+        return st
+
+    monkeypatch.setattr(ex.ro, "ro_cache_evict", watched)
+    ex.run(videos=200, frames=60, wave=16, budget=33, seed=5)
+    assert len(cuts) > 3
+    for lens, score, budget, sinks, recent, keep, held, kept_score in cuts:
+        assert torch.equal(held, lens.clamp(max=budget)) and int(lens.max()) > budget
+        for s in range(lens.numel()):
+            n = int(held[s])
+            for h in range(score.shape[1]):
+                idx = ref.evict(int(lens[s]), score[s, h].numpy(), budget, sinks, recent)
+                assert np.array_equal(keep[s, h, :n].numpy(), idx)
+                assert torch.equal(kept_score[s, h, :n], score[s, h, torch.as_tensor(idx)])
