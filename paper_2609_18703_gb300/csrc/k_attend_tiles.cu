@@ -430,8 +430,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
       const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
                                       fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * scale);
-      if (__any_sync(0xffffffffu, mn > m + AT_SLACK)) {
-        // the maximum moves for the whole warp: rescale what was summed so far
+      if (__any_sync(0xffffffffu, mine && mn > m + AT_SLACK)) {
+        // The maximum moves for the whole warp: rescale what was summed so far.
+        // (Rows that are no token's have no say: theirs may hold whatever an
+        // earlier kernel left, and would decide how the others are rounded.)
         const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
         m = mn;
         l *= f;
