@@ -25,9 +25,10 @@
  * with no side effects (RO_E_OVERFLOW beyond a stated limit).  What only the
  * GPU can see is recorded in the context and returned by the next call that
  * synchronises: RO_E_CAPACITY where a length exceeds the sequence's pages or
- * an output, RO_E_INVAL where a page, a sequence or a token range is out of
- * bounds.  Nothing outside the described arrays is read or written even then:
- * the tokens concerned are left out, and the call's results are void.
+ * an output, RO_E_INVAL where a page, a sequence, a token range or a range of a
+ * page list (beyond the list's last offset) is out of bounds.  Nothing outside
+ * the described arrays is read or written even then: the tokens concerned are
+ * left out, and the call's results are void.
  * Workspaces belong to the context and grow on demand, so a call that will be
  * captured into a CUDA graph runs once uncaptured first.
  *

@@ -31,7 +31,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 __device__ __forceinline__ uint32_t cached(const EvictArgs& a, uint32_t s, bool first) {
   const uint64_t p0 = a.c.page_base[s], p1 = a.c.page_base[s + 1];
   uint32_t len = a.len[s];
-  if (p1 < p0 || len >= 0x80000000u) {
+  if (p1 < p0 || p1 > a.c.page_base[a.c.n_seqs] || len >= 0x80000000u) {
     if (first) record(a.err, ERR_INVAL);
     return 0;
   }
@@ -214,9 +214,10 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
   // cut keeps as much: a cut of a cut length changes nothing.
   if (h == 0 && part == 0 && threadIdx.x == 0) a.len_out[s] = kept;
   const uint64_t b0 = a.dst_base[s], b1 = a.dst_base[s + 1], p0 = a.c.page_base[s];
-  const uint64_t room = b1 > b0 ? (b1 - b0) * a.c.page_size : 0;
+  const bool in_list = b0 <= b1 && b1 <= a.dst_base[a.c.n_seqs];
+  const uint64_t room = in_list ? (b1 - b0) * a.c.page_size : 0;
   const uint32_t n = (uint32_t)min((uint64_t)kept, room);
-  if (n < kept && part == 0 && threadIdx.x == 0) record(a.err, b1 < b0 ? ERR_INVAL : ERR_CAPACITY);
+  if (n < kept && part == 0 && threadIdx.x == 0) record(a.err, in_list ? ERR_CAPACITY : ERR_INVAL);
   const uint32_t per = a.c.head_dim / 8;                 // 16-byte pieces of a row
   const uint32_t* keep = a.keep + (uint64_t)unit * a.budget;
   const uint64_t items = (uint64_t)n * per, stride = (uint64_t)a.parts * EM_THREADS;

@@ -120,7 +120,8 @@ __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& c, const RowsArgs& 
   q.n = (uint32_t)(t1 - t0);
   q.len = len;
   q.page0 = p0;
-  q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && len < 0x80000000u;
+  q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && p1 <= c.page_base[c.n_seqs] &&
+         len < 0x80000000u;
   if (!q.ok) {
     if ((threadIdx.x & 31u) == 0) record(err, ERR_INVAL);
     q.n = 0;
