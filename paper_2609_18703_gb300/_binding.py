@@ -86,7 +86,7 @@ class ro_cache(C.Structure):
             raise ValueError("ro_cache: the last dimension must be contiguous")
         n_pages, heads, slots, dim = d_k.shape
         super().__init__(_ptr(d_k), _ptr(d_v), _dtype(d_k), n_pages, slots, heads, dim, d_page_base.numel() - 1,
-                         d_k.stride(0), d_k.stride(1), d_k.stride(2), _list(d_page_base, 8), _list(d_pages, 4))
+                         d_k.stride(0), d_k.stride(1), d_k.stride(2), _list(d_page_base, _I64), _list(d_pages, _I32))
         self._tensors = (d_k, d_v, d_page_base, d_pages)
         self._kind = (d_k.dtype, dim)             # what rows beside the cache must be
         self._units = (d_page_base.numel() - 1, heads)
@@ -184,21 +184,31 @@ def _dtype(x) -> int:
     return code
 
 
-def _list(x, size):
-    """A dense integer or float array of elements of `size` bytes."""
+_I32, _I64, _F32 = "32-bit integers", "64-bit integers", "32-bit floats"
+_ELEMENTS = {}   # torch dtype -> what its elements are, filled as they come up
+
+
+def _list(x, elements, least=0):
+    """A dense array of `elements`, at least `least` of them."""
     if x is None or isinstance(x, int):
         return x
-    if x.itemsize != size or not x.is_contiguous():
-        raise ValueError(f"argument must be contiguous, {size} bytes an element")
+    known = x.dtype
+    if known not in _ELEMENTS:
+        name = str(known)
+        _ELEMENTS[known] = {"torch.int32": _I32, "torch.uint32": _I32, "torch.int64": _I64, "torch.uint64": _I64,
+                            "torch.float32": _F32}.get(name, name)
+    if _ELEMENTS[known] is not elements or not x.is_contiguous():
+        raise ValueError(f"argument must be contiguous {elements}")
+    if least and x.numel() < least:
+        raise ValueError(f"argument has {x.numel()} elements where {least} are read or written")
     return x.data_ptr() if x.is_cuda else _ptr(x)
 
 
-def _rows(x, dtype, dim):
-    """(pointer, token stride, head stride) of a [tokens, heads, dim] tensor of the type."""
+def _rows(x, dtype):
+    """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor of the type."""
     tok, head, one = x.stride()
-    if one != 1 or x.dtype is not dtype or x.shape[2] != dim:
-        raise ValueError("argument must be [tokens, heads, head_dim], contiguous in the last dimension, of the others' "
-                         "type and head_dim")
+    if one != 1 or x.dtype is not dtype:
+        raise ValueError("argument must be [tokens, heads, head_dim], contiguous in the last dimension, of the others' type")
     return x.data_ptr() if x.is_cuda else _ptr(x), tok, head
 
 
@@ -414,52 +424,55 @@ def ro_rotary(ctx, d_x, d_out, d_pos, rope, inverse: bool = False) -> int:
     n, heads, dim = shape
     if shape != d_out.shape or d_pos.numel() != n * rope._axes:
         raise ValueError("ro_rotary: x, out and positions do not fit one another")
-    return (_lib or load()).ro_rotary(ctx, _DTYPES.get(dtype) or _dtype(d_x), *_rows(d_x, dtype, dim),
-                                      *_rows(d_out, dtype, dim), n, heads, dim, _list(d_pos, 4), rope._ref, inverse)
+    return (_lib or load()).ro_rotary(ctx, _DTYPES.get(dtype) or _dtype(d_x), *_rows(d_x, dtype),
+                                      *_rows(d_out, dtype), n, heads, dim, _list(d_pos, _I32), rope._ref, inverse)
 
 
 def ro_cache_append(ctx, cache, d_tok_base, d_tok_seq, d_len, d_pos, rope, d_q, d_q_out, d_k, d_v) -> int:
     """Put a step's tokens into the cache, k and q turned (rope None: as they
     are; d_q None: keys and values alone)."""
-    kind = cache._kind
+    (dtype, dim), (seqs, heads) = cache._kind, cache._units
     shape = d_k.shape
     n = shape[0]
-    if d_v.shape != shape or shape[1] != cache._units[1] or d_tok_seq.numel() < n or (
+    if d_v.shape != shape or shape[1] != heads or shape[-1] != dim or (
             rope is not None and d_pos.numel() != n * rope._axes):
         raise ValueError("ro_cache_append: tensors do not fit one another")
     if d_q is None:
         q = (None, 0, 0, 0, None, 0, 0)
     else:
         shape = d_q.shape
-        if shape != d_q_out.shape or shape[0] != n:
+        if shape != d_q_out.shape or shape[0] != n or shape[-1] != dim:
             raise ValueError("ro_cache_append: tensors do not fit one another")
-        q = (*_rows(d_q, *kind), shape[1], *_rows(d_q_out, *kind))
-    return (_lib or load()).ro_cache_append(ctx, cache._ref, _list(d_tok_base, 8), _list(d_tok_seq, 4), n,
-                                            _list(d_len, 4), _list(d_pos, 4), None if rope is None else rope._ref, *q,
-                                            *_rows(d_k, *kind), *_rows(d_v, *kind))
+        q = (*_rows(d_q, dtype), shape[1], *_rows(d_q_out, dtype))
+    turn = (None, None) if rope is None else (_list(d_pos, _I32), rope._ref)
+    return (_lib or load()).ro_cache_append(ctx, cache._ref, _list(d_tok_base, _I64, seqs + 1),
+                                            _list(d_tok_seq, _I32, n), n, _list(d_len, _I32, seqs), *turn, *q,
+                                            *_rows(d_k, dtype), *_rows(d_v, dtype))
 
 
 def ro_cache_attend(ctx, cache, d_tok_base, max_new, d_len, max_len, d_q, scale, window, sinks, d_out,
                     d_lse=None) -> int:
     """Attention of a step's tokens over the cache that holds them."""
-    kind, shape = cache._kind, d_q.shape
-    if d_out.shape != shape or (d_lse is not None and d_lse.shape != shape[:2]):
+    (dtype, dim), shape, seqs = cache._kind, d_q.shape, cache._units[0]
+    if d_out.shape != shape or shape[-1] != dim or (d_lse is not None and d_lse.shape != shape[:2]):
         raise ValueError("ro_cache_attend: q, out and lse do not fit one another")
-    return (_lib or load()).ro_cache_attend(ctx, cache._ref, _list(d_tok_base, 8), shape[0], max_new, _list(d_len, 4),
-                                            max_len, *_rows(d_q, *kind), shape[1], scale, window, sinks,
-                                            *_rows(d_out, *kind), _list(d_lse, 4))
+    return (_lib or load()).ro_cache_attend(ctx, cache._ref, _list(d_tok_base, _I64, seqs + 1), shape[0], max_new,
+                                            _list(d_len, _I32, seqs), max_len, *_rows(d_q, dtype), shape[1], scale,
+                                            window, sinks, *_rows(d_out, dtype), _list(d_lse, _F32))
 
 
 def ro_cache_weigh(ctx, cache, d_tok_base, max_new, d_len, d_q, scale, window, sinks, d_lse, decay, d_past,
                    d_score) -> int:
     """Attention weight per cached token, d_score [sequences, heads, slots] from
     d_past (None: nothing yet; may be d_score)."""
-    shape, slots = d_q.shape, d_score.shape
-    if d_lse.shape != shape[:2] or slots[:2] != cache._units or (d_past is not None and d_past.shape != slots):
+    (dtype, dim), shape, slots, seqs = cache._kind, d_q.shape, d_score.shape, cache._units[0]
+    if shape[-1] != dim or d_lse.shape != shape[:2] or slots[:2] != cache._units or (
+            d_past is not None and d_past.shape != slots):
         raise ValueError("ro_cache_weigh: q, lse and scores do not fit one another")
-    return (_lib or load()).ro_cache_weigh(ctx, cache._ref, _list(d_tok_base, 8), shape[0], max_new, _list(d_len, 4),
-                                           *_rows(d_q, *cache._kind), shape[1], scale, window, sinks, _list(d_lse, 4),
-                                           decay, _list(d_past, 4), _list(d_score, 4), slots[2])
+    return (_lib or load()).ro_cache_weigh(ctx, cache._ref, _list(d_tok_base, _I64, seqs + 1), shape[0], max_new,
+                                           _list(d_len, _I32, seqs), *_rows(d_q, dtype), shape[1], scale, window,
+                                           sinks, _list(d_lse, _F32), decay, _list(d_past, _F32), _list(d_score, _F32),
+                                           slots[2])
 
 
 def ro_cache_evict(ctx, cache, d_len, d_score, budget, sinks, recent, d_dst_base, d_dst_pages, d_keep, d_len_out,
@@ -470,6 +483,7 @@ def ro_cache_evict(ctx, cache, d_len, d_score, budget, sinks, recent, d_dst_base
     if slots[:2] != units or d_keep.shape != units + (budget,) or d_dst_base.numel() != units[0] + 1 or (
             d_score_out is not None and d_score_out.shape != slots):
         raise ValueError("ro_cache_evict: scores, kept slots or page lists do not fit the cache")
-    return (_lib or load()).ro_cache_evict(ctx, cache._ref, _list(d_len, 4), _list(d_score, 4), slots[2], budget,
-                                           sinks, recent, _list(d_dst_base, 8), _list(d_dst_pages, 4), _list(d_keep, 4),
-                                           _list(d_len_out, 4), _list(d_score_out, 4))
+    return (_lib or load()).ro_cache_evict(ctx, cache._ref, _list(d_len, _I32, units[0]), _list(d_score, _F32),
+                                           slots[2], budget, sinks, recent, _list(d_dst_base, _I64), _list(d_dst_pages, _I32),
+                                           _list(d_keep, _I32), _list(d_len_out, _I32, units[0]),
+                                           _list(d_score_out, _F32))
