@@ -35,7 +35,9 @@
  * Types: RO_BF16 and RO_F16 (ro_rotary also RO_F32).  Sums, softmax
  * statistics, rotations and scores are computed in 32 bits and rounded once,
  * to the output's type; attention rounds the softmax weights of a tile to the
- * cache's type for the matrix product with the values.
+ * cache's type for the matrix product with the values (f16 weights are held
+ * higher by a power of two for it: none above 2^-36 of its row's largest is
+ * lost).
  * Tensors are [tokens][heads][head_dim] with an element stride of 1 in the
  * last dimension and token and head strides in elements.  Where not said
  * otherwise the cache operators want 16-byte aligned pointers and strides that

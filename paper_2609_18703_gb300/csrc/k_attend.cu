@@ -194,8 +194,9 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     for (int z = 0; z < 2; ++z) {
       nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 1));
       nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
-      sub[z] = nm[z] == -INFINITY ? 0.f : nm[z];     // a row that has seen nothing yet
-      f[z] = exp2f(m[z] - sub[z]);
+      const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
+      f[z] = exp2f(m[z] - top);
+      sub[z] = top - WEIGHT_UP<T>;
       m[z] = nm[z];
       l[z] *= f[z];
     }
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     if (n_chunks > 1) {
       if ((lane & 3) == 0) __stcg((float2*)(pp + DP), make_float2(m[z], l[z]));
     } else if ((lane & 3) == 0 && a.lse) {
-      a.lse[t * a.n_q_heads + h] = l[z] == 0.f ? -INFINITY : (m[z] + log2f(l[z])) * LN2;
+      a.lse[t * a.n_q_heads + h] = row_lse<T>(m[z], l[z]);
     }
 #pragma unroll
     for (int i = 0; i < DP / 8; ++i) {
@@ -290,7 +291,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
     if (d < D)
       *(uint32_t*)(out + t * a.out_tok + h * a.out_head + d) = pack2<T>(acc.x * inv, acc.y * inv);
-    if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+    if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = row_lse<T>(M, L);
   }
   if (tid == 0) a.counter[blockIdx.x] = 0u;   // for the next call
 }

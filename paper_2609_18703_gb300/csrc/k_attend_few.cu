@@ -132,8 +132,9 @@ struct FewRows {
   for (int z = 0; z < 2; ++z) {
     nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 1));
     nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
-    sub[z] = nm[z] == -INFINITY ? 0.f : nm[z];     // a row that has seen nothing yet
-    f[z] = ex2(m[z] - sub[z]);
+    const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
+    f[z] = ex2(m[z] - top);
+    sub[z] = top - WEIGHT_UP<T>;
   }
   if (__any_sync(0xffffffffu, nm[0] > m[0] || nm[1] > m[1])) {
 #pragma unroll
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
       if (d < D)
         *(uint2*)(out + t * a.out_tok + h * a.out_head + d) =
             make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-      if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+      if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = row_lse<T>(M, L);
     }
   }
   if (n_chunks == 1) return;
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
     if (d < D)
       *(uint2*)(out + t * a.out_tok + h * a.out_head + d) =
           make_uint2(pack2<T>(acc.x * inv, acc.y * inv), pack2<T>(acc.z * inv, acc.w * inv));
-    if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+    if (d == 0 && a.lse) a.lse[t * a.n_q_heads + h] = row_lse<T>(M, L);
   }
   if (g.cluster)
     cluster_sync();                               // no CTA leaves while another reads its shared memory
@@ -440,7 +441,7 @@ __global__ void __launch_bounds__(32) attend_short_kernel(const __grid_constant_
 #pragma unroll
     for (int i = 0; i < DP / 8; ++i)
       if ((uint32_t)i * 8 + (lane & 3) * 2 < D) *(uint32_t*)(out + i * 8) = pack2<T>(f.o[i][z * 2] * inv, f.o[i][z * 2 + 1] * inv);
-    if ((lane & 3) == 0 && a.lse) a.lse[t * a.n_q_heads + h] = f.l[z] == 0.f ? -INFINITY : (f.m[z] + log2f(f.l[z])) * LN2;
+    if ((lane & 3) == 0 && a.lse) a.lse[t * a.n_q_heads + h] = row_lse<T>(f.m[z], f.l[z]);
   }
 }
 

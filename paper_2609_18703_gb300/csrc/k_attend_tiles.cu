@@ -11,7 +11,8 @@
 // into a ring of key and value tiles, a warp that issues the products, and for
 // each row tile four warps of softmax, a thread a row.  S and O live in TMEM;
 // P replaces S there and is the left operand of the second product.  m only
-// moves when a row's maximum grew by more than 2^8, so O is seldom rescaled.
+// moves when a row's maximum grew by more than 2^8 (f16: 2^4), so O is seldom
+// rescaled.
 // Slots that no row of the CTA sees are never loaded or are zeroed in shared
 // memory first (a weight of 0 does not silence a NaN in a matrix product).
 // A CTA stays on its SM and takes pairs of row tiles as it gets free, heavy ones
@@ -37,7 +38,12 @@ constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then a warp ea
 #define AT_REGS_SOFTMAX 216
 #define AT_REGS_OTHERS 72
 constexpr uint32_t AT_TMEM_COLS = 512;
-constexpr float AT_SLACK = 8.f;   // log2 of what a row's maximum may grow before O is rescaled
+// log2 of what a row's maximum may grow before O is rescaled; f16 weights, at
+// most 2^15, have to hold it beside the bits they are held higher by
+template <typename T>
+constexpr int AT_SLACK = 8;
+template <>
+constexpr int AT_SLACK<__half> = 4;
 
 template <int DP>
 struct TileShape {
@@ -430,7 +436,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
       const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
                                       fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * scale);
-      if (__any_sync(0xffffffffu, mine && mn > m + AT_SLACK)) {
+      if (__any_sync(0xffffffffu, mine && mn > m + AT_SLACK<T>)) {
         // The maximum moves for the whole warp: rescale what was summed so far.
         // (Rows that are no token's have no say: theirs may hold whatever an
         // earlier kernel left, and would decide how the others are rounded.)
@@ -449,7 +455,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           }
         }
       }
-      const float sub = m == -INFINITY ? 0.f : m;   // a row that has seen nothing yet
+      const float sub = (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>;   // -inf: a row that has seen nothing yet
       const uint64_t scale2 = pair(scale, scale), sub2 = pair(-sub, -sub);
       uint64_t sum[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
 #pragma unroll
@@ -529,7 +535,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       for (int i = 0; i < DP / 2; i += 4)
         if ((uint32_t)i * 2 < a.c.head_dim) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
     }
-    if (a.lse) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+    if (a.lse) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
   }
   __syncwarp();
   tc_fence_before();
@@ -572,7 +578,7 @@ __global__ void __launch_bounds__(2 * AT_ROWS) attend_join_kernel(const __grid_c
   if (c * 4 < a.c.head_dim)
     *(uint2*)((T*)a.out + t * a.out_tok + (uint64_t)head * a.out_head + c * 4) =
         make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
-  if (c == 0 && a.lse) a.lse[t * a.n_q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+  if (c == 0 && a.lse) a.lse[t * a.n_q_heads + head] = row_lse<T, AT_SLACK<T>>(m, l);
 }
 
 // ---- host ------------------------------------------------------------------------------------

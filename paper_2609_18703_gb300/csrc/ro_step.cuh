@@ -72,6 +72,23 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
+// Softmax weights are rounded to the cache's type for the product with the
+// values.  f16 has nothing below 2^-25, so its weights are held 2^UP times
+// higher, up to 2^15: behind a heavy first token the light ones, many of them,
+// would else add to the row's sum and not to its output.  The sums l and o are
+// 2^UP times higher too; only the logarithm of l has to know.  bf16 has the
+// exponents of 32 bits.  SLACK: log2 of what weights may pass 1.
+template <typename T, int SLACK = 0>
+constexpr int WEIGHT_UP = 0;
+template <int SLACK>
+constexpr int WEIGHT_UP<__half, SLACK> = 15 - SLACK;
+// ln sum_j exp(..) of a row from its maximum (in log2) and its sum
+template <typename T, int SLACK = 0>
+__device__ __forceinline__ float row_lse(float m, float l) {
+  constexpr float down = 1.f / (1u << WEIGHT_UP<T, SLACK>);
+  return l == 0.f ? -INFINITY : (m + log2f(l * down)) * LN2;
+}
+
 // ---- clusters ------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
