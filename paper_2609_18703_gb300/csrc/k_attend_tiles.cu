@@ -607,7 +607,7 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int
   g.box = page_box(a.c.page_size, AT_KEYS);
   g.wide = a.c.head_dim % 16 == 0 && a.out_tok % 16 == 0 && a.out_head % 16 == 0 &&
            reinterpret_cast<uintptr_t>(a.out) % 32 == 0;
-  if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
+  if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, a.r.group, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
       !pool_map(&g.v, a.c, a.c.v, dtype, g.box))
     return false;
   const bool narrow = a.c.head_dim <= 64;

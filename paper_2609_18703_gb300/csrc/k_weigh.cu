@@ -78,23 +78,17 @@ __global__ void __launch_bounds__(WG_THREADS) weigh_kernel(const __grid_constant
 #pragma unroll
       for (int i = 0; i < (int)WG_ROWS / RPP; ++i) {
         const uint32_t r = i * RPP + pr;
-        const bool ok = r < rn && piece_ok;
-        uint64_t e = 0;
-        if (ok) {
-          const uint32_t x = r0 + r, t = i0 + x / G, g = x % G;
-          e = (q.tok0 + t) * a.r.q_tok + (uint64_t)(kh * G + g) * a.r.q_head + pc * 8;
-        }
-        cp_async16_or_zero(sm + r * DP * 2 + ((pc ^ (r & 7)) * 16), (const T*)a.r.q + e, ok);
+        const uint32_t x = r0 + min(r, rn - 1), t = i0 + x / G, g = x % G;
+        const uint64_t e = piece_ok ? (q.tok0 + t) * a.r.q_tok + (uint64_t)(kh * G + g) * a.r.q_head + pc * 8 : 0;
+        cp_async16_or_zero(sm + r * DP * 2 + ((pc ^ (r & 7)) * 16), (const T*)a.r.q + e, piece_ok);
       }
       cp_async_commit();
       if (tid < (int)WG_ROWS) {
-        float z = INFINITY;   // rows past the end and rows that see nothing add 0
-        uint32_t t = 0;
+        const uint32_t x = r0 + min((uint32_t)tid, rn - 1), t = i0 + x / G, g = x % G;
+        float z = LSE_FILL;
         if (tid < (int)rn) {
-          const uint32_t x = r0 + tid, g = x % G;
-          t = i0 + x / G;
           z = a.lse[(q.tok0 + t) * a.n_q_heads + kh * G + g] * 1.44269504088896340736f;
-          if (z == -INFINITY) z = INFINITY;
+          if (z == -INFINITY) z = INFINITY;   // rows that see nothing add 0
         }
         s_lse[tid] = z;
         s_at[tid] = t;
@@ -121,7 +115,6 @@ __global__ void __launch_bounds__(WG_THREADS) weigh_kernel(const __grid_constant
             const uint32_t c = n0 + n * 8 + (lane & 3) * 2 + (z & 1);
             float p = exp2f(s[n][z] * a.r.scale_log2 - s_lse[c]);
             if (!all && !sees(a.r, q.first + s_at[c], my_key[z >> 1])) p = 0.f;
-            // (rows past the end: s is 0 and lse +inf)
             sum[z >> 1] += p;
           }
       }

@@ -95,14 +95,14 @@ __global__ void __launch_bounds__(WF_THREADS, 4) weigh_few_kernel(const __grid_c
     load_stages<T, DP, KEYS, false>(a.c, &g.k, &g.k, g.tma != 0, g.box, WF_STAGES, slots, c0, n, kh, q.page0, sm, b_full,
                                                b_empty, &s_gave_up, a.err);
   } else {
-    // query rows as the right operand, two groups of eight; each row's lse, +inf for rows that add nothing
+    // query rows as the right operand, two groups of eight; each row's lse, +inf for rows that see nothing
     uint32_t qf[DP / 16][4];
     float lse[4];
     int64_t at[4];
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
       const uint32_t x = (z >> 1) * 8 + (lane & 3) * 2 + (z & 1);
-      lse[z] = INFINITY;
+      lse[z] = LSE_FILL;
       at[z] = INT64_MIN / 2;
       if (x < rows) {
         const uint32_t i = x / G;
@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(WF_THREADS, 4) weigh_few_kernel(const __grid_c
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const uint32_t x = z * 8 + lane / 4;
-      const T* p = x < rows ? (const T*)r.q + (q.tok0 + x / G) * r.q_tok + (uint64_t)(kh * G + x % G) * r.q_head : nullptr;
+      const uint32_t x = min(z * 8 + lane / 4, rows - 1);
+      const T* p = rows > 0 ? (const T*)r.q + (q.tok0 + x / G) * r.q_tok + (uint64_t)(kh * G + x % G) * r.q_head : nullptr;
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k)
 #pragma unroll

@@ -128,11 +128,6 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  // rows that no tile has (the group does not divide 128) are zero: their product is 0, their weight exp2(-inf)
-  for (uint32_t x = g.toks * G * 8 + tid; x < WT_ROWS * 8; x += WT_THREADS)
-    for (uint32_t b = 0; b < S::STAGES * S::BLOCKS; ++b)
-      asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_q + b * S::BLOCK_BYTES + x * 16), "r"(0u) : "memory");
-  fence_async_smem();
   if (warp == 8) tmem_alloc(step_smem(&s_tmem), WT_TMEM_COLS);
   tc_fence_before();
   __syncthreads();
@@ -270,10 +265,14 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
         if (uses >= S::STAGES) bar_wait(b_empty + 8 * slot, parity, &s_gave_up, a.err);
         if (has_given_up(&s_gave_up)) break;
         if (lane == 0) {
-          bar_expect(b_full + 8 * slot, S::BLOCKS * g.toks * G * 128);
-          for (uint32_t b = 0; b < S::BLOCKS; ++b)
-            tma3(sm_q + slot * S::TILE_BYTES + b * S::BLOCK_BYTES, &g.q, b * 64, (int)(kh * G), (int)(tok + t * g.toks),
-                 b_full + 8 * slot);
+          const uint32_t rows = g.toks * G;   // fewer than a tile's where the group does not divide it
+          bar_expect(b_full + 8 * slot, S::TILE_BYTES);
+          for (uint32_t b = 0; b < S::BLOCKS; ++b) {
+            const uint32_t dst = sm_q + slot * S::TILE_BYTES + b * S::BLOCK_BYTES;
+            tma3(dst, &g.q, b * 64, (int)(kh * G), (int)(tok + t * g.toks), b_full + 8 * slot);
+            if (rows < WT_ROWS)
+              tma3(dst + rows * 128, &g.fill, b * 64, (int)(kh * G), (int)(tok + t * g.toks), b_full + 8 * slot);
+          }
         }
         __syncwarp();
         uses = min(uses + 1, S::STAGES);
@@ -338,10 +337,12 @@ __global__ void __launch_bounds__(WT_THREADS, 2) weigh_tiles_kernel(const __grid
       }
       uint64_t acc[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
       // this thread's row of a tile, fetched a turn ahead: minus its lse, -inf for
-      // rows past the end and rows that see nothing (they add 0)
+      // rows past the end and rows that see nothing (they add 0); LSE_FILL for rows
+      // that fill up a tile
       const float* lse = a.lse + (tok0 + i0 + row / G) * a.n_q_heads + kh * G + row % G;
       auto row_lse = [&](uint32_t t) -> float {
-        if (t >= n || row >= g.toks * G || i0 + t * g.toks + row / G >= i1) return INFINITY;
+        if (row >= g.toks * G) return LSE_FILL * LN2;
+        if (t >= n || i0 + t * g.toks + row / G >= i1) return INFINITY;
         return lse[(uint64_t)t * g.toks * a.n_q_heads];
       };
       uint32_t t = (w ^ tiles) & 1;
@@ -433,7 +434,10 @@ bool launch_weigh_tiles(const LaunchCfg& L, const WeighArgs& a, int dtype, int s
   g.a = a;
   g.toks = WT_ROWS / a.r.group;
   g.box = page_box(a.c.page_size, WT_KEYS);
-  if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, g.toks) || !pool_map(&g.k, a.c, a.c.k, dtype, g.box))
+  const uint32_t fill = WT_ROWS - g.toks * a.r.group;   // fewer than the group
+  if (!rows_map(&g.q, a.r, a.c.head_dim, a.n_q_heads, dtype, a.r.group, g.toks) ||
+      !pool_map(&g.k, a.c, a.c.k, dtype, g.box) ||
+      (fill && !rows_map(&g.fill, a.r, a.c.head_dim, a.n_q_heads, dtype, fill, 1)))
     return false;
   if (a.unseen) {
     WeighArgs p = a;

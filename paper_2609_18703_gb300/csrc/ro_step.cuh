@@ -89,6 +89,12 @@ __device__ __forceinline__ float row_lse(float m, float l) {
   return l == 0.f ? -INFINITY : (m + log2f(l * down)) * LN2;
 }
 
+// Rows that fill up a tile of weights repeat a row of the tile, with this for
+// the lse (in log2): their weights are 0 where that row's are finite, and
+// infinite or NaN only where its are.  (Rows of zeros would make NaN of a key
+// with an infinity, whose own weight is 0.)
+constexpr float LSE_FILL = 1e38f;
+
 // ---- clusters ------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;

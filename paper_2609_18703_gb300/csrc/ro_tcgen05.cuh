@@ -340,8 +340,9 @@ bool tile_map(CUtensorMap* m, int dtype, const void* p, int dims, const uint64_t
               const uint32_t* box);
 // a cache's pool, boxes of `box` slots of one page and head
 bool pool_map(CUtensorMap* m, const PagedArgs& c, const void* pool, int dtype, uint32_t box);
-// the query rows, boxes of `toks` tokens times one group of heads
-bool rows_map(CUtensorMap* m, const RowsArgs& r, uint32_t head_dim, uint32_t n_q_heads, int dtype, uint32_t toks);
+// the query rows, boxes of `toks` tokens times `heads` heads
+bool rows_map(CUtensorMap* m, const RowsArgs& r, uint32_t head_dim, uint32_t n_q_heads, int dtype, uint32_t heads,
+              uint32_t toks);
 
 struct AttendTileArgs {
   AttendArgs a;
@@ -358,6 +359,7 @@ struct WeighFewArgs {
 struct WeighTileArgs {
   WeighArgs a;
   CUtensorMap q, k;
+  CUtensorMap fill;          // the heads of one token that fill up a row tile
   uint32_t toks, box;
 };
 struct AttendFewArgs {

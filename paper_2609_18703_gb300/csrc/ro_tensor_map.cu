@@ -43,10 +43,11 @@ bool pool_map(CUtensorMap* m, const PagedArgs& c, const void* pool, int dtype, u
   return tile_map(m, dtype, pool, 4, size, stride, boxes);
 }
 
-bool rows_map(CUtensorMap* m, const RowsArgs& r, uint32_t head_dim, uint32_t n_q_heads, int dtype, uint32_t toks) {
+bool rows_map(CUtensorMap* m, const RowsArgs& r, uint32_t head_dim, uint32_t n_q_heads, int dtype, uint32_t heads,
+              uint32_t toks) {
   const uint64_t size[3] = {head_dim, n_q_heads, r.n_tokens};
   const uint64_t stride[3] = {1, r.q_head, r.q_tok};
-  const uint32_t boxes[3] = {64, r.group, toks};
+  const uint32_t boxes[3] = {64, heads, toks};
   return tile_map(m, dtype, r.q, 3, size, stride, boxes);
 }
 
