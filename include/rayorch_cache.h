@@ -151,7 +151,8 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
  *     + sum over s's new tokens and h's query heads of
  *       exp(scale * q.k_j - lse), where the token sees slot j.
  * Arguments as in ro_cache_attend; d_lse is its d_lse output.  d_past and
- * d_score are float[n_seqs][n_heads][score_cap]; they may be the same array.
+ * d_score are float[n_seqs][n_heads][score_cap]; they may be the same array
+ * (but may not overlap otherwise).
  * Slots from d_len[s] on are not touched.  A length above score_cap is
  * recorded (RO_E_CAPACITY).  Equal calls give equal bits.
  */
@@ -179,7 +180,7 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
  *   d_len_out   uint32[n_seqs] out: min(length, budget); may be d_len (but may
  *               not overlap it otherwise: RO_E_INVAL).
  *   d_score_out float[n_seqs][n_heads][score_cap] out or NULL: kept scores;
- *               not d_score.
+ *               no part of d_score.
  * sinks + recent <= budget, budget >= 1.
  */
 ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_len,

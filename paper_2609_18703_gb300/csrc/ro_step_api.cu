@@ -27,6 +27,11 @@ bool overlap(const void* p, const void* q, uint64_t bytes) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return (a < b ? b - a : a - b) < bytes;
 }
+// rows that are turned in place lie where they were
+bool in_place_elsewhere(const void* x, uint64_t x_tok, uint64_t x_head, const void* y, uint64_t y_tok, uint64_t y_head,
+                        uint64_t n_tokens, uint32_t n_heads) {
+  return x == y && ((n_tokens > 1 && x_tok != y_tok) || (n_heads > 1 && x_head != y_head));
+}
 
 ro_status check_rope(StepCall& c, const char* fn, const ro_rope* r, uint32_t head_dim) {
   if (r->n_axes < 1 || r->n_axes > 4) return c.refuse(RO_E_INVAL, "%s: 1 to 4 axes", fn);
@@ -160,6 +165,8 @@ ro_status ro_rotary(ro_ctx* ctx, int32_t dtype, const void* d_x, uint64_t x_tok,
   RO_TRY(check_rope(c, fn, rope, head_dim));
   const size_t elem = dtype == RO_F32 ? 4 : 2;
   if (!aligned(d_x, elem) || !aligned(d_out, elem)) return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
+  if (in_place_elsewhere(d_x, x_tok, x_head, d_out, out_tok, out_head, n_tokens, n_heads))
+    return c.refuse(RO_E_INVAL, "%s: in place with other strides", fn);
   if (n_tokens == 0 || n_heads == 0) return RO_OK;
   RO_TRY(c.begin());
   TurnArgs a = {};
@@ -194,6 +201,8 @@ ro_status ro_cache_append(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
     if (!aligned(p, 16)) return c.refuse(RO_E_INVAL, "%s: pointers must be 16-byte aligned", fn);
   for (uint64_t s : {q_tok, q_head, qo_tok, qo_head, k_tok, k_head, v_tok, v_head})
     if (s % 8) return c.refuse(RO_E_INVAL, "%s: strides must be multiples of 8 elements", fn);
+  if (n_q_heads && in_place_elsewhere(d_q, q_tok, q_head, d_q_out, qo_tok, qo_head, n_tokens, n_q_heads))
+    return c.refuse(RO_E_INVAL, "%s: q in place with other strides", fn);
   if (n_tokens == 0) return RO_OK;
   RO_TRY(c.begin());
   TurnArgs a = {};
@@ -233,6 +242,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
   if (!aligned(d_out, 16) || out_tok % 8 || out_head % 8)
     return c.refuse(RO_E_INVAL, "%s: the output wants a 16-byte pointer and strides of 8 elements", fn);
   if (n_tokens == 0) return RO_OK;
+  if (d_out == d_q) return c.refuse(RO_E_INVAL, "%s: the output cannot be q", fn);
   RO_TRY(c.begin());
   AttendArgs a = {};
   a.c = paged(cache);
@@ -358,6 +368,8 @@ ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_t
   if (units > MAX_GRID || ceil_div(score_cap, WG_KEYS) > MAX_GRID / units)
     return c.refuse(RO_E_OVERFLOW, "%s: too many scores", fn);
   if (score_cap == 0) return RO_OK;
+  if (d_past && d_past != d_score && overlap(d_past, d_score, units * score_cap * sizeof(float)))
+    return c.refuse(RO_E_INVAL, "%s: past scores are d_score or another array", fn);
   RO_TRY(c.begin());
   WeighArgs a = {};
   a.c = paged(cache);
@@ -413,11 +425,12 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
     return c.refuse(RO_E_INVAL, "%s: sinks and recent tokens must fit the budget", fn);
   if (d_len_out != d_len && overlap(d_len, d_len_out, (uint64_t)cache->n_seqs * sizeof(uint32_t)))
     return c.refuse(RO_E_INVAL, "%s: lengths are cut in place or into another array", fn);
-  if (d_score_out && d_score_out == d_score) return c.refuse(RO_E_INVAL, "%s: scores cannot be cut in place", fn);
   if (score_cap >= 0x80000000ull || budget >= 0x80000000u)
     return c.refuse(RO_E_OVERFLOW, "%s: 2^31 scores or a budget of 2^31 or more", fn);
   if ((uint64_t)cache->n_seqs * cache->n_heads > MAX_GRID / 4096)
     return c.refuse(RO_E_OVERFLOW, "%s: too many sequences and heads", fn);
+  if (d_score_out && overlap(d_score, d_score_out, (uint64_t)cache->n_seqs * cache->n_heads * score_cap * sizeof(float)))
+    return c.refuse(RO_E_INVAL, "%s: scores cannot be cut in place", fn);
   RO_TRY(c.begin());
   EvictArgs a = {};
   a.c = paged(cache);
