@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     // four columns of a row together, rows next to one another: a warp's
     // accesses are whole lines
     float4* part = (float4*)a.partial + (uint64_t)unit * a.max_chunks * (DP / 4) * STEP + prow;
-    float2* ml = (float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * STEP * DP) +
+    float2* ml = (float2*)(a.partial + (uint64_t)a.pairs * a.max_chunks * STEP * DP) +
                  (uint64_t)unit * a.max_chunks * STEP + prow;
     if (n_runs > 1) {   // joined by attend_join_kernel
       if (mine) {
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(2 * AT_ROWS) attend_join_kernel(const __grid_c
   const uint32_t i = w * g.toks + row / a.r.group, head = (unit % a.c.n_heads) * a.r.group + row % a.r.group;
   if (runs < 2 || runs > a.max_chunks || row >= g.toks * a.r.group || i >= it.n || it.tok + i >= a.r.n_tokens) return;
   const float4* part = (const float4*)a.partial + ((uint64_t)unit * a.max_chunks * (DP / 4) + c) * STEP + prow;
-  const float2* ml = (const float2*)(a.partial + (uint64_t)a.tiles * a.c.n_heads * a.max_chunks * STEP * DP) +
+  const float2* ml = (const float2*)(a.partial + (uint64_t)a.pairs * a.max_chunks * STEP * DP) +
                      (uint64_t)unit * a.max_chunks * STEP + prow;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -589,7 +589,7 @@ uint32_t attend_tile_tokens(uint32_t group) { return 2 * (AT_ROWS / group); }
 size_t attend_tiles_join(const AttendArgs& a) { return (size_t)a.tiles * a.c.n_heads * sizeof(JoinItem); }
 size_t attend_tiles_partial(const AttendArgs& a) {
   const size_t dp = a.c.head_dim <= 64 ? 64 : 128;
-  return (size_t)a.tiles * a.c.n_heads * a.max_chunks * 2 * AT_ROWS * (dp + 2) * sizeof(float);
+  return (size_t)a.pairs * a.max_chunks * 2 * AT_ROWS * (dp + 2) * sizeof(float);
 }
 
 template <typename T, int DP>

@@ -97,6 +97,7 @@ struct AttendArgs {
   PagedArgs c;
   RowsArgs r;
   uint32_t tiles;            // row tiles per cache head, at most
+  uint32_t pairs;            // attend_tiles: (pair of row tiles, head) that there can be
   uint32_t chunk;            // of one CTA, more where max_chunks would not reach: keys
                              // (attend_rows), stages (attend_few), tiles (attend_tiles)
   uint32_t max_chunks;

@@ -12,7 +12,8 @@ namespace {
 constexpr uint32_t MAX_HEADS = 65535;
 constexpr uint64_t MAX_GRID = 0x7FFFFFFFull;
 // Runs whose partial results a call keeps: 1,024 of attend_tiles' 133 KB,
-// 16,384 of attend_few's 8 KB (about 136 MB either way).
+// 16,384 of attend_few's 8 KB (about 136 MB either way, and the workspace's
+// headroom of an eighth).
 constexpr uint64_t MAX_RUNS = 1024, MAX_FEW_RUNS = 16384;
 
 #define RO_TRY(x)               \
@@ -318,6 +319,7 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
         runs = k;
       }
     }
+    a.pairs = (uint32_t)pairs;   // whose numbers have no gaps: partial results for these alone
     a.chunk = runs == 1 ? 0x40000000u : (uint32_t)ceil_div(slots, runs);
     a.max_chunks = runs == 1 ? 1u : (uint32_t)ceil_div(slots, a.chunk);
     RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
