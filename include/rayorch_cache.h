@@ -30,7 +30,9 @@
  * the described arrays is read or written even then: the tokens concerned are
  * left out, and the call's results are void.
  * Workspaces belong to the context and grow on demand, so a call that will be
- * captured into a CUDA graph runs once uncaptured first.
+ * captured into a CUDA graph runs once uncaptured first.  Graphs stay good when
+ * a later call needs larger ones: those that captured calls use live as long as
+ * the context.
  *
  * Types: RO_BF16 and RO_F16 (ro_rotary also RO_F32).  Sums, softmax
  * statistics, rotations and scores are computed in 32 bits and rounded once,

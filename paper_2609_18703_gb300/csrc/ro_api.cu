@@ -186,6 +186,8 @@ struct ro_ctx {
   DevBuf code;
   DevBuf selftest;                      // ro_ctx_selftest_timeout scratch
   DevBuf step[SS_COUNT];                // model-step workspaces (ro_step.h)
+  bool step_captured[SS_COUNT] = {};    // a captured call uses this one: its graph may be replayed
+  std::vector<DevBuf> step_kept[SS_COUNT];   // outgrown ones of captured calls
   DevBuf x_mb, x_coff, x_mtfp, x_hdr;   // explicit-list assembly scratch
   // parent-bound reservation scratch (see ParentArgs)
   DevBuf pb_key[2], pb_val[2], pb_child, pb_hist, pb_dtot, pb_first, pb_endp, pb_hsz, pb_left,
@@ -408,8 +410,10 @@ ro_status sync_and_check(ro_ctx* c) {
   if (!err) return RO_OK;
   cudaMemsetAsync(&c->ds->err, 0, sizeof(uint32_t), c->stream);
   // (a model-step kernel that gave up may have left its counters behind)
-  if ((err & ERR_TIMEOUT) && c->step[SS_COUNTER].p)
+  if ((err & ERR_TIMEOUT) && c->step[SS_COUNTER].p) {
     cudaMemsetAsync(c->step[SS_COUNTER].p, 0, c->step[SS_COUNTER].cap, c->stream);
+    for (const DevBuf& b : c->step_kept[SS_COUNTER]) cudaMemsetAsync(b.p, 0, b.cap, c->stream);
+  }
   if (err & ERR_TIMEOUT)
     return fail(c, RO_E_TIMEOUT, (err & ERR_DRAIN)
                                      ? "a device-side wait timed out (a copy CTA exited with bulk "
@@ -682,6 +686,8 @@ ro_status ro_ctx_destroy(ro_ctx* c) {
     free_buf(t.flag); free_buf(t.agg); free_buf(t.inc);
   }
   for (DevBuf& b : c->step) free_buf(b);
+  for (auto& kept : c->step_kept)
+    for (DevBuf& b : kept) free_buf(b);
   free_buf(c->code); free_buf(c->selftest); free_buf(c->x_mb); free_buf(c->x_coff); free_buf(c->x_mtfp); free_buf(c->x_hdr);
   for (DevBuf* b : {&c->pb_key[0], &c->pb_key[1], &c->pb_val[0], &c->pb_val[1], &c->pb_child,
                     &c->pb_hist, &c->pb_dtot, &c->pb_first, &c->pb_endp, &c->pb_hsz, &c->pb_left,
@@ -1615,8 +1621,18 @@ ro_status StepCall::refuse(ro_status st, const char* fmt, ...) {
 }
 ro_status StepCall::launched(const char* what) { return check_launch(c_, what); }
 ro_status StepCall::scratch(int which, size_t bytes, void** p) {
-  const ro_status st = ensure(c_, c_->step[which], bytes, "a model-step workspace");
-  *p = c_->step[which].p;
+  DevBuf& b = c_->step[which];
+  const bool capturing = capture_id(c_->stream) != 0;
+  // A graph holds the address: a workspace that one uses is kept when it is
+  // outgrown (captured calls themselves do not grow one).
+  if (b.cap < bytes && c_->step_captured[which] && !capturing) {
+    c_->step_kept[which].push_back(b);
+    b = DevBuf();
+    c_->step_captured[which] = false;
+  }
+  const ro_status st = ensure(c_, b, bytes, "a model-step workspace");
+  if (st == RO_OK && capturing) c_->step_captured[which] = true;
+  *p = b.p;
   return st;
 }
 const LaunchCfg& StepCall::launch() const { return c_->L; }

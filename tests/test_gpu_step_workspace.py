@@ -56,3 +56,53 @@ def test_partial_results_of_a_long_sequence(new, heads, kv, slots):
             assert bool(((out[t, h].double() - p @ rows).abs() <= tol).all())
             assert abs(float(lse[t, h]) - float(torch.logsumexp(x, 0))) < 1e-4
     ro.ro_ctx_destroy(ctx)
+
+
+@pytest.mark.parametrize("new,heads,kv,slots,page", [(1, 8, 8, 20_000, 64), (64, 8, 2, 20_000, 64), (20, 2, 1, 9_000, 5)])
+def test_graphs_outlive_the_growth_of_a_workspace(new, heads, kv, slots, page):
+    """A captured call that splits its slots, replayed after calls that need larger workspaces."""
+    dim, n = 64, -(-slots // page)
+    g = torch.Generator(device="cuda").manual_seed(new)
+    pool = torch.randn(n, kv, page, dim, generator=g, device="cuda").half()
+    pages = torch.randperm(n, generator=g, device="cuda").int()
+    stream = torch.cuda.Stream()
+    ctx = ro.ro_ctx_create(0, stream, 1)
+
+    def setup(seqs):
+        cache = ro.ro_cache(pool, pool, torch.arange(seqs + 1, device="cuda") * n, pages.repeat(seqs))
+        q = torch.randn(seqs * new, heads, dim, generator=g, device="cuda").half()
+        tok = torch.arange(seqs + 1, device="cuda") * new
+        lens = torch.full((seqs,), slots, dtype=torch.int32, device="cuda")
+        out, lse = torch.zeros_like(q), torch.zeros(seqs * new, heads, device="cuda")
+        torch.cuda.synchronize()
+
+        def call():
+            assert ro.ro_cache_attend(ctx, cache, tok, new, lens, slots, q, 0.125, 0, 0, out, lse) == ro.RO_OK, \
+                ro.ro_last_error(ctx)
+        return call, out, lse
+
+    small, out, lse = setup(1)
+    small()
+    assert ro.ro_ctx_sync(ctx) == ro.RO_OK
+    want = out.clone(), lse.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        small()
+    for seqs in (5, 40):
+        large, large_out, large_lse = setup(seqs)
+        large()
+        assert ro.ro_ctx_sync(ctx) == ro.RO_OK
+        taken = [torch.full((1 << 22,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]   # what was let go of
+        first = large_out.clone(), large_lse.clone()
+        for _ in range(2):
+            out.zero_()
+            lse.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        assert all(bool((x == 7).all()) for x in taken)
+        large()
+        assert ro.ro_ctx_sync(ctx) == ro.RO_OK
+        assert torch.equal(large_out, first[0]) and torch.equal(large_lse, first[1])
+    ro.ro_ctx_destroy(ctx)
