@@ -61,116 +61,116 @@ struct FewRows {
   // rows past the tile's are zero
   __device__ __forceinline__ void load(const AttendArgs& a, const SeqInfo& q, uint32_t kh, uint32_t rows, uint32_t lane) {
     const uint32_t G = a.r.group, D = a.c.head_dim;
-  const T* qp[2];
+    const T* qp[2];
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    const uint32_t r = lane / 4 + 8 * z;
-    qp[z] = nullptr;
-    row_a[z] = INT64_MIN / 2;
-    if (r < rows) {
-      const uint32_t i = r / G, h = kh * G + r % G;
-      qp[z] = (const T*)a.r.q + (q.tok0 + i) * a.r.q_tok + (uint64_t)h * a.r.q_head;
-      row_a[z] = q.first + i;
+    for (int z = 0; z < 2; ++z) {
+      const uint32_t r = lane / 4 + 8 * z;
+      qp[z] = nullptr;
+      row_a[z] = INT64_MIN / 2;
+      if (r < rows) {
+        const uint32_t i = r / G, h = kh * G + r % G;
+        qp[z] = (const T*)a.r.q + (q.tok0 + i) * a.r.q_tok + (uint64_t)h * a.r.q_head;
+        row_a[z] = q.first + i;
+      }
     }
-  }
 #pragma unroll
-  for (int k = 0; k < DP / 16; ++k)
+    for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      const uint32_t d = k * 16 + (z >> 1) * 8 + (lane & 3) * 2;
-      const T* p = qp[z & 1];
-      qf[k][z] = p && d < D ? *(const uint32_t*)(p + d) : 0u;
-    }
+      for (int z = 0; z < 4; ++z) {
+        const uint32_t d = k * 16 + (z >> 1) * 8 + (lane & 3) * 2;
+        const T* p = qp[z & 1];
+        qf[k][z] = p && d < D ? *(const uint32_t*)(p + d) : 0u;
+      }
   }
   // one stage: its keys at kb in shared memory, its values behind them
   __device__ __forceinline__ void stage(const AttendArgs& a, const SeqInfo& q, const SlotTile& st, uint32_t kb, uint32_t lane) {
-  const uint32_t vb = kb + S::SIDE;
-  const bool whole = st.lo == st.t0 && st.hi == st.t0 + KEYS;
-  if (!whole) {   // values no row sees must not reach the product: a weight of 0 does not silence a NaN
-    for (uint32_t r = lane; r < (uint32_t)KEYS; r += 32)
-      if (st.t0 + r < st.lo || st.t0 + r >= st.hi)
+    const uint32_t vb = kb + S::SIDE;
+    const bool whole = st.lo == st.t0 && st.hi == st.t0 + KEYS;
+    if (!whole) {   // values no row sees must not reach the product: a weight of 0 does not silence a NaN
+      for (uint32_t r = lane; r < (uint32_t)KEYS; r += 32)
+        if (st.t0 + r < st.lo || st.t0 + r >= st.hi)
 #pragma unroll
-        for (uint32_t x = 0; x < S::BLOCKS * 8; ++x)
-          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vb + (x / 8) * S::BLOCK_BYTES + r * 128 +
-                                                                    (x % 8) * 16),
-                       "r"(0u)
-                       : "memory");
-    __syncwarp();
-  }
-  float s[KEYS / 8][4];
-#pragma unroll
-  for (int i = 0; i < KEYS / 8; ++i)
-#pragma unroll
-    for (int z = 0; z < 4; ++z) s[i][z] = 0.f;
-#pragma unroll
-  for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-    for (int x = 0; x < KEYS / 16; ++x) {
-      const uint32_t r = x * 16 + (lane & 7) + ((lane >> 4) << 3), c = k * 2 + ((lane >> 3) & 1);
-      uint32_t b[4];
-      ldsm4(b, kb + (c / 8) * S::BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) * 16));
-      mma16<T>(s[2 * x], qf[k], b[0], b[1]);
-      mma16<T>(s[2 * x + 1], qf[k], b[2], b[3]);
+          for (uint32_t x = 0; x < S::BLOCKS * 8; ++x)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vb + (x / 8) * S::BLOCK_BYTES + r * 128 +
+                                                                      (x % 8) * 16),
+                         "r"(0u)
+                         : "memory");
+      __syncwarp();
     }
-  const bool all = whole && (st.sink || ((int64_t)st.t0 + KEYS - 1 <= q.first &&
-                                         (a.r.window == 0u || (int64_t)st.t0 > (q.first + q.n - 1) - (int64_t)a.r.window)));
-  float nm[2] = {m[0], m[1]};
+    float s[KEYS / 8][4];
 #pragma unroll
-  for (int x = 0; x < KEYS / 8; ++x)
+    for (int i = 0; i < KEYS / 8; ++i)
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      float y = s[x][z] * a.r.scale_log2;
-      if (!all) {
-        const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
-        if (j < st.lo || j >= st.hi || !sees(a.r, row_a[z >> 1], j)) y = -INFINITY;
+      for (int z = 0; z < 4; ++z) s[i][z] = 0.f;
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+      for (int x = 0; x < KEYS / 16; ++x) {
+        const uint32_t r = x * 16 + (lane & 7) + ((lane >> 4) << 3), c = k * 2 + ((lane >> 3) & 1);
+        uint32_t b[4];
+        ldsm4(b, kb + (c / 8) * S::BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) * 16));
+        mma16<T>(s[2 * x], qf[k], b[0], b[1]);
+        mma16<T>(s[2 * x + 1], qf[k], b[2], b[3]);
       }
-      s[x][z] = y;
-      nm[z >> 1] = fmaxf(nm[z >> 1], y);
-    }
-  float f[2], sub[2];
+    const bool all = whole && (st.sink || ((int64_t)st.t0 + KEYS - 1 <= q.first &&
+                                           (a.r.window == 0u || (int64_t)st.t0 > (q.first + q.n - 1) - (int64_t)a.r.window)));
+    float nm[2] = {m[0], m[1]};
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 1));
-    nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
-    const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
-    f[z] = ex2(m[z] - top);
-    sub[z] = top - WEIGHT_UP<T>;
-  }
-  if (__any_sync(0xffffffffu, nm[0] > m[0] || nm[1] > m[1])) {
+    for (int x = 0; x < KEYS / 8; ++x)
 #pragma unroll
-    for (int i = 0; i < DP / 8; ++i)
-#pragma unroll
-      for (int z = 0; z < 4; ++z) o[i][z] *= f[z >> 1];
+      for (int z = 0; z < 4; ++z) {
+        float y = s[x][z] * a.r.scale_log2;
+        if (!all) {
+          const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
+          if (j < st.lo || j >= st.hi || !sees(a.r, row_a[z >> 1], j)) y = -INFINITY;
+        }
+        s[x][z] = y;
+        nm[z >> 1] = fmaxf(nm[z >> 1], y);
+      }
+    float f[2], sub[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      l[z] *= f[z];
-      m[z] = nm[z];
+      nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 1));
+      nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
+      const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
+      f[z] = ex2(m[z] - top);
+      sub[z] = top - WEIGHT_UP<T>;
     }
-  }
-  uint32_t p[KEYS / 16][4];
+    if (__any_sync(0xffffffffu, nm[0] > m[0] || nm[1] > m[1])) {
 #pragma unroll
-  for (int x = 0; x < KEYS / 8; ++x) {
-    float e[4];
+      for (int i = 0; i < DP / 8; ++i)
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      e[z] = ex2(s[x][z] - sub[z >> 1]);
-      l[z >> 1] += e[z];
+        for (int z = 0; z < 4; ++z) o[i][z] *= f[z >> 1];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        l[z] *= f[z];
+        m[z] = nm[z];
+      }
     }
-    // rounded to the cache's type for the product with V; l sums what is not rounded
-    p[x / 2][(x & 1) * 2] = pack2<T>(e[0], e[1]);
-    p[x / 2][(x & 1) * 2 + 1] = pack2<T>(e[2], e[3]);
-  }
+    uint32_t p[KEYS / 16][4];
 #pragma unroll
-  for (int x = 0; x < KEYS / 16; ++x)
+    for (int x = 0; x < KEYS / 8; ++x) {
+      float e[4];
 #pragma unroll
-    for (int d = 0; d < DP / 16; ++d) {
-      const uint32_t r = x * 16 + (lane & 15), c = d * 2 + (lane >> 4);
-      uint32_t b[4];
-      ldsm4_t(b, vb + (c / 8) * S::BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) * 16));
-      mma16<T>(o[2 * d], p[x], b[0], b[1]);
-      mma16<T>(o[2 * d + 1], p[x], b[2], b[3]);
+      for (int z = 0; z < 4; ++z) {
+        e[z] = ex2(s[x][z] - sub[z >> 1]);
+        l[z >> 1] += e[z];
+      }
+      // rounded to the cache's type for the product with V; l sums what is not rounded
+      p[x / 2][(x & 1) * 2] = pack2<T>(e[0], e[1]);
+      p[x / 2][(x & 1) * 2 + 1] = pack2<T>(e[2], e[3]);
     }
-  if (!whole) fence_async_smem();   // (this warp's zeros lie in a stage that TMA writes next)
+#pragma unroll
+    for (int x = 0; x < KEYS / 16; ++x)
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) {
+        const uint32_t r = x * 16 + (lane & 15), c = d * 2 + (lane >> 4);
+        uint32_t b[4];
+        ldsm4_t(b, vb + (c / 8) * S::BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) * 16));
+        mma16<T>(o[2 * d], p[x], b[0], b[1]);
+        mma16<T>(o[2 * d + 1], p[x], b[2], b[3]);
+      }
+    if (!whole) fence_async_smem();   // (this warp's zeros lie in a stage that TMA writes next)
   }
   __device__ __forceinline__ void sum_rows() {
 #pragma unroll

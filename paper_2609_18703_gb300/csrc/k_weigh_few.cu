@@ -25,7 +25,7 @@ constexpr int WF_WARPS = 3, WF_THREADS = 32 * (WF_WARPS + 1);
 // tokens over up to 200 slots: 59 us against 103; 128 over 1,000 slots 47 against
 // 54; one of 100,000 slots 38 against 37).
 constexpr uint32_t WF_STAGES = 3, WF_STAGE = 16384;
-static_assert(WF_STAGES % WF_WARPS == 0, "a place of the ring belongs to one warp");
+static_assert(WF_STAGES == WF_WARPS, "a place of the ring belongs to one warp, and each has one");
 constexpr uint32_t WF_SMEM = 1024 + WF_STAGES * WF_STAGE;
 template <int DP>
 constexpr int wf_keys() {
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(WF_THREADS, 4) weigh_few_kernel(const __grid_c
     if (gap1 > gap0)
       decay_past<32 * WF_WARPS>(a, row, gap0 * KEYS, min(gap1 * KEYS, len), tid);   // (no new slot among them)
     for (uint32_t t = warp; t < n; t += WF_WARPS) {
-      const uint32_t round = t / WF_WARPS, rounds = WF_STAGES / WF_WARPS, slot = warp + WF_WARPS * (round % rounds);
+      const uint32_t round = t / WF_WARPS, slot = warp;
       const SlotTile st = slots.at(c0 + t);
       float past[KEYS / 32];   // under way while the keys arrive
 #pragma unroll
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(WF_THREADS, 4) weigh_few_kernel(const __grid_c
         const uint32_t j = st.t0 + i * 32 + lane;
         past[i] = a.past && j < st.hi && (int64_t)j < q.first ? a.past[row + j] : 0.f;
       }
-      bar_wait(b_full + 8 * slot, (round / rounds) & 1, &s_gave_up, a.err);
+      bar_wait(b_full + 8 * slot, round & 1, &s_gave_up, a.err);
       {
         const bool all = (int64_t)st.t0 + KEYS - 1 <= q.first && (r.window == 0u || (int64_t)st.t0 > a_max - (int64_t)r.window);
 #pragma unroll
