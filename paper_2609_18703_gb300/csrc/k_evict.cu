@@ -29,9 +29,9 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 }
 
 __device__ __forceinline__ uint32_t cached(const EvictArgs& a, uint32_t s, bool first) {
-  const uint64_t p0 = a.c.page_base[s], p1 = a.c.page_base[s + 1];
+  const uint64_t p0 = a.c.page_base[s], p1 = a.c.page_base[s + 1], end = a.c.page_base[a.c.n_seqs];
   uint32_t len = a.len[s];
-  if (p1 < p0 || p1 > a.c.page_base[a.c.n_seqs] || len >= 0x80000000u) {
+  if (p1 < p0 || p1 > end || len >= 0x80000000u) {
     if (first) record(a.err, ERR_INVAL);
     return 0;
   }
@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
   // have to read what the sequence held.  Whoever reads a length here after it is
   // cut keeps as much: a cut of a cut length changes nothing.
   if (h == 0 && part == 0 && threadIdx.x == 0) a.len_out[s] = kept;
-  const uint64_t b0 = a.dst_base[s], b1 = a.dst_base[s + 1], p0 = a.c.page_base[s];
-  const bool in_list = b0 <= b1 && b1 <= a.dst_base[a.c.n_seqs];
+  const uint64_t b0 = a.dst_base[s], b1 = a.dst_base[s + 1], end = a.dst_base[a.c.n_seqs], p0 = a.c.page_base[s];
+  const bool in_list = b0 <= b1 && b1 <= end;
   const uint64_t room = in_list ? (b1 - b0) * a.c.page_size : 0;
   const uint32_t n = (uint32_t)min((uint64_t)kept, room);
   if (n < kept && part == 0 && threadIdx.x == 0) record(a.err, in_list ? ERR_CAPACITY : ERR_INVAL);

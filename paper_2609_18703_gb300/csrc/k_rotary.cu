@@ -46,9 +46,10 @@ __global__ void __launch_bounds__(TURN_THREADS) turn_kernel(const __grid_constan
     uint64_t at = ~0ull;
     bool bad = s >= a.n_seqs, full = false;
     if (!bad) {
-      const uint64_t b0 = a.tok_base[s], b1 = a.tok_base[s + 1], p0 = a.page_base[s], p1 = a.page_base[s + 1];
+      const uint64_t b0 = a.tok_base[s], b1 = a.tok_base[s + 1], p0 = a.page_base[s], p1 = a.page_base[s + 1],
+                     end = a.page_base[a.n_seqs];
       const uint32_t len = a.len[s];
-      bad = t < b0 || t >= b1 || p1 < p0 || p1 > a.page_base[a.n_seqs] || len >= 0x80000000u;
+      bad = t < b0 || t >= b1 || p1 < p0 || p1 > end || len >= 0x80000000u;
       const int64_t slot = (int64_t)len - (int64_t)(b1 - b0) + (int64_t)(t - b0);
       if (!bad && slot >= 0) {
         const uint32_t pi = (uint32_t)slot / a.page_size;

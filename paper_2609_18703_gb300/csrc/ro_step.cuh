@@ -137,13 +137,15 @@ struct SeqInfo {
 // Checks what the GPU alone can see; a sequence that fails is left out (ok false).
 __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& c, const RowsArgs& r, uint32_t s, uint32_t* err) {
   SeqInfo q;
-  const uint64_t t0 = r.tok_base[s], t1 = r.tok_base[s + 1], p0 = c.page_base[s], p1 = c.page_base[s + 1];
+  // (all loads at once: a short-circuited one would wait for the others)
+  const uint64_t t0 = r.tok_base[s], t1 = r.tok_base[s + 1], p0 = c.page_base[s], p1 = c.page_base[s + 1],
+                 end = c.page_base[c.n_seqs];
   const uint32_t len = r.len[s];
   q.tok0 = t0;
   q.n = (uint32_t)(t1 - t0);
   q.len = len;
   q.page0 = p0;
-  q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && p1 <= c.page_base[c.n_seqs] &&
+  q.ok = t0 <= t1 && t1 <= r.n_tokens && t1 - t0 <= r.max_new && p0 <= p1 && p1 <= end &&
          len < 0x80000000u;
   if (!q.ok) {
     if ((threadIdx.x & 31u) == 0) record(err, ERR_INVAL);
