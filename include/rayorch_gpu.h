@@ -206,7 +206,8 @@ enum {
   RO_K_PB_HIST = 12, RO_K_PB_ROWSCAN = 13, RO_K_PB_SORT = 14, RO_K_PB_BOUNDS = 15,
   RO_K_PB_HEADS = 16, RO_K_PB_MARK = 17, RO_K_PB_SCAN = 18, RO_K_PB_EMIT = 19,
   RO_K_COMMIT_FIX = 20, RO_K_READY_FUSED = 21,
-  /* rayorch_cache.h */
+  /* rayorch_cache.h: the attention's kernels without tensor tiles are all
+   * ATTEND_ROWS, the weights' without and those behind a window WEIGH */
   RO_K_ROTARY = 22, RO_K_ATTEND_ROWS = 23, RO_K_ATTEND_TILES = 24, RO_K_WEIGH = 25,
   RO_K_WEIGH_TILES = 26, RO_K_EVICT_SELECT = 27, RO_K_EVICT_MOVE = 28,
   RO_K_ATTEND_JOIN = 29, RO_K_COUNT = 30

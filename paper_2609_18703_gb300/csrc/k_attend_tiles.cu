@@ -21,8 +21,8 @@
 // the slots are split into runs, whose (m, l, O) a second kernel joins in order.
 //
 // Measured: 8 ragged chunks of up to 2,048 tokens over up to 16,384 slots, 32
-// heads on 8 of 128: 415 us, 1.55 PFLOP/s (cuBLAS's burst: 1.95); 512 tokens over
-// 64,000 slots 303 us, 1.76 PFLOP/s.  A pair of products takes 2,050 cycles at the
+// heads on 8 of 128: 420 us, 1.54 PFLOP/s (cuBLAS's burst: 1.95); 512 tokens over
+// 64,000 slots 307 us, 1.74 PFLOP/s.  A pair of products takes 2,050 cycles at the
 // tensor cores' rate; a pair's cycle takes about 2,800, of which its softmax
 // is 1,400 (the maxima 500, the exponentials 900, 512 of them the XU's).
 #include <algorithm>

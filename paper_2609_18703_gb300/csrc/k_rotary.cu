@@ -4,7 +4,8 @@
 //   (x0, x1) -> (x0 cos - x1 sin, x1 cos + x0 sin),  theta negated turns back.
 // The frequency is held in 1/2^64 of a turn, so the 64-bit product with the
 // integer position is the angle modulo a turn, exactly: nothing is lost for
-// large positions, and the 32 bits that are used resolve 1.5e-9 radians.
+// large positions.  Its upper 32 bits become a float for the sine and cosine,
+// which errs by 9.4e-8 radians at most (near half a turn).
 //
 // Bound by memory: every element is read and written once.  A CTA takes a few
 // tokens, computes their R sines and cosines once in shared memory and turns
