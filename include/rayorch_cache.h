@@ -18,6 +18,15 @@
  *   ro_cache_weigh   the attention weight every cached token gathered
  *   ro_cache_evict   keeps each head's heaviest tokens, in fresh pages
  *
+ * and for steps that branch and answer:
+ *
+ *   ro_cache_attend_biased  attention with capped scores, a distance bias,
+ *                           document and prefix masks
+ *   ro_sample               tokens from logits and given random numbers
+ *   ro_cache_fork           sequences go on in any number of continuations
+ *   ro_cache_compact        the pages in use move to the low end of the pool
+ *   ro_cache_copy           the same copies of pages in another layer's pool
+ *
  * The conventions of rayorch_gpu.h hold: d_ pointers are device memory of the
  * context's GPU and are not kept; work is issued on the context's stream, in
  * call order, after the Calls' pending admissions; nothing waits on the host
@@ -189,6 +198,121 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
                          const float* d_score, uint64_t score_cap, uint32_t budget, uint32_t sinks,
                          uint32_t recent, const uint64_t* d_dst_base, const uint32_t* d_dst_pages,
                          uint32_t* d_keep, uint32_t* d_len_out, float* d_score_out);
+
+/* ------------------------------------------------------------------------
+ * ro_cache_attend_biased — attention whose scores are capped, fall with
+ * distance, or are masked by documents and prefixes.  With a = the slot of a
+ * new token t and x_j = scale * q.k_j:
+ *   cap > 0:   x_j becomes cap * tanh(x_j / cap);
+ *   d_slope:   then slope[query head] * |a - j| is taken off (finite slopes;
+ *              distances count slots);
+ *   d_first:   t sees no slot before d_first[t], the first one of its
+ *              document; sinks are the `sinks` slots from there on.  A token
+ *              whose d_first lies behind its own slot sees nothing (tokens
+ *              that only pad a chunk);
+ *   d_until:   t also sees the slots behind its own that lie before d_until[t]
+ *              (a prefix's or a frame's end; clipped to the sequence's length).
+ * So t sees slot j when first <= a, first <= j < max(a + 1, until) and
+ * window == 0, j > a - window, or j < first + sinks.  Everything else is
+ * ro_cache_attend's: arguments, outputs, empty rows (out 0, lse -inf), unseen
+ * slots never used, equal bits for equal calls.
+ * cap must be 0 or finite, at least 1e-6, with scale / cap at most 1e30.
+ */
+typedef struct {
+  float cap;                    /* 0: none */
+  const float* d_slope;         /* float[n_q_heads] or NULL (0) */
+  const uint32_t* d_first;      /* uint32[n_tokens] or NULL (0) */
+  const uint32_t* d_until;      /* uint32[n_tokens] or NULL (0) */
+} ro_bias;
+
+ro_status ro_cache_attend_biased(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_tok_base,
+                                 uint64_t n_tokens, uint32_t max_new, const uint32_t* d_len,
+                                 uint32_t max_len, const void* d_q, uint64_t q_tok, uint64_t q_head,
+                                 uint32_t n_q_heads, float scale, uint32_t window, uint32_t sinks,
+                                 const ro_bias* bias, void* d_out, uint64_t out_tok,
+                                 uint64_t out_head, float* d_lse);
+
+/* ------------------------------------------------------------------------
+ * Pages of a cache that several sequences share.  d_refs counts for every pool
+ * page how many entries of page lists name it (and whatever else holds it); a
+ * page with 0 is free.  Shared pages are full ones: a page that a sequence still
+ * writes is its own.
+ */
+/* Copies of pages: d_n[0] of them (at most cap), copy i the first d_slots[i]
+ * slots of pool page d_from[i] to page d_to[i]. */
+typedef struct {
+  uint32_t* d_from;             /* uint32[cap] */
+  uint32_t* d_to;               /* uint32[cap] */
+  uint32_t* d_slots;            /* uint32[cap] */
+  uint32_t* d_n;                /* uint32 (one) */
+  uint64_t cap;
+} ro_moves;
+
+/* A page list's entry for which the pool had no page. */
+#define RO_NO_PAGE 0xFFFFFFFFu
+
+/* ------------------------------------------------------------------------
+ * ro_cache_fork — sequences go on in their continuations: an expansion
+ * sequences -> continuations.  A sequence without any ends (its pages are
+ * released), one with one goes on, one with several is forked; continuations
+ * and their pages are the children of another expansion, continuations -> pages,
+ * and any of them may have more pages than its tokens fill (room to grow).
+ *   d_len        uint32[n_seqs]: tokens each sequence holds.
+ *   d_child_base uint64[n_seqs+1], d_child_parent uint32[n_children]: the
+ *                expansion sequences -> continuations (see ro_expand).
+ *   d_dst_base   uint64[n_children+1], d_dst_seq uint32[n_dst]: the expansion
+ *                continuations -> pages; n_dst its children.
+ *   d_refs       uint32[cache->n_pages] (see above).
+ *   d_refs_out   uint32[n_pages] out: with the old lists' entries taken off and
+ *                the new ones' added; may be d_refs.
+ *   d_dst_pages  uint32[n_dst] out: the continuations' page lists.  Pages full
+ *                of tokens are the parent's; so are the further ones for its
+ *                first continuation, where d_refs is 1; every other entry, in
+ *                order, gets the next page that is free in d_refs, lowest first.
+ *   d_len_out    uint32[n_children] out: tokens of each continuation, its
+ *                parent's (not d_len).
+ *   moves        out: the copies of open pages, parent to continuation, in
+ *                order; cap >= n_children.  The cache's pools are copied by this
+ *                call, those of other layers with ro_cache_copy.
+ * Recorded: RO_E_CAPACITY when the pool has too few free pages (those entries
+ * are RO_NO_PAGE, and not copied to) or a continuation's pages do not hold its
+ * parent's tokens; RO_E_INVAL for parents, pages and ranges out of bounds, and
+ * for a page whose d_refs is below its entries.
+ */
+ro_status ro_cache_fork(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_len,
+                        const uint64_t* d_child_base, const uint32_t* d_child_parent,
+                        uint64_t n_children, const uint64_t* d_dst_base, const uint32_t* d_dst_seq,
+                        uint64_t n_dst, uint32_t* d_dst_pages, uint32_t* d_len_out,
+                        const uint32_t* d_refs, uint32_t* d_refs_out, const ro_moves* moves);
+
+/* ------------------------------------------------------------------------
+ * ro_cache_compact — the U pages in use (d_refs > 0) move to the U lowest
+ * places: the k-th used page at or above U goes to the k-th free one below U.
+ *   d_pages_out  uint32[n_list] out: cache->d_pages with moved pages renamed;
+ *                may be d_pages.  n_list >= d_page_base[n_seqs], else
+ *                RO_E_CAPACITY is recorded and the rest is not written.
+ *   d_refs       uint32[n_pages]; d_refs_out uint32[n_pages] out, moved along
+ *                (0 from U on); may be d_refs.
+ *   d_n_used     uint32 out: U.
+ *   moves        out: the moves, ascending, of page_size slots each; cap at
+ *                least n_pages / 2.  The cache's pools are copied by this call,
+ *                those of other layers with ro_cache_copy.
+ * Recorded: RO_E_INVAL for a list's page that is out of bounds or free (it
+ * keeps its name).
+ */
+ro_status ro_cache_compact(ro_ctx* ctx, const ro_cache* cache, uint32_t* d_pages_out,
+                           uint64_t n_list, const uint32_t* d_refs, uint32_t* d_refs_out,
+                           uint32_t* d_n_used, const ro_moves* moves);
+
+/* ------------------------------------------------------------------------
+ * ro_cache_copy — copy pages within the cache's pools (k and v), for instance
+ * those of another layer after ro_cache_fork or ro_cache_compact.  No page that
+ * a copy writes may be read or written by another one.  Recorded: RO_E_INVAL for
+ * a page or a number of slots out of bounds (that copy is left out),
+ * RO_E_CAPACITY when d_n is above cap (cap copies are made).
+ * cache->d_page_base and d_pages are not read.
+ */
+ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* moves);
 
 #ifdef __cplusplus
 }

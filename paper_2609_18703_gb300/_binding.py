@@ -28,6 +28,8 @@ RO_ACCEPT, RO_REJ_INVALID, RO_REJ_NOT_INFLIGHT, RO_REJ_STALE_GEN, RO_REJ_DUPLICA
 
 # element types of the model-step operators
 RO_BF16, RO_F16, RO_F32 = range(3)
+# a page list's entry for which the pool had no page
+RO_NO_PAGE = 0xFFFFFFFF
 
 STATUS_NAMES = {0: "RO_OK", 1: "RO_E_INVAL", 2: "RO_E_CAPACITY", 3: "RO_E_OVERFLOW",
                 4: "RO_E_STATE", 5: "RO_E_OOM", 6: "RO_E_CUDA", 7: "RO_E_TIMEOUT"}
@@ -35,14 +37,15 @@ STATUS_NAMES = {0: "RO_OK", 1: "RO_E_INVAL", 2: "RO_E_CAPACITY", 3: "RO_E_OVERFL
 EXPORTS = ("ro_ctx_create", "ro_ctx_destroy", "ro_ctx_reset", "ro_ctx_sync", "ro_ctx_stats",
            "ro_ctx_set_streams", "ro_ctx_set_call_streams", "ro_ctx_join", "ro_ctx_selftest_timeout", "ro_last_error", "ro_ctx_profile", "ro_ctx_profile_read", "ro_expand", "ro_batch_ready",
            "ro_batch_ready_calls", "ro_retry", "ro_batch_ready_parent", "ro_gather_commit", "ro_assemble", "ro_assemble_list", "ro_filter_reports",
-           "ro_expand_noalloc", "ro_rotary", "ro_cache_append", "ro_cache_attend", "ro_cache_weigh", "ro_cache_evict")
+           "ro_expand_noalloc", "ro_rotary", "ro_cache_append", "ro_cache_attend", "ro_cache_weigh", "ro_cache_evict", "ro_cache_attend_biased", "ro_cache_fork",
+           "ro_cache_compact", "ro_cache_copy")
 
 # kernel ids (RO_K_*), in launch order of the path
 KERNELS = ("expand_scan", "expand_fill", "ready_count", "ready_scatter", "commit_scatter",
            "commit_plan", "asm_parents", "asm_members", "asm_copy", "retry_claim", "retry_scatter",
            "pb_keys", "pb_hist", "pb_rowscan", "pb_sort", "pb_bounds", "pb_heads", "pb_mark",
            "pb_scan", "pb_emit", "commit_fix", "ready_fused", "rotary", "attend_rows", "attend_tiles",
-           "weigh", "weigh_tiles", "evict_select", "evict_move", "attend_join")
+           "weigh", "weigh_tiles", "evict_select", "evict_move", "attend_join", "pages")
 
 
 class RoError(RuntimeError):
@@ -90,6 +93,36 @@ class ro_cache(C.Structure):
         self._tensors = (d_k, d_v, d_page_base, d_pages)
         self._kind = (d_k.dtype, dim)             # what rows beside the cache must be
         self._units = (d_page_base.numel() - 1, heads)
+        self._ref = C.byref(self)
+
+
+class ro_bias(C.Structure):
+    """What biased attention adds to the scores (see the header): a cap, each
+    query head's slope (32-bit floats), each new token's first slot and the slot
+    its prefix ends before (32-bit integers).  Keeps the tensors alive."""
+    _fields_ = [("cap", C.c_float), ("d_slope", C.c_void_p), ("d_first", C.c_void_p), ("d_until", C.c_void_p)]
+
+    def __init__(self, cap: float = 0.0, d_slope=None, d_first=None, d_until=None):
+        super().__init__(float(cap), _list(d_slope, _F32), _list(d_first, _I32), _list(d_until, _I32))
+        self._tensors = (d_slope, d_first, d_until)
+        self._ref = C.byref(self)
+
+    def _check(self, heads, tokens):
+        for x, n in zip(self._tensors, (heads, tokens, tokens)):
+            if x is not None and not isinstance(x, int) and x.numel() < n:
+                raise ValueError(f"ro_bias: an array has {x.numel()} elements where {n} are read")
+
+
+class ro_moves(C.Structure):
+    """Copies of pages: source, target and slots of each (32-bit integers, alike
+    in number) and their count d_n.  Keeps the tensors alive."""
+    _fields_ = [("d_from", C.c_void_p), ("d_to", C.c_void_p), ("d_slots", C.c_void_p), ("d_n", C.c_void_p),
+                ("cap", C.c_uint64)]
+
+    def __init__(self, d_from, d_to, d_slots, d_n):
+        cap = min(x.numel() for x in (d_from, d_to, d_slots))
+        super().__init__(_list(d_from, _I32), _list(d_to, _I32), _list(d_slots, _I32), _list(d_n, _I32, 1), cap)
+        self._tensors = (d_from, d_to, d_slots, d_n)
         self._ref = C.byref(self)
 
 
@@ -146,8 +179,14 @@ def load(path: Optional[str] = None):
     L.ro_cache_append.argtypes = [_vp, cache, _vp, _vp, _u64, _vp, _vp, rope] + rows + [_vp, _u64, _u64] * 3
     L.ro_cache_attend.argtypes = [_vp, cache, _vp, _u64, _u32, _vp, _u32] + rows + [f32, _u32, _u32, _vp, _u64, _u64,
                                                                                  _vp]
+    L.ro_cache_attend_biased.argtypes = ([_vp, cache, _vp, _u64, _u32, _vp, _u32] + rows +
+                                         [f32, _u32, _u32, C.POINTER(ro_bias), _vp, _u64, _u64, _vp])
     L.ro_cache_weigh.argtypes = [_vp, cache, _vp, _u64, _u32, _vp] + rows + [f32, _u32, _u32, _vp, f32, _vp, _vp, _u64]
     L.ro_cache_evict.argtypes = [_vp, cache, _vp, _vp, _u64, _u32, _u32, _u32, _vp, _vp, _vp, _vp, _vp]
+    moves = C.POINTER(ro_moves)
+    L.ro_cache_fork.argtypes = [_vp, cache, _vp, _vp, _vp, _u64, _vp, _vp, _u64, _vp, _vp, _vp, _vp, moves]
+    L.ro_cache_compact.argtypes = [_vp, cache, _vp, _u64, _vp, _vp, _vp, moves]
+    L.ro_cache_copy.argtypes = [_vp, cache, moves]
     for f in EXPORTS:
         if f != "ro_last_error":
             getattr(L, f).restype = C.c_int32
@@ -461,6 +500,19 @@ def ro_cache_attend(ctx, cache, d_tok_base, max_new, d_len, max_len, d_q, scale,
                                             window, sinks, *_rows(d_out, dtype), _list(d_lse, _F32))
 
 
+def ro_cache_attend_biased(ctx, cache, d_tok_base, max_new, d_len, max_len, d_q, scale, window, sinks, bias, d_out,
+                           d_lse=None) -> int:
+    """Attention whose scores are capped, fall with distance, or are masked by documents and prefixes."""
+    (dtype, dim), shape, seqs = cache._kind, d_q.shape, cache._units[0]
+    if d_out.shape != shape or shape[-1] != dim or (d_lse is not None and d_lse.shape != shape[:2]):
+        raise ValueError("ro_cache_attend_biased: q, out and lse do not fit one another")
+    bias._check(shape[1], shape[0])
+    return (_lib or load()).ro_cache_attend_biased(ctx, cache._ref, _list(d_tok_base, _I64, seqs + 1), shape[0], max_new,
+                                                   _list(d_len, _I32, seqs), max_len, *_rows(d_q, dtype), shape[1],
+                                                   scale, window, sinks, bias._ref, *_rows(d_out, dtype),
+                                                   _list(d_lse, _F32))
+
+
 def ro_cache_weigh(ctx, cache, d_tok_base, max_new, d_len, d_q, scale, window, sinks, d_lse, decay, d_past,
                    d_score) -> int:
     """Attention weight per cached token, d_score [sequences, heads, slots] from
@@ -487,3 +539,31 @@ def ro_cache_evict(ctx, cache, d_len, d_score, budget, sinks, recent, d_dst_base
                                            slots[2], budget, sinks, recent, _list(d_dst_base, _I64), _list(d_dst_pages, _I32),
                                            _list(d_keep, _I32), _list(d_len_out, _I32, units[0]),
                                            _list(d_score_out, _F32))
+
+
+def ro_cache_fork(ctx, cache, d_len, d_child_base, d_child_parent, d_dst_base, d_dst_seq, d_dst_pages, d_len_out, d_refs,
+                  d_refs_out, moves) -> int:
+    """Sequences go on in their continuations, whose page lists are d_dst_pages."""
+    seqs, pages, kids, n = cache._units[0], cache.n_pages, d_child_parent.numel(), d_dst_seq.numel()
+    if moves.cap < kids:
+        raise ValueError("ro_cache_fork: fewer moves than continuations")
+    return (_lib or load()).ro_cache_fork(ctx, cache._ref, _list(d_len, _I32, seqs), _list(d_child_base, _I64, seqs + 1),
+                                          _list(d_child_parent, _I32), kids, _list(d_dst_base, _I64, kids + 1),
+                                          _list(d_dst_seq, _I32), n, _list(d_dst_pages, _I32, n),
+                                          _list(d_len_out, _I32, kids), _list(d_refs, _I32, pages),
+                                          _list(d_refs_out, _I32, pages), moves._ref)
+
+
+def ro_cache_compact(ctx, cache, d_pages_out, d_refs, d_refs_out, d_n_used, moves) -> int:
+    """The pages in use move to the low end of the pool; lists and counts follow."""
+    pages = cache.n_pages
+    if moves.cap < pages // 2:
+        raise ValueError("ro_cache_compact: fewer moves than half the pages")
+    return (_lib or load()).ro_cache_compact(ctx, cache._ref, _list(d_pages_out, _I32), d_pages_out.numel(),
+                                             _list(d_refs, _I32, pages), _list(d_refs_out, _I32, pages),
+                                             _list(d_n_used, _I32, 1), moves._ref)
+
+
+def ro_cache_copy(ctx, cache, moves) -> int:
+    """Copy pages within the cache's pools, for instance another layer's after ro_cache_fork."""
+    return (_lib or load()).ro_cache_copy(ctx, cache._ref, moves._ref)

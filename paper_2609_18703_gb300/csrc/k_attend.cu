@@ -28,7 +28,7 @@ constexpr size_t attend_rows_smem() {
   return (size_t)AR_STAGES * 2 * AR_KEYS * DP * 2;
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool BIASED>
 __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int KW = AR_KEYS, ROWS = AR_ROWS;
   constexpr int CH = DP / 8;                         // 16-byte pieces of a row
@@ -57,7 +57,12 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
   const uint32_t i0 = s_part * toks, i1 = min(q.n, i0 + toks);
   if (i0 >= i1) return;
   const uint32_t rows = (i1 - i0) * gn;
-  const KeySpan ks = key_span(q, a.r, i0, i1);
+  const auto ks = [&] {
+    if constexpr (BIASED)
+      return bias_span(q, a.r, a.b, i0, i1);
+    else
+      return key_span(q, a.r, i0, i1);
+  }();
   // runs of `chunk` keys, longer ones where max_chunks of them would not reach
   const uint32_t chunk = max(a.chunk, (ks.total / a.max_chunks / AR_KEYS + 1) * AR_KEYS);
   const uint32_t n_chunks = max(1u, (ks.total + chunk - 1) / chunk);
@@ -74,7 +79,10 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
   auto row_at = [&](uint32_t u) -> uint64_t {
     if (u >= u1) return ~0ull;
     uint32_t pi, slot;
-    split_slot(a.c, ks.slot(u), &pi, &slot);
+    const uint32_t j = ks.slot(u);
+    if constexpr (BIASED)
+      if (!somebody_sees(q, a.r, a.b, ks.holes, ks.s_lo + ks.s_n, i0, i1, j)) return ~0ull;
+    split_slot(a.c, j, &pi, &slot);
     const uint32_t page = a.c.pages[q.page0 + pi];
     if (page >= a.c.n_pages) {
       record(a.err, ERR_INVAL);
@@ -112,6 +120,8 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
   // queries as matrix fragments; rows past the tile's are zero
   uint32_t qf[DP / 16][4];
   int64_t row_a[2];
+  RowSee see[2] = {};          // biased: what the rows see, their slopes
+  float slope[2] = {0.f, 0.f};
   {
     const T* qp[2];
 #pragma unroll
@@ -123,6 +133,10 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
         const uint32_t i = i0 + r / gn, g = g0 + r % gn;
         qp[z] = (const T*)a.r.q + (q.tok0 + i) * a.r.q_tok + (uint64_t)(kh * G + g) * a.r.q_head;
         row_a[z] = q.first + i;
+        if constexpr (BIASED) {
+          see[z] = row_see(q, a.r, a.b, i);
+          slope[z] = a.b.slope ? a.b.slope[kh * G + g] * LOG2E : 0.f;
+        }
       }
     }
 #pragma unroll
@@ -171,16 +185,24 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
     // what each row sees of these keys
     const uint32_t ub = u0 + step * AR_KEYS;
     const uint32_t j_lo = ks.slot(ub), j_hi = ks.slot(min(ub + AR_KEYS, u1) - 1);
-    const bool all = ub + AR_KEYS <= u1 && (int64_t)j_hi <= a_min &&
-                     (a.r.window == 0u || (int64_t)j_lo > a_max - (int64_t)a.r.window);
+    bool all = ub + AR_KEYS <= u1;
+    if constexpr (BIASED)
+      all = all && ks.holes == 0u && j_lo >= ks.all_lo && j_hi < ks.all_hi;
+    else
+      all = all && (int64_t)j_hi <= a_min && (a.r.window == 0u || (int64_t)j_lo > a_max - (int64_t)a.r.window);
 #pragma unroll
     for (int n = 0; n < KW / 8; ++n)
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
-        float x = s[n][z] * a.r.scale_log2;
-        if (!all) {
-          const uint32_t u = ub + n * 8 + (lane & 3) * 2 + (z & 1);
-          if (u >= u1 || !sees(a.r, row_a[z >> 1], ks.slot(u))) x = -INFINITY;
+        const uint32_t u = ub + n * 8 + (lane & 3) * 2 + (z & 1);
+        float x;
+        if constexpr (BIASED) {
+          const uint32_t j = ks.slot(u);
+          x = biased_score(a.b, a.r.scale_log2, s[n][z], slope[z >> 1], fabsf((float)(row_a[z >> 1] - (int64_t)j)));
+          if (!all && (u >= u1 || !see[z >> 1].sees(j))) x = -INFINITY;
+        } else {
+          x = s[n][z] * a.r.scale_log2;
+          if (!all && (u >= u1 || !sees(a.r, row_a[z >> 1], ks.slot(u)))) x = -INFINITY;
         }
         s[n][z] = x;
       }
@@ -298,8 +320,8 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
 
 template <typename T, int DP>
 static void launch_rows(const LaunchCfg& L, const AttendArgs& a) {
-  launch_k(L, K_ATTEND_ROWS, attend_rows_kernel<T, DP>, dim3(a.tiles * a.c.n_heads, a.max_chunks), AR_THREADS,
-           attend_rows_smem<DP>(), a);
+  launch_k(L, K_ATTEND_ROWS, a.biased ? attend_rows_kernel<T, DP, true> : attend_rows_kernel<T, DP, false>,
+           dim3(a.tiles * a.c.n_heads, a.max_chunks), AR_THREADS, attend_rows_smem<DP>(), a);
 }
 void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype) {
   const bool narrow = a.c.head_dim <= 64;
@@ -311,8 +333,12 @@ void launch_attend_rows(const LaunchCfg& L, const AttendArgs& a, int dtype) {
 
 template <typename T, int DP>
 static cudaError_t allow() {
-  return cudaFuncSetAttribute(attend_rows_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)attend_rows_smem<DP>());
+  const int bytes = (int)attend_rows_smem<DP>();
+  const cudaError_t e =
+      cudaFuncSetAttribute(attend_rows_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e != cudaSuccess
+             ? e
+             : cudaFuncSetAttribute(attend_rows_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 cudaError_t prepare_attend_kernels() {
   for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})

@@ -8,7 +8,7 @@
 
 namespace ro {
 
-constexpr float LN2 = 0.69314718055994530942f;
+constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
 __device__ __forceinline__ uint32_t step_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void record(uint32_t* err, uint32_t bit) { atomicOr(err, bit); }
@@ -94,6 +94,17 @@ __device__ __forceinline__ float row_lse(float m, float l) {
 // infinite or NaN only where its are.  (Rows of zeros would make NaN of a key
 // with an infinity, whose own weight is 0.)
 constexpr float LSE_FILL = 1e38f;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // ---- clusters ------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -188,6 +199,121 @@ __device__ __forceinline__ KeySpan key_span(const SeqInfo& q, const RowsArgs& r,
 }
 __device__ __forceinline__ bool sees(const RowsArgs& r, int64_t a, uint32_t j) {
   return (int64_t)j <= a && (r.window == 0u || (int64_t)j > a - (int64_t)r.window || j < r.sinks);
+}
+
+// ---- biased attention: what a token sees, and its scores ---------------------------------
+// A token sees the slots [a0, a1) (its document's first ones, behind a window)
+// and [c0, c1).  Its own slot is one of the latter unless it sees nothing.
+struct RowSee {
+  uint32_t a0, a1, c0, c1;
+  __device__ __forceinline__ bool sees(uint32_t j) const { return (j >= c0 && j < c1) || (j >= a0 && j < a1); }
+  __device__ __forceinline__ bool some() const { return c1 > c0 || a1 > a0; }
+};
+__device__ __forceinline__ RowSee row_see(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t i) {
+  RowSee s = {0, 0, 0, 0};
+  const int64_t a = q.first + i;
+  const uint32_t first = b.first ? b.first[q.tok0 + i] : 0u, until = b.until ? b.until[q.tok0 + i] : 0u;
+  if (a < 0 || (int64_t)first > a) return s;
+  s.c1 = (uint32_t)min((int64_t)q.len, max(a + 1, (int64_t)until));
+  s.a0 = min(first, s.c1);
+  s.c0 = r.window ? (uint32_t)max((int64_t)first, a - (int64_t)r.window + 1) : first;
+  s.c0 = min(s.c0, s.c1);
+  s.a1 = min(s.c0, first + r.sinks);   // (both below 2^31)
+  return s;
+}
+// What a tile of tokens sees together, numbered without the gap: the slots
+// [s_lo, s_lo + s_n) and [lo, lo + total - s_n).  Consecutive tokens see their
+// own slots and what lies before them in one piece, so every slot of it is seen
+// by one of them, except slots of tokens that see nothing and, where documents
+// lie in one another, slots behind the first document's sinks (holes).
+// Every token sees all of [all_lo, all_hi), except those that see nothing.
+struct BiasSpan {
+  uint32_t s_lo, s_n, lo, total;
+  uint32_t all_lo, all_hi;
+  uint32_t holes;              // 1: some tokens see nothing; 2: sinks of several documents
+  __device__ __forceinline__ uint32_t slot(uint32_t u) const { return u < s_n ? s_lo + u : lo + (u - s_n); }
+};
+// a whole warp, the tokens [i0, i1) of a sequence
+__device__ __forceinline__ BiasSpan bias_span(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t i0,
+                                              uint32_t i1) {
+  const uint32_t lane = threadIdx.x & 31u;
+  BiasSpan k;
+  uint32_t lo = ~0u, hi = 0, all_lo = 0, all_hi = ~0u, none = 0;
+  for (uint32_t i = i0 + lane; i < i1; i += 32) {
+    const RowSee s = row_see(q, r, b, i);
+    if (!s.some()) {
+      none = 1;
+      continue;
+    }
+    lo = min(lo, s.c0);
+    hi = max(hi, s.c1);
+    all_lo = max(all_lo, s.c0);
+    all_hi = min(all_hi, s.c1);
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  k.all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+  k.all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+  k.holes = __reduce_or_sync(0xffffffffu, none);
+  k.s_lo = k.s_n = 0;
+  if (lo > hi) lo = hi;        // nobody sees anything
+  if (r.window != 0u && r.sinks != 0u) {
+    uint32_t s_lo = ~0u, s_top = 0, s_hi = 0;
+    for (uint32_t i = i0 + lane; i < i1; i += 32) {
+      const RowSee s = row_see(q, r, b, i);
+      if (s.a0 >= s.a1 || s.a0 >= lo) continue;
+      s_lo = min(s_lo, s.a0);
+      s_top = max(s_top, s.a0);
+      s_hi = max(s_hi, s.a1);
+    }
+    s_lo = __reduce_min_sync(0xffffffffu, s_lo);
+    s_top = __reduce_max_sync(0xffffffffu, s_top);
+    s_hi = min(lo, __reduce_max_sync(0xffffffffu, s_hi));
+    if (s_lo < s_hi) {
+      k.s_lo = s_lo;
+      k.s_n = s_hi - s_lo;
+      if (s_top > s_lo) k.holes |= 2u;
+    }
+  }
+  k.lo = lo;
+  k.total = k.s_n + (hi - lo);
+  return k;
+}
+// Whether one of the tokens [i0, i1) sees slot j of their span.
+__device__ __forceinline__ bool somebody_sees(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t holes,
+                                              uint32_t s_end, uint32_t i0, uint32_t i1, uint32_t j) {
+  if (holes == 0u) return true;
+  if ((holes & 2u) == 0u || j >= s_end) {   // then only slots of tokens that see nothing are in question
+    const int64_t i = (int64_t)j - q.first;
+    if (i < (int64_t)i0 || i >= (int64_t)i1 || row_see(q, r, b, (uint32_t)i).some()) return true;
+  }
+  for (uint32_t i = i0; i < i1; ++i)
+    if (row_see(q, r, b, i).sees(j)) return true;
+  return false;
+}
+
+// tanh(z) within 2^-22 of its value: a polynomial of z^2 fitted to tanh(z) / z
+// for |z| <= 1 (3.7e-9 off), and 1 - 2 / (1 + e^2z) beyond, where nothing cancels.
+constexpr float TANH_C1 = -0.3333328366279602f, TANH_C2 = 0.13332240283489227f, TANH_C3 = -0.05387570336461067f,
+                TANH_C4 = 0.02147844433784485f, TANH_C5 = -0.007937350310385227f, TANH_C6 = 0.002296661725267768f,
+                TANH_C7 = -0.00035745822242461145f;
+__device__ __forceinline__ float tanh_of(float z) {
+  const float w = z * z;
+  float p = TANH_C7;
+  p = fmaf(p, w, TANH_C6);
+  p = fmaf(p, w, TANH_C5);
+  p = fmaf(p, w, TANH_C4);
+  p = fmaf(p, w, TANH_C3);
+  p = fmaf(p, w, TANH_C2);
+  p = fmaf(p, w, TANH_C1);
+  p = fmaf(p, w, 1.f);
+  const float far = fmaf(-2.f, rcp(1.f + ex2(z * 2.885390081777927f)), 1.f);
+  return w <= 1.f ? z * p : far;
+}
+// A product q.k's score in log2, `apart` slots from the token; slope in log2.
+__device__ __forceinline__ float biased_score(const BiasArgs& b, float scale_log2, float dot, float slope, float apart) {
+  const float x = b.cap_log2 != 0.f ? b.cap_log2 * tanh_of(dot * b.to_z) : dot * scale_log2;
+  return fmaf(-slope, apart, x);
 }
 
 // The slots that a CTA's rows see, cut into tiles of KEYS: tiles over the

@@ -32,7 +32,7 @@ class StepCall {
   int prev_ = -1;
 };
 // (SS_COUNTER is zero between calls, whichever kernel used it last)
-enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_JOIN = 2, SS_COUNT };
+enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_JOIN = 2, SS_PAGES = 3, SS_COUNT };
 
 // ---- rotary, append -----------------------------------------------------------------
 constexpr uint32_t ROPE_MAX_PAIRS = 128;
@@ -93,9 +93,19 @@ struct RowsArgs {             // the step's query rows
   uint32_t window, sinks;
   float scale_log2;          // scale * log2(e)
 };
+// ro_cache_attend_biased: x = cap tanh(scale q.k / cap) - slope |a - j|, in log2.
+struct BiasArgs {
+  float cap_log2;            // cap * log2(e); 0: none
+  float to_z;                // scale / cap
+  const float* slope;        // optional
+  const uint32_t* first;     // optional
+  const uint32_t* until;     // optional
+};
 struct AttendArgs {
   PagedArgs c;
   RowsArgs r;
+  BiasArgs b;                // of use where biased
+  uint32_t biased;
   uint32_t tiles;            // row tiles per cache head, at most
   uint32_t pairs;            // attend_tiles: (pair of row tiles, head) that there can be
   uint32_t chunk;            // of one CTA, more where max_chunks would not reach: keys
@@ -180,5 +190,54 @@ struct EvictArgs {
 };
 void launch_evict(const LaunchCfg& L, const EvictArgs& a, int sms);
 cudaError_t prepare_evict_kernels();
+
+// ---- fork, compact, copy --------------------------------------------------------------
+constexpr int PG_THREADS = 1024;
+constexpr uint32_t PG_WARPS = PG_THREADS / 32;
+// A warp counts what its run of the lists and of the pool holds.
+struct __align__(16) PageCounts {
+  uint32_t fresh, moves, free, pad;
+};
+struct MoveArgs {
+  uint32_t* from;
+  uint32_t* to;
+  uint32_t* slots;
+  uint32_t* n;
+  uint64_t cap;
+};
+struct PagesArgs {
+  PagedArgs c;
+  MoveArgs m;
+  const uint32_t* refs;
+  uint32_t* refs_out;
+  PageCounts* counts;        // [gridDim][PG_WARPS]
+  uint32_t* list;            // [n_pages]: fork: free pages by rank; compact: a late page's rank;
+                             // then the pool's flags, 32 pages a word
+  // fork
+  const uint32_t* len;
+  const uint64_t* child_base;
+  const uint32_t* child_parent;
+  const uint64_t* dst_base;
+  const uint32_t* dst_seq;
+  uint32_t* dst_pages;
+  uint32_t* len_out;
+  uint64_t n_children, n_dst;
+  // compact
+  uint32_t* pages_out;
+  uint64_t n_list;
+  uint32_t* n_used;
+  uint32_t* err;
+};
+uint32_t pages_ctas(uint64_t items, int sms);
+void launch_fork(const LaunchCfg& L, const PagesArgs& a, uint32_t ctas);
+void launch_compact(const LaunchCfg& L, const PagesArgs& a, uint32_t ctas);
+struct PageCopyArgs {
+  PagedArgs c;
+  MoveArgs m;
+  uint32_t pieces;           // 4 KB pieces of a page's head
+  uint32_t dense;            // a head's slots follow one another
+  uint32_t* err;
+};
+void launch_page_copy(const LaunchCfg& L, const PagedArgs& c, const MoveArgs& m, uint32_t* err, int sms);
 
 }  // namespace ro

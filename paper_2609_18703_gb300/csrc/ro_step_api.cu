@@ -148,6 +148,166 @@ RowsArgs rows_of(const uint64_t* tok_base, const uint32_t* len, uint64_t n_token
   return r;
 }
 
+ro_status check_moves(StepCall& c, const char* fn, const ro_moves* m, uint64_t least, MoveArgs* out) {
+  if (!m || !m->d_n || (m->cap && (!m->d_from || !m->d_to || !m->d_slots))) return c.refuse(RO_E_INVAL, "%s: NULL in the moves", fn);
+  if (m->cap < least) return c.refuse(RO_E_INVAL, "%s: room for %llu moves, %llu can be needed", fn, (unsigned long long)m->cap,
+                                      (unsigned long long)least);
+  if (m->cap >= 0x80000000ull) return c.refuse(RO_E_OVERFLOW, "%s: 2^31 moves or more", fn);
+  *out = {m->d_from, m->d_to, m->d_slots, m->d_n, m->cap};
+  return RO_OK;
+}
+// ranges of bytes that share one
+bool touch(const void* p, uint64_t p_bytes, const void* q, uint64_t q_bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p_bytes && q_bytes && a < b + q_bytes && b < a + p_bytes;
+}
+// Flags, ranks and counts of a plan over the pool's pages.
+ro_status plan_scratch(StepCall& c, uint64_t items, PagesArgs* a, uint32_t* ctas) {
+  *ctas = pages_ctas(items, c.sms());
+  const uint64_t counts = (uint64_t)*ctas * PG_WARPS, pages = a->c.n_pages;
+  void* p = nullptr;
+  RO_TRY(c.scratch(SS_PAGES, counts * sizeof(PageCounts) + (pages + ceil_div(pages, 32)) * sizeof(uint32_t), &p));
+  a->counts = (PageCounts*)p;
+  a->list = (uint32_t*)(a->counts + counts);
+  return RO_OK;
+}
+
+// ro_cache_attend and, with a bias, ro_cache_attend_biased
+ro_status attend(const char* fn, StepCall& c, const ro_cache* cache, const uint64_t* d_tok_base, uint64_t n_tokens,
+                 uint32_t max_new, const uint32_t* d_len, uint32_t max_len, const void* d_q, uint64_t q_tok,
+                 uint64_t q_head, uint32_t n_q_heads, float scale, uint32_t window, uint32_t sinks,
+                 const ro_bias* bias, void* d_out, uint64_t out_tok, uint64_t out_head, float* d_lse) {
+  RO_TRY(check_cache(c, fn, cache));
+  RO_TRY(check_rows(c, fn, cache, d_tok_base, n_tokens, d_len, d_q, q_tok, q_head, n_q_heads, scale));
+  if (n_tokens && !d_out) return c.refuse(RO_E_INVAL, "%s: NULL output", fn);
+  if (!aligned(d_out, 16) || out_tok % 8 || out_head % 8)
+    return c.refuse(RO_E_INVAL, "%s: the output wants a 16-byte pointer and strides of 8 elements", fn);
+  if (bias) {
+    if (!(bias->cap == 0.f || (bias->cap >= 1e-6f && std::isfinite(bias->cap) && std::fabs(scale / bias->cap) <= 1e30f)))
+      return c.refuse(RO_E_INVAL, "%s: cap must be 0 or finite, at least 1e-6, and scale / cap at most 1e30", fn);
+    if (!aligned(bias->d_slope, 4) || !aligned(bias->d_first, 4) || !aligned(bias->d_until, 4))
+      return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
+  }
+  if (n_tokens == 0) return RO_OK;
+  if (d_out == d_q) return c.refuse(RO_E_INVAL, "%s: the output cannot be q", fn);
+  RO_TRY(c.begin());
+  AttendArgs a = {};
+  a.c = paged(cache);
+  const uint32_t group = n_q_heads / cache->n_heads;
+  a.r = rows_of(d_tok_base, d_len, n_tokens, max_new, group, d_q, q_tok, q_head, window, sinks, scale);
+  a.out = d_out;
+  a.out_tok = out_tok;
+  a.out_head = out_head;
+  a.lse = d_lse;
+  a.n_q_heads = n_q_heads;
+  a.err = c.err();
+  if (bias) {
+    a.biased = 1;
+    a.b.cap_log2 = bias->cap * 1.44269504088896340736f;
+    a.b.to_z = bias->cap != 0.f ? scale / bias->cap : 0.f;
+    a.b.slope = bias->d_slope;
+    a.b.first = bias->d_first;
+    a.b.until = bias->d_until;
+  }
+  uint64_t keys = max_len ? max_len : 0x7FFFFFFFu;
+  keys = std::min<uint64_t>(keys, (uint64_t)cache->n_pages * cache->page_size);
+  if (a.r.window) keys = std::min<uint64_t>(keys, (uint64_t)a.r.window + a.r.sinks + a.r.max_new);
+  keys = std::max<uint64_t>(keys, 1);
+  const uint64_t max_rows = (uint64_t)a.r.max_new * group;
+  void* p = nullptr;
+  // At most 16 rows a sequence: bound by the cache's bytes.
+  if (max_rows <= 16 && !bias) {
+    const uint64_t work = (uint64_t)cache->n_seqs * cache->n_heads, stage = attend_few_keys(cache->head_dim);
+    if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many sequences and heads", fn);
+    a.tiles = cache->n_seqs;
+    // Runs that fill two CTAs an SM in whole rounds, of at most 96 stages of
+    // 16 KB (longer ones leave SMs idle at the end where lengths differ) and
+    // at least 3, one for each warp (shorter ones cost more than they
+    // save).  One sequence of 777 slots, 4 heads of 64: 7.2 us at 3 stages, 9.1
+    // at 8, 7.8 at 2; of 100,000 slots, 8 heads of 128: 70 us in one round, 84 in
+    // two; 64 ragged sequences of up to 32,000 slots: 432 us at 96 stages, 476 at
+    // 32, 565 at 16.
+    const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
+    const uint64_t each = ceil_div(stages * work, places);
+    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 96)));
+    a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk),
+                                                std::min<uint64_t>(1024, std::max<uint64_t>(1, MAX_FEW_RUNS / work)));
+    // Up to eight runs that the GPU holds at once are a cluster and join in
+    // shared memory; more go through L2 and a ticket.
+    const bool cluster = a.max_chunks > 1 && a.max_chunks <= 8 && work * a.max_chunks <= places;
+    if (a.max_chunks > 1 && !cluster) {
+      RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));
+      a.partial = (float*)p;
+      RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
+      a.counter = (uint32_t*)p;
+    }
+    // Many short sequences: a warp alone for each (sequence, head), where its
+    // stages one after another, about 1 us for 8 KB, take less than the rounds
+    // of larger CTAs, about 6 us each.  2,048 of 40 slots of 128: 13 us against
+    // 41, of 300: 55 against 79; 5,600 of up to 150: 42 against 110.  On either
+    // side of the rule: 1,024 of up to 300 slots 23.4 against 24.4, of up to 600
+    // 44 against 32.
+    const bool alone = a.max_chunks == 1 && work > places && ceil_div(keys, attend_short_keys(cache->head_dim)) * places <= 5 * work;
+    launch_attend_few(c.launch(), a, cache->dtype, cluster, alone);
+    return c.launched(fn);
+  }
+  // More: the tensor-core kernel, if the pages and the group fit its tiles.
+  if (!bias && attend_tiles_fits(a)) {
+    const uint32_t toks = attend_tile_tokens(group);
+    const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
+    const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
+    if (work > MAX_GRID / 256) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
+    a.tiles = (uint32_t)tiles;
+    // One CTA an SM takes pairs of row tiles in turn.  Where that is few rounds,
+    // split the slots into the number of runs that takes the least time: rounds
+    // of runs, each its tiles of slots plus about 6 tiles' time of its own.
+    // (512 new tokens over 64,000 slots: 327 us in 2 runs, 311 in 7, 611 unsplit;
+    // 64 over 32,000: 38 us in 16 runs, 53 in 8, 319 unsplit.)
+    const uint64_t sms = (uint64_t)c.sms();
+    const uint64_t pairs = std::min<uint64_t>(work, (uint64_t)cache->n_seqs * ceil_div(a.r.max_new, toks) * cache->n_heads);
+    uint64_t runs = 1, least = ~0ull;
+    for (uint64_t k = 1; k == 1 || (k <= 32 && pairs < 4 * sms && pairs * k <= MAX_RUNS); ++k) {
+      const uint64_t each = ceil_div(slots, k), time = ceil_div(pairs * ceil_div(slots, each), sms) * (each + 6);
+      if (time < least) {
+        least = time;
+        runs = k;
+      }
+    }
+    a.pairs = (uint32_t)pairs;   // whose numbers have no gaps: partial results for these alone
+    a.chunk = runs == 1 ? 0x40000000u : (uint32_t)ceil_div(slots, runs);
+    a.max_chunks = runs == 1 ? 1u : (uint32_t)ceil_div(slots, a.chunk);
+    RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
+    a.counter = (uint32_t*)p;
+    if (a.max_chunks > 1) {
+      RO_TRY(c.scratch(SS_JOIN, attend_tiles_join(a), &a.join));
+      RO_TRY(c.scratch(SS_PARTIAL, attend_tiles_partial(a), &p));
+      a.partial = (float*)p;
+    }
+    if (launch_attend_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
+  }
+  const uint32_t rows = 64;
+  const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);
+  const uint64_t tiles =
+      (a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1) * row_tiles;
+  const uint64_t work = tiles * cache->n_heads;
+  if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
+  a.tiles = (uint32_t)tiles;
+  // Keys of one CTA: about four CTAs' worth of work per place of the GPU, in
+  // steps of 64 keys and at least 128 (a shorter run costs more in its join
+  // than it saves).
+  const uint64_t split = std::max<uint64_t>(1, (uint64_t)c.sms() * 2 * 4 / work);
+  a.chunk = (uint32_t)std::min<uint64_t>(0x40000000u, std::max<uint64_t>(128, ceil_div(ceil_div(keys, split), 64) * 64));
+  a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(keys, a.chunk), 1024);
+  if (a.max_chunks > 1) {
+    RO_TRY(c.scratch(SS_PARTIAL, (size_t)work * a.max_chunks * rows * ((cache->head_dim <= 64 ? 64 : 128) + 2) * 4, &p));
+    a.partial = (float*)p;
+    RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
+    a.counter = (uint32_t*)p;
+  }
+  launch_attend_rows(c.launch(), a, cache->dtype);
+  return c.launched(fn);
+}
+
 }  // namespace
 
 extern "C" {
@@ -234,124 +394,22 @@ ro_status ro_cache_attend(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
                           uint32_t max_new, const uint32_t* d_len, uint32_t max_len, const void* d_q, uint64_t q_tok,
                           uint64_t q_head, uint32_t n_q_heads, float scale, uint32_t window, uint32_t sinks,
                           void* d_out, uint64_t out_tok, uint64_t out_head, float* d_lse) {
-  const char* fn = "ro_cache_attend";
   StepCall c(ctx);
   RO_TRY(c.status);
-  RO_TRY(check_cache(c, fn, cache));
-  RO_TRY(check_rows(c, fn, cache, d_tok_base, n_tokens, d_len, d_q, q_tok, q_head, n_q_heads, scale));
-  if (n_tokens && !d_out) return c.refuse(RO_E_INVAL, "%s: NULL output", fn);
-  if (!aligned(d_out, 16) || out_tok % 8 || out_head % 8)
-    return c.refuse(RO_E_INVAL, "%s: the output wants a 16-byte pointer and strides of 8 elements", fn);
-  if (n_tokens == 0) return RO_OK;
-  if (d_out == d_q) return c.refuse(RO_E_INVAL, "%s: the output cannot be q", fn);
-  RO_TRY(c.begin());
-  AttendArgs a = {};
-  a.c = paged(cache);
-  const uint32_t group = n_q_heads / cache->n_heads;
-  a.r = rows_of(d_tok_base, d_len, n_tokens, max_new, group, d_q, q_tok, q_head, window, sinks, scale);
-  a.out = d_out;
-  a.out_tok = out_tok;
-  a.out_head = out_head;
-  a.lse = d_lse;
-  a.n_q_heads = n_q_heads;
-  a.err = c.err();
-  uint64_t keys = max_len ? max_len : 0x7FFFFFFFu;
-  keys = std::min<uint64_t>(keys, (uint64_t)cache->n_pages * cache->page_size);
-  if (a.r.window) keys = std::min<uint64_t>(keys, (uint64_t)a.r.window + a.r.sinks + a.r.max_new);
-  keys = std::max<uint64_t>(keys, 1);
-  const uint64_t max_rows = (uint64_t)a.r.max_new * group;
-  void* p = nullptr;
-  // At most 16 rows a sequence: bound by the cache's bytes.
-  if (max_rows <= 16) {
-    const uint64_t work = (uint64_t)cache->n_seqs * cache->n_heads, stage = attend_few_keys(cache->head_dim);
-    if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many sequences and heads", fn);
-    a.tiles = cache->n_seqs;
-    // Runs that fill two CTAs an SM in whole rounds, of at most 96 stages of
-    // 16 KB (longer ones leave SMs idle at the end where lengths differ) and
-    // at least 3, one for each warp (shorter ones cost more than they
-    // save).  One sequence of 777 slots, 4 heads of 64: 7.2 us at 3 stages, 9.1
-    // at 8, 7.8 at 2; of 100,000 slots, 8 heads of 128: 70 us in one round, 84 in
-    // two; 64 ragged sequences of up to 32,000 slots: 432 us at 96 stages, 476 at
-    // 32, 565 at 16.
-    const uint64_t stages = ceil_div(keys, stage), places = (uint64_t)c.sms() * 2;
-    const uint64_t each = ceil_div(stages * work, places);
-    a.chunk = (uint32_t)std::max<uint64_t>(3, ceil_div(each, ceil_div(each, 96)));
-    a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(stages, a.chunk),
-                                                std::min<uint64_t>(1024, std::max<uint64_t>(1, MAX_FEW_RUNS / work)));
-    // Up to eight runs that the GPU holds at once are a cluster and join in
-    // shared memory; more go through L2 and a ticket.
-    const bool cluster = a.max_chunks > 1 && a.max_chunks <= 8 && work * a.max_chunks <= places;
-    if (a.max_chunks > 1 && !cluster) {
-      RO_TRY(c.scratch(SS_PARTIAL, attend_few_partial(a), &p));
-      a.partial = (float*)p;
-      RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
-      a.counter = (uint32_t*)p;
-    }
-    // Many short sequences: a warp alone for each (sequence, head), where its
-    // stages one after another, about 1 us for 8 KB, take less than the rounds
-    // of larger CTAs, about 6 us each.  2,048 of 40 slots of 128: 13 us against
-    // 41, of 300: 55 against 79; 5,600 of up to 150: 42 against 110.  On either
-    // side of the rule: 1,024 of up to 300 slots 23.4 against 24.4, of up to 600
-    // 44 against 32.
-    const bool alone = a.max_chunks == 1 && work > places && ceil_div(keys, attend_short_keys(cache->head_dim)) * places <= 5 * work;
-    launch_attend_few(c.launch(), a, cache->dtype, cluster, alone);
-    return c.launched(fn);
-  }
-  // More: the tensor-core kernel, if the pages and the group fit its tiles.
-  if (attend_tiles_fits(a)) {
-    const uint32_t toks = attend_tile_tokens(group);
-    const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
-    const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
-    if (work > MAX_GRID / 256) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
-    a.tiles = (uint32_t)tiles;
-    // One CTA an SM takes pairs of row tiles in turn.  Where that is few rounds,
-    // split the slots into the number of runs that takes the least time: rounds
-    // of runs, each its tiles of slots plus about 6 tiles' time of its own.
-    // (512 new tokens over 64,000 slots: 327 us in 2 runs, 311 in 7, 611 unsplit;
-    // 64 over 32,000: 38 us in 16 runs, 53 in 8, 319 unsplit.)
-    const uint64_t sms = (uint64_t)c.sms();
-    const uint64_t pairs = std::min<uint64_t>(work, (uint64_t)cache->n_seqs * ceil_div(a.r.max_new, toks) * cache->n_heads);
-    uint64_t runs = 1, least = ~0ull;
-    for (uint64_t k = 1; k == 1 || (k <= 32 && pairs < 4 * sms && pairs * k <= MAX_RUNS); ++k) {
-      const uint64_t each = ceil_div(slots, k), time = ceil_div(pairs * ceil_div(slots, each), sms) * (each + 6);
-      if (time < least) {
-        least = time;
-        runs = k;
-      }
-    }
-    a.pairs = (uint32_t)pairs;   // whose numbers have no gaps: partial results for these alone
-    a.chunk = runs == 1 ? 0x40000000u : (uint32_t)ceil_div(slots, runs);
-    a.max_chunks = runs == 1 ? 1u : (uint32_t)ceil_div(slots, a.chunk);
-    RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
-    a.counter = (uint32_t*)p;
-    if (a.max_chunks > 1) {
-      RO_TRY(c.scratch(SS_JOIN, attend_tiles_join(a), &a.join));
-      RO_TRY(c.scratch(SS_PARTIAL, attend_tiles_partial(a), &p));
-      a.partial = (float*)p;
-    }
-    if (launch_attend_tiles(c.launch(), a, cache->dtype, c.sms())) return c.launched(fn);
-  }
-  const uint32_t rows = 64;
-  const uint32_t toks = std::max<uint32_t>(1, rows / group), row_tiles = (uint32_t)ceil_div(group, rows);
-  const uint64_t tiles =
-      (a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1) * row_tiles;
-  const uint64_t work = tiles * cache->n_heads;
-  if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many row tiles", fn);
-  a.tiles = (uint32_t)tiles;
-  // Keys of one CTA: about four CTAs' worth of work per place of the GPU, in
-  // steps of 64 keys and at least 128 (a shorter run costs more in its join
-  // than it saves).
-  const uint64_t split = std::max<uint64_t>(1, (uint64_t)c.sms() * 2 * 4 / work);
-  a.chunk = (uint32_t)std::min<uint64_t>(0x40000000u, std::max<uint64_t>(128, ceil_div(ceil_div(keys, split), 64) * 64));
-  a.max_chunks = (uint32_t)std::min<uint64_t>(ceil_div(keys, a.chunk), 1024);
-  if (a.max_chunks > 1) {
-    RO_TRY(c.scratch(SS_PARTIAL, (size_t)work * a.max_chunks * rows * ((cache->head_dim <= 64 ? 64 : 128) + 2) * 4, &p));
-    a.partial = (float*)p;
-    RO_TRY(c.scratch(SS_COUNTER, (size_t)work * 4, &p));
-    a.counter = (uint32_t*)p;
-  }
-  launch_attend_rows(c.launch(), a, cache->dtype);
-  return c.launched(fn);
+  return attend("ro_cache_attend", c, cache, d_tok_base, n_tokens, max_new, d_len, max_len, d_q, q_tok, q_head,
+                n_q_heads, scale, window, sinks, nullptr, d_out, out_tok, out_head, d_lse);
+}
+
+ro_status ro_cache_attend_biased(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_tok_base, uint64_t n_tokens,
+                                 uint32_t max_new, const uint32_t* d_len, uint32_t max_len, const void* d_q,
+                                 uint64_t q_tok, uint64_t q_head, uint32_t n_q_heads, float scale, uint32_t window,
+                                 uint32_t sinks, const ro_bias* bias, void* d_out, uint64_t out_tok, uint64_t out_head,
+                                 float* d_lse) {
+  StepCall c(ctx);
+  RO_TRY(c.status);
+  if (!bias) return c.refuse(RO_E_INVAL, "ro_cache_attend_biased: NULL bias");
+  return attend("ro_cache_attend_biased", c, cache, d_tok_base, n_tokens, max_new, d_len, max_len, d_q, q_tok, q_head,
+                n_q_heads, scale, window, sinks, bias, d_out, out_tok, out_head, d_lse);
 }
 
 ro_status ro_cache_weigh(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_tok_base, uint64_t n_tokens,
@@ -449,6 +507,96 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
   a.score_out = d_score_out;
   a.err = c.err();
   launch_evict(c.launch(), a, c.sms());
+  return c.launched(fn);
+}
+
+ro_status ro_cache_fork(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_len, const uint64_t* d_child_base,
+                        const uint32_t* d_child_parent, uint64_t n_children, const uint64_t* d_dst_base,
+                        const uint32_t* d_dst_seq, uint64_t n_dst, uint32_t* d_dst_pages, uint32_t* d_len_out,
+                        const uint32_t* d_refs, uint32_t* d_refs_out, const ro_moves* moves) {
+  const char* fn = "ro_cache_fork";
+  StepCall c(ctx);
+  RO_TRY(c.status);
+  RO_TRY(check_cache(c, fn, cache));
+  if (!d_len || !d_child_base || !d_refs || !d_refs_out || (n_children && (!d_child_parent || !d_dst_base || !d_len_out)) ||
+      (n_dst && (!d_dst_seq || !d_dst_pages)))
+    return c.refuse(RO_E_INVAL, "%s: NULL argument", fn);
+  if (n_children >= 0x80000000ull || n_dst >= 0x80000000ull || cache->n_pages >= 0xFFFFFFFEu)
+    return c.refuse(RO_E_OVERFLOW, "%s: too many continuations or pages", fn);
+  if (n_dst && !n_children) return c.refuse(RO_E_INVAL, "%s: pages without continuations", fn);
+  PagesArgs a = {};
+  RO_TRY(check_moves(c, fn, moves, n_children, &a.m));
+  const uint64_t pool = (uint64_t)cache->n_pages * sizeof(uint32_t);
+  if (d_refs_out != d_refs && touch(d_refs, pool, d_refs_out, pool))
+    return c.refuse(RO_E_INVAL, "%s: counts change in place or in another array", fn);
+  if (touch(d_len, (uint64_t)cache->n_seqs * 4, d_len_out, n_children * 4) || touch(cache->d_pages, 4, d_dst_pages, n_dst * 4))
+    return c.refuse(RO_E_INVAL, "%s: the continuations' lengths and pages go to arrays of their own", fn);
+  RO_TRY(c.begin());
+  a.c = paged(cache);
+  a.refs = d_refs;
+  a.refs_out = d_refs_out;
+  a.len = d_len;
+  a.child_base = d_child_base;
+  a.child_parent = d_child_parent;
+  a.dst_base = d_dst_base;
+  a.dst_seq = d_dst_seq;
+  a.dst_pages = d_dst_pages;
+  a.len_out = d_len_out;
+  a.n_children = n_children;
+  a.n_dst = n_dst;
+  a.err = c.err();
+  uint32_t ctas = 0;
+  RO_TRY(plan_scratch(c, std::max<uint64_t>(n_dst, cache->n_pages), &a, &ctas));
+  launch_fork(c.launch(), a, ctas);
+  MoveArgs copies = a.m;
+  copies.cap = n_children;   // one a continuation at most
+  launch_page_copy(c.launch(), a.c, copies, a.err, c.sms());
+  return c.launched(fn);
+}
+
+ro_status ro_cache_compact(ro_ctx* ctx, const ro_cache* cache, uint32_t* d_pages_out, uint64_t n_list,
+                           const uint32_t* d_refs, uint32_t* d_refs_out, uint32_t* d_n_used, const ro_moves* moves) {
+  const char* fn = "ro_cache_compact";
+  StepCall c(ctx);
+  RO_TRY(c.status);
+  RO_TRY(check_cache(c, fn, cache));
+  if ((n_list && !d_pages_out) || !d_refs || !d_refs_out || !d_n_used) return c.refuse(RO_E_INVAL, "%s: NULL argument", fn);
+  if (n_list >= 0x80000000ull || cache->n_pages >= 0xFFFFFFFEu)
+    return c.refuse(RO_E_OVERFLOW, "%s: too many pages or entries", fn);
+  PagesArgs a = {};
+  RO_TRY(check_moves(c, fn, moves, cache->n_pages / 2, &a.m));
+  const uint64_t pool = (uint64_t)cache->n_pages * sizeof(uint32_t);
+  if (d_refs_out != d_refs && touch(d_refs, pool, d_refs_out, pool))
+    return c.refuse(RO_E_INVAL, "%s: counts change in place or in another array", fn);
+  if (d_pages_out != cache->d_pages && touch(cache->d_pages, n_list * 4, d_pages_out, n_list * 4))
+    return c.refuse(RO_E_INVAL, "%s: lists change in place or in another array", fn);
+  RO_TRY(c.begin());
+  a.c = paged(cache);
+  a.refs = d_refs;
+  a.refs_out = d_refs_out;
+  a.pages_out = d_pages_out;
+  a.n_list = n_list;
+  a.n_used = d_n_used;
+  a.err = c.err();
+  uint32_t ctas = 0;
+  RO_TRY(plan_scratch(c, std::max<uint64_t>(n_list, cache->n_pages), &a, &ctas));
+  launch_compact(c.launch(), a, ctas);
+  MoveArgs copies = a.m;
+  copies.cap = cache->n_pages / 2;
+  launch_page_copy(c.launch(), a.c, copies, a.err, c.sms());
+  return c.launched(fn);
+}
+
+ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* moves) {
+  const char* fn = "ro_cache_copy";
+  StepCall c(ctx);
+  RO_TRY(c.status);
+  RO_TRY(check_cache(c, fn, cache));
+  MoveArgs m = {};
+  RO_TRY(check_moves(c, fn, moves, 0, &m));
+  if (m.cap == 0) return RO_OK;
+  RO_TRY(c.begin());
+  launch_page_copy(c.launch(), paged(cache), m, c.err(), c.sms());
   return c.launched(fn);
 }
 
