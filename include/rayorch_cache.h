@@ -314,6 +314,42 @@ ro_status ro_cache_compact(ro_ctx* ctx, const ro_cache* cache, uint32_t* d_pages
  */
 ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* moves);
 
+/* ------------------------------------------------------------------------
+ * ro_sample — draw each row's token from its logits and a given random number.
+ * With w_i = exp((x_i - max x) / temperature) and the tokens in order, larger
+ * logit first and equal ones (0 and -0 among them) by index, a token stays when
+ *   top_k:  it is among the first top_k (0: all);
+ *   top_p:  the sum of w over the tokens ahead of it is less than top_p times
+ *           the sum over those that top_k leaves (1: all stay; 0: the first);
+ *   min_p:  w_i >= min_p (0: all).
+ * The token drawn is the first of those that stay, by index, whose running sum
+ * of w passes u times the sum over all of them.  temperature 0 draws the
+ * largest logit, the first of equal ones.  A logit that is -inf or NaN is never
+ * drawn and does not count.
+ *   d_logits   [n_rows][vocab] of `dtype` (bf16, f16 or f32), row_stride
+ *              elements from row to row, any alignment to the element.
+ *   how        settings of each row, NULL (also in it): the neutral ones.
+ *   d_u        float[n_rows], 0 <= u < 1.
+ *   d_token    uint32[n_rows] out; RO_NO_TOKEN where nothing can be drawn.
+ *   d_logp     float[n_rows] out or NULL: ln of the drawn token's share of the
+ *              sum over those that stay (-inf where none).
+ *   d_kept     uint32[n_rows] out or NULL: how many stay (drawing the largest: 1).
+ * Weights are about 2^-40 exact and their sums are exact: tokens do not depend
+ * on how the work is split.  vocab is at most 393,216.  Recorded: RO_E_INVAL for
+ * a row whose settings or u are out of range or NaN (RO_NO_TOKEN there).
+ */
+#define RO_NO_TOKEN 0xFFFFFFFFu
+typedef struct {
+  const float* d_temperature;   /* float[n_rows] or NULL (1); finite, at least 0 */
+  const uint32_t* d_top_k;      /* uint32[n_rows] or NULL (0) */
+  const float* d_top_p;         /* float[n_rows] or NULL (1); 0 to 1 */
+  const float* d_min_p;         /* float[n_rows] or NULL (0); 0 to 1 */
+} ro_sampling;
+
+ro_status ro_sample(ro_ctx* ctx, int32_t dtype, const void* d_logits, uint64_t row_stride,
+                    uint64_t n_rows, uint32_t vocab, const ro_sampling* how, const float* d_u,
+                    uint32_t* d_token, float* d_logp, uint32_t* d_kept);
+
 #ifdef __cplusplus
 }
 #endif

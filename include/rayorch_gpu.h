@@ -210,7 +210,8 @@ enum {
    * ATTEND_ROWS, the weights' without and those behind a window WEIGH */
   RO_K_ROTARY = 22, RO_K_ATTEND_ROWS = 23, RO_K_ATTEND_TILES = 24, RO_K_WEIGH = 25,
   RO_K_WEIGH_TILES = 26, RO_K_EVICT_SELECT = 27, RO_K_EVICT_MOVE = 28,
-  RO_K_ATTEND_JOIN = 29, RO_K_PAGES = 30, RO_K_COUNT = 31
+  RO_K_ATTEND_JOIN = 29, RO_K_PAGES = 30,
+  RO_K_SAMPLE = 31, RO_K_COUNT = 32
 };
 /* Tracing (no counterpart in the paper; it instruments the path).  Every
  * kernel launch is counted; kernels whose bit (1 << RO_K_*) is set in

@@ -30,6 +30,8 @@ RO_ACCEPT, RO_REJ_INVALID, RO_REJ_NOT_INFLIGHT, RO_REJ_STALE_GEN, RO_REJ_DUPLICA
 RO_BF16, RO_F16, RO_F32 = range(3)
 # a page list's entry for which the pool had no page
 RO_NO_PAGE = 0xFFFFFFFF
+# a row's token where none can be drawn
+RO_NO_TOKEN = 0xFFFFFFFF
 
 STATUS_NAMES = {0: "RO_OK", 1: "RO_E_INVAL", 2: "RO_E_CAPACITY", 3: "RO_E_OVERFLOW",
                 4: "RO_E_STATE", 5: "RO_E_OOM", 6: "RO_E_CUDA", 7: "RO_E_TIMEOUT"}
@@ -38,14 +40,14 @@ EXPORTS = ("ro_ctx_create", "ro_ctx_destroy", "ro_ctx_reset", "ro_ctx_sync", "ro
            "ro_ctx_set_streams", "ro_ctx_set_call_streams", "ro_ctx_join", "ro_ctx_selftest_timeout", "ro_last_error", "ro_ctx_profile", "ro_ctx_profile_read", "ro_expand", "ro_batch_ready",
            "ro_batch_ready_calls", "ro_retry", "ro_batch_ready_parent", "ro_gather_commit", "ro_assemble", "ro_assemble_list", "ro_filter_reports",
            "ro_expand_noalloc", "ro_rotary", "ro_cache_append", "ro_cache_attend", "ro_cache_weigh", "ro_cache_evict", "ro_cache_attend_biased", "ro_cache_fork",
-           "ro_cache_compact", "ro_cache_copy")
+           "ro_cache_compact", "ro_cache_copy", "ro_sample")
 
 # kernel ids (RO_K_*), in launch order of the path
 KERNELS = ("expand_scan", "expand_fill", "ready_count", "ready_scatter", "commit_scatter",
            "commit_plan", "asm_parents", "asm_members", "asm_copy", "retry_claim", "retry_scatter",
            "pb_keys", "pb_hist", "pb_rowscan", "pb_sort", "pb_bounds", "pb_heads", "pb_mark",
            "pb_scan", "pb_emit", "commit_fix", "ready_fused", "rotary", "attend_rows", "attend_tiles",
-           "weigh", "weigh_tiles", "evict_select", "evict_move", "attend_join", "pages")
+           "weigh", "weigh_tiles", "evict_select", "evict_move", "attend_join", "pages", "sample")
 
 
 class RoError(RuntimeError):
@@ -126,6 +128,19 @@ class ro_moves(C.Structure):
         self._ref = C.byref(self)
 
 
+class ro_sampling(C.Structure):
+    """How each row's token is drawn: temperature, top-p and min-p (32-bit
+    floats), top-k (32-bit integers), a value for every row or None.  Keeps the
+    tensors alive."""
+    _fields_ = [("d_temperature", C.c_void_p), ("d_top_k", C.c_void_p), ("d_top_p", C.c_void_p), ("d_min_p", C.c_void_p)]
+
+    def __init__(self, d_temperature=None, d_top_k=None, d_top_p=None, d_min_p=None):
+        super().__init__(_list(d_temperature, _F32), _list(d_top_k, _I32), _list(d_top_p, _F32), _list(d_min_p, _F32))
+        self._tensors = (d_temperature, d_top_k, d_top_p, d_min_p)
+        self._rows = min([x.numel() for x in self._tensors if x is not None and not isinstance(x, int)], default=None)
+        self._ref = C.byref(self)
+
+
 _lib = None
 _vp = C.c_void_p
 _u64 = C.c_uint64
@@ -187,6 +202,7 @@ def load(path: Optional[str] = None):
     L.ro_cache_fork.argtypes = [_vp, cache, _vp, _vp, _vp, _u64, _vp, _vp, _u64, _vp, _vp, _vp, _vp, moves]
     L.ro_cache_compact.argtypes = [_vp, cache, _vp, _u64, _vp, _vp, _vp, moves]
     L.ro_cache_copy.argtypes = [_vp, cache, moves]
+    L.ro_sample.argtypes = [_vp, _i32, _vp, _u64, _u64, _u32, C.POINTER(ro_sampling), _vp, _vp, _vp, _vp]
     for f in EXPORTS:
         if f != "ro_last_error":
             getattr(L, f).restype = C.c_int32
@@ -567,3 +583,16 @@ def ro_cache_compact(ctx, cache, d_pages_out, d_refs, d_refs_out, d_n_used, move
 def ro_cache_copy(ctx, cache, moves) -> int:
     """Copy pages within the cache's pools, for instance another layer's after ro_cache_fork."""
     return (_lib or load()).ro_cache_copy(ctx, cache._ref, moves._ref)
+
+
+def ro_sample(ctx, d_logits, how, d_u, d_token, d_logp=None, d_kept=None) -> int:
+    """Draw each row's token from its logits [rows, vocabulary] and a random number (how None: from all of them)."""
+    rows, vocab = d_logits.shape
+    if vocab > 1 and d_logits.stride(1) != 1:
+        raise ValueError("ro_sample: logits must be [rows, vocabulary], contiguous in the last dimension")
+    if how is not None and how._rows is not None and how._rows < rows:
+        raise ValueError("ro_sample: fewer settings than rows")
+    return (_lib or load()).ro_sample(ctx, _dtype(d_logits), d_logits.data_ptr() if d_logits.is_cuda else _ptr(d_logits),
+                                      d_logits.stride(0), rows, vocab, None if how is None else how._ref,
+                                      _list(d_u, _F32, rows), _list(d_token, _I32, rows), _list(d_logp, _F32, rows),
+                                      _list(d_kept, _I32, rows))

@@ -611,7 +611,7 @@ ro_status ro_ctx_create(ro_ctx** out, int32_t device, void* stream, uint32_t n_c
   if (prepare_assemble_kernels() != cudaSuccess || prepare_attend_kernels() != cudaSuccess ||
       prepare_attend_tiles_kernels() != cudaSuccess || prepare_attend_few_kernels() != cudaSuccess ||
       prepare_weigh_tiles_kernels() != cudaSuccess || prepare_weigh_few_kernels() != cudaSuccess ||
-      prepare_evict_kernels() != cudaSuccess) {
+      prepare_evict_kernels() != cudaSuccess || prepare_sample_kernels() != cudaSuccess) {
     cudaGetLastError();
     free_scalars(c);
     delete c;
@@ -786,7 +786,7 @@ const char* ro_last_error(const ro_ctx* c) { return c ? c->err.c_str() : "no con
 
 ro_status ro_ctx_profile(ro_ctx* c, uint32_t kernel_mask) {
   RO_TRY(enter(c));
-  c->prof.mask = kernel_mask & ((1u << K_COUNT) - 1u);
+  c->prof.mask = kernel_mask & (uint32_t)((1ull << K_COUNT) - 1u);
   return RO_OK;
 }
 

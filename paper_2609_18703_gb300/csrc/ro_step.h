@@ -240,4 +240,25 @@ struct PageCopyArgs {
 };
 void launch_page_copy(const LaunchCfg& L, const PagedArgs& c, const MoveArgs& m, uint32_t* err, int sms);
 
+// ---- sample -----------------------------------------------------------------------------
+constexpr uint32_t MAX_VOCAB = 393216;   // eight slices of 192 KB of 32-bit logits
+struct SampleArgs {
+  const void* x;
+  uint64_t stride;
+  uint32_t rows, vocab;
+  const float* temperature;  // these four optional
+  const uint32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  uint32_t* token;
+  float* logp;               // optional
+  uint32_t* kept;            // optional
+  uint32_t cluster, blocks;  // CTAs of a row, 16-byte blocks of a slice
+  uint32_t frac_bits;        // of a weight
+  uint32_t* err;
+};
+void launch_sample(const LaunchCfg& L, const SampleArgs& a, int dtype, int sms);
+cudaError_t prepare_sample_kernels();
+
 }  // namespace ro

@@ -600,4 +600,42 @@ ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* move
   return c.launched(fn);
 }
 
+ro_status ro_sample(ro_ctx* ctx, int32_t dtype, const void* d_logits, uint64_t row_stride, uint64_t n_rows,
+                    uint32_t vocab, const ro_sampling* how, const float* d_u, uint32_t* d_token, float* d_logp,
+                    uint32_t* d_kept) {
+  const char* fn = "ro_sample";
+  StepCall c(ctx);
+  RO_TRY(c.status);
+  if (dtype != RO_BF16 && dtype != RO_F16 && dtype != RO_F32) return c.refuse(RO_E_INVAL, "%s: unknown type", fn);
+  if (n_rows && (!d_logits || !d_u || !d_token)) return c.refuse(RO_E_INVAL, "%s: NULL argument", fn);
+  if (vocab == 0) return c.refuse(RO_E_INVAL, "%s: no tokens to draw from", fn);
+  if (vocab > MAX_VOCAB || n_rows > MAX_GRID / 8)
+    return c.refuse(RO_E_OVERFLOW, "%s: more than %u tokens or too many rows", fn, MAX_VOCAB);
+  if (!aligned(d_logits, dtype == RO_F32 ? 4 : 2)) return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
+  for (const void* p : {(const void*)d_u, (const void*)d_token, (const void*)d_logp, (const void*)d_kept,
+                        how ? (const void*)how->d_temperature : nullptr, how ? (const void*)how->d_top_k : nullptr,
+                        how ? (const void*)how->d_top_p : nullptr, how ? (const void*)how->d_min_p : nullptr})
+    if (!aligned(p, 4)) return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
+  if (n_rows == 0) return RO_OK;
+  RO_TRY(c.begin());
+  SampleArgs a = {};
+  a.x = d_logits;
+  a.stride = row_stride;
+  a.rows = (uint32_t)n_rows;
+  a.vocab = vocab;
+  if (how) {
+    a.temperature = how->d_temperature;
+    a.top_k = how->d_top_k;
+    a.top_p = how->d_top_p;
+    a.min_p = how->d_min_p;
+  }
+  a.u = d_u;
+  a.token = d_token;
+  a.logp = d_logp;
+  a.kept = d_kept;
+  a.err = c.err();
+  launch_sample(c.launch(), a, dtype, c.sms());
+  return c.launched(fn);
+}
+
 }  // extern "C"
