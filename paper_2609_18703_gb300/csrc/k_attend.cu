@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
         float x;
         if constexpr (BIASED) {
           const uint32_t j = ks.slot(u);
-          x = biased_score(a.b, a.r.scale_log2, s[n][z], slope[z >> 1], fabsf((float)(row_a[z >> 1] - (int64_t)j)));
+          x = a.b.cap_log2 != 0.f ? capped(a.b, s[n][z]) : s[n][z] * a.r.scale_log2;
+          x = fmaf(-slope[z >> 1], fabsf((float)(row_a[z >> 1] - (int64_t)j)), x);
           if (!all && (u >= u1 || !see[z >> 1].sees(j))) x = -INFINITY;
         } else {
           x = s[n][z] * a.r.scale_log2;

@@ -39,9 +39,22 @@ struct FewShape {
   static_assert(BLOCKS * BLOCK_BYTES == SIDE, "a stage holds its keys and values");
 };
 
+// What the rows of a tile see together, and the tiles it is cut into.
+template <bool B>
+using FewSpan = std::conditional_t<B, BiasSpan, KeySpan>;
+template <bool B, int KEYS>
+using FewTiles = std::conditional_t<B, BiasTiles<KEYS>, SlotTiles<KEYS>>;
+template <bool B>
+__device__ __forceinline__ FewSpan<B> few_span(const AttendArgs& a, const SeqInfo& q) {
+  if constexpr (B)
+    return bias_span(q, a.r, a.b, 0, q.n);
+  else
+    return key_span(q, a.r, 0, q.n);
+}
+
 // A warp's share of a tile of rows: the queries as matrix fragments, and the
-// (m, l, o) of the slots it has seen.
-template <typename T, int DP, uint32_t STAGE = AF_STAGE>
+// (m, l, o) of the slots it has seen.  B: biased (ro_cache_attend_biased).
+template <typename T, int DP, bool B, uint32_t STAGE = AF_STAGE>
 struct FewRows {
   using S = FewShape<DP, STAGE>;
   static constexpr int KEYS = S::KEYS;
@@ -49,6 +62,8 @@ struct FewRows {
   int64_t row_a[2];
   float o[DP / 8][4];
   float m[2], l[2];
+  RowSee see[2];             // biased: what the rows see, their slopes in log2
+  float slope[2];
 
   __device__ __forceinline__ void clear() {
     m[0] = m[1] = -INFINITY;
@@ -67,10 +82,18 @@ struct FewRows {
       const uint32_t r = lane / 4 + 8 * z;
       qp[z] = nullptr;
       row_a[z] = INT64_MIN / 2;
+      if constexpr (B) {
+        see[z] = {0, 0, 0, 0};
+        slope[z] = 0.f;
+      }
       if (r < rows) {
         const uint32_t i = r / G, h = kh * G + r % G;
         qp[z] = (const T*)a.r.q + (q.tok0 + i) * a.r.q_tok + (uint64_t)h * a.r.q_head;
         row_a[z] = q.first + i;
+        if constexpr (B) {
+          see[z] = row_see(q, a.r, a.b, i);
+          if (a.b.slope) slope[z] = a.b.slope[h] * LOG2E;
+        }
       }
     }
 #pragma unroll
@@ -83,12 +106,19 @@ struct FewRows {
       }
   }
   // one stage: its keys at kb in shared memory, its values behind them
-  __device__ __forceinline__ void stage(const AttendArgs& a, const SeqInfo& q, const SlotTile& st, uint32_t kb, uint32_t lane) {
+  __device__ __forceinline__ void stage(const AttendArgs& a, const SeqInfo& q, const FewSpan<B>& ks, const SlotTile& st,
+                                        uint32_t kb, uint32_t lane) {
     const uint32_t vb = kb + S::SIDE;
-    const bool whole = st.lo == st.t0 && st.hi == st.t0 + KEYS;
+    bool whole = st.lo == st.t0 && st.hi == st.t0 + KEYS;
+    if constexpr (B) whole = whole && ks.holes == 0u;
+    auto unseen = [&](uint32_t j) {
+      if (j < st.lo || j >= st.hi) return true;
+      if constexpr (B) return !somebody_sees(q, a.r, a.b, ks.holes, ks.s_lo + ks.s_n, 0, q.n, j);
+      return false;
+    };
     if (!whole) {   // values no row sees must not reach the product: a weight of 0 does not silence a NaN
       for (uint32_t r = lane; r < (uint32_t)KEYS; r += 32)
-        if (st.t0 + r < st.lo || st.t0 + r >= st.hi)
+        if (unseen(st.t0 + r))
 #pragma unroll
           for (uint32_t x = 0; x < S::BLOCKS * 8; ++x)
             asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(vb + (x / 8) * S::BLOCK_BYTES + r * 128 +
@@ -112,21 +142,47 @@ struct FewRows {
         mma16<T>(s[2 * x], qf[k], b[0], b[1]);
         mma16<T>(s[2 * x + 1], qf[k], b[2], b[3]);
       }
-    const bool all = whole && (st.sink || ((int64_t)st.t0 + KEYS - 1 <= q.first &&
-                                           (a.r.window == 0u || (int64_t)st.t0 > (q.first + q.n - 1) - (int64_t)a.r.window)));
     float nm[2] = {m[0], m[1]};
+    if constexpr (B) {
+      const bool all = whole && st.t0 >= ks.all_lo && st.t0 + KEYS <= ks.all_hi;
+      float(&flat)[KEYS / 2] = reinterpret_cast<float(&)[KEYS / 2]>(s);
+      if (a.b.cap_log2 != 0.f) {
+        cap_scores(a.b, flat);
+      } else {
 #pragma unroll
-    for (int x = 0; x < KEYS / 8; ++x)
-#pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        float y = s[x][z] * a.r.scale_log2;
-        if (!all) {
-          const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
-          if (j < st.lo || j >= st.hi || !sees(a.r, row_a[z >> 1], j)) y = -INFINITY;
-        }
-        s[x][z] = y;
-        nm[z >> 1] = fmaxf(nm[z >> 1], y);
+        for (int i = 0; i < KEYS / 2; ++i) flat[i] *= a.r.scale_log2;
       }
+      if (a.b.slope) {   // distances from the row to its first column of the stage on
+        const float d[2] = {(float)(row_a[0] - (int64_t)st.t0 - (lane & 3) * 2), (float)(row_a[1] - (int64_t)st.t0 - (lane & 3) * 2)};
+#pragma unroll
+        for (int x = 0; x < KEYS / 8; ++x)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) s[x][z] = fmaf(-slope[z >> 1], fabsf(d[z >> 1] - (float)(x * 8 + (z & 1))), s[x][z]);
+      }
+#pragma unroll
+      for (int x = 0; x < KEYS / 8; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
+          if (!all && (j < st.lo || j >= st.hi || !see[z >> 1].sees(j))) s[x][z] = -INFINITY;
+          nm[z >> 1] = fmaxf(nm[z >> 1], s[x][z]);
+        }
+    } else {
+      const bool all = whole && (st.sink || ((int64_t)st.t0 + KEYS - 1 <= q.first &&
+                                             (a.r.window == 0u || (int64_t)st.t0 > (q.first + q.n - 1) - (int64_t)a.r.window)));
+#pragma unroll
+      for (int x = 0; x < KEYS / 8; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          float y = s[x][z] * a.r.scale_log2;
+          if (!all) {
+            const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
+            if (j < st.lo || j >= st.hi || !sees(a.r, row_a[z >> 1], j)) y = -INFINITY;
+          }
+          s[x][z] = y;
+          nm[z >> 1] = fmaxf(nm[z >> 1], y);
+        }
+    }
     float f[2], sub[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
@@ -181,7 +237,7 @@ struct FewRows {
   }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, bool B>
 __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_constant__ AttendFewArgs g) {
   using S = FewShape<DP>;
   constexpr int KEYS = S::KEYS;
@@ -197,8 +253,8 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
   const SeqInfo q = seq_info(a.c, a.r, seq, a.err);
   if (q.n == 0) return;
   const uint32_t rows = q.n * G;
-  const KeySpan ks = key_span(q, a.r, 0, q.n);
-  const SlotTiles<KEYS> slots(ks, g.box);
+  const FewSpan<B> ks = few_span<B>(a, q);
+  const FewTiles<B, KEYS> slots(ks, g.box);
   const uint32_t per = max(a.chunk, slots.n / a.max_chunks + 1);   // stages of a run
   const uint32_t n_chunks = max(1u, (slots.n + per - 1) / per);
   if (blockIdx.y >= n_chunks) return;
@@ -222,7 +278,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
                                               b_empty, &s_gave_up, a.err);
   }
 
-  FewRows<T, DP> f;
+  FewRows<T, DP, B> f;
   f.clear();
   if (warp < AF_WARPS) {
     f.load(a, q, kh, rows, lane);
@@ -230,7 +286,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
       const uint32_t slot = t % AF_STAGES;
       const SlotTile st = slots.at(c0 + t);
       bar_wait(b_full + 8 * slot, (t / AF_STAGES) & 1, &s_gave_up, a.err);
-      f.stage(a, q, st, sm + slot * AF_STAGE, lane);
+      f.stage(a, q, ks, st, sm + slot * AF_STAGE, lane);
       __syncwarp();
       if (lane == 0) bar_arrive(b_empty + 8 * slot);
     }
@@ -358,7 +414,7 @@ __global__ void __launch_bounds__(AF_THREADS, 2) attend_few_kernel(const __grid_
 // CTAs of four warps), over 300 slots 55 us (79; its bytes at the copy rate: 48);
 // 1,000 over up to 200 slots 63 us (159).  Two stages: 14, 65, 57; four: 17, 69, 73.
 constexpr uint32_t AS_STAGES = 3, AS_STAGE = 8192;
-template <typename T, int DP>
+template <typename T, int DP, bool B>
 __global__ void __launch_bounds__(32) attend_short_kernel(const __grid_constant__ AttendFewArgs g) {
   using S = FewShape<DP, AS_STAGE>;
   constexpr int KEYS = S::KEYS;
@@ -380,7 +436,8 @@ __global__ void __launch_bounds__(32) attend_short_kernel(const __grid_constant_
   const SeqInfo q = seq_info(a.c, a.r, seq, a.err);
   if (q.n == 0) return;
   const uint32_t rows = q.n * G;
-  const SlotTiles<KEYS> slots(key_span(q, a.r, 0, q.n), g.box);
+  const FewSpan<B> ks = few_span<B>(a, q);
+  const FewTiles<B, KEYS> slots(ks, g.box);
   const uint32_t n = slots.n;
   const uint32_t boxes = KEYS / g.box, ahead = 32 / boxes;   // boxes of a stage, a lane each; stages whose pages the lanes hold
   auto has_box = [&](const SlotTile& st, uint32_t j) { return j < st.hi && j + g.box > st.lo; };
@@ -418,13 +475,13 @@ __global__ void __launch_bounds__(32) attend_short_kernel(const __grid_constant_
     }
   };
   for (uint32_t t = 0; t < min(n, AS_STAGES); ++t) issue(t);
-  FewRows<T, DP, AS_STAGE> f;
+  FewRows<T, DP, B, AS_STAGE> f;
   f.clear();
   f.load(a, q, kh, rows, lane);
   for (uint32_t t = 0; t < n; ++t) {
     bar_wait(b_full + 8 * (t % AS_STAGES), (t / AS_STAGES) & 1, &s_gave_up, a.err);
     if (has_given_up(&s_gave_up)) break;
-    f.stage(a, q, slots.at(t), sm + (t % AS_STAGES) * AS_STAGE, lane);
+    f.stage(a, q, ks, slots.at(t), sm + (t % AS_STAGES) * AS_STAGE, lane);
     __syncwarp();
     if (t + AS_STAGES < n) issue(t + AS_STAGES);
   }
@@ -454,14 +511,18 @@ size_t attend_few_partial(const AttendArgs& a) {
   return (size_t)a.tiles * a.c.n_heads * a.max_chunks * AF_ROWS * (dp + 2) * sizeof(float);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool B>
 static void launch_few(const LaunchCfg& L, const AttendFewArgs& g, bool alone) {
   if (alone) {
-    launch_k(L, K_ATTEND_ROWS, attend_short_kernel<T, DP>, g.a.tiles * g.a.c.n_heads, 32, 1024 + AS_STAGES * AS_STAGE, g);
+    launch_k(L, K_ATTEND_ROWS, attend_short_kernel<T, DP, B>, g.a.tiles * g.a.c.n_heads, 32, 1024 + AS_STAGES * AS_STAGE, g);
     return;
   }
-  launch_k(L, K_ATTEND_ROWS, attend_few_kernel<T, DP>, dim3(g.a.tiles * g.a.c.n_heads, g.a.max_chunks), AF_THREADS,
+  launch_k(L, K_ATTEND_ROWS, attend_few_kernel<T, DP, B>, dim3(g.a.tiles * g.a.c.n_heads, g.a.max_chunks), AF_THREADS,
            FewShape<DP>::SMEM, g, dim3(1, g.cluster ? g.a.max_chunks : 1));
+}
+template <typename T, int DP>
+static void launch_few(const LaunchCfg& L, const AttendFewArgs& g, bool alone) {
+  g.a.biased ? launch_few<T, DP, true>(L, g, alone) : launch_few<T, DP, false>(L, g, alone);
 }
 void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool cluster, bool alone) {
   AttendFewArgs g;
@@ -478,18 +539,23 @@ void launch_attend_few(const LaunchCfg& L, const AttendArgs& a, int dtype, bool 
     narrow ? launch_few<__half, 64>(L, g, alone) : launch_few<__half, 128>(L, g, alone);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool B>
 static cudaError_t allow() {
-  const cudaError_t e = cudaFuncSetAttribute(attend_short_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const cudaError_t e = cudaFuncSetAttribute(attend_short_kernel<T, DP, B>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)(1024 + AS_STAGES * AS_STAGE));
   return e != cudaSuccess ? e
-                          : cudaFuncSetAttribute(attend_few_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                          : cudaFuncSetAttribute(attend_few_kernel<T, DP, B>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)FewShape<DP>::SMEM);
 }
-cudaError_t prepare_attend_few_kernels() {
-  for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})
+template <bool B>
+static cudaError_t allow_all() {
+  for (cudaError_t e : {allow<__nv_bfloat16, 64, B>(), allow<__nv_bfloat16, 128, B>(), allow<__half, 64, B>(), allow<__half, 128, B>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
+}
+cudaError_t prepare_attend_few_kernels() {
+  const cudaError_t e = allow_all<false>();
+  return e != cudaSuccess ? e : allow_all<true>();
 }
 
 }  // namespace ro

@@ -56,10 +56,13 @@ struct TileShape {
 
 // A piece of work: a pair of row tiles of one sequence and head, and a run of
 // the slots they see.
+template <bool B>
 struct TileItem {
   uint64_t tok0, page0;
   int64_t first;             // slot of the chunk's first token
-  KeySpan span;
+  std::conditional_t<B, BiasSpan, KeySpan> span;
+  uint32_t len;              // biased: cached tokens; slots that every token of a row
+  uint32_t all_lo[2], all_hi[2];   // tile sees, but for those that see nothing
   uint32_t i0, i1;           // the chunk's tokens in the row tiles
   uint32_t kh, unit;         // head; (tile, head)
   uint32_t c0, n;            // the run's slot tiles
@@ -77,13 +80,78 @@ constexpr uint32_t AT_ITEMS = 2;
 // which runs dry could do.
 constexpr uint32_t AT_AHEAD = 8;
 
-template <typename T, int DP>
+// Scores in log2 of a row's products, in pairs: under a cap, and falling with the
+// distance from slot `pos` (columns from t0 on; `both`: slots behind pos count too).
+template <int N>
+__device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float ahead, bool both,
+                                            uint32_t (&x)[N]) {
+  if (b.cap_log2 != 0.f) {
+    float mx[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+      mx[(i / 2) & 3] = fmaxf(fmaxf(mx[(i / 2) & 3], fabsf(__uint_as_float(x[i]))), fabsf(__uint_as_float(x[i + 1])));
+    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * fabsf(b.to_z);
+    const uint64_t to_z = pair(b.to_z, b.to_z), to_y = pair(scale_log2, scale_log2);
+    auto near = [&](auto terms, auto term) {   // x in log2 times tanh(z) / z
+      constexpr int TERMS = decltype(terms)::value;
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        const uint64_t v = pair_bits(x[i], x[i + 1]), z = mul_pair(v, to_z), w = mul_pair(z, z);
+        uint64_t p = pair(term(TERMS), term(TERMS));
+#pragma unroll
+        for (int k = TERMS - 1; k >= 0; --k) p = fma_pair(p, w, pair(term(k), term(k)));
+        const uint64_t y = mul_pair(mul_pair(v, to_y), p);
+        x[i] = (uint32_t)y;
+        x[i + 1] = (uint32_t)(y >> 32);
+      }
+    };
+    if (!__any_sync(0xffffffffu, top > 0.5f))
+      near(std::integral_constant<int, TANH_SHORT_TERMS>(), [](int k) { return tanh_short_term(k); });
+    else if (!__any_sync(0xffffffffu, top > 1.f))
+      near(std::integral_constant<int, TANH_TERMS>(), [](int k) { return tanh_term(k); });
+    else
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])));
+  } else {
+    const uint64_t to_y = pair(scale_log2, scale_log2);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint64_t y = mul_pair(pair_bits(x[i], x[i + 1]), to_y);
+      x[i] = (uint32_t)y;
+      x[i + 1] = (uint32_t)(y >> 32);
+    }
+  }
+  if (b.slope) {
+    const uint64_t fall = pair(-slope, -slope), step = pair(-8.f, -8.f);
+    uint64_t d[4];             // distances of four pairs of columns, a chain each (whole numbers: exact to 2^24)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = pair(ahead - 2 * i, ahead - 2 * i - 1);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      uint64_t v = d[(i / 2) & 3];
+      d[(i / 2) & 3] = add_pair(v, step);
+      if (both) v &= 0x7FFFFFFF7FFFFFFFull;
+      const uint64_t y = fma_pair(fall, v, pair_bits(x[i], x[i + 1]));
+      x[i] = (uint32_t)y;
+      x[i + 1] = (uint32_t)(y >> 32);
+    }
+  }
+}
+// bits [lo, hi) of 32
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
+  const uint32_t below = hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u;
+  return lo >= 32 ? 0u : lo <= 0 ? below : below & ~((1u << lo) - 1u);
+}
+
+// B: biased (ro_cache_attend_biased).
+template <typename T, int DP, bool B>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
   using S = TileShape<DP>;
+  using Tiles = std::conditional_t<B, BiasTiles<AT_KEYS>, SlotTiles<AT_KEYS>>;
   const AttendArgs& a = g.a;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 10 + 2 * AT_ITEMS + 1];
-  __shared__ TileItem s_item[AT_ITEMS];
+  __shared__ TileItem<B> s_item[AT_ITEMS];
   __shared__ uint32_t s_tmem, s_gave_up;
   wait_predecessor();
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -127,7 +195,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   if (warp >= AT_SOFTMAX / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AT_REGS_OTHERS));
     // the k-th item, to a whole warp; released once its reader is done with it
-    auto item = [&](uint32_t k) -> const TileItem& {
+    auto item = [&](uint32_t k) -> const TileItem<B>& {
       bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
       return s_item[k % AT_ITEMS];
     };
@@ -142,7 +210,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       const uint32_t items = a.tiles * a.c.n_heads * a.max_chunks;
       uint32_t k = 0;
       for (uint32_t id = blockIdx.x;;) {
-        TileItem it = {};
+        TileItem<B> it = {};
         it.last = id >= items;
         bool some = true;
         if (!it.last) {
@@ -162,7 +230,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           }
           it.unit = tile * a.c.n_heads + it.kh;
           uint32_t s = 0, p = 0;
-          some = a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
+          const bool falling = !B || a.b.first == nullptr;   // a document's tiles see no more than it
+          some = falling && a.r.window == 0u && a.c.n_seqs <= 32 * FT_SEQS && a.r.max_new > 2 * g.toks
                      ? find_tile_heavy(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err)
                      : find_tile(a.r, a.c.n_seqs, tile, 2 * g.toks, &s, &p, a.err);
           if (some) {
@@ -173,8 +242,18 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
             it.i0 = p * 2 * g.toks;
             it.i1 = min(q.n, it.i0 + 2 * g.toks);
             some = it.i0 < it.i1;
-            it.span = key_span(q, a.r, it.i0, max(it.i1, it.i0));
-            const uint32_t n = SlotTiles<AT_KEYS>(it.span, g.box).n;
+            if constexpr (B) {
+              it.len = q.len;
+              it.span = bias_span(q, a.r, a.b, it.i0, max(it.i1, it.i0));
+              for (uint32_t w = 0; w < 2; ++w) {
+                const BiasSpan half = bias_span(q, a.r, a.b, min(it.i1, it.i0 + w * g.toks), min(it.i1, it.i0 + (w + 1) * g.toks));
+                it.all_lo[w] = half.all_lo;
+                it.all_hi[w] = half.total ? half.all_hi : 0u;
+              }
+            } else {
+              it.span = key_span(q, a.r, it.i0, max(it.i1, it.i0));
+            }
+            const uint32_t n = Tiles(it.span, g.box).n;
             const uint32_t per = max(a.chunk, n / a.max_chunks + 1);   // slot tiles of a run
             it.n_runs = max(1u, (n + per - 1) / per);
             it.c0 = it.run * per;
@@ -207,11 +286,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       const uint32_t boxes = AT_KEYS / g.box;
       uint32_t slot = 0, parity = 1, uses = 0, qi = 0;   // parity of the ring's round before
       for (uint32_t k = 0;; ++k) {
-        const TileItem& it = item(k);
+        const TileItem<B>& it = item(k);
         if (it.last || has_given_up(&s_gave_up)) break;
         const uint32_t n = it.n, c0 = it.c0, kh = it.kh;
         const uint64_t page0 = it.page0;
-        const SlotTiles<AT_KEYS> slots(it.span, g.box);
+        const Tiles slots(it.span, g.box);
         if (n > 0) {
           if (qi > 0) bar_wait(b_qe, (qi - 1) & 1, &s_gave_up, a.err);
           if (lane == 0) {
@@ -294,7 +373,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         if (++slot == S::SLOTS) slot = 0, parity ^= 1;
       };
       for (uint32_t k = 0;; ++k) {
-        const TileItem& it = item(k);
+        const TileItem<B>& it = item(k);
         if (it.last || has_given_up(&s_gave_up)) break;
         const uint32_t n = it.n;
         release(k);
@@ -357,10 +436,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   uint32_t tiles = 0, vslot = 1, vpar = 0, done = 0;       // tiles so far; the ring's place of V; items with slots so far
   for (uint32_t k = 0;; ++k) {
     bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
-    const TileItem& it = s_item[k % AT_ITEMS];
+    const TileItem<B>& it = s_item[k % AT_ITEMS];
     if (it.last || has_given_up(&s_gave_up)) break;
     const uint32_t n = it.n, c0 = it.c0, i1 = it.i1, n_runs = it.n_runs;
-    const SlotTiles<AT_KEYS> slots(it.span, g.box);
+    const Tiles slots(it.span, g.box);
     const uint32_t j0 = it.i0 + w * g.toks, j1 = min(i1, j0 + g.toks);   // the row tile's tokens
     const bool live = j0 < i1;
     const uint32_t tok = j0 + row / G, head = it.kh * G + row % G;
@@ -368,8 +447,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     const int64_t pos = it.first + tok;                    // the row's slot
     // The run's tiles whose every slot every row of this row tile sees: those
     // of the sinks before `sinks_all`, and [all_from, all_to).
-    uint32_t sinks_all, all_from, all_to;
-    {
+    uint32_t sinks_all = 0, all_from = 0, all_to = 0;
+    // biased: what the row sees, how fast its scores fall; its row tile and its CTA together
+    RowSee see = {0, 0, 0, 0};
+    float slope = 0.f;
+    uint32_t all_lo = 0, all_hi = 0, holes = 0, s_end = 0;
+    SeqInfo q = {};
+    if constexpr (B) {
+      q.tok0 = it.tok0;
+      q.first = it.first;
+      q.len = it.len;
+      all_lo = it.all_lo[w];
+      all_hi = it.all_hi[w];
+      holes = it.span.holes;
+      s_end = it.span.s_lo + it.span.s_n;
+      if (mine) {
+        see = row_see(q, a.r, a.b, tok);
+        if (a.b.slope) slope = a.b.slope[head] * LOG2E;
+      }
+    } else {
       const int64_t a_lo = it.first + j0, a_hi = it.first + (live ? j1 : j0 + 1) - 1;
       const int64_t from = max((int64_t)slots.lo, a.r.window ? a_hi - (int64_t)a.r.window + 1 : (int64_t)0);
       const int64_t to = min((int64_t)slots.hi, a_lo + 1);
@@ -383,10 +479,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     }
     const uint64_t out_at = (it.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
     const uint64_t lse_at = (it.tok0 + tok) * a.n_q_heads + head;
-    const uint32_t unit = it.unit, run = it.run;
+    const uint32_t unit = it.unit, run = it.run, i0 = it.i0;
+    const bool sees_some = B ? see.some() : mine;
+    // (rows that see nothing have no say in the others' maximum, and are set to nothing at the end)
+    const bool voter = mine && sees_some;
+    // Scores under a cap of at most 2^80 need no running maximum where the weights
+    // have the exponents of 32 bits: no weight, sum or product leaves their range.
+    const bool held = B && std::is_same_v<T, __nv_bfloat16> && a.b.cap_log2 != 0.f && a.b.cap_log2 <= 80.f && !a.b.slope;
     __syncwarp();
     if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
-    float m = -INFINITY, l = 0.f;
+    float m = held ? 0.f : -INFINITY, l = 0.f;
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
@@ -394,8 +496,41 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 #pragma unroll
       for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
       tc_wait_ld(x);
-      const bool all = t < sinks_all || (t >= all_from && t < all_to);
-      if (!all) {
+      bool all = t < sinks_all || (t >= all_from && t < all_to);
+      if constexpr (B) {
+        const SlotTile st = slots.at(c0 + t);
+        all = !st.sink && st.t0 >= all_lo && st.t0 + AT_KEYS <= all_hi;
+        const float ahead = (float)(pos - (int64_t)st.t0);
+        bias_scores(a.b, scale, slope, ahead, a.b.until != nullptr, x);
+        if (!all) {
+          const int t0 = (int)st.t0, lo = (int)st.lo - t0, hi = (int)st.hi - t0;
+          const int c_lo = max((int)see.c0 - t0, lo), c_hi = min((int)see.c1 - t0, hi);
+          const int a_lo = max((int)see.a0 - t0, lo), a_hi = min((int)see.a1 - t0, hi);
+#pragma unroll
+          for (int k = 0; k < AT_KEYS / 32; ++k) {
+            const uint32_t in = bits_between(c_lo - 32 * k, c_hi - 32 * k) | bits_between(a_lo - 32 * k, a_hi - 32 * k);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(in >> i & 1u)) x[32 * k + i] = 0xff800000u;
+          }
+          // Values no row sees must not reach the product (see below).
+          if (w == 0 && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS || holes)) {
+            bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
+            const uint32_t j = st.t0 + row;
+            if (j < st.lo || j >= st.hi || !somebody_sees(q, a.r, a.b, holes, s_end, i0, i1, j)) {
+#pragma unroll
+              for (uint32_t i = 0; i < S::BLOCKS; ++i)
+#pragma unroll
+                for (uint32_t z = 0; z < 8; ++z)
+                  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
+                                                                            i * S::BLOCK_BYTES + row * 128 + z * 16),
+                               "r"(0u)
+                               : "memory");
+            }
+            fence_async_smem();
+          }
+        }
+      } else if (!all) {
         const SlotTile st = slots.at(c0 + t);
         // columns [b, e) count; of those the ones below `sinks` or from the window's first on
         const int64_t t0 = st.t0;
@@ -428,42 +563,45 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           fence_async_smem();
         }
       }
-      float mx[8];   // eight chains: one of 128 would cost its latency 128 times
+      if (!held) {
+        float mx[8];   // eight chains: one of 128 would cost its latency 128 times
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+        for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
 #pragma unroll
-      for (int i = 16; i < AT_KEYS; i += 2)
-        mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
-      const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
-                                      fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * scale);
-      if (__any_sync(0xffffffffu, mine && mn > m + AT_SLACK<T>)) {
-        // The maximum moves for the whole warp: rescale what was summed so far.
-        // (Rows that are no token's have no say: theirs may hold whatever an
-        // earlier kernel left, and would decide how the others are rounded.)
-        const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
-        m = mn;
-        l *= f;
-        if (t > 0) {
-          uint32_t o[16];
+        for (int i = 16; i < AT_KEYS; i += 2)
+          mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
+        const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
+                                        fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * (B ? 1.f : scale));
+        if (__any_sync(0xffffffffu, voter && mn > m + AT_SLACK<T>)) {
+          // The maximum moves for the whole warp: rescale what was summed so far.
+          // (Rows that are no token's have no say: theirs may hold whatever an
+          // earlier kernel left, and would decide how the others are rounded.)
+          const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
+          m = mn;
+          l *= f;
+          if (t > 0) {
+            uint32_t o[16];
 #pragma unroll 1
-          for (int i = 0; i < DP / 16; ++i) {
-            tc_ld16(to + i * 16, o);
-            tc_wait_ld(o);
+            for (int i = 0; i < DP / 16; ++i) {
+              tc_ld16(to + i * 16, o);
+              tc_wait_ld(o);
 #pragma unroll
-            for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
-            tc_st16(to + i * 16, o);
+              for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
+              tc_st16(to + i * 16, o);
+            }
           }
         }
       }
       const float sub = (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>;   // -inf: a row that has seen nothing yet
-      const uint64_t scale2 = pair(scale, scale), sub2 = pair(-sub, -sub);
+      const uint64_t scale2 = B ? pair(1.f, 1.f) : pair(scale, scale), sub2 = pair(-sub, -sub);
       uint64_t sum[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t p[16];
 #pragma unroll
         for (int z = 0; z < 16; ++z) {
-          const uint64_t y = fma_pair(pair_bits(x[i * 32 + 2 * z], x[i * 32 + 2 * z + 1]), scale2, sub2);
+          const uint64_t s2 = pair_bits(x[i * 32 + 2 * z], x[i * 32 + 2 * z + 1]);
+          const uint64_t y = B ? add_pair(s2, sub2) : fma_pair(s2, scale2, sub2);
           const float e0 = ex2(pair_lo(y)), e1 = ex2(pair_hi(y));
           sum[z & 3] = add_pair(sum[z & 3], pair(e0, e1));
           p[z] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
@@ -497,6 +635,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 #pragma unroll
       for (int i = 0; i < DP; ++i) o[i] = 0u;
     }
+    if constexpr (B)
+      if (!sees_some) {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < DP; ++i) o[i] = 0u;
+      }
     const uint32_t prow = w * AT_ROWS + row;               // the row among the pair's 256
     constexpr uint32_t STEP = 2 * AT_ROWS;                 // rows of a run
     // four columns of a row together, rows next to one another: a warp's
@@ -595,7 +740,7 @@ size_t attend_tiles_partial(const AttendArgs& a) {
 template <typename T, int DP>
 static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
-  launch_k(L, K_ATTEND_TILES, attend_tiles_kernel<T, DP>, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), AT_THREADS,
+  launch_k(L, K_ATTEND_TILES, g.a.biased ? attend_tiles_kernel<T, DP, true> : attend_tiles_kernel<T, DP, false>, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), AT_THREADS,
            TileShape<DP>::SMEM, g);
   if (g.a.max_chunks > 1)
     launch_k(L, K_ATTEND_JOIN, attend_join_kernel<T, DP>, g.a.tiles * g.a.c.n_heads * (DP / 4), 2 * AT_ROWS, 0, g);
@@ -620,8 +765,11 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int
 
 template <typename T, int DP>
 static cudaError_t allow() {
-  return cudaFuncSetAttribute(attend_tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)TileShape<DP>::SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)TileShape<DP>::SMEM);
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(attend_tiles_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)TileShape<DP>::SMEM);
 }
 cudaError_t prepare_attend_tiles_kernels() {
   for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})

@@ -292,28 +292,51 @@ __device__ __forceinline__ bool somebody_sees(const SeqInfo& q, const RowsArgs& 
   return false;
 }
 
-// tanh(z) within 2^-22 of its value: a polynomial of z^2 fitted to tanh(z) / z
-// for |z| <= 1 (3.7e-9 off), and 1 - 2 / (1 + e^2z) beyond, where nothing cancels.
-constexpr float TANH_C1 = -0.3333328366279602f, TANH_C2 = 0.13332240283489227f, TANH_C3 = -0.05387570336461067f,
-                TANH_C4 = 0.02147844433784485f, TANH_C5 = -0.007937350310385227f, TANH_C6 = 0.002296661725267768f,
-                TANH_C7 = -0.00035745822242461145f;
-__device__ __forceinline__ float tanh_of(float z) {
-  const float w = z * z;
-  float p = TANH_C7;
-  p = fmaf(p, w, TANH_C6);
-  p = fmaf(p, w, TANH_C5);
-  p = fmaf(p, w, TANH_C4);
-  p = fmaf(p, w, TANH_C3);
-  p = fmaf(p, w, TANH_C2);
-  p = fmaf(p, w, TANH_C1);
-  p = fmaf(p, w, 1.f);
-  const float far = fmaf(-2.f, rcp(1.f + ex2(z * 2.885390081777927f)), 1.f);
-  return w <= 1.f ? z * p : far;
+// tanh(z) within 2^-22 of its value: z times a polynomial of z^2 fitted to
+// tanh(z) / z for |z| <= 1 (3.7e-9 off) or, shorter, for |z| <= 1/2 (1.3e-8
+// off), and 1 - 2 / (1 + e^2z) beyond, where nothing cancels.
+constexpr int TANH_TERMS = 7, TANH_SHORT_TERMS = 4;
+__device__ __forceinline__ constexpr float tanh_term(int i) {
+  constexpr float c[TANH_TERMS + 1] = {1.f, -0.3333328366279602f, 0.13332240283489227f, -0.05387570336461067f,
+                                       0.02147844433784485f, -0.007937350310385227f, 0.002296661725267768f,
+                                       -0.00035745822242461145f};
+  return c[i];
 }
-// A product q.k's score in log2, `apart` slots from the token; slope in log2.
-__device__ __forceinline__ float biased_score(const BiasArgs& b, float scale_log2, float dot, float slope, float apart) {
-  const float x = b.cap_log2 != 0.f ? b.cap_log2 * tanh_of(dot * b.to_z) : dot * scale_log2;
-  return fmaf(-slope, apart, x);
+__device__ __forceinline__ constexpr float tanh_short_term(int i) {
+  constexpr float c[TANH_SHORT_TERMS + 1] = {1.f, -0.33333075046539307f, 0.13324907422065735f, -0.052994247525930405f,
+                                             0.017151307314634323f};
+  return c[i];
+}
+__device__ __forceinline__ float tanh_ratio(float w) {   // tanh(z) / z of w = z^2 <= 1
+  float p = tanh_term(TANH_TERMS);
+#pragma unroll
+  for (int i = TANH_TERMS - 1; i >= 0; --i) p = fmaf(p, w, tanh_term(i));
+  return p;
+}
+__device__ __forceinline__ float tanh_far(float z) {
+  return fmaf(-2.f, rcp(1.f + ex2(z * 2.885390081777927f)), 1.f);
+}
+// A product q.k's score in log2 under a cap.
+__device__ __forceinline__ float capped(const BiasArgs& b, float dot) {
+  const float z = dot * b.to_z, w = z * z;
+  return b.cap_log2 * (w <= 1.f ? z * tanh_ratio(w) : tanh_far(z));
+}
+// Scores in log2 of a warp's products: where all lie within |z| <= 1, without the far form.
+template <int N>
+__device__ __forceinline__ void cap_scores(const BiasArgs& b, float (&x)[N]) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
+  if (__any_sync(0xffffffffu, top * fabsf(b.to_z) > 1.f)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = capped(b, x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = x[i] * b.to_z;
+      x[i] = b.cap_log2 * z * tanh_ratio(z * z);
+    }
+  }
 }
 
 // The slots that a CTA's rows see, cut into tiles of KEYS: tiles over the
@@ -340,6 +363,30 @@ struct SlotTiles {
     s.sink = t < sink_tiles;
     s.t0 = s.sink ? t * KEYS : first + (t - sink_tiles) * KEYS;
     s.lo = s.sink ? s.t0 : max(s.t0, lo);
+    s.hi = min(s.t0 + KEYS, s.sink ? s_hi : hi);
+    return s;
+  }
+};
+
+// The same of a biased span, whose sinks start at a document's first slot.
+template <int KEYS>
+struct BiasTiles {
+  uint32_t s_lo, s_hi, s_first, lo, hi, first, sink_tiles, n;
+  __device__ __forceinline__ BiasTiles(const BiasSpan& ks, uint32_t box) {
+    s_lo = ks.s_lo;
+    s_hi = ks.s_lo + ks.s_n;
+    s_first = s_lo & ~(box - 1u);
+    lo = ks.lo;
+    hi = ks.lo + (ks.total - ks.s_n);
+    first = lo & ~(box - 1u);
+    sink_tiles = s_hi > s_lo ? (s_hi - s_first + KEYS - 1) / KEYS : 0;
+    n = sink_tiles + (hi > lo ? (hi - first + KEYS - 1) / KEYS : 0);
+  }
+  __device__ __forceinline__ SlotTile at(uint32_t t) const {
+    SlotTile s;
+    s.sink = t < sink_tiles;
+    s.t0 = s.sink ? s_first + t * KEYS : first + (t - sink_tiles) * KEYS;
+    s.lo = max(s.t0, s.sink ? s_lo : lo);
     s.hi = min(s.t0 + KEYS, s.sink ? s_hi : hi);
     return s;
   }

@@ -216,7 +216,7 @@ ro_status attend(const char* fn, StepCall& c, const ro_cache* cache, const uint6
   const uint64_t max_rows = (uint64_t)a.r.max_new * group;
   void* p = nullptr;
   // At most 16 rows a sequence: bound by the cache's bytes.
-  if (max_rows <= 16 && !bias) {
+  if (max_rows <= 16) {
     const uint64_t work = (uint64_t)cache->n_seqs * cache->n_heads, stage = attend_few_keys(cache->head_dim);
     if (work > MAX_GRID) return c.refuse(RO_E_OVERFLOW, "%s: too many sequences and heads", fn);
     a.tiles = cache->n_seqs;
@@ -252,7 +252,7 @@ ro_status attend(const char* fn, StepCall& c, const ro_cache* cache, const uint6
     return c.launched(fn);
   }
   // More: the tensor-core kernel, if the pages and the group fit its tiles.
-  if (!bias && attend_tiles_fits(a)) {
+  if (attend_tiles_fits(a)) {
     const uint32_t toks = attend_tile_tokens(group);
     const uint64_t tiles = a.r.max_new <= toks ? (uint64_t)cache->n_seqs : n_tokens / toks + cache->n_seqs + 1;
     const uint64_t work = tiles * cache->n_heads, slots = ceil_div(keys, 128);
