@@ -35,6 +35,21 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 __device__ __forceinline__ float key_logit(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
+// an item of CTA `rank` of the cluster: added to, fetched and added to, written
+__device__ __forceinline__ void cluster_count(const uint32_t* p, uint32_t rank) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], 1;" ::"r"(cluster_at(step_smem(p), rank)) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_take(const uint32_t* p, uint32_t rank, uint32_t n) {
+  uint32_t v;
+  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;"
+               : "=r"(v)
+               : "r"(cluster_at(step_smem(p), rank)), "r"(n)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_write(const unsigned long long* p, uint32_t rank, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "l"(v) : "memory");
+}
 template <class V>
 __device__ __forceinline__ V cluster_read(const V* p, uint32_t rank) {
   static_assert(sizeof(V) == 4 || sizeof(V) == 8, "a word or two");
@@ -89,10 +104,45 @@ __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_
 template <>
 __device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xFF80); }
 
+// Sorts the first n of v, a power of two, by one CTA: falling or rising.
+// (Exchanges over at most 32 places stay within a warp's 64 items.)
+__device__ __forceinline__ void sort_items(unsigned long long* v, uint32_t n, bool falling) {
+  const uint32_t t = threadIdx.x;
+  for (uint32_t size = 2; size <= n; size *= 2)
+    for (uint32_t step = size / 2; step > 0; step /= 2) {
+      if (step >= 32 || size == 2)
+        __syncthreads();
+      else
+        __syncwarp();
+      for (uint32_t c = t; c < n / 2; c += SM_THREADS) {
+        const uint32_t i = 2 * c - (c & (step - 1)), j = i + step;
+        const unsigned long long a = v[i], b = v[j];
+        if ((a < b) == (((i & size) == 0) == falling) && a != b) {
+          v[i] = b;
+          v[j] = a;
+        }
+      }
+    }
+  __syncthreads();
+}
+__device__ const unsigned long long EXP_COARSE[32] = {RO_EXP_COARSE}, EXP_FINE[32] = {RO_EXP_FINE};
+
 // What a row's tokens have to pass: keys above `key`, and the first `ties` equal to it.
 struct Threshold {
   uint32_t key, ties;
 };
+
+// A row's candidates: the few tokens that can stay, where settings leave few.
+constexpr uint32_t SM_LIST = 1024;
+static_assert(2 * SM_LIST <= SM_BINS, "candidates and their weights lie where the bins do");
+// Tokens that the candidates are meant to hold where top-p alone decides, and at
+// most; and of the threads' largest logits.
+constexpr uint32_t SM_WANT = 512, SM_WANT_MOST = 704;
+constexpr uint32_t SM_COARSE = 512;
+// What 32-bit weights and their sum may be off, relative to the sum: the
+// argument, below 64, by 2^-23 of itself, and roundings of 2^-22.
+constexpr double SM_SLACK = 1.0 / (1 << 16);
+enum SampleWay : uint32_t { WAY_DONE, WAY_MASS, WAY_WIDE };
 
 struct SampleShared {
   unsigned long long mass[SM_BINS];
@@ -100,6 +150,11 @@ struct SampleShared {
   unsigned long long warp_mass[SM_WARPS];
   uint32_t warp_ties[SM_WARPS], warp_count[SM_WARPS];
   unsigned long long best;                 // key and ~place of the largest logit
+  uint32_t least;                          // key of the threads' smallest maximum
+  uint32_t coarse[SM_COARSE];              // the threads' maxima, counted by distance from the largest
+  uint32_t cut, listed, way;
+  float rough;                             // the sum of all weights in 32 bits
+  float warp_rough[SM_WARPS];
   unsigned long long scan[SM_WARPS];
   unsigned long long found_left;
   uint32_t found;
@@ -178,11 +233,25 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
       for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
       if (lane == 0) s.best = b;
     }
+    const uint32_t low = __reduce_min_sync(0xffffffffu, top == -INFINITY ? ~0u : logit_key(top));
+    if (lane == 0) s.warp_count[warp] = low;
+    for (uint32_t i = tid; i < SM_COARSE; i += SM_THREADS) s.coarse[i] = 0;
+    if (tid == 0) s.listed = 0;
+    __syncthreads();
+    if (warp == 0) {
+      const uint32_t all = __reduce_min_sync(0xffffffffu, lane < SM_WARPS ? s.warp_count[lane] : ~0u);
+      if (lane == 0) s.least = all;
+    }
   }
+  const float my_top = top;
   sync();
   unsigned long long best = s.best;
+  uint32_t least = s.least;
   if (nc > 1)
-    for (uint32_t r = 0; r < nc; ++r) best = max(best, cluster_read(&s.best, r));
+    for (uint32_t r = 0; r < nc; ++r) {
+      best = max(best, cluster_read(&s.best, r));
+      least = min(least, cluster_read(&s.least, r));
+    }
   const float T_ = s.temperature, top_p = s.top_p;
   uint32_t top_k = s.top_k;
   auto finish = [&](uint32_t token, float logp, uint32_t kept) {
@@ -205,8 +274,7 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
   // ---- weights ----
   const double c = 1.4426950408889634074 / (double)T_;
   const ExpScale scale = {(float)c, (float)(c - (double)(float)c)};
-  const unsigned long long coarse_of[32] = {RO_EXP_COARSE}, fine_of[32] = {RO_EXP_FINE};
-  const unsigned long long my_coarse = coarse_of[lane], my_fine = fine_of[lane];
+  const unsigned long long my_coarse = EXP_COARSE[lane], my_fine = EXP_FINE[lane];
   // of a whole warp's logits; 0 where !in
   auto weight = [&](float y, bool in) -> uint64_t {
     const uint64_t z = in ? exp_argument(top, y, scale) : ~0ull;
@@ -221,8 +289,8 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
   // ---- thresholds ----
   Threshold th = {KEY_NONE, 0};
   if (s.min_p > 0.f) {   // w >= min_p; the smallest such float
-    const float least = __double2float_ru((double)top + (double)T_ * log((double)s.min_p));
-    th.key = max(KEY_NONE, logit_key(least) - 1u);
+    const float least_x = __double2float_ru((double)top + (double)T_ * log((double)s.min_p));
+    th.key = max(KEY_NONE, logit_key(least_x) - 1u);
   }
   // Every thread's items of a pass: this CTA's blocks, a warp's side by side, all warps alike in number.
   const uint32_t rounds = (n + SM_THREADS - 1) / SM_THREADS;
@@ -358,6 +426,226 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
     sync();   // read by all before it is written again
     return t;
   };
+
+  // ---- few candidates ----
+  // At least `want` tokens lie at or above the want-th largest of the threads'
+  // maxima, and seldom many more.  Where top-k, top-p or min-p leaves only some
+  // of those, they are gathered and sorted by the first CTA, and the rest of the
+  // row is not looked at again.  The sum that top-p is a share of is first taken
+  // in 32 bits; only if a border lies within what that may be off, exactly.
+  const bool by_k = top_k != 0u && top_k < a.vocab, by_p = top_p < 1.f, by_min = s.min_p > 0.f;
+  const uint32_t threads = nc * SM_THREADS, most = min(SM_WANT_MOST, threads * 3 / 4);
+  uint32_t way = WAY_WIDE;
+  if ((by_k || by_p || by_min) && top < INFINITY) {
+    const uint32_t want = by_k && top_k <= most ? top_k : min(SM_WANT, most);
+    const bool all_of_k = by_k && top_k <= most;   // the candidates hold the first top_k
+    // maxima counted by how far they lie below the largest
+    // (as far as weights go: beyond 45 T they are below 2^-64)
+    const float per_bin = (float)SM_COARSE / fmaxf(fminf(top - key_logit(least), 45.f * T_), 1e-30f);
+    auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_COARSE - 1)); };
+    if (my_top > -INFINITY) {
+      const uint32_t b = bin_of(my_top);
+      if (nc > 1)
+        for (uint32_t r = 0; r < nc; ++r) cluster_count(&s.coarse[b], r);
+      else
+        atomicAdd(&s.coarse[b], 1u);
+    }
+    if (by_p && !all_of_k) {
+      float sum = 0.f;
+      for (uint32_t i = tid; i < n; i += SM_THREADS) {
+        const uint4 v = slice[i];
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k) {
+          const float y = Logits<T>::at(v, k);
+          if (y > -INFINITY) {                      // (and no NaN)
+            const float d = top - y, z = d * scale.hi, e = fmaf(d, scale.lo, fmaf(d, scale.hi, -z));
+            if (z < 64.f) sum = fmaf(ex2(-z), fmaf(e, -LN2, 1.f), sum);
+          }
+        }
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) s.warp_rough[warp] = sum;
+    }
+    sync();
+    // the bin at which `want` maxima are reached: its far end is the cut
+    static_assert(SM_COARSE == SM_THREADS, "a bin a thread");
+    if (tid == 0) {
+      s.cut = SM_COARSE;
+      float sum = 0.f;
+      for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
+      s.rough = sum;
+    }
+    const uint32_t mine = s.coarse[tid], inc = warp_incl_scan(mine);
+    if (lane == 31) s.warp_count[warp] = inc;
+    __syncthreads();
+    uint32_t before = inc - mine;
+    for (uint32_t w = 0; w < warp; ++w) before += s.warp_count[w];
+    if (before < want && before + mine >= want) s.cut = tid;
+    __syncthreads();
+    const uint32_t cut = s.cut;                      // SM_COARSE: fewer maxima than wanted, so every token
+    const bool with_min = by_min && !all_of_k;       // (top-p's sum is over the first top_k, whatever min-p says)
+    auto candidate = [&](float y) {
+      return y > -INFINITY && (cut == SM_COARSE || bin_of(y) <= cut) && (!with_min || logit_key(y) > th.key);
+    };
+    if (candidate(my_top))
+      for (uint32_t i = tid; i < n; i += SM_THREADS) {
+        const uint4 v = slice[i];
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k) {
+          const float y = Logits<T>::at(v, k);
+          if (!candidate(y)) continue;
+          const unsigned long long item = (unsigned long long)logit_key(y) << 32 | ~((b0 + i) * E + k - off);
+          if (nc > 1) {
+            const uint32_t at = cluster_take(&s.listed, 0, 1u);
+            if (at < SM_LIST) cluster_write(&s.mass[at], 0, item);
+          } else {
+            const uint32_t at = atomicAdd(&s.listed, 1u);
+            if (at < SM_LIST) s.mass[at] = item;
+          }
+        }
+      }
+    sync();
+    // ---- the first CTA's ----
+    unsigned long long* list = s.mass;
+    unsigned long long* weights = s.mass + SM_LIST;
+    // Whether every token that min-p leaves is a candidate, or every token.
+    const uint32_t listed = rank == 0 ? s.listed : 0;
+    uint64_t own[2] = {0, 0}, ahead[2] = {0, 0};               // weights of this thread's two candidates, and of those ahead
+    bool whole = false;
+    double rough = 0.0;
+    // how many stay, given the sum that top-p is a share of; false: not the tokens alone decide
+    auto count_below = [&](uint64_t limit, uint32_t first) -> uint32_t {
+      const uint32_t mine2 = (2 * tid < first && ahead[0] < limit) + (2 * tid + 1 < first && ahead[1] < limit);
+      return (uint32_t)__syncthreads_count(mine2 >= 1) + (uint32_t)__syncthreads_count(mine2 >= 2);
+    };
+    uint32_t stay = 0, first = 0;
+    if (rank == 0) {
+      way = WAY_WIDE;
+      if (listed > 0 && listed <= SM_LIST) {
+        uint32_t size = 2;
+        while (size < listed) size *= 2;
+        for (uint32_t i = listed + tid; i < size; i += SM_THREADS) list[i] = 0;
+        sort_items(list, size, true);
+        uint64_t sum = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          const uint32_t i = 2 * tid + j;
+          own[j] = weight(key_logit((uint32_t)(list[min(i, SM_LIST - 1)] >> 32)), i < listed);
+          if (i < listed) weights[i] = own[j];
+          sum += own[j];
+        }
+        const uint64_t run = warp_incl_scan(sum);
+        if (lane == 31) s.scan[warp] = run;
+        __syncthreads();
+        uint64_t base = run - sum;
+        for (uint32_t w = 0; w < warp; ++w) base += s.scan[w];
+        ahead[0] = base;
+        ahead[1] = base + own[0];
+        uint64_t list_mass = 0;
+        for (uint32_t w = 0; w < SM_WARPS; ++w) list_mass += s.scan[w];
+        // min-p's
+        uint32_t by_limit = listed;
+        if (by_min) {
+          const uint32_t in = (2 * tid < listed && (uint32_t)(list[2 * tid] >> 32) > th.key) +
+                              (2 * tid + 1 < listed && (uint32_t)(list[2 * tid + 1] >> 32) > th.key);
+          by_limit = (uint32_t)__syncthreads_count(in >= 1) + (uint32_t)__syncthreads_count(in >= 2);
+        }
+        // every token that counts for the outcome of top-k and min-p is listed:
+        // all of them, the first top_k, or all that min-p leaves
+        whole = cut == SM_COARSE || all_of_k || by_limit < listed || (with_min && bin_of(key_logit(th.key + 1u)) <= cut);
+        first = all_of_k ? min(top_k, listed) : listed;
+        stay = min(first, by_limit);
+        if (!by_p) {
+          if (by_k) stay = min(stay, top_k);
+          way = whole ? WAY_DONE : WAY_WIDE;
+        } else if (all_of_k || (cut == SM_COARSE && !with_min && !by_k)) {   // the sum is the listed ones'
+          const uint64_t sum_first = first == listed ? list_mass : [&] {
+            if (tid == first / 2) s.found_left = ahead[first & 1];
+            __syncthreads();
+            return (uint64_t)s.found_left;
+          }();
+          stay = min(stay, max(1u, count_below(scaled(sum_first, top_p, true), first)));
+          way = WAY_DONE;
+        } else if (!by_k) {
+          if (nc > 1) {
+            for (uint32_t r = 0; r < nc; ++r) rough += (double)__uint_as_float(cluster_read((const uint32_t*)&s.rough, r));
+          } else {
+            rough = (double)s.rough;
+          }
+          rough *= exp2((double)a.frac_bits) * (double)top_p;
+          const uint32_t lo = max(1u, count_below((uint64_t)(rough * (1.0 - SM_SLACK)), listed));
+          const uint32_t hi = max(1u, count_below((uint64_t)(rough * (1.0 + SM_SLACK)) + 2, listed));
+          // (hi == listed: top-p may leave tokens that are not listed)
+          if (!whole && hi == listed)
+            way = WAY_WIDE;
+          else if (min(lo, stay) == min(hi, stay))
+            way = WAY_DONE, stay = min(lo, stay);
+          else
+            way = WAY_MASS;
+        }
+      }
+      if (tid < nc) {   // to every CTA's own: this one may be gone before they look
+        if (nc > 1)
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_at(step_smem(&s.way), tid)), "r"(way) : "memory");
+        else
+          s.way = way;
+      }
+    }
+    sync();
+    way = s.way;
+    if (way == WAY_MASS) {
+      const Threshold keep = th;
+      th = {KEY_NONE, 0};
+      const uint64_t sum = sums(true).mass;
+      th = keep;
+      if (rank == 0) stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), listed)));
+      way = WAY_DONE;
+    }
+    if (way == WAY_DONE) {
+      if (rank == 0) {
+        // the sum of those that stay, then where it passes the goal, by index
+        if (2 * tid < stay && stay <= 2 * tid + 2) s.found_left = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
+        __syncthreads();
+        const uint64_t total = s.found_left, goal = scaled(total, s.u, false);
+        uint32_t size = 2;
+        while (size < stay) size *= 2;
+        unsigned long long item[2];
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) item[j] = 2 * tid + j < stay ? list[2 * tid + j] : 0;
+        __syncthreads();
+        // places rise, and each remembers its candidate; keys and weights stay where they are
+        unsigned long long* order = (unsigned long long*)s.count;   // 1,024 of them
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j)
+          if (2 * tid + j < size)
+            order[2 * tid + j] = 2 * tid + j < stay ? (unsigned long long)~(uint32_t)item[j] << 32 | (2 * tid + j) : ~0ull;
+        sort_items(order, size, false);
+        uint64_t w2[2], sum = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          w2[j] = 2 * tid + j < stay ? weights[(uint32_t)order[2 * tid + j]] : 0;
+          sum += w2[j];
+        }
+        const uint64_t run = warp_incl_scan(sum);
+        if (lane == 31) s.scan[warp] = run;
+        __syncthreads();
+        uint64_t at = run - sum;
+        for (uint32_t w = 0; w < warp; ++w) at += s.scan[w];
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          if (goal >= at && goal < at + w2[j]) {
+            const unsigned long long o = order[2 * tid + j];
+            const float y = key_logit((uint32_t)(list[(uint32_t)o] >> 32));
+            const double less = y == top ? 0.0 : ((double)top - (double)y) / (double)T_;
+            finish((uint32_t)(o >> 32), -(float)(less + log((double)total * exp2(-(double)a.frac_bits))), stay);
+          }
+          at += w2[j];
+        }
+      }
+      return;
+    }
+  }
 
   if (top_k != 0u && top_k < a.vocab) {
     if (sums(false).count > top_k) {

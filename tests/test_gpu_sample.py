@@ -272,3 +272,35 @@ def test_refusals(ctx):
     assert token.tolist() == [0, 0, 0]
     ok(ctx, ro.ro_sample(ctx, dev, None, du, token))
     ok(ctx, ro.ro_ctx_sync(ctx))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows_of", [1, 30, 200])
+def test_borders_of_the_candidates(ctx, dtype, rows_of):
+    """Settings on either side of what is kept as a list of candidates: as many tokens as it holds, one more, twice as
+    many, all of them equal but a few, far outliers and far lows."""
+    V = 20_011
+    x, u = rows(rows_of, V, dtype, 21, spread=1.0)
+    for k in (383, 384, 385, 511, 512, 513, 704, 705, 1023, 1024, 1025, 2048, V - 1):
+        check(ctx, x[:4], u[:4], top_k=k, top_p=[1.0, 0.9, 0.999, 0.5][:min(4, rows_of)])
+    check(ctx, x[:4], u[:4], min_p=[0.2, 0.02, 0.002, 0.0002][:min(4, rows_of)], top_k=700)
+    check(ctx, x[:4], u[:4], min_p=[0.2, 0.02, 0.002, 0.0002][:min(4, rows_of)], top_p=0.97)
+    x[:, 100:1200] = x[:, :1]              # a run of equal ones, more than are listed
+    check(ctx, x[:4], u[:4], top_k=50, min_p=0.001)
+    check(ctx, x[:4], u[:4], top_p=0.3)
+    x[:, 7] = 3e4
+    check(ctx, x[:4], u[:4], top_k=50, top_p=0.999)
+    x[:, ::5] = -6e4
+    check(ctx, x[:4], u[:4], top_k=500, top_p=0.9, temperature=30.0)
+    check(ctx, x[:4], u[:4], top_p=0.9999, temperature=3e4)
+
+
+def test_sums_next_to_a_border(ctx):
+    """Equal tokens whose running sum meets top-p's share exactly, and one step to either side."""
+    n, V = 64, 40_960
+    x = torch.full((1, V), -30.0)
+    x[0, ::40] = 2.0                       # 1,024 equal ones
+    for p in (0.25, 0.5, 0.125, 0.75):
+        for q in (p, np.nextafter(np.float32(p), np.float32(0)), np.nextafter(np.float32(p), np.float32(1))):
+            check(ctx, x, torch.tensor([0.999]), top_p=float(q), top_k=1024)
+            check(ctx, x.expand(n, V)[:2], torch.tensor([0.2, 0.999]), top_p=float(q))
