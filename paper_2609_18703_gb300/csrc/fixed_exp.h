@@ -3,19 +3,22 @@
 //
 // A token is drawn by comparing u * (sum of the weights) with running sums.  In
 // 32-bit floats such a sum is off by 2^-22 or so, and one row in some hundred
-// would get its neighbour's token; integers are summed without error in any
+// would get its neighbour's token; whole numbers are summed without error in any
 // order, so what is left is each weight's own error.
 //
-//   w = 2^S e^-((max - x) / T) = 2^(S - z),  z = (max - x) log2(e) / T
+//   w = 2^B e^-((max - x) / T) = 2^(B - z),  z = (max - x) log2(e) / T,  B <= 50
 //
-// z is a product of two sums of two floats each (max - x with its rounding
-// error, log2(e) / T with its own), taken to 43 bits behind the point.  Of its
-// fraction ten bits choose 2^-(j/32) and 2^-(k/1024) from tables, and the rest r
-// < 2^-10 enters as 1 - 2^-r = t - t^2/2 + t^3/6 with t = r ln 2 (the next term
-// is below 2^-46).
+// in pairs of 32-bit floats (the GPU's 64-bit floats are few, its 64-bit
+// integers slow: a weight took 270 cycles of a warp's issue in integers, 60 in
+// pairs of floats): z from the difference with its rounding error and the factor
+// with its own; z = m / 32 + r, |r| <= 1 / 64, gives 2^-(m / 32) from a table and
+// an exponent, and 2^-r = 1 + g + g^2 / 2 + .. with g = -r ln 2, whose first two
+// terms are pairs (the fifth is below 2^-39, the sixth below 2^-48).  Every
+// operation is rounded as written: a weight is the same wherever it is computed.
 #pragma once
 
 #include <cstdint>
+#include <cstring>
 #ifndef __CUDACC__
 #include <cmath>
 #endif
@@ -30,71 +33,116 @@
 
 namespace ro {
 
-// floor(2^63 2^-(j/32)) and floor(2^63 2^-(j/1024))
-#define RO_EXP_COARSE \
-    0x8000000000000000ull, 0x7D41D96DB915019Dull, 0x7A92BE8A92436616ull, 0x77F25CCDEE6D7AE6ull, \
-    0x75606373EE921C97ull, 0x72DC8373BE41A454ull, 0x70666F76154A7089ull, 0x6DFDDBCBED791BABull, \
-    0x6BA27E656B4EB57Aull, 0x69540EC8F895722Dull, 0x6712460A8FC24072ull, 0x64DCDEC3371793D1ull, \
-    0x62B39508AA836D6Full, 0x6096266533384A2Bull, 0x5E8451CFAC061B5Full, 0x5C7DD7A3B17DCF75ull, \
-    0x5A827999FCEF3242ull, 0x5891FAC0E95612C8ull, 0x56AC1F752150A563ull, 0x54D0AD5A753E077Cull, \
-    0x52FF6B54D8A89C75ull, 0x513821818624B40Cull, 0x4F7A993048D088D7ull, 0x4DC69CDCEAA72A9Cull, \
-    0x4C1BF828C6DC54B8ull, 0x4A7A77D47F7B84B1ull, 0x48E1E9B9D588E19Bull, 0x47521CC5A2E6A9E0ull, \
-    0x45CAE0F1F545EB73ull, 0x444C0740496D4294ull, 0x42D561B3E6243D8Aull, 0x4166C34C5615D0ECull
-#define RO_EXP_FINE \
-    0x8000000000000000ull, 0x7FE9D3A8E07BF086ull, 0x7FD3AB290E46D769ull, 0x7FBD867FDF0ACB3Bull, \
-    0x7FA765ACA88F6453ull, 0x7F9148AEC0B9B7B1ull, 0x7F7B2F857D8C51E5ull, 0x7F651A30352731EEull, \
-    0x7F4F08AE3DC7C426ull, 0x7F38FAFEEDC8DD26ull, 0x7F22F1219BA2B4AEull, 0x7F0CEB159DEAE091ull, \
-    0x7EF6E8DA4B544F9Aull, 0x7EE0EA6EFAAF4479ull, 0x7ECAEFD302E950AFull, 0x7EB4F905BB0D4F78ull, \
-    0x7E9F06067A4360BAull, 0x7E8916D497D0E3F4ull, 0x7E732B6F6B18732Aull, 0x7E5D43D64B99DDD7ull, \
-    0x7E47600890F223DEull, 0x7E31800592DB7078ull, 0x7E1BA3CCA92D152Cull, 0x7E05CB5D2BDB84BEull, \
-    0x7DEFF6B672F84E24ull, 0x7DDA25D7D6B2177Full, 0x7DC458C0AF549908ull, 0x7DAE8F7055489813ull, \
-    0x7D98C9E62113E1FAull, 0x7D8308216B594720ull, 0x7D6D4A218CD895E5ull, 0x7D578FE5DE6E95A0ull
+// 2^-(j/32) in two floats
+#define RO_EXP_HI \
+    0x1.0000000000000p+0f, 0x1.f507660000000p-1f, 0x1.ea4afa0000000p-1f, 0x1.dfc9740000000p-1f, \
+    0x1.d5818e0000000p-1f, 0x1.cb720e0000000p-1f, 0x1.c199be0000000p-1f, 0x1.b7f7700000000p-1f, \
+    0x1.ae89fa0000000p-1f, 0x1.a5503c0000000p-1f, 0x1.9c49180000000p-1f, 0x1.93737c0000000p-1f, \
+    0x1.8ace540000000p-1f, 0x1.82589a0000000p-1f, 0x1.7a11480000000p-1f, 0x1.71f75e0000000p-1f, \
+    0x1.6a09e60000000p-1f, 0x1.6247ec0000000p-1f, 0x1.5ab07e0000000p-1f, 0x1.5342b60000000p-1f, \
+    0x1.4bfdae0000000p-1f, 0x1.44e0860000000p-1f, 0x1.3dea640000000p-1f, 0x1.371a740000000p-1f, \
+    0x1.306fe00000000p-1f, 0x1.29e9e00000000p-1f, 0x1.2387a60000000p-1f, 0x1.1d48740000000p-1f, \
+    0x1.172b840000000p-1f, 0x1.11301e0000000p-1f, 0x1.0b55860000000p-1f, 0x1.059b0e0000000p-1f
+#define RO_EXP_LO \
+    0x0.0p+0f, -0x1.246eb00000000p-27f, 0x1.52486c0000000p-28f, -0x1.908c940000000p-26f, \
+    -0x1.822dbc0000000p-28f, -0x1.8837cc0000000p-28f, -0x1.3d56b20000000p-28f, -0x1.a094380000000p-26f, \
+    -0x1.a94b140000000p-27f, -0x1.b83b540000000p-26f, 0x1.51f8480000000p-28f, -0x1.e647440000000p-26f, \
+    0x1.15506e0000000p-28f, -0x1.accc7c0000000p-27f, -0x1.829fd00000000p-26f, 0x1.1d8bee0000000p-26f, \
+    0x1.9fcef40000000p-27f, -0x1.f8b5500000000p-26f, -0x1.5bd5ec0000000p-28f, -0x1.2c56100000000p-26f, \
+    -0x1.593abc0000000p-26f, 0x1.8624b40000000p-31f, 0x1.8246840000000p-26f, -0x1.18aac60000000p-26f, \
+    0x1.4636e20000000p-26f, -0x1.5c04240000000p-26f, 0x1.ceac480000000p-26f, -0x1.d2e8ca0000000p-26f, \
+    -0x1.c157420000000p-28f, -0x1.fdb4960000000p-26f, 0x1.9f31220000000p-26f, -0x1.9d4f520000000p-26f
+
+constexpr uint32_t WEIGHT_BITS = 50;   // B at most
+
+#ifdef __CUDA_ARCH__
+#define RO_MUL(a, b) __fmul_rn(a, b)
+#define RO_ADD(a, b) __fadd_rn(a, b)
+#define RO_FMA(a, b, c) __fmaf_rn(a, b, c)
+#else   // (compiled without contraction)
+#define RO_MUL(a, b) ((a) * (b))
+#define RO_ADD(a, b) ((a) + (b))
+#define RO_FMA(a, b, c) fmaf(a, b, c)
+#endif
+RO_HD int32_t float_bits(float x) {
+#ifdef __CUDA_ARCH__
+  return __float_as_int(x);
+#else
+  int32_t i;
+  memcpy(&i, &x, 4);
+  return i;
+#endif
+}
+RO_HD float bits_float(int32_t i) {
+#ifdef __CUDA_ARCH__
+  return __int_as_float(i);
+#else
+  float x;
+  memcpy(&x, &i, 4);
+  return x;
+#endif
+}
 
 struct ExpScale {
   float hi, lo;   // log2(e) / T in two floats
 };
-RO_HD uint64_t mul_hi64(uint64_t a, uint64_t b) {
+struct Pair32 {
+  float hi, lo;
+};
+// z, x <= top, neither a NaN; its higher part is 64 or more (or NaN) for weights of 0.
+RO_HD Pair32 exp_argument(float top, float x, ExpScale c) {
+  const float d = x == top ? 0.f : RO_ADD(top, -x);
+  const float v = RO_ADD(d, -top);               // what d's rounding lost, exactly:
+  const float lost = x == top ? 0.f : RO_ADD(RO_ADD(top, -RO_ADD(d, -v)), RO_ADD(-x, -v));
+  Pair32 z;
+  z.hi = d == 0.f ? 0.f : RO_MUL(d, c.hi);
+  z.lo = d == 0.f ? 0.f : RO_FMA(lost, c.hi, RO_FMA(d, c.lo, RO_FMA(d, c.hi, -z.hi)));
+  return z;
+}
+// A weight in two whole numbers, hi 2^(B - 20) + lo (lo of either sign), and sums of a few.
+struct Weight {
+  int32_t hi;
+  int64_t lo;
+};
+RO_HD uint64_t whole(Weight w, uint32_t B) { return (uint64_t)(((int64_t)w.hi << (B - 20)) + w.lo); }
+RO_HD int32_t nearest(float x) {
 #ifdef __CUDA_ARCH__
-  return __umul64hi(a, b);
+  return __float2int_rn(x);
 #else
-  return (uint64_t)(((unsigned __int128)a * b) >> 64);
+  return (int32_t)lrintf(x);
 #endif
 }
-// z = (top - x) (c.hi + c.lo) in units of 2^-43; ~0 when it is 64 or more.
-// x <= top, neither a NaN; equal ones give 0.
-RO_HD uint64_t exp_argument(float top, float x, ExpScale c) {
-  if (x == top) return 0;
-  const float d = top - x;                       // and what its rounding lost, exactly:
-  const float v = d - top, lost = (top - (d - v)) + (-x - v);
-  const float p = d * c.hi;
-  if (!(p < 64.f)) return ~0ull;
-  float e = fmaf(d, c.hi, -p);
-  e = fmaf(d, c.lo, e);
-  e = fmaf(lost, c.hi, e);
-  const float q = p * 131072.f;                  // 2^17: below 2^23
-  const int32_t whole = (int32_t)q;
-  const int64_t rest = (int64_t)(int32_t)((q - (float)whole) * 67108864.f) + (int32_t)(e * 8796093022208.f);   // 2^26, 2^43
-  const int64_t z = ((int64_t)whole << 26) + rest;
-  return z > 0 ? (uint64_t)z : 0;
-}
-// 2^(S - z) for z in units of 2^-43, rounded to a whole number: S <= 46.
-// coarse(j), fine(k): the tables; called for every argument, by whole warps.
-template <class Coarse, class Fine>
-RO_HD uint64_t exp_weight(uint64_t z, uint32_t S, Coarse coarse, Fine fine) {
-  const uint32_t top = (uint32_t)(z >> 33);      // whole part and ten bits
-  const uint64_t ab = mul_hi64(coarse((top >> 5) & 31u), fine(top & 31u));    // 2^62 2^-(..)
-  const uint32_t r = (uint32_t)(z >> 1);         // the rest in units of 2^-42: 32 bits
-#ifdef __CUDA_ARCH__
-  const uint32_t t = __umulhi(r, 0xB17217F8u);   // ln 2 in 2^-32
-#else
-  const uint32_t t = (uint32_t)(((uint64_t)r * 0xB17217F8u) >> 32);
-#endif
-  const float f = (float)t * 2.2737367544323206e-13f;   // 2^-42
-  const uint32_t less = (uint32_t)(f * f * (0.5f - f * 0.16666667f) * 4398046511104.f);
-  const uint64_t w = ab - (((ab >> 32) * (uint64_t)(t - less)) >> 10);
-  const uint32_t shift = 62u - S + (top >> 10);
-  if (shift >= 64u) return 0;
-  return shift == 0u ? w : (w + (1ull << (shift - 1))) >> shift;
+// The weight of argument z in steps of 1 / unit = 2^-B.  table(j): 2^-(j/32);
+// called for every argument, by whole warps.
+template <class Table>
+RO_HD Weight exp_weight(Pair32 z, float unit, Table table) {
+  const bool none = !(z.hi < 64.f);
+  const float p = none ? 0.f : z.hi;
+  const float t = RO_FMA(p, 32.f, 12582912.f);   // 1.5 2^23: the last bits are m
+  const int32_t m = float_bits(t) - 0x4B400000;
+  const float r0 = RO_FMA(RO_ADD(t, -12582912.f), -0.03125f, p);   // exact
+  const float r = RO_ADD(r0, z.lo), rl = RO_ADD(RO_ADD(r0, -r), z.lo);
+  const Pair32 T = table((uint32_t)m & 31u);
+  // g = -(r + rl) ln 2, and e^g - 1 = u
+  const float gh = RO_MUL(r, -0x1.62e43p-1f);
+  const float gl = RO_FMA(rl, -0x1.62e43p-1f, RO_FMA(r, 0x1.05c61p-29f, RO_FMA(r, -0x1.62e43p-1f, -gh)));
+  const float half = RO_MUL(gh, 0.5f), qh = RO_MUL(gh, half), ql = RO_FMA(gh, gl, RO_FMA(gh, half, -qh));
+  const float more = RO_MUL(RO_MUL(gh, gh), RO_MUL(gh, RO_FMA(gh, RO_FMA(gh, 0x1.111112p-7f, 0x1.555556p-5f), 0x1.555556p-3f)));
+  const float uh = RO_ADD(gh, qh), ul = RO_ADD(RO_ADD(RO_ADD(RO_ADD(gh, -uh), qh), gl), RO_ADD(ql, more));
+  // T (1 + u)
+  const float ph = RO_MUL(T.hi, uh), pl = RO_FMA(T.hi, uh, -ph);
+  const float s0 = RO_ADD(T.hi, ph);
+  const float s1 = RO_ADD(RO_ADD(RO_ADD(RO_ADD(T.hi, -s0), ph), pl), RO_FMA(T.hi, ul, RO_FMA(T.lo, uh, T.lo)));
+  const float sh = RO_ADD(s0, s1), sl = RO_ADD(RO_ADD(s0, -sh), s1);
+  // times 2^-(m / 32 rounded down), in steps of 2^-20, what is left in steps of 2^-B
+  const float down = bits_float((127 - (m >> 5)) << 23);
+  const float wh = RO_MUL(sh, down), wl = RO_MUL(sl, down);
+  const float a = RO_ADD(wh, 12.f);              // 1.5 2^3: 23 bits below are 2^-20
+  const float b = RO_MUL(RO_ADD(wh, -RO_ADD(a, -12.f)), unit), c = RO_MUL(wl, unit);   // at most 2^29 + 2^25
+  Weight w;
+  w.hi = none ? 0 : float_bits(a) - 0x41400000;
+  w.lo = none ? 0 : nearest(b) + nearest(c);
+  return w;
 }
 
 }  // namespace ro

@@ -9,10 +9,19 @@
 // Weights and sums are 64-bit fixed point (fixed_exp.h), so no sum depends on
 // its order and tokens do not depend on how a row is split.
 //
-// A cluster of CTAs takes a row, a slice each in shared memory, read once from
-// memory.  Thresholds come from passes over the bits of the logits' keys (which
-// order alike), a histogram of counts (top-k) or of weights (top-p) summed over
-// the cluster in each.
+// Where the settings leave few tokens, those are found without a threshold being
+// known: among the threads' largest logits the want-th largest has at least `want`
+// tokens at or above it, and seldom many more.  These candidates are gathered,
+// sorted and summed by one CTA, and the rest of the row is not looked at again.
+// Other rows are wide: top-k's border is found by passes over the bits of the
+// logits' keys (which order alike), top-p's by a histogram of weights in 32 bits
+// that names the border's bin, an exact pass that sums what lies above the bin,
+// and a sort of the bin itself.
+//
+// Few rows are split over clusters of CTAs, which hold their slices in shared
+// memory.  Many rows take a CTA each, which reads its row from memory once and
+// what it needs of it again from L2; the wide ones among them are left to a
+// second kernel of clusters.
 #include <algorithm>
 
 #include "fixed_exp.h"
@@ -22,8 +31,8 @@ namespace ro {
 
 constexpr int SM_THREADS = 512;
 constexpr uint32_t SM_WARPS = SM_THREADS / 32, SM_BINS = 2048, SM_MAX_CLUSTER = 8;
-// bytes of a slice that a CTA holds at most
-constexpr uint32_t SM_SLICE = 192 * 1024;
+// bytes of a slice that a CTA holds at most, two of them on an SM; a longer one is read again
+constexpr uint32_t SM_SLICE = 80 * 1024;
 constexpr uint32_t NO_TOKEN = 0xFFFFFFFFu;
 constexpr uint32_t KEY_NONE = 0x007FFFFFu;   // of -inf
 
@@ -35,10 +44,7 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 __device__ __forceinline__ float key_logit(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
-// an item of CTA `rank` of the cluster: added to, fetched and added to, written
-__device__ __forceinline__ void cluster_count(const uint32_t* p, uint32_t rank) {
-  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], 1;" ::"r"(cluster_at(step_smem(p), rank)) : "memory");
-}
+// an item of CTA `rank` of the cluster: fetched and added to, written
 __device__ __forceinline__ uint32_t cluster_take(const uint32_t* p, uint32_t rank, uint32_t n) {
   uint32_t v;
   asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;"
@@ -49,6 +55,9 @@ __device__ __forceinline__ uint32_t cluster_take(const uint32_t* p, uint32_t ran
 }
 __device__ __forceinline__ void cluster_write(const unsigned long long* p, uint32_t rank, unsigned long long v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "l"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_write(const uint32_t* p, uint32_t rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "r"(v) : "memory");
 }
 template <class V>
 __device__ __forceinline__ V cluster_read(const V* p, uint32_t rank) {
@@ -94,6 +103,25 @@ struct Logits {
     else
       return __uint_as_float(h << 16);
   }
+  // the largest of them, NaN aside
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(T) == 4) {
+      return fmaxf(fmaxf(at(v, 0), at(v, 1)), fmaxf(at(v, 2), at(v, 3)));
+    } else if constexpr (std::is_same_v<T, __half>) {
+      __half2 m[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = *reinterpret_cast<const __half2*>(&w[i]);
+      const __half2 x = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
+      return fmaxf(__low2float(x), __high2float(x));
+    } else {
+      __nv_bfloat162 m[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+      const __nv_bfloat162 x = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
+      return fmaxf(__low2float(x), __high2float(x));
+    }
+  }
 };
 template <typename T>
 __device__ __forceinline__ T minus_infinity();
@@ -114,8 +142,8 @@ __device__ __forceinline__ void sort_items(unsigned long long* v, uint32_t n, bo
         __syncthreads();
       else
         __syncwarp();
-      for (uint32_t c = t; c < n / 2; c += SM_THREADS) {
-        const uint32_t i = 2 * c - (c & (step - 1)), j = i + step;
+      if (t < n / 2) {
+        const uint32_t i = 2 * t - (t & (step - 1)), j = i + step;
         const unsigned long long a = v[i], b = v[j];
         if ((a < b) == (((i & size) == 0) == falling) && a != b) {
           v[i] = b;
@@ -125,55 +153,58 @@ __device__ __forceinline__ void sort_items(unsigned long long* v, uint32_t n, bo
     }
   __syncthreads();
 }
-__device__ const unsigned long long EXP_COARSE[32] = {RO_EXP_COARSE}, EXP_FINE[32] = {RO_EXP_FINE};
+__device__ const float EXP_HI[32] = {RO_EXP_HI}, EXP_LO[32] = {RO_EXP_LO};
 
 // What a row's tokens have to pass: keys above `key`, and the first `ties` equal to it.
 struct Threshold {
   uint32_t key, ties;
 };
 
-// A row's candidates: the few tokens that can stay, where settings leave few.
-constexpr uint32_t SM_LIST = 1024;
+// Candidates held, two a thread; tokens they are meant to hold where top-k does
+// not say, and at most.
+constexpr uint32_t SM_LIST = 2 * SM_THREADS, SM_WANT = 512, SM_WANT_MOST = 704;
 static_assert(2 * SM_LIST <= SM_BINS, "candidates and their weights lie where the bins do");
-// Tokens that the candidates are meant to hold where top-p alone decides, and at
-// most; and of the threads' largest logits.
-constexpr uint32_t SM_WANT = 512, SM_WANT_MOST = 704;
-constexpr uint32_t SM_COARSE = 512;
-// What 32-bit weights and their sum may be off, relative to the sum: the
-// argument, below 64, by 2^-23 of itself, and roundings of 2^-22.
-constexpr double SM_SLACK = 1.0 / (1 << 16);
+constexpr uint32_t SM_COARSE = SM_THREADS;   // bins of the threads' maxima
+// What a sum of weights in 32 bits may be off, relative to itself: a weight's
+// argument, below 64, by 2^-23 of itself, its exponential by 2^-22; a thread's
+// terms, at most 800 in two levels of sums of at most 200, by 2^-24 a sum.
+constexpr float SM_SLACK = 1.f / (1 << 15);
 enum SampleWay : uint32_t { WAY_DONE, WAY_MASS, WAY_WIDE };
 
-struct SampleShared {
+struct __align__(16) SampleShared {
   unsigned long long mass[SM_BINS];
   uint32_t count[SM_BINS];
-  unsigned long long warp_mass[SM_WARPS];
+  unsigned long long warp_mass[SM_WARPS], warp_above[SM_WARPS];
   uint32_t warp_ties[SM_WARPS], warp_count[SM_WARPS];
-  unsigned long long best;                 // key and ~place of the largest logit
-  uint32_t least;                          // key of the threads' smallest maximum
-  uint32_t coarse[SM_COARSE];              // the threads' maxima, counted by distance from the largest
-  uint32_t cut, listed, way;
-  float rough;                             // the sum of all weights in 32 bits
-  float warp_rough[SM_WARPS];
   unsigned long long scan[SM_WARPS];
   unsigned long long found_left;
   uint32_t found;
-  uint32_t total_ties;
+  uint32_t best, least;                    // keys of the largest logit, and of the threads' smallest maximum
+  uint32_t place;                          // of the largest logit, the first of equal ones
+  uint32_t coarse[SM_COARSE];              // the threads' maxima, counted by distance from the largest
+  uint32_t cut, listed, way, row;
+  Threshold border;
+  uint4 edge[2];                           // a row's first and last block, where it does not fill them
+  struct {
+    uint32_t first, last;
+    uint64_t at, ties;                     // weight and tokens on the threshold before it
+  } run;
+  float rough, warp_rough[SM_WARPS];       // sums of weights in 32 bits
+  uint8_t flags[SM_WARPS][64];             // halves of a warp's threads that hold a candidate
   float temperature, top_p, min_p, u;
   uint32_t top_k, valid;
+  double reach;                            // how far below the largest logit min-p reaches
 };
 
+// One row, by a cluster of a.cluster CTAs (or one).  false: it is left to the
+// clusters (a.later), whole CTAs alike.
 template <typename T>
-__global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constant__ SampleArgs a) {
+__device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s, uint4* slice, uint32_t row) {
   constexpr uint32_t E = Logits<T>::E;
   // the low bits of a 16-bit logit's key follow from its sign
   constexpr int LOW = std::is_same_v<T, float> ? 0 : std::is_same_v<T, __half> ? 11 : 16;
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  __shared__ SampleShared s;
-  uint4* slice = (uint4*)smem_raw;
-  wait_predecessor();
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t nc = a.cluster, rank = nc > 1 ? cluster_rank() : 0, row = blockIdx.x / nc;
+  const uint32_t nc = a.cluster, rank = nc > 1 ? cluster_rank() : 0;
   auto sync = [&] {
     if (nc > 1)
       cluster_sync();
@@ -186,6 +217,13 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
   const uint4* blocks = (const uint4*)(x - off);
   const uint32_t n_blocks = (end + E - 1) / E;
   const uint32_t b0 = min(n_blocks, rank * a.blocks), n = min(n_blocks, b0 + a.blocks) - b0;
+  // Block i of this CTA's.  The first and the last one of a row, which may hold
+  // other data beside it, are kept with -inf there; [in0, in1) are whole.
+  const uint32_t in0 = b0 == 0 && off != 0 ? 1u : 0u, in1 = b0 + n == n_blocks && end % E != 0 ? max(n, 1u) - 1u : n;
+  auto block = [&](uint32_t i) -> uint4 {
+    if (a.staged) return slice[i];
+    return i >= in0 && i < in1 ? blocks[b0 + i] : s.edge[b0 + i == 0 ? 0 : 1];
+  };
   if (tid == 0) {
     s.temperature = a.temperature ? a.temperature[row] : 1.f;
     s.top_p = a.top_p ? a.top_p[row] : 1.f;
@@ -195,104 +233,438 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
     s.valid = s.temperature >= 0.f && s.temperature < INFINITY && s.top_p >= 0.f && s.top_p <= 1.f && s.min_p >= 0.f &&
               s.min_p <= 1.f && s.u >= 0.f && s.u < 1.f;
     if (!s.valid && rank == 0) record(a.err, ERR_INVAL);
+    s.listed = 0;
+    s.place = ~0u;
+    // (64-bit floats in one thread only, while the loads are under way: they are
+    // rare on this GPU; all 512 threads' logarithms took 10 us)
+    s.reach = s.min_p > 0.f ? (double)s.temperature * log((double)s.min_p) : 0.0;
   }
-  // ---- the slice, and the largest logit (the first of equal ones) ----
-  float top = -INFINITY;
-  uint32_t place = 0;
-#pragma unroll 4
-  for (uint32_t i = tid; i < n; i += SM_THREADS) {
+  s.coarse[tid] = 0;
+  // ---- the slice, and its largest logit: of every second block of a thread's, two maxima ----
+  float my_top[2] = {-INFINITY, -INFINITY};
+  uint4 none;
+  {
+    __align__(16) T e[E];
+#pragma unroll
+    for (uint32_t k = 0; k < E; ++k) e[k] = minus_infinity<T>();
+    none = *(const uint4*)e;
+  }
+  constexpr uint32_t AHEAD = 8;   // loads of a thread under way
+  for (uint32_t i = tid; i < n; i += AHEAD * SM_THREADS) {
+    uint4 v[AHEAD];
+#pragma unroll
+    for (uint32_t q = 0; q < AHEAD; ++q) {
+      const uint32_t j = i + q * SM_THREADS;
+      v[q] = j >= in0 && j < in1 ? blocks[b0 + j] : none;
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < AHEAD; ++q) {
+      const uint32_t j = i + q * SM_THREADS;
+      if (a.staged && j >= in0 && j < in1) slice[j] = v[q];
+      my_top[q & 1] = fmaxf(my_top[q & 1], Logits<T>::largest(v[q]));
+    }
+  }
+#pragma unroll
+  for (uint32_t h = 0; h < 2; ++h) {   // a block at the row's edge, by the thread that has it
+    const uint32_t i = h == 0 ? 0u : n - 1u;
+    if (n == 0u || (h == 0 ? in0 == 0u : in1 == n || (n == 1u && in0 != 0u)) || i % SM_THREADS != tid) continue;
     const uint32_t p0 = (b0 + i) * E;
-    uint4 v;
-    if (p0 >= off && p0 + E <= end) {
-      v = __ldcs(blocks + b0 + i);
-    } else {
-      __align__(16) T e[E];
+    __align__(16) T e[E];
 #pragma unroll
-      for (uint32_t k = 0; k < E; ++k) e[k] = p0 + k >= off && p0 + k < end ? x[p0 + k - off] : minus_infinity<T>();
-      v = *(const uint4*)e;
-    }
-    slice[i] = v;
-#pragma unroll
-    for (uint32_t k = 0; k < E; ++k) {
-      const float y = Logits<T>::at(v, k);
-      if (y > top) {
-        top = y;
-        place = p0 + k;
-      }
-    }
+    for (uint32_t k = 0; k < E; ++k) e[k] = p0 + k >= off && p0 + k < end ? x[p0 + k - off] : minus_infinity<T>();
+    const uint4 v = *(const uint4*)e;
+    if (a.staged)
+      slice[i] = v;
+    else
+      s.edge[b0 + i == 0 ? 0 : 1] = v;
+    my_top[i / SM_THREADS & 1] = fmaxf(my_top[i / SM_THREADS & 1], Logits<T>::largest(v));
   }
   {
-    unsigned long long b = top == -INFINITY ? 0 : (unsigned long long)logit_key(top) << 32 | ~place;
+    uint32_t low = ~0u;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
-    if (lane == 0) s.scan[warp] = b;
-    __syncthreads();
-    if (warp == 0) {
-      b = lane < SM_WARPS ? s.scan[lane] : 0;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
-      if (lane == 0) s.best = b;
-    }
-    const uint32_t low = __reduce_min_sync(0xffffffffu, top == -INFINITY ? ~0u : logit_key(top));
-    if (lane == 0) s.warp_count[warp] = low;
-    for (uint32_t i = tid; i < SM_COARSE; i += SM_THREADS) s.coarse[i] = 0;
-    if (tid == 0) s.listed = 0;
-    __syncthreads();
-    if (warp == 0) {
-      const uint32_t all = __reduce_min_sync(0xffffffffu, lane < SM_WARPS ? s.warp_count[lane] : ~0u);
-      if (lane == 0) s.least = all;
+    for (int h = 0; h < 2; ++h)
+      if (my_top[h] > -INFINITY) low = min(low, logit_key(my_top[h]));
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, logit_key(fmaxf(my_top[0], my_top[1])));
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (lane == 0) {
+      s.warp_count[warp] = hi;
+      s.warp_ties[warp] = low;
     }
   }
-  const float my_top = top;
-  sync();
-  unsigned long long best = s.best;
-  uint32_t least = s.least;
-  if (nc > 1)
+  __syncthreads();
+  uint32_t best = __reduce_max_sync(0xffffffffu, lane < SM_WARPS ? s.warp_count[lane] : 0u);
+  uint32_t least = __reduce_min_sync(0xffffffffu, lane < SM_WARPS ? s.warp_ties[lane] : ~0u);
+  if (nc > 1) {
+    if (tid == 0) {
+      s.best = best;
+      s.least = least;
+    }
+    cluster_sync();
     for (uint32_t r = 0; r < nc; ++r) {
       best = max(best, cluster_read(&s.best, r));
       least = min(least, cluster_read(&s.least, r));
     }
-  const float T_ = s.temperature, top_p = s.top_p;
-  uint32_t top_k = s.top_k;
+  } else {
+    __syncthreads();   // read by all before they are written again
+  }
+  const float top = key_logit(best), T_ = s.temperature, top_p = s.top_p;
+  const uint32_t top_k = s.top_k;
   auto finish = [&](uint32_t token, float logp, uint32_t kept) {
     a.token[row] = token;
     if (a.logp) a.logp[row] = logp;
     if (a.kept) a.kept[row] = kept;
   };
-  if (!s.valid || best == 0 || T_ == 0.f || top_k == 1u || top_p == 0.f) {   // (the whole cluster)
-    if (rank == 0 && tid == 0) {
-      if (!s.valid || best == 0)
-        finish(NO_TOKEN, -INFINITY, 0);
-      else
-        finish(~(uint32_t)best - off, 0.f, 1);
-    }
-    if (nc > 1) cluster_sync();
-    return;
+  if (!s.valid || best == KEY_NONE) {
+    if (rank == 0 && tid == 0) finish(NO_TOKEN, -INFINITY, 0);
+    return true;
   }
-  top = key_logit((uint32_t)(best >> 32));
+  if (T_ == 0.f || top_k == 1u || top_p == 0.f) {   // the first of the largest
+    uint32_t place = ~0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (my_top[h] == top)
+        for (uint32_t i = tid + h * SM_THREADS; i < n && place == ~0u; i += 2 * SM_THREADS) {
+          const uint4 v = block(i);
+#pragma unroll
+          for (uint32_t k = E; k-- > 0;)
+            if (Logits<T>::at(v, k) == top) place = (b0 + i) * E + k - off;
+        }
+    if (place != ~0u) atomicMin(&s.place, place);
+    sync();
+    if (rank == 0) {
+      if (lane < nc && warp == 0) place = nc > 1 ? cluster_read(&s.place, lane) : s.place;
+      place = __reduce_min_sync(0xffffffffu, warp == 0 && lane < nc ? place : ~0u);
+      if (tid == 0) finish(place, 0.f, 1);
+    }
+    return true;
+  }
 
   // ---- weights ----
-  const double c = 1.4426950408889634074 / (double)T_;
-  const ExpScale scale = {(float)c, (float)(c - (double)(float)c)};
-  const unsigned long long my_coarse = EXP_COARSE[lane], my_fine = EXP_FINE[lane];
-  // of a whole warp's logits; 0 where !in
+  // log2(e) / T in two floats: the quotient, and its remainder's
+  const float c = 1.44269502162933349609f / T_;
+  const ExpScale scale = {c, c < 3.0e38f ? (fmaf(-c, T_, 1.44269502162933349609f) + 1.92596299112661746887e-8f) / T_ : 0.f};
+  const float my_hi = EXP_HI[lane], my_lo = EXP_LO[lane];   // the table, an entry a lane
+  // Bits of a weight behind the point: as many as keep the sum below 2^63, where
+  // it is known roughly, and so few that none is lost (many light tokens together count).
+  uint32_t bits = WEIGHT_BITS;
+  auto bits_for = [&](float sum) { bits = min(WEIGHT_BITS, 61u - (uint32_t)ilogbf(fmaxf(sum, 1.f))); };
+  // Of a whole warp's logits, some a lane; 0 where !in.  (Up to four together:
+  // one after another each would wait for its chain of some 60 instructions.)
+  auto weigh = [&](auto& y, auto& in, auto& w) {
+    constexpr int N = (int)(sizeof(y) / sizeof(y[0])), G = N < 4 ? N : 4;
+#pragma unroll
+    for (int g = 0; g < N; g += G) {
+      bool some = false;
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        some = some || in[g + k];
+        w[g + k] = {0, 0};
+      }
+      if (!__any_sync(0xffffffffu, some)) continue;
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        const Weight v = exp_weight(exp_argument(top, in[g + k] ? y[g + k] : top, scale), (float)(1ull << bits), [&](uint32_t j) {
+          return Pair32{__shfl_sync(0xffffffffu, my_hi, j), __shfl_sync(0xffffffffu, my_lo, j)};
+        });
+        if (in[g + k]) w[g + k] = v;
+      }
+    }
+  };
   auto weight = [&](float y, bool in) -> uint64_t {
-    const uint64_t z = in ? exp_argument(top, y, scale) : ~0ull;
-    if (!__any_sync(0xffffffffu, z != ~0ull)) return 0;
-    const uint64_t w = exp_weight(
-        z, a.frac_bits, [&](uint32_t j) { return (uint64_t)__shfl_sync(0xffffffffu, my_coarse, j); },
-        [&](uint32_t j) { return (uint64_t)__shfl_sync(0xffffffffu, my_fine, j); });
-    return z != ~0ull ? w : 0;
+    const float ys[1] = {y};
+    const bool ins[1] = {in};
+    Weight w[1];
+    weigh(ys, ins, w);
+    return whole(w[0], bits);
+  };
+  auto total_of = [&](const auto& w) -> uint64_t {   // of a few
+    Weight m = {0, 0};
+#pragma unroll
+    for (uint32_t k = 0; k < sizeof(w) / sizeof(w[0]); ++k) {
+      m.hi += w[k].hi;
+      m.lo += w[k].lo;
+    }
+    return whole(m, bits);
+  };
+  // in 32 bits, of a logit that is no NaN
+  auto rough_weight = [&](float y) -> float {
+    if (y == top) return 1.f;
+    const float d = top - y, z = d * scale.hi, e = fmaf(d, scale.lo, fmaf(d, scale.hi, -z));
+    return z < 64.f ? ex2(-z) * fmaf(e, -LN2, 1.f) : 0.f;
   };
   auto key_of = [&](float y) -> uint32_t { return y == y ? logit_key(y) : KEY_NONE; };   // (a NaN is never drawn)
+  auto each_block = [&](auto&& use) {
+    for (uint32_t i = tid; i < n; i += SM_THREADS) use(i, block(i));
+  };
+  // a thread's 32-bit sums, of the CTA: in s.rough once the CTA has met
+  auto rough_sum = [&](float above) {
+    float sum = 0.f;
+    each_block([&](uint32_t, const uint4& v) {
+      float part = 0.f;
+#pragma unroll
+      for (uint32_t k = 0; k < E; ++k) {
+        const float y = Logits<T>::at(v, k);
+        if (y > above) part += rough_weight(y);
+      }
+      sum += part;
+    });
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) s.warp_rough[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+      sum = 0.f;
+      for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
+      s.rough = sum;
+    }
+  };
+  auto rough_total = [&]() -> float {
+    if (nc == 1) return s.rough;
+    float sum = 0.f;
+    for (uint32_t r = 0; r < nc; ++r) sum += __uint_as_float(cluster_read((const uint32_t*)&s.rough, r));
+    return sum;
+  };
+  auto with_log = [&](uint32_t token, float y, uint64_t total, uint32_t kept) {
+    const Pair32 z = exp_argument(top, y, scale);
+    const double less = ((double)z.hi + (double)z.lo) * 0.69314718055994530942;
+    finish(token, -(float)(less + log((double)total * (1.0 / (double)(1ull << bits)))), kept);
+  };
 
   // ---- thresholds ----
   Threshold th = {KEY_NONE, 0};
   if (s.min_p > 0.f) {   // w >= min_p; the smallest such float
-    const float least_x = __double2float_ru((double)top + (double)T_ * log((double)s.min_p));
+    const float least_x = __double2float_ru((double)top + s.reach);
     th.key = max(KEY_NONE, logit_key(least_x) - 1u);
   }
-  // Every thread's items of a pass: this CTA's blocks, a warp's side by side, all warps alike in number.
+  const bool by_k = top_k != 0u && top_k < a.vocab, by_p = top_p < 1.f, by_min = s.min_p > 0.f;
+  // (as far as weights go: beyond 45 T they are below 2^-64)
+  const float span = fmaxf(fminf(top - key_logit(least), 45.f * T_), 1e-30f);
+  unsigned long long* list = s.mass;              // candidates: keys and ~indices
+  unsigned long long* weights = s.mass + SM_LIST;
+  auto enlist = [&](float y, uint32_t index) {    // to the first CTA's list
+    const unsigned long long item = (unsigned long long)logit_key(y) << 32 | ~index;
+    if (nc > 1) {
+      const uint32_t at = cluster_take(&s.listed, 0, 1u);
+      if (at < SM_LIST) cluster_write(&s.mass[at], 0, item);
+    } else {
+      const uint32_t at = atomicAdd(&s.listed, 1u);
+      if (at < SM_LIST) s.mass[at] = item;
+    }
+  };
+  // The first CTA: sorts what is listed; the weights of this thread's two items
+  // and of those ahead of them; returns all their weight.
+  uint64_t own[2] = {0, 0}, ahead[2] = {0, 0};
+  auto sort_list = [&](uint32_t listed) -> uint64_t {
+    uint32_t size = 2;
+    while (size < listed) size *= 2;
+    for (uint32_t i = listed + tid; i < size; i += SM_THREADS) list[i] = 0;
+    sort_items(list, size, true);
+    const float ys[2] = {key_logit((uint32_t)(list[2 * tid] >> 32)), key_logit((uint32_t)(list[2 * tid + 1] >> 32))};
+    const bool ins[2] = {2 * tid < listed, 2 * tid + 1 < listed};
+    Weight w[2];
+    weigh(ys, ins, w);
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j) {
+      own[j] = whole(w[j], bits);
+      if (ins[j]) weights[2 * tid + j] = own[j];
+    }
+    const uint64_t sum = own[0] + own[1];
+    const uint64_t run = warp_incl_scan(sum);
+    if (lane == 31) s.scan[warp] = run;
+    __syncthreads();
+    uint64_t base = run - sum, all = 0;
+    for (uint32_t w = 0; w < SM_WARPS; ++w) {
+      if (w < warp) base += s.scan[w];
+      all += s.scan[w];
+    }
+    ahead[0] = base;
+    ahead[1] = base + own[0];
+    return all;
+  };
+  // how many of the first `first` items have less than `limit` ahead of them
+  auto count_below = [&](uint64_t limit, uint32_t first) -> uint32_t {
+    const uint32_t mine = (2 * tid < first && ahead[0] < limit) + (2 * tid + 1 < first && ahead[1] < limit);
+    return (uint32_t)__syncthreads_count(mine >= 1) + (uint32_t)__syncthreads_count(mine >= 2);
+  };
+
+  // ---- few candidates ----
+  const uint32_t most = min(SM_WANT_MOST, nc * SM_THREADS * 3 / 2);   // of the threads' maxima
+  uint32_t way = WAY_WIDE;
+  if ((by_k || by_p || by_min) && top < INFINITY) {
+    const uint32_t want = by_k && top_k <= most ? top_k : min(SM_WANT, most);
+    const bool all_of_k = by_k && top_k <= most;   // the candidates hold the first top_k
+    const float per_bin = (float)SM_COARSE / span;
+    auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_COARSE - 1)); };
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (my_top[h] > -INFINITY) atomicAdd(&s.coarse[bin_of(my_top[h])], 1u);
+    // the sum that top-p is a share of, first in 32 bits
+    if (by_p && !all_of_k && !by_k) rough_sum(-INFINITY);
+    if (tid == 0) s.cut = SM_COARSE;
+    sync();
+    // the bin at which `want` maxima are reached is the last that is listed
+    uint32_t mine = 0;
+    for (uint32_t r = 0; r < nc; ++r) mine += nc > 1 ? cluster_read(&s.coarse[tid], r) : s.coarse[tid];
+    const uint32_t inc = warp_incl_scan(mine);
+    if (lane == 31) s.warp_count[warp] = inc;
+    __syncthreads();
+    uint32_t before = inc - mine;
+    for (uint32_t w = 0; w < warp; ++w) before += s.warp_count[w];
+    if (before < want && before + mine >= want) s.cut = tid;
+    __syncthreads();
+    const uint32_t cut = s.cut;                      // SM_COARSE: fewer maxima than wanted, so every token
+    const bool with_min = by_min && !all_of_k;       // (top-p's sum is over the first top_k, whatever min-p says)
+    // (bin_of(y) <= cut, without its conversion)
+    const float reach = (float)(cut + 1), limit = with_min ? key_logit(th.key) : -INFINITY;
+    const bool far = cut >= SM_COARSE - 1;
+    auto candidate = [&](float y) { return y > limit && (far || (top - y) * per_bin < reach); };
+    // A warp goes through the blocks of those of its threads' halves whose maximum is one, several at a time.
+    uint8_t* flags = s.flags[warp];
+    const uint32_t flag0 = __ballot_sync(0xffffffffu, candidate(my_top[0])), flag1 = __ballot_sync(0xffffffffu, candidate(my_top[1]));
+    const uint32_t below = (1u << lane) - 1u;
+    if (flag0 >> lane & 1u) flags[__popc(flag0 & below)] = (uint8_t)lane;
+    if (flag1 >> lane & 1u) flags[__popc(flag0) + __popc(flag1 & below)] = (uint8_t)(lane | 32u);
+    __syncwarp();
+    const uint32_t runs = (n + 2 * SM_THREADS - 1) / (2 * SM_THREADS), visits = (__popc(flag0) + __popc(flag1)) * runs;
+    for (uint32_t x0 = 0; x0 < visits; x0 += 4 * 32) {
+      uint4 v[4];
+      uint32_t at[4];
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        const uint32_t visit = x0 + q * 32 + lane, f = visit / runs;
+        at[q] = n;
+        if (visit < visits) at[q] = warp * 32 + (flags[f] & 31u) + (flags[f] >> 5) * SM_THREADS + (visit - f * runs) * 2 * SM_THREADS;
+        v[q] = at[q] < n ? block(at[q]) : none;
+      }
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q)
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k)
+          if (const float y = Logits<T>::at(v[q], k); candidate(y)) enlist(y, (b0 + at[q]) * E + k - off);
+    }
+    sync();
+    if (by_p && !all_of_k && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
+    // ---- the first CTA's ----
+    const uint32_t listed = rank == 0 ? s.listed : 0;
+    uint32_t stay = 0;
+    if (rank == 0) {
+      if (listed > 0 && listed <= SM_LIST) {
+        const uint64_t list_mass = sort_list(listed);
+        uint32_t by_limit = listed;                  // min-p's
+        if (by_min) {
+          const uint32_t in = (2 * tid < listed && (uint32_t)(list[2 * tid] >> 32) > th.key) +
+                              (2 * tid + 1 < listed && (uint32_t)(list[2 * tid + 1] >> 32) > th.key);
+          by_limit = (uint32_t)__syncthreads_count(in >= 1) + (uint32_t)__syncthreads_count(in >= 2);
+        }
+        // whether every token that can stay by top-k and min-p is listed
+        const bool whole = cut == SM_COARSE || all_of_k || by_limit < listed ||
+                           (with_min && bin_of(key_logit(th.key + 1u)) <= cut);
+        const uint32_t first = by_k ? min(top_k, listed) : listed;
+        stay = min(first, by_limit);
+        if (!by_p) {
+          way = whole ? WAY_DONE : WAY_WIDE;
+        } else if (all_of_k || (cut == SM_COARSE && !with_min)) {   // the sum is the listed ones'
+          uint64_t sum = list_mass;
+          if (first < listed) {
+            if (tid == first / 2) s.found_left = ahead[first & 1];
+            __syncthreads();
+            sum = s.found_left;
+          }
+          stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), first)));
+          way = WAY_DONE;
+        } else if (!by_k) {
+          const float rough = rough_total() * top_p * (float)(1ull << bits);
+          const uint32_t lo = max(1u, count_below((uint64_t)(rough * (1.f - SM_SLACK)), listed));
+          const uint32_t hi = max(1u, count_below((uint64_t)(rough * (1.f + SM_SLACK)) + 2, listed));
+          if (!whole && hi == listed) {              // tokens that are not listed may stay
+            way = WAY_WIDE;
+          } else if (min(lo, stay) == min(hi, stay)) {
+            way = WAY_DONE;
+            stay = min(lo, stay);
+          } else {
+            way = WAY_MASS;
+          }
+        }
+      }
+      if (tid < nc) {   // to every CTA's own: this one may be gone before they look
+        if (nc > 1)
+          cluster_write(&s.way, tid, way);
+        else
+          s.way = way;
+      }
+    }
+    sync();
+    way = s.way;
+    if (way == WAY_DONE || (way == WAY_MASS && !a.later)) {
+      if (way == WAY_MASS) {   // the border lies within what 32 bits may be off
+        uint64_t sum = 0;
+        for (uint32_t i = warp * 32; i < n; i += SM_THREADS) {
+          const bool have = i + lane < n;
+          const uint4 v = have ? block(i + lane) : make_uint4(0, 0, 0, 0);
+          float y[E];
+          bool in[E];
+          Weight w[E];
+#pragma unroll
+          for (uint32_t k = 0; k < E; ++k) {
+            y[k] = Logits<T>::at(v, k);
+            in[k] = have && y[k] > -INFINITY;
+          }
+          weigh(y, in, w);
+          sum += total_of(w);
+        }
+        sum = warp_sum64(sum);
+        if (lane == 0) s.warp_mass[warp] = sum;
+        sync();
+        sum = 0;
+        for (uint32_t q = lane; q < nc * SM_WARPS; q += 32)
+          sum += nc > 1 ? cluster_read(&s.warp_mass[q % SM_WARPS], q / SM_WARPS) : s.warp_mass[q % SM_WARPS];
+        sum = warp_sum64(sum);
+        if (rank == 0) stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), listed)));
+        sync();
+      }
+      if (rank == 0) {
+        // the sum of those that stay, then where it passes the goal, by index
+        if (2 * tid < stay && stay <= 2 * tid + 2) s.found_left = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
+        __syncthreads();
+        const uint64_t total = s.found_left, goal = scaled(total, s.u, false);
+        uint32_t size = 2;
+        while (size < stay) size *= 2;
+        // indices rise, and each remembers its candidate
+        unsigned long long* order = (unsigned long long*)s.count;
+        static_assert(SM_LIST * 8 <= sizeof(s.count), "the order lies where the counts do");
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          const uint32_t i = 2 * tid + j;
+          if (i < size) order[i] = i < stay ? (unsigned long long)~(uint32_t)list[i] << 32 | i : ~0ull;
+        }
+        sort_items(order, size, false);
+        uint64_t w2[2], sum = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          w2[j] = 2 * tid + j < stay ? weights[(uint32_t)order[2 * tid + j]] : 0;
+          sum += w2[j];
+        }
+        const uint64_t run = warp_incl_scan(sum);
+        if (lane == 31) s.scan[warp] = run;
+        __syncthreads();
+        uint64_t at = run - sum;
+        for (uint32_t w = 0; w < warp; ++w) at += s.scan[w];
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+          if (goal >= at && goal < at + w2[j]) {
+            const unsigned long long o = order[2 * tid + j];
+            with_log((uint32_t)(o >> 32), key_logit((uint32_t)(list[(uint32_t)o] >> 32)), total, stay);
+          }
+          at += w2[j];
+        }
+      }
+      return true;
+    }
+  }
+  if (a.later) return false;
+
+  // ---- wide rows ----
+  bits_for((float)a.vocab);
   const uint32_t rounds = (n + SM_THREADS - 1) / SM_THREADS;
   // Finds the key where the tokens above `th`, largest first, reach `want` (in
   // tokens or in weight), which they do: leaves the key and what is still wanted of it.
@@ -312,7 +684,7 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
       __syncthreads();
       for (uint32_t r = 0; r < rounds; ++r) {
         const uint32_t i = r * SM_THREADS + tid;
-        const uint4 v = i < n ? slice[i] : make_uint4(0, 0, 0, 0);
+        const uint4 v = i < n ? block(i) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (uint32_t k = 0; k < E; ++k) {
           const float y = Logits<T>::at(v, k);
@@ -345,12 +717,11 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
         }
         sum += mine[j];
       }
-      uint64_t inc = warp_incl_scan(sum);
+      const uint64_t inc = warp_incl_scan(sum);
       if (lane == 31) s.scan[warp] = inc;
       __syncthreads();
-      uint64_t before = 0;
+      uint64_t before = inc - sum;
       for (uint32_t q = 0; q < warp; ++q) before += s.scan[q];
-      before += inc - sum;
 #pragma unroll
       for (uint32_t j = 0; j < SM_BINS / SM_THREADS; ++j) {
         if (before < want && before + mine[j] >= want) {
@@ -372,32 +743,50 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
   // Sums of what passes the threshold: over this warp's run of the slice, then over all before it.
   const uint32_t per = (n + SM_WARPS - 1) / SM_WARPS, i0 = min(n, warp * per), i1 = min(n, i0 + per);
   struct Sums {
-    uint64_t mass, before, ties_before;   // of all; before this warp: weight above the threshold, tokens on it
-    uint64_t ties, count;                 // on it, above it, in all
-    uint64_t own;                         // this warp's weight above it
+    uint64_t mass, above, before, ties_before;   // of all; of the bins above the border's; before this warp:
+                                                 // weight above the threshold, tokens on it
+    uint64_t ties, count;                        // on it, above it, in all
+    uint64_t own;                                // this warp's weight above it
     uint32_t own_ties;
   };
-  auto sums = [&](bool with_mass) -> Sums {
-    uint64_t m = 0;
+  // extra(y, index, in): whether its weight counts as `above`
+  auto sums = [&](auto weighed, auto&& extra) -> Sums {
+    constexpr bool W = decltype(weighed)::value;
+    const float limit = key_logit(th.key);
+    uint64_t m = 0, up = 0;
     uint32_t on = 0, above = 0;
     for (uint32_t i = i0; i < i1; i += 32) {
       const bool have = i + lane < i1;
-      const uint4 v = have ? slice[i + lane] : make_uint4(0, 0, 0, 0);
+      const uint4 v = have ? block(i + lane) : make_uint4(0, 0, 0, 0);
+      float y[E];
+      bool in[E];
+      Weight w[E], more = {0, 0};
 #pragma unroll
       for (uint32_t k = 0; k < E; ++k) {
-        const float y = Logits<T>::at(v, k);
-        const uint32_t key = key_of(y);
-        const bool in = have && key > th.key;
-        if (with_mass) m += weight(y, in);
-        above += in;
-        on += have && key == th.key;
+        y[k] = Logits<T>::at(v, k);
+        in[k] = have && y[k] > limit;
+        above += in[k];
+        on += have && y[k] == limit;
+      }
+      if constexpr (W) {
+        weigh(y, in, w);
+        m += total_of(w);
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k)
+          if (extra(y[k], (b0 + i + lane) * E + k - off, in[k])) {
+            more.hi += w[k].hi;
+            more.lo += w[k].lo;
+          }
+        up += whole(more, bits);
       }
     }
     m = warp_sum64(m);
+    up = warp_sum64(up);
     on = __reduce_add_sync(0xffffffffu, on);
     above = __reduce_add_sync(0xffffffffu, above);
     if (lane == 0) {
       s.warp_mass[warp] = m;
+      s.warp_above[warp] = up;
       s.warp_ties[warp] = on;
       s.warp_count[warp] = above;
     }
@@ -408,9 +797,11 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
     for (uint32_t q = lane; q < nc * SM_WARPS; q += 32) {
       const uint32_t r = q / SM_WARPS, w = q % SM_WARPS;
       const uint64_t wm = nc > 1 ? cluster_read(&s.warp_mass[w], r) : s.warp_mass[w];
+      const uint64_t wu = nc > 1 ? cluster_read(&s.warp_above[w], r) : s.warp_above[w];
       const uint32_t wt = nc > 1 ? cluster_read(&s.warp_ties[w], r) : s.warp_ties[w];
       const uint32_t wc = nc > 1 ? cluster_read(&s.warp_count[w], r) : s.warp_count[w];
       t.mass += wm;
+      t.above += wu;
       t.ties += wt;
       t.count += wc;
       if (q < rank * SM_WARPS + warp) {
@@ -419,6 +810,7 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
       }
     }
     t.mass = warp_sum64(t.mass);
+    t.above = warp_sum64(t.above);
     t.ties = warp_sum64(t.ties);
     t.count = warp_sum64(t.count);
     t.before = warp_sum64(t.before);
@@ -426,345 +818,276 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constan
     sync();   // read by all before it is written again
     return t;
   };
-
-  // ---- few candidates ----
-  // At least `want` tokens lie at or above the want-th largest of the threads'
-  // maxima, and seldom many more.  Where top-k, top-p or min-p leaves only some
-  // of those, they are gathered and sorted by the first CTA, and the rest of the
-  // row is not looked at again.  The sum that top-p is a share of is first taken
-  // in 32 bits; only if a border lies within what that may be off, exactly.
-  const bool by_k = top_k != 0u && top_k < a.vocab, by_p = top_p < 1.f, by_min = s.min_p > 0.f;
-  const uint32_t threads = nc * SM_THREADS, most = min(SM_WANT_MOST, threads * 3 / 4);
-  uint32_t way = WAY_WIDE;
-  if ((by_k || by_p || by_min) && top < INFINITY) {
-    const uint32_t want = by_k && top_k <= most ? top_k : min(SM_WANT, most);
-    const bool all_of_k = by_k && top_k <= most;   // the candidates hold the first top_k
-    // maxima counted by how far they lie below the largest
-    // (as far as weights go: beyond 45 T they are below 2^-64)
-    const float per_bin = (float)SM_COARSE / fmaxf(fminf(top - key_logit(least), 45.f * T_), 1e-30f);
-    auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_COARSE - 1)); };
-    if (my_top > -INFINITY) {
-      const uint32_t b = bin_of(my_top);
-      if (nc > 1)
-        for (uint32_t r = 0; r < nc; ++r) cluster_count(&s.coarse[b], r);
-      else
-        atomicAdd(&s.coarse[b], 1u);
-    }
-    if (by_p && !all_of_k) {
-      float sum = 0.f;
-      for (uint32_t i = tid; i < n; i += SM_THREADS) {
-        const uint4 v = slice[i];
-#pragma unroll
-        for (uint32_t k = 0; k < E; ++k) {
-          const float y = Logits<T>::at(v, k);
-          if (y > -INFINITY) {                      // (and no NaN)
-            const float d = top - y, z = d * scale.hi, e = fmaf(d, scale.lo, fmaf(d, scale.hi, -z));
-            if (z < 64.f) sum = fmaf(ex2(-z), fmaf(e, -LN2, 1.f), sum);
-          }
-        }
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (lane == 0) s.warp_rough[warp] = sum;
-    }
-    sync();
-    // the bin at which `want` maxima are reached: its far end is the cut
-    static_assert(SM_COARSE == SM_THREADS, "a bin a thread");
-    if (tid == 0) {
-      s.cut = SM_COARSE;
-      float sum = 0.f;
-      for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
-      s.rough = sum;
-    }
-    const uint32_t mine = s.coarse[tid], inc = warp_incl_scan(mine);
-    if (lane == 31) s.warp_count[warp] = inc;
-    __syncthreads();
-    uint32_t before = inc - mine;
-    for (uint32_t w = 0; w < warp; ++w) before += s.warp_count[w];
-    if (before < want && before + mine >= want) s.cut = tid;
-    __syncthreads();
-    const uint32_t cut = s.cut;                      // SM_COARSE: fewer maxima than wanted, so every token
-    const bool with_min = by_min && !all_of_k;       // (top-p's sum is over the first top_k, whatever min-p says)
-    auto candidate = [&](float y) {
-      return y > -INFINITY && (cut == SM_COARSE || bin_of(y) <= cut) && (!with_min || logit_key(y) > th.key);
-    };
-    if (candidate(my_top))
-      for (uint32_t i = tid; i < n; i += SM_THREADS) {
-        const uint4 v = slice[i];
-#pragma unroll
-        for (uint32_t k = 0; k < E; ++k) {
-          const float y = Logits<T>::at(v, k);
-          if (!candidate(y)) continue;
-          const unsigned long long item = (unsigned long long)logit_key(y) << 32 | ~((b0 + i) * E + k - off);
-          if (nc > 1) {
-            const uint32_t at = cluster_take(&s.listed, 0, 1u);
-            if (at < SM_LIST) cluster_write(&s.mass[at], 0, item);
-          } else {
-            const uint32_t at = atomicAdd(&s.listed, 1u);
-            if (at < SM_LIST) s.mass[at] = item;
-          }
-        }
-      }
-    sync();
-    // ---- the first CTA's ----
-    unsigned long long* list = s.mass;
-    unsigned long long* weights = s.mass + SM_LIST;
-    // Whether every token that min-p leaves is a candidate, or every token.
-    const uint32_t listed = rank == 0 ? s.listed : 0;
-    uint64_t own[2] = {0, 0}, ahead[2] = {0, 0};               // weights of this thread's two candidates, and of those ahead
-    bool whole = false;
-    double rough = 0.0;
-    // how many stay, given the sum that top-p is a share of; false: not the tokens alone decide
-    auto count_below = [&](uint64_t limit, uint32_t first) -> uint32_t {
-      const uint32_t mine2 = (2 * tid < first && ahead[0] < limit) + (2 * tid + 1 < first && ahead[1] < limit);
-      return (uint32_t)__syncthreads_count(mine2 >= 1) + (uint32_t)__syncthreads_count(mine2 >= 2);
-    };
-    uint32_t stay = 0, first = 0;
-    if (rank == 0) {
-      way = WAY_WIDE;
-      if (listed > 0 && listed <= SM_LIST) {
-        uint32_t size = 2;
-        while (size < listed) size *= 2;
-        for (uint32_t i = listed + tid; i < size; i += SM_THREADS) list[i] = 0;
-        sort_items(list, size, true);
-        uint64_t sum = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-          const uint32_t i = 2 * tid + j;
-          own[j] = weight(key_logit((uint32_t)(list[min(i, SM_LIST - 1)] >> 32)), i < listed);
-          if (i < listed) weights[i] = own[j];
-          sum += own[j];
-        }
-        const uint64_t run = warp_incl_scan(sum);
-        if (lane == 31) s.scan[warp] = run;
-        __syncthreads();
-        uint64_t base = run - sum;
-        for (uint32_t w = 0; w < warp; ++w) base += s.scan[w];
-        ahead[0] = base;
-        ahead[1] = base + own[0];
-        uint64_t list_mass = 0;
-        for (uint32_t w = 0; w < SM_WARPS; ++w) list_mass += s.scan[w];
-        // min-p's
-        uint32_t by_limit = listed;
-        if (by_min) {
-          const uint32_t in = (2 * tid < listed && (uint32_t)(list[2 * tid] >> 32) > th.key) +
-                              (2 * tid + 1 < listed && (uint32_t)(list[2 * tid + 1] >> 32) > th.key);
-          by_limit = (uint32_t)__syncthreads_count(in >= 1) + (uint32_t)__syncthreads_count(in >= 2);
-        }
-        // every token that counts for the outcome of top-k and min-p is listed:
-        // all of them, the first top_k, or all that min-p leaves
-        whole = cut == SM_COARSE || all_of_k || by_limit < listed || (with_min && bin_of(key_logit(th.key + 1u)) <= cut);
-        first = all_of_k ? min(top_k, listed) : listed;
-        stay = min(first, by_limit);
-        if (!by_p) {
-          if (by_k) stay = min(stay, top_k);
-          way = whole ? WAY_DONE : WAY_WIDE;
-        } else if (all_of_k || (cut == SM_COARSE && !with_min && !by_k)) {   // the sum is the listed ones'
-          const uint64_t sum_first = first == listed ? list_mass : [&] {
-            if (tid == first / 2) s.found_left = ahead[first & 1];
-            __syncthreads();
-            return (uint64_t)s.found_left;
-          }();
-          stay = min(stay, max(1u, count_below(scaled(sum_first, top_p, true), first)));
-          way = WAY_DONE;
-        } else if (!by_k) {
-          if (nc > 1) {
-            for (uint32_t r = 0; r < nc; ++r) rough += (double)__uint_as_float(cluster_read((const uint32_t*)&s.rough, r));
-          } else {
-            rough = (double)s.rough;
-          }
-          rough *= exp2((double)a.frac_bits) * (double)top_p;
-          const uint32_t lo = max(1u, count_below((uint64_t)(rough * (1.0 - SM_SLACK)), listed));
-          const uint32_t hi = max(1u, count_below((uint64_t)(rough * (1.0 + SM_SLACK)) + 2, listed));
-          // (hi == listed: top-p may leave tokens that are not listed)
-          if (!whole && hi == listed)
-            way = WAY_WIDE;
-          else if (min(lo, stay) == min(hi, stay))
-            way = WAY_DONE, stay = min(lo, stay);
-          else
-            way = WAY_MASS;
-        }
-      }
-      if (tid < nc) {   // to every CTA's own: this one may be gone before they look
-        if (nc > 1)
-          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_at(step_smem(&s.way), tid)), "r"(way) : "memory");
-        else
-          s.way = way;
-      }
-    }
-    sync();
-    way = s.way;
-    if (way == WAY_MASS) {
-      const Threshold keep = th;
-      th = {KEY_NONE, 0};
-      const uint64_t sum = sums(true).mass;
-      th = keep;
-      if (rank == 0) stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), listed)));
-      way = WAY_DONE;
-    }
-    if (way == WAY_DONE) {
-      if (rank == 0) {
-        // the sum of those that stay, then where it passes the goal, by index
-        if (2 * tid < stay && stay <= 2 * tid + 2) s.found_left = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
-        __syncthreads();
-        const uint64_t total = s.found_left, goal = scaled(total, s.u, false);
-        uint32_t size = 2;
-        while (size < stay) size *= 2;
-        unsigned long long item[2];
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) item[j] = 2 * tid + j < stay ? list[2 * tid + j] : 0;
-        __syncthreads();
-        // places rise, and each remembers its candidate; keys and weights stay where they are
-        unsigned long long* order = (unsigned long long*)s.count;   // 1,024 of them
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j)
-          if (2 * tid + j < size)
-            order[2 * tid + j] = 2 * tid + j < stay ? (unsigned long long)~(uint32_t)item[j] << 32 | (2 * tid + j) : ~0ull;
-        sort_items(order, size, false);
-        uint64_t w2[2], sum = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-          w2[j] = 2 * tid + j < stay ? weights[(uint32_t)order[2 * tid + j]] : 0;
-          sum += w2[j];
-        }
-        const uint64_t run = warp_incl_scan(sum);
-        if (lane == 31) s.scan[warp] = run;
-        __syncthreads();
-        uint64_t at = run - sum;
-        for (uint32_t w = 0; w < warp; ++w) at += s.scan[w];
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-          if (goal >= at && goal < at + w2[j]) {
-            const unsigned long long o = order[2 * tid + j];
-            const float y = key_logit((uint32_t)(list[(uint32_t)o] >> 32));
-            const double less = y == top ? 0.0 : ((double)top - (double)y) / (double)T_;
-            finish((uint32_t)(o >> 32), -(float)(less + log((double)total * exp2(-(double)a.frac_bits))), stay);
-          }
-          at += w2[j];
-        }
-      }
-      return;
-    }
-  }
-
-  if (top_k != 0u && top_k < a.vocab) {
-    if (sums(false).count > top_k) {
+  auto nothing = [](float, uint32_t, bool) { return false; };
+  auto cut_to_k = [&] {
+    if (by_k && sums(std::false_type(), nothing).count > top_k) {
       uint64_t left;
       th.key = select(std::false_type(), top_k, &left);
       th.ties = (uint32_t)left;
     }
-  }
-  if (top_p < 1.f) {
-    // the mass of the first k: with min-p's cut it is not that, so top-k's own threshold counts
-    Threshold cut = th;
-    Threshold k_only = {KEY_NONE, 0};
-    if (s.min_p > 0.f) {
-      th = k_only;
-      if (top_k != 0u && top_k < a.vocab && sums(false).count > top_k) {
-        uint64_t left;
-        th.key = select(std::false_type(), top_k, &left);
-        th.ties = (uint32_t)left;
-      }
+  };
+
+  cut_to_k();
+  if (by_p) {
+    const Threshold cut = th;
+    if (by_min) {          // top-p's sum is over the first top_k, whatever min-p says
+      th = {KEY_NONE, 0};
+      cut_to_k();
     }
-    const Sums t = sums(true);
     const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
+    // The border's bin, by weights in 32 bits: `bins` of equal width, whole
+    // numbers that add up to about 2^31.
+    const float per_bin = (float)SM_BINS / span;
+    auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_BINS - 1)); };
+    uint32_t border = SM_BINS;
+    if (top < INFINITY) {
+      const float limit = key_logit(th.key);
+      rough_sum(limit);
+      for (uint32_t i = tid; i < SM_BINS; i += SM_THREADS) s.count[i] = 0;
+      if (tid == 0) {
+        s.found = SM_BINS;
+        s.listed = 0;
+      }
+      sync();
+      const float sum_f = rough_total(), unit = 2147483648.f / sum_f;
+      if (th.ties == 0u) bits_for(sum_f);
+      each_block([&](uint32_t, const uint4& v) {
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k) {
+          const float y = Logits<T>::at(v, k);
+          if (y > limit) atomicAdd(&s.count[bin_of(y)], (uint32_t)fmaf(rough_weight(y), unit, 0.5f));
+        }
+      });
+      sync();
+      constexpr uint32_t EACH = SM_BINS / SM_THREADS;
+      uint64_t mine[EACH], sum = 0;
+#pragma unroll
+      for (uint32_t j = 0; j < EACH; ++j) {
+        mine[j] = 0;
+        for (uint32_t q = 0; q < nc; ++q)
+          mine[j] += nc > 1 ? cluster_read(&s.count[tid * EACH + j], q) : s.count[tid * EACH + j];
+        sum += mine[j];
+      }
+      const uint64_t inc = warp_incl_scan(sum);
+      if (lane == 31) s.scan[warp] = inc;
+      __syncthreads();
+      uint64_t before = inc - sum, all = 0;
+      for (uint32_t q = 0; q < SM_WARPS; ++q) {
+        if (q < warp) before += s.scan[q];
+        all += s.scan[q];
+      }
+      const float ties_f = (float)(tie * th.ties) / (float)(1ull << bits) * unit;
+      const uint64_t want = max((uint64_t)1, (uint64_t)(((float)all + ties_f) * top_p));
+#pragma unroll
+      for (uint32_t j = 0; j < EACH; ++j) {
+        if (before < want && before + mine[j] >= want) s.found = tid * EACH + j;
+        before += mine[j];
+      }
+      sync();
+      border = s.found;
+    }
+    // exactly: all of it, what lies above the bin, and the bin's tokens
+    const Sums t = sums(std::true_type(), [&](float y, uint32_t index, bool in) {
+      if (!in || border == SM_BINS) return false;
+      const uint32_t b = bin_of(y);
+      if (b == border) enlist(y, index);
+      return b < border;
+    });
     const uint64_t want = scaled(t.mass + tie * th.ties, top_p, true);
-    if (want <= t.mass) {
-      uint64_t left;
-      const uint32_t key = select(std::true_type(), want, &left);
-      const uint64_t w = weight(key_logit(key), true);
-      th.key = key;
-      th.ties = (uint32_t)min((left + w - 1) / w, (uint64_t)0xFFFFFFFFu);
-    } else {
+    if (want > t.mass) {
       th.ties = (uint32_t)min((want - t.mass + tie - 1) / tie, (uint64_t)th.ties);
+    } else {
+      if (rank == 0) {
+        Threshold found = {0, 0};
+        const uint32_t listed = s.listed;
+        if (border != SM_BINS && want > t.above && listed > 0 && listed <= SM_LIST) {
+          const uint64_t all = sort_list(listed);
+          if (want <= t.above + all) {
+            const uint32_t n_in = count_below(want - t.above, listed);   // at least 1
+            const uint32_t key = (uint32_t)(list[n_in - 1] >> 32);
+            const uint32_t on = (2 * tid < n_in && (uint32_t)(list[2 * tid] >> 32) == key) +
+                                (2 * tid + 1 < n_in && (uint32_t)(list[2 * tid + 1] >> 32) == key);
+            found = {key, (uint32_t)__syncthreads_count(on >= 1) + (uint32_t)__syncthreads_count(on >= 2)};
+          }
+        }
+        if (tid < nc) {
+          if (nc > 1) {
+            cluster_write(&s.border.key, tid, found.key);
+            cluster_write(&s.border.ties, tid, found.ties);
+          } else {
+            s.border = found;
+          }
+        }
+      }
+      sync();
+      const Threshold found = s.border;
+      if (found.ties != 0u) {
+        th = found;
+      } else {             // too many tokens in the bin, or 32 bits named a wrong one
+        uint64_t left;
+        const uint32_t key = select(std::true_type(), want, &left);
+        const uint64_t w = weight(key_logit(key), true);
+        th.key = key;
+        th.ties = (uint32_t)min((left + w - 1) / w, (uint64_t)0xFFFFFFFFu);
+      }
     }
     if (cut.key > th.key || (cut.key == th.key && cut.ties < th.ties)) th = cut;
   }
 
   // ---- the token ----
-  const Sums t = sums(true);
+  const Sums t = sums(std::true_type(), nothing);
   const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
   const uint64_t ties = min((uint64_t)th.ties, t.ties);
   const uint64_t total = t.mass + tie * ties;
   const uint64_t goal = scaled(total, s.u, false);   // the first running sum above it
-  uint64_t ties_before = min(ties, t.ties_before);
-  uint64_t at = t.before + tie * ties_before;
-  const uint64_t own = t.own + tie * (min(ties, t.ties_before + t.own_ties) - ties_before);
-  if (goal >= at && goal < at + own) {              // this warp's run has it
-    for (uint32_t i = i0; i < i1; i += 32) {
-      const bool have = i + lane < i1;
-      const uint4 v = have ? slice[i + lane] : make_uint4(0, 0, 0, 0);
-      uint64_t w[E], sum = 0;
-      uint32_t on = 0;
+  uint64_t ties_before = t.ties_before;
+  uint64_t at = t.before + tie * min(ties, ties_before);
+  const uint64_t mine = t.own + tie * (min(ties, ties_before + t.own_ties) - min(ties, ties_before));
+  // The warp whose run has it shares the run with the CTA's other warps.
+  const bool has = goal >= at && goal < at + mine;
+  if (has && lane == 0) s.run = {i0, i1, at, ties_before};
+  if (!__syncthreads_or(has)) return true;
+  const uint32_t r1 = s.run.last, part = (r1 - s.run.first + SM_WARPS - 1) / SM_WARPS;
+  const uint32_t j0 = min(r1, s.run.first + warp * part), j1 = min(r1, j0 + part);
+  // a lane's weights of its block, those on the threshold aside, which `on` counts
+  const float limit = key_logit(th.key);
+  auto step = [&](uint32_t i, float (&y)[E], Weight (&w)[E], uint32_t* on) {
+    const bool have = i + lane < j1;
+    const uint4 v = have ? block(i + lane) : make_uint4(0, 0, 0, 0);
+    bool in[E];
+    *on = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < E; ++k) {
+      y[k] = Logits<T>::at(v, k);
+      in[k] = have && y[k] > limit;
+      *on += have && y[k] == limit;
+    }
+    weigh(y, in, w);
+  };
+  float y[E];
+  Weight w[E];
+  uint64_t m = 0;
+  uint32_t on = 0, all_on = 0;
+  for (uint32_t i = j0; i < j1; i += 32) {
+    step(i, y, w, &on);
+    all_on += on;
+    m += total_of(w);
+  }
+  m = warp_sum64(m);
+  all_on = __reduce_add_sync(0xffffffffu, all_on);
+  if (lane == 0) {
+    s.warp_mass[warp] = m;
+    s.warp_ties[warp] = all_on;
+  }
+  __syncthreads();
+  at = s.run.at + warp_sum64(lane < warp ? s.warp_mass[lane] : 0);
+  ties_before = s.run.ties + __reduce_add_sync(0xffffffffu, lane < warp ? s.warp_ties[lane] : 0u);
+  // (`at` counts what lies above the threshold; ties are added as they come)
+  at += tie * (min(ties, ties_before) - min(ties, s.run.ties));
+  if (goal < at || goal >= at + m + tie * (min(ties, ties_before + all_on) - min(ties, ties_before))) return true;
+  for (uint32_t i = j0; i < j1; i += 32) {
+    step(i, y, w, &on);
+    const uint32_t on_inc = warp_incl_scan(on);
+    uint64_t rank_on = ties_before + on_inc - on;
+    const uint64_t sum = total_of(w) + tie * (min(ties, rank_on + on) - min(ties, rank_on));
+    const uint64_t inc = warp_incl_scan(sum), all = __shfl_sync(0xffffffffu, inc, 31);
+    if (goal < at + all) {
+      uint64_t upto = at + inc - sum;
+      bool done = !(goal >= upto && goal < upto + sum);
 #pragma unroll
       for (uint32_t k = 0; k < E; ++k) {
-        const float y = Logits<T>::at(v, k);
-        const uint32_t key = key_of(y);
-        w[k] = weight(y, have && key > th.key);
-        sum += w[k];
-        on += have && key == th.key;
-      }
-      const uint32_t on_inc = warp_incl_scan(on);
-      uint64_t rank_on = ties_before + on_inc - on;  // (counted on past `ties`, where it has no effect)
-      const uint64_t kept_on = min(ties, rank_on + on) - min(ties, rank_on);
-      sum += tie * kept_on;
-      const uint64_t inc = warp_incl_scan(sum);
-      const uint64_t all = __shfl_sync(0xffffffffu, inc, 31);
-      if (goal < at + all) {
-        uint64_t run = at + inc - sum;
-        if (goal >= run && goal < run + sum) {
-          bool done = false;
-#pragma unroll
-          for (uint32_t k = 0; k < E; ++k) {
-            uint64_t wk = w[k];
-            const float y = Logits<T>::at(v, k);
-            if (have && key_of(y) == th.key) {
-              if (rank_on < ties) wk = tie;
-              ++rank_on;
-            }
-            run += wk;
-            if (!done && goal < run) {
-              done = true;
-              const double less = y == top ? 0.0 : ((double)top - (double)y) / (double)T_;
-              finish((b0 + i + lane) * E + k - off, -(float)(less + log((double)total * exp2(-(double)a.frac_bits))),
-                     (uint32_t)(t.count + ties));
-            }
-          }
+        uint64_t wk = whole(w[k], bits);
+        if (i + lane < j1 && y[k] == limit) {
+          if (rank_on < ties) wk = tie;
+          ++rank_on;
         }
-        break;
+        upto += wk;
+        if (!done && goal < upto) {
+          done = true;
+          with_log((b0 + i + lane) * E + k - off, y[k], total, (uint32_t)(t.count + ties));
+        }
       }
-      at += all;
-      ties_before += __shfl_sync(0xffffffffu, on_inc, 31);
+      break;
     }
+    at += all;
+    ties_before += __shfl_sync(0xffffffffu, on_inc, 31);
   }
-  if (nc > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
+  return true;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  __shared__ SampleShared s;
+  wait_predecessor();
+  const uint32_t nc = a.cluster;
+  if (!a.queued) {         // a row a cluster
+    const uint32_t row = blockIdx.x / nc;
+    const bool done = sample_row<T>(a, s, (uint4*)smem_raw, row);
+    if (!done && threadIdx.x == 0 && blockIdx.x % nc == 0) a.queue[atomicAdd(a.counter, 1u)] = row;
+    if (nc > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
+    return;
+  }
+  // the rows that were left, in turn
+  const uint32_t rows = *(volatile uint32_t*)a.counter;
+  for (uint32_t i = blockIdx.x / nc; i < rows; i += gridDim.x / nc) {
+    sample_row<T>(a, s, (uint4*)smem_raw, a.queue[i]);
+    if (nc > 1)
+      cluster_sync();
+    else
+      __syncthreads();
+  }
+  // the last CTA to leave sets the count back for the next call
+  __syncthreads();
+  if (threadIdx.x == 0 && ticket(a.counter + 1) == gridDim.x - 1) {
+    a.counter[0] = 0u;
+    a.counter[1] = 0u;
+  }
 }
 
 template <typename T>
 static uint32_t sample_blocks(uint32_t vocab) { return vocab / Logits<T>::E + 2; }
 
-template <typename T>
-static void launch(const LaunchCfg& L, SampleArgs a, int sms) {
-  // CTAs of a row: as many as its slices need, and more while the GPU has room
-  const uint32_t blocks = sample_blocks<T>(a.vocab);
+// CTAs of a row: as many as two an SM leave room for, of at least two blocks a
+// thread.  Of a wide row where it is on its own: as many as there can be.
+static uint32_t row_ctas(uint32_t blocks, uint64_t rows, int sms) {
   uint32_t nc = 1;
-  while (nc < SM_MAX_CLUSTER && ((uint64_t)ceil_div(blocks, nc) * 16 > SM_SLICE / 3 ||
-                                 ((uint64_t)a.rows * nc * 2 <= (uint64_t)sms && blocks / (nc * 2) >= SM_THREADS)))
-    nc *= 2;
-  a.cluster = nc;
-  a.blocks = (uint32_t)ceil_div(blocks, nc);
-  // the largest sum of weights stays below 2^63
-  a.frac_bits = 46;
-  while (((uint64_t)a.vocab << a.frac_bits) >> 62) --a.frac_bits;
-  launch_k(L, K_SAMPLE, sample_kernel<T>, a.rows * nc, SM_THREADS, (size_t)a.blocks * 16, a, dim3(nc));
+  while (nc < SM_MAX_CLUSTER && rows * nc * 2 <= (uint64_t)sms * 2 && blocks / (nc * 2) >= 2 * SM_THREADS) nc *= 2;
+  return nc;
+}
+static uint32_t blocks_of(uint32_t vocab, int dtype) {
+  return dtype == RO_F32 ? sample_blocks<float>(vocab) : sample_blocks<__half>(vocab);
+}
+bool sample_queues(uint32_t vocab, int dtype, uint64_t rows, int sms) {
+  const uint32_t blocks = blocks_of(vocab, dtype);
+  return row_ctas(blocks, rows, sms) * 2 < row_ctas(blocks, 1, sms);
+}
+template <typename T>
+static void launch(const LaunchCfg& L, SampleArgs a, int dtype, int sms) {
+  const uint32_t blocks = blocks_of(a.vocab, dtype);
+  auto go = [&](uint32_t nc, uint32_t clusters) {
+    a.cluster = nc;
+    a.blocks = (uint32_t)ceil_div(blocks, nc);
+    a.staged = (uint64_t)a.blocks * 16 <= SM_SLICE;
+    launch_k(L, K_SAMPLE, sample_kernel<T>, clusters * nc, SM_THREADS, a.staged ? (size_t)a.blocks * 16 : 0, a, dim3(nc));
+  };
+  a.later = a.queue != nullptr;
+  go(row_ctas(blocks, a.rows, sms), a.rows);
+  if (!a.later) return;
+  a.later = 0;
+  a.queued = 1;
+  const uint32_t wide = row_ctas(blocks, 1, sms);
+  go(wide, std::min<uint32_t>(a.rows, (uint32_t)sms * 2 / wide));
 }
 void launch_sample(const LaunchCfg& L, const SampleArgs& a, int dtype, int sms) {
-  dtype == RO_F32 ? launch<float>(L, a, sms) : dtype == RO_F16 ? launch<__half>(L, a, sms) : launch<__nv_bfloat16>(L, a, sms);
+  dtype == RO_F32   ? launch<float>(L, a, dtype, sms)
+  : dtype == RO_F16 ? launch<__half>(L, a, dtype, sms)
+                    : launch<__nv_bfloat16>(L, a, dtype, sms);
 }
 
 template <typename T>
 static cudaError_t allow() {
-  return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SM_SLICE + 64));
+  return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SM_SLICE);
 }
 cudaError_t prepare_sample_kernels() {
   for (cudaError_t e : {allow<float>(), allow<__half>(), allow<__nv_bfloat16>()})

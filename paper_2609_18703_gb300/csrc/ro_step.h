@@ -32,7 +32,7 @@ class StepCall {
   int prev_ = -1;
 };
 // (SS_COUNTER is zero between calls, whichever kernel used it last)
-enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_JOIN = 2, SS_PAGES = 3, SS_COUNT };
+enum StepScratch { SS_PARTIAL = 0, SS_COUNTER = 1, SS_JOIN = 2, SS_PAGES = 3, SS_ROWS = 4, SS_COUNT };
 
 // ---- rotary, append -----------------------------------------------------------------
 constexpr uint32_t ROPE_MAX_PAIRS = 128;
@@ -241,7 +241,7 @@ struct PageCopyArgs {
 void launch_page_copy(const LaunchCfg& L, const PagedArgs& c, const MoveArgs& m, uint32_t* err, int sms);
 
 // ---- sample -----------------------------------------------------------------------------
-constexpr uint32_t MAX_VOCAB = 393216;   // eight slices of 192 KB of 32-bit logits
+constexpr uint32_t MAX_VOCAB = 393216;   // a thread's share of it bounds the error of its 32-bit sums
 struct SampleArgs {
   const void* x;
   uint64_t stride;
@@ -255,9 +255,15 @@ struct SampleArgs {
   float* logp;               // optional
   uint32_t* kept;            // optional
   uint32_t cluster, blocks;  // CTAs of a row, 16-byte blocks of a slice
-  uint32_t frac_bits;        // of a weight
+  uint32_t staged;           // slices are held in shared memory
+  uint32_t later;            // wide rows are queued
+  uint32_t queued;           // the queue's rows are taken
+  uint32_t* queue;           // [rows]
+  uint32_t* counter;         // of the queue, and a ticket: zero between calls
   uint32_t* err;
 };
+// whether wide rows are queued for a second kernel (a.queue and a.counter are then given)
+bool sample_queues(uint32_t vocab, int dtype, uint64_t rows, int sms);
 void launch_sample(const LaunchCfg& L, const SampleArgs& a, int dtype, int sms);
 cudaError_t prepare_sample_kernels();
 

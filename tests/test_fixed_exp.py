@@ -16,7 +16,6 @@ def test_weights_are_exp_to_forty_bits(tmp_path):
     subprocess.run([shutil.which("g++"), "-std=c++17", "-O1", "-ffp-contract=off", "-I", CSRC,
                     os.path.join(HERE, "fixed_exp_model.cpp"), "-o", exe], check=True)
     worst, risen, one, none = subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()
-    # z below 29 in units of 2^-43, off by three such units and 2^-24 of the correction's 2^-18: 2^-41 of z, ln 2 of it
-    # in the weight; the tables' and products' floors 2^-43 each
+    # pairs of floats: some 2^-44 for the argument, the table and each of the terms
     assert float(worst) < 2.0
     assert (risen, one, none) == ("0", "1", "1")
