@@ -166,10 +166,11 @@ constexpr uint32_t SM_LIST = 2 * SM_THREADS, SM_WANT = 512, SM_WANT_MOST = 704;
 static_assert(2 * SM_LIST <= SM_BINS, "candidates and their weights lie where the bins do");
 constexpr uint32_t SM_COARSE = SM_THREADS;   // bins of the threads' maxima
 // What a sum of weights in 32 bits may be off, relative to itself: a weight's
-// argument, below 64, by 2^-23 of itself, its exponential by 2^-22; a thread's
-// terms, at most 800 in two levels of sums of at most 200, by 2^-24 a sum.
+// argument, below 64, by three roundings, 2^-17; its exponential by 2^-22; a
+// thread's terms, at most 800 in two levels of sums of at most 200, by 2^-24 a sum.
 constexpr float SM_SLACK = 1.f / (1 << 15);
 enum SampleWay : uint32_t { WAY_DONE, WAY_MASS, WAY_WIDE };
+constexpr uint32_t QUEUE_WIDE = 0x80000000u;   // beside a queued row: WAY_WIDE
 
 struct __align__(16) SampleShared {
   unsigned long long mass[SM_BINS];
@@ -196,10 +197,11 @@ struct __align__(16) SampleShared {
   double reach;                            // how far below the largest logit min-p reaches
 };
 
-// One row, by a cluster of a.cluster CTAs (or one).  false: it is left to the
-// clusters (a.later), whole CTAs alike.
-template <typename T>
-__device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s, uint4* slice, uint32_t row) {
+// One row, by a cluster of a.cluster CTAs (or one).  WIDE: whatever its
+// settings; else, unless the way is WAY_DONE, it is left to others.  known_wide:
+// not by its candidates.
+template <typename T, bool WIDE>
+__device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared& s, uint4* slice, uint32_t row, bool known_wide) {
   constexpr uint32_t E = Logits<T>::E;
   // the low bits of a 16-bit logit's key follow from its sign
   constexpr int LOW = std::is_same_v<T, float> ? 0 : std::is_same_v<T, __half> ? 11 : 16;
@@ -316,7 +318,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
   };
   if (!s.valid || best == KEY_NONE) {
     if (rank == 0 && tid == 0) finish(NO_TOKEN, -INFINITY, 0);
-    return true;
+    return WAY_DONE;
   }
   if (T_ == 0.f || top_k == 1u || top_p == 0.f) {   // the first of the largest
     uint32_t place = ~0u;
@@ -336,7 +338,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
       place = __reduce_min_sync(0xffffffffu, warp == 0 && lane < nc ? place : ~0u);
       if (tid == 0) finish(place, 0.f, 1);
     }
-    return true;
+    return WAY_DONE;
   }
 
   // ---- weights ----
@@ -388,25 +390,30 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
   };
   // in 32 bits, of a logit that is no NaN
   auto rough_weight = [&](float y) -> float {
-    if (y == top) return 1.f;
-    const float d = top - y, z = d * scale.hi, e = fmaf(d, scale.lo, fmaf(d, scale.hi, -z));
-    return z < 64.f ? ex2(-z) * fmaf(e, -LN2, 1.f) : 0.f;
+    const float z = (top - y) * scale.hi;
+    return z < 64.f ? ex2(-z) : 0.f;
   };
   auto key_of = [&](float y) -> uint32_t { return y == y ? logit_key(y) : KEY_NONE; };   // (a NaN is never drawn)
-  auto each_block = [&](auto&& use) {
-    for (uint32_t i = tid; i < n; i += SM_THREADS) use(i, block(i));
+  auto each_block = [&](auto&& use) {              // several loads at a time
+    for (uint32_t i = tid; i < n; i += 4 * SM_THREADS) {
+      uint4 v[4];
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) v[q] = i + q * SM_THREADS < n ? block(i + q * SM_THREADS) : none;
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) use(v[q]);
+    }
   };
   // a thread's 32-bit sums, of the CTA: in s.rough once the CTA has met
   auto rough_sum = [&](float above) {
     float sum = 0.f;
-    each_block([&](uint32_t, const uint4& v) {
-      float part = 0.f;
+    each_block([&](const uint4& v) {
+      float part[2] = {0.f, 0.f};
 #pragma unroll
       for (uint32_t k = 0; k < E; ++k) {
-        const float y = Logits<T>::at(v, k);
-        if (y > above) part += rough_weight(y);
+        const float y = Logits<T>::at(v, k), w = rough_weight(y);
+        part[k & 1] += y > above ? w : 0.f;
       }
-      sum += part;
+      sum += part[0] + part[1];
     });
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -490,7 +497,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
   // ---- few candidates ----
   const uint32_t most = min(SM_WANT_MOST, nc * SM_THREADS * 3 / 2);   // of the threads' maxima
   uint32_t way = WAY_WIDE;
-  if ((by_k || by_p || by_min) && top < INFINITY) {
+  if ((by_k || by_p || by_min) && top < INFINITY && !known_wide) {
     const uint32_t want = by_k && top_k <= most ? top_k : min(SM_WANT, most);
     const bool all_of_k = by_k && top_k <= most;   // the candidates hold the first top_k
     const float per_bin = (float)SM_COARSE / span;
@@ -595,7 +602,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
     }
     sync();
     way = s.way;
-    if (way == WAY_DONE || (way == WAY_MASS && !a.later)) {
+    if (way == WAY_DONE || (WIDE && way == WAY_MASS)) {
       if (way == WAY_MASS) {   // the border lies within what 32 bits may be off
         uint64_t sum = 0;
         for (uint32_t i = warp * 32; i < n; i += SM_THREADS) {
@@ -658,11 +665,12 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
           at += w2[j];
         }
       }
-      return true;
+      return WAY_DONE;
     }
   }
-  if (a.later) return false;
-
+  if constexpr (!WIDE) {
+    return way;
+  } else {
   // ---- wide rows ----
   bits_for((float)a.vocab);
   const uint32_t rounds = (n + SM_THREADS - 1) / SM_THREADS;
@@ -851,7 +859,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
       sync();
       const float sum_f = rough_total(), unit = 2147483648.f / sum_f;
       if (th.ties == 0u) bits_for(sum_f);
-      each_block([&](uint32_t, const uint4& v) {
+      each_block([&](const uint4& v) {
 #pragma unroll
         for (uint32_t k = 0; k < E; ++k) {
           const float y = Logits<T>::at(v, k);
@@ -859,32 +867,41 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
         }
       });
       sync();
-      constexpr uint32_t EACH = SM_BINS / SM_THREADS;
-      uint64_t mine[EACH], sum = 0;
+      if (rank == 0) {   // the first CTA's alone: a bin of each of the others is a load from its shared memory
+        constexpr uint32_t EACH = SM_BINS / SM_THREADS;
+        static_assert(EACH == 4, "four bins a thread");
+        uint64_t mine[EACH] = {0, 0, 0, 0};
+        for (uint32_t q = 0; q < nc; ++q) {
+          uint4 v;
+          const uint32_t at = step_smem(&s.count[tid * EACH]);
+          asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                       : "r"(nc > 1 ? cluster_at(at, q) : at)
+                       : "memory");
+          mine[0] += v.x; mine[1] += v.y; mine[2] += v.z; mine[3] += v.w;
+        }
+        const uint64_t sum = mine[0] + mine[1] + mine[2] + mine[3];
+        const uint64_t inc = warp_incl_scan(sum);
+        if (lane == 31) s.scan[warp] = inc;
+        __syncthreads();
+        uint64_t before = inc - sum, all = 0;
+        for (uint32_t q = 0; q < SM_WARPS; ++q) {
+          if (q < warp) before += s.scan[q];
+          all += s.scan[q];
+        }
+        const float ties_f = (float)(tie * th.ties) / (float)(1ull << bits) * unit;
+        const uint64_t want = max((uint64_t)1, (uint64_t)(((float)all + ties_f) * top_p));
 #pragma unroll
-      for (uint32_t j = 0; j < EACH; ++j) {
-        mine[j] = 0;
-        for (uint32_t q = 0; q < nc; ++q)
-          mine[j] += nc > 1 ? cluster_read(&s.count[tid * EACH + j], q) : s.count[tid * EACH + j];
-        sum += mine[j];
-      }
-      const uint64_t inc = warp_incl_scan(sum);
-      if (lane == 31) s.scan[warp] = inc;
-      __syncthreads();
-      uint64_t before = inc - sum, all = 0;
-      for (uint32_t q = 0; q < SM_WARPS; ++q) {
-        if (q < warp) before += s.scan[q];
-        all += s.scan[q];
-      }
-      const float ties_f = (float)(tie * th.ties) / (float)(1ull << bits) * unit;
-      const uint64_t want = max((uint64_t)1, (uint64_t)(((float)all + ties_f) * top_p));
-#pragma unroll
-      for (uint32_t j = 0; j < EACH; ++j) {
-        if (before < want && before + mine[j] >= want) s.found = tid * EACH + j;
-        before += mine[j];
+        for (uint32_t j = 0; j < EACH; ++j) {
+          if (before < want && before + mine[j] >= want) s.found = tid * EACH + j;
+          before += mine[j];
+        }
+        __syncthreads();
+        if (tid < nc && nc > 1) cluster_write(&s.cut, tid, s.found);
+        if (nc == 1 && tid == 0) s.cut = s.found;
       }
       sync();
-      border = s.found;
+      border = s.cut;
     }
     // exactly: all of it, what lies above the bin, and the bin's tokens
     const Sums t = sums(std::true_type(), [&](float y, uint32_t index, bool in) {
@@ -946,7 +963,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
   // The warp whose run has it shares the run with the CTA's other warps.
   const bool has = goal >= at && goal < at + mine;
   if (has && lane == 0) s.run = {i0, i1, at, ties_before};
-  if (!__syncthreads_or(has)) return true;
+  if (!__syncthreads_or(has)) return WAY_DONE;
   const uint32_t r1 = s.run.last, part = (r1 - s.run.first + SM_WARPS - 1) / SM_WARPS;
   const uint32_t j0 = min(r1, s.run.first + warp * part), j1 = min(r1, j0 + part);
   // a lane's weights of its block, those on the threshold aside, which `on` counts
@@ -984,7 +1001,7 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
   ties_before = s.run.ties + __reduce_add_sync(0xffffffffu, lane < warp ? s.warp_ties[lane] : 0u);
   // (`at` counts what lies above the threshold; ties are added as they come)
   at += tie * (min(ties, ties_before) - min(ties, s.run.ties));
-  if (goal < at || goal >= at + m + tie * (min(ties, ties_before + all_on) - min(ties, ties_before))) return true;
+  if (goal < at || goal >= at + m + tie * (min(ties, ties_before + all_on) - min(ties, ties_before))) return WAY_DONE;
   for (uint32_t i = j0; i < j1; i += 32) {
     step(i, y, w, &on);
     const uint32_t on_inc = warp_incl_scan(on);
@@ -1012,26 +1029,41 @@ __device__ __forceinline__ bool sample_row(const SampleArgs& a, SampleShared& s,
     at += all;
     ties_before += __shfl_sync(0xffffffffu, on_inc, 31);
   }
-  return true;
+  return WAY_DONE;
+}
 }
 
+// A row a cluster (or a CTA), whatever its settings.
 template <typename T>
-__global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(SM_THREADS) sample_kernel(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ SampleShared s;
   wait_predecessor();
-  const uint32_t nc = a.cluster;
-  if (!a.queued) {         // a row a cluster
-    const uint32_t row = blockIdx.x / nc;
-    const bool done = sample_row<T>(a, s, (uint4*)smem_raw, row);
-    if (!done && threadIdx.x == 0 && blockIdx.x % nc == 0) a.queue[atomicAdd(a.counter, 1u)] = row;
-    if (nc > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
-    return;
-  }
-  // the rows that were left, in turn
-  const uint32_t rows = *(volatile uint32_t*)a.counter;
+  sample_row<T, true>(a, s, (uint4*)smem_raw, blockIdx.x / a.cluster, false);
+  if (a.cluster > 1) cluster_sync();   // no CTA leaves while another reads its shared memory
+}
+// The same for those of many rows that few candidates decide; the others are queued.
+template <typename T>
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_many_kernel(const __grid_constant__ SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  __shared__ SampleShared s;
+  wait_predecessor();
+  const uint32_t row = blockIdx.x / a.cluster;
+  const uint32_t way = sample_row<T, false>(a, s, (uint4*)smem_raw, row, false);
+  if (way != WAY_DONE && threadIdx.x == 0 && blockIdx.x % a.cluster == 0)
+    a.queue[atomicAdd(a.counter, 1u)] = row | (way == WAY_WIDE ? QUEUE_WIDE : 0u);
+  if (a.cluster > 1) cluster_sync();
+}
+// The queued rows, in turn.
+template <typename T>
+__global__ void __launch_bounds__(SM_THREADS) sample_queue_kernel(const __grid_constant__ SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  __shared__ SampleShared s;
+  wait_predecessor();
+  const uint32_t nc = a.cluster, rows = *(volatile uint32_t*)a.counter;
   for (uint32_t i = blockIdx.x / nc; i < rows; i += gridDim.x / nc) {
-    sample_row<T>(a, s, (uint4*)smem_raw, a.queue[i]);
+    const uint32_t row = a.queue[i];
+    sample_row<T, true>(a, s, (uint4*)smem_raw, row & ~QUEUE_WIDE, (row & QUEUE_WIDE) != 0u);
     if (nc > 1)
       cluster_sync();
     else
@@ -1048,36 +1080,38 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_kernel(const __grid_cons
 template <typename T>
 static uint32_t sample_blocks(uint32_t vocab) { return vocab / Logits<T>::E + 2; }
 
-// CTAs of a row: as many as two an SM leave room for, of at least two blocks a
-// thread.  Of a wide row where it is on its own: as many as there can be.
-static uint32_t row_ctas(uint32_t blocks, uint64_t rows, int sms) {
+// CTAs of a row: as many as `places` leave room for, of at least two blocks a thread.
+static uint32_t row_ctas(uint32_t blocks, uint64_t rows, uint64_t places) {
   uint32_t nc = 1;
-  while (nc < SM_MAX_CLUSTER && rows * nc * 2 <= (uint64_t)sms * 2 && blocks / (nc * 2) >= 2 * SM_THREADS) nc *= 2;
+  while (nc < SM_MAX_CLUSTER && rows * nc * 2 <= places && blocks / (nc * 2) >= 2 * SM_THREADS) nc *= 2;
   return nc;
 }
 static uint32_t blocks_of(uint32_t vocab, int dtype) {
   return dtype == RO_F32 ? sample_blocks<float>(vocab) : sample_blocks<__half>(vocab);
 }
 bool sample_queues(uint32_t vocab, int dtype, uint64_t rows, int sms) {
+  // Few rows: each a cluster, which does whatever the row's settings ask for, a
+  // CTA an SM.  More: candidates by as many CTAs as fit twice an SM, and the
+  // wide rows after them by clusters as large as for a single row.
   const uint32_t blocks = blocks_of(vocab, dtype);
   return row_ctas(blocks, rows, sms) * 2 < row_ctas(blocks, 1, sms);
 }
 template <typename T>
 static void launch(const LaunchCfg& L, SampleArgs a, int dtype, int sms) {
   const uint32_t blocks = blocks_of(a.vocab, dtype);
-  auto go = [&](uint32_t nc, uint32_t clusters) {
+  auto go = [&](void (*kernel)(SampleArgs), uint32_t nc, uint32_t clusters) {
     a.cluster = nc;
     a.blocks = (uint32_t)ceil_div(blocks, nc);
     a.staged = (uint64_t)a.blocks * 16 <= SM_SLICE;
-    launch_k(L, K_SAMPLE, sample_kernel<T>, clusters * nc, SM_THREADS, a.staged ? (size_t)a.blocks * 16 : 0, a, dim3(nc));
+    launch_k(L, K_SAMPLE, kernel, clusters * nc, SM_THREADS, a.staged ? (size_t)a.blocks * 16 : 0, a, dim3(nc));
   };
-  a.later = a.queue != nullptr;
-  go(row_ctas(blocks, a.rows, sms), a.rows);
-  if (!a.later) return;
-  a.later = 0;
-  a.queued = 1;
+  if (!a.queue) {
+    go(sample_kernel<T>, row_ctas(blocks, a.rows, sms), a.rows);
+    return;
+  }
   const uint32_t wide = row_ctas(blocks, 1, sms);
-  go(wide, std::min<uint32_t>(a.rows, (uint32_t)sms * 2 / wide));
+  go(sample_many_kernel<T>, row_ctas(blocks, a.rows, 2ull * sms), a.rows);
+  go(sample_queue_kernel<T>, wide, std::min<uint32_t>(a.rows, (uint32_t)sms / wide));
 }
 void launch_sample(const LaunchCfg& L, const SampleArgs& a, int dtype, int sms) {
   dtype == RO_F32   ? launch<float>(L, a, dtype, sms)
@@ -1087,7 +1121,10 @@ void launch_sample(const LaunchCfg& L, const SampleArgs& a, int dtype, int sms) 
 
 template <typename T>
 static cudaError_t allow() {
-  return cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SM_SLICE);
+  for (auto kernel : {sample_kernel<T>, sample_many_kernel<T>, sample_queue_kernel<T>})
+    if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SM_SLICE); e != cudaSuccess)
+      return e;
+  return cudaSuccess;
 }
 cudaError_t prepare_sample_kernels() {
   for (cudaError_t e : {allow<float>(), allow<__half>(), allow<__nv_bfloat16>()})

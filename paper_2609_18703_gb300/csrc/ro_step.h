@@ -256,9 +256,7 @@ struct SampleArgs {
   uint32_t* kept;            // optional
   uint32_t cluster, blocks;  // CTAs of a row, 16-byte blocks of a slice
   uint32_t staged;           // slices are held in shared memory
-  uint32_t later;            // wide rows are queued
-  uint32_t queued;           // the queue's rows are taken
-  uint32_t* queue;           // [rows]
+  uint32_t* queue;           // [rows], where wide ones are queued
   uint32_t* counter;         // of the queue, and a ticket: zero between calls
   uint32_t* err;
 };
