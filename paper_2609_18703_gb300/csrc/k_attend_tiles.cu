@@ -80,19 +80,22 @@ constexpr uint32_t AT_ITEMS = 2;
 // which runs dry could do.
 constexpr uint32_t AT_AHEAD = 8;
 
-// Scores in log2 of a row's products, in pairs: under a cap, and falling with the
-// distance from slot `pos` (columns from t0 on; `both`: slots behind pos count too).
+// Scores in log2 of N of a row's products, in pairs: under a cap, and falling with
+// the distance: `ahead` slots from the first column to the row's; `both`: columns
+// behind it count too.  voter: the row's products may be believed (others may hold
+// anything, and would decide which form the whole warp takes).
 template <int N>
 __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float ahead, bool both,
-                                            uint32_t (&x)[N]) {
+                                            bool voter, uint32_t (&x)[N]) {
+  const uint64_t to_y = pair(scale_log2, scale_log2);
   if (b.cap_log2 != 0.f) {
     float mx[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < N; i += 2)
       mx[(i / 2) & 3] = fmaxf(fmaxf(mx[(i / 2) & 3], fabsf(__uint_as_float(x[i]))), fabsf(__uint_as_float(x[i + 1])));
-    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * fabsf(b.to_z);
-    const uint64_t to_z = pair(b.to_z, b.to_z), to_y = pair(scale_log2, scale_log2);
-    auto near = [&](auto terms, auto term) {   // x in log2 times tanh(z) / z
+    const float top = voter ? fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * fabsf(b.to_z) : 0.f;
+    const uint64_t to_z = pair(b.to_z, b.to_z);
+    auto near = [&](auto terms, auto term) {   // the scaled product times tanh(z) / z
       constexpr int TERMS = decltype(terms)::value;
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
@@ -105,15 +108,15 @@ __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2,
         x[i + 1] = (uint32_t)(y >> 32);
       }
     };
-    if (!__any_sync(0xffffffffu, top > 0.5f))
+    if (!__any_sync(0xffffffffu, top > 0.5f)) {
       near(std::integral_constant<int, TANH_SHORT_TERMS>(), [](int k) { return tanh_short_term(k); });
-    else if (!__any_sync(0xffffffffu, top > 1.f))
+    } else if (!__any_sync(0xffffffffu, top > 1.f)) {
       near(std::integral_constant<int, TANH_TERMS>(), [](int k) { return tanh_term(k); });
-    else
+    } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])));
+    }
   } else {
-    const uint64_t to_y = pair(scale_log2, scale_log2);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
       const uint64_t y = mul_pair(pair_bits(x[i], x[i + 1]), to_y);
@@ -488,120 +491,76 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     const bool held = B && std::is_same_v<T, __nv_bfloat16> && a.b.cap_log2 != 0.f && a.b.cap_log2 <= 80.f && !a.b.slope;
     __syncwarp();
     if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
+    const bool turned = B && (a.b.cap_log2 != 0.f || a.b.slope);
     float m = held ? 0.f : -INFINITY, l = 0.f;
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
-      uint32_t x[AT_KEYS];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
-      tc_wait_ld(x);
       bool all = t < sinks_all || (t >= all_from && t < all_to);
+      const SlotTile st = slots.at(c0 + t);
+      // biased: slots from the tile's first to the row's, the columns it sees
+      float ahead = 0.f;
+      int c_lo = 0, c_hi = 0, a_lo = 0, a_hi = 0;
+      bool zero = !all && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS);
       if constexpr (B) {
-        const SlotTile st = slots.at(c0 + t);
         all = !st.sink && st.t0 >= all_lo && st.t0 + AT_KEYS <= all_hi;
-        const float ahead = (float)(pos - (int64_t)st.t0);
-        bias_scores(a.b, scale, slope, ahead, a.b.until != nullptr, x);
-        if (!all) {
-          const int t0 = (int)st.t0, lo = (int)st.lo - t0, hi = (int)st.hi - t0;
-          const int c_lo = max((int)see.c0 - t0, lo), c_hi = min((int)see.c1 - t0, hi);
-          const int a_lo = max((int)see.a0 - t0, lo), a_hi = min((int)see.a1 - t0, hi);
-#pragma unroll
-          for (int k = 0; k < AT_KEYS / 32; ++k) {
-            const uint32_t in = bits_between(c_lo - 32 * k, c_hi - 32 * k) | bits_between(a_lo - 32 * k, a_hi - 32 * k);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(in >> i & 1u)) x[32 * k + i] = 0xff800000u;
-          }
-          // Values no row sees must not reach the product (see below).
-          if (w == 0 && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS || holes)) {
-            bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
-            const uint32_t j = st.t0 + row;
-            if (j < st.lo || j >= st.hi || !somebody_sees(q, a.r, a.b, holes, s_end, i0, i1, j)) {
-#pragma unroll
-              for (uint32_t i = 0; i < S::BLOCKS; ++i)
-#pragma unroll
-                for (uint32_t z = 0; z < 8; ++z)
-                  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
-                                                                            i * S::BLOCK_BYTES + row * 128 + z * 16),
-                               "r"(0u)
-                               : "memory");
-            }
-            fence_async_smem();
-          }
-        }
-      } else if (!all) {
-        const SlotTile st = slots.at(c0 + t);
-        // columns [b, e) count; of those the ones below `sinks` or from the window's first on
-        const int64_t t0 = st.t0;
-        const int e = (int)max((int64_t)0, min((int64_t)st.hi, pos + 1) - t0), b = (int)(st.lo - st.t0);
-        int s_end = AT_KEYS, w_from = 0;
-        if (a.r.window != 0u && !st.sink) {
-          s_end = (int)max((int64_t)0, min((int64_t)AT_KEYS, (int64_t)a.r.sinks - t0));
-          w_from = (int)max((int64_t)0, min((int64_t)AT_KEYS, pos - (int64_t)a.r.window + 1 - t0));
-        }
-#pragma unroll
-        for (int i = 0; i < AT_KEYS; ++i) {
-          const bool in = i >= b && i < e && (i < s_end || i >= w_from);
-          if (!in) x[i] = 0xff800000u;
-        }
-        // Values no row sees must not reach the product: zero them where the
-        // tile is not whole (the products of both row tiles come after this).
-        if (w == 0 && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS)) {
-          bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
-          const uint32_t j = st.t0 + row;
-          if (j < st.lo || j >= st.hi) {
-#pragma unroll
-            for (uint32_t i = 0; i < S::BLOCKS; ++i)
-#pragma unroll
-              for (uint32_t z = 0; z < 8; ++z)
-                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
-                                                                          i * S::BLOCK_BYTES + row * 128 + z * 16),
-                             "r"(0u)
-                             : "memory");
-          }
-          fence_async_smem();
-        }
+        zero = !all && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS || holes);
+        ahead = (float)(pos - (int64_t)st.t0);
+        const int t0 = (int)st.t0, lo = (int)st.lo - t0, hi = (int)st.hi - t0;
+        c_lo = max((int)see.c0 - t0, lo), c_hi = min((int)see.c1 - t0, hi);
+        a_lo = max((int)see.a0 - t0, lo), a_hi = min((int)see.a1 - t0, hi);
       }
-      if (!held) {
-        float mx[8];   // eight chains: one of 128 would cost its latency 128 times
+      // Values no row sees must not reach the product: zero them where the
+      // tile is not whole (the products of both row tiles come after this).
+      if (w == 0 && zero) {
+        bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
+        const uint32_t j = st.t0 + row;
+        bool unseen = j < st.lo || j >= st.hi;
+        if constexpr (B) unseen = unseen || !somebody_sees(q, a.r, a.b, holes, s_end, i0, i1, j);
+        if (unseen) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+          for (uint32_t i = 0; i < S::BLOCKS; ++i)
 #pragma unroll
-        for (int i = 16; i < AT_KEYS; i += 2)
-          mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
-        const float mn = fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
-                                        fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * (B ? 1.f : scale));
-        if (__any_sync(0xffffffffu, voter && mn > m + AT_SLACK<T>)) {
-          // The maximum moves for the whole warp: rescale what was summed so far.
-          // (Rows that are no token's have no say: theirs may hold whatever an
-          // earlier kernel left, and would decide how the others are rounded.)
-          const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
-          m = mn;
-          l *= f;
-          if (t > 0) {
-            uint32_t o[16];
+            for (uint32_t z = 0; z < 8; ++z)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
+                                                                        i * S::BLOCK_BYTES + row * 128 + z * 16),
+                           "r"(0u)
+                           : "memory");
+        }
+        fence_async_smem();
+      }
+      // The columns of [32 k, 32 k + 32) that a biased row sees.
+      auto seen = [&](int k) {
+        return bits_between(c_lo - 32 * k, c_hi - 32 * k) | bits_between(a_lo - 32 * k, a_hi - 32 * k);
+      };
+      // The row's maximum so far is mn: where it grew much, or first came up, it
+      // moves for the whole warp, and what was summed so far is rescaled.
+      // (Rows that are no token's have no say: theirs may hold whatever an
+      // earlier kernel left, and would decide how the others are rounded.)
+      auto raise = [&](float mn) {
+        if (!__any_sync(0xffffffffu, voter && mn > m + AT_SLACK<T>)) return;
+        const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
+        m = mn;
+        l *= f;
+        if (t > 0) {
+          uint32_t o[16];
 #pragma unroll 1
-            for (int i = 0; i < DP / 16; ++i) {
-              tc_ld16(to + i * 16, o);
-              tc_wait_ld(o);
+          for (int i = 0; i < DP / 16; ++i) {
+            tc_ld16(to + i * 16, o);
+            tc_wait_ld(o);
 #pragma unroll
-              for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
-              tc_st16(to + i * 16, o);
-            }
+            for (int z = 0; z < 16; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
+            tc_st16(to + i * 16, o);
           }
         }
-      }
-      const float sub = (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>;   // -inf: a row that has seen nothing yet
-      const uint64_t scale2 = B ? pair(1.f, 1.f) : pair(scale, scale), sub2 = pair(-sub, -sub);
+      };
       uint64_t sum[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      // The weights of the i-th 32 columns, into TMEM.
+      auto weights = [&](int i, const uint32_t* y32, auto argument) {
         uint32_t p[16];
 #pragma unroll
         for (int z = 0; z < 16; ++z) {
-          const uint64_t s2 = pair_bits(x[i * 32 + 2 * z], x[i * 32 + 2 * z + 1]);
-          const uint64_t y = B ? add_pair(s2, sub2) : fma_pair(s2, scale2, sub2);
+          const uint64_t y = argument(pair_bits(y32[2 * z], y32[2 * z + 1]));
           const float e0 = ex2(pair_lo(y)), e1 = ex2(pair_hi(y));
           sum[z & 3] = add_pair(sum[z & 3], pair(e0, e1));
           p[z] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
@@ -613,6 +572,77 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           __syncwarp();
           if (lane == 0) bar_arrive(b_p + 16 * w + (i / 2) * 8);
         }
+      };
+      auto below = [&] { return (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>; };   // -inf: a row that has seen nothing yet
+      if (B && turned) {
+        uint32_t y[AT_KEYS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, y + i * 32);
+        tc_wait_ld(y);
+        bias_scores(a.b, scale, slope, ahead, a.b.until != nullptr, voter, y);
+        if (!all) {
+          uint32_t in[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) in[k] = seen(k);
+#pragma unroll
+          for (int i = 0; i < AT_KEYS; ++i)
+            if (!(in[i / 32] >> (i % 32) & 1u)) y[i] = 0xff800000u;
+        }
+        if (!held) {
+          float mx[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1]));
+#pragma unroll
+          for (int i = 16; i < AT_KEYS; i += 2)
+            mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(y[i])), __uint_as_float(y[i + 1]));
+          raise(fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
+                               fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])))));
+        }
+        const float sub = below();
+        const uint64_t sub2 = pair(-sub, -sub);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights(i, y + 32 * i, [&](uint64_t s2) { return add_pair(s2, sub2); });
+      } else {
+        uint32_t x[AT_KEYS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
+        tc_wait_ld(x);
+        if (!all) {
+          if constexpr (B) {
+            uint32_t in[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) in[k] = seen(k);
+#pragma unroll
+            for (int i = 0; i < AT_KEYS; ++i)
+              if (!(in[i / 32] >> (i % 32) & 1u)) x[i] = 0xff800000u;
+          } else {
+            // columns [b, e) count; of those the ones below `sinks` or from the window's first on
+            const int64_t t0 = st.t0;
+            const int e = (int)max((int64_t)0, min((int64_t)st.hi, pos + 1) - t0), b = (int)(st.lo - st.t0);
+            int s_end = AT_KEYS, w_from = 0;
+            if (a.r.window != 0u && !st.sink) {
+              s_end = (int)max((int64_t)0, min((int64_t)AT_KEYS, (int64_t)a.r.sinks - t0));
+              w_from = (int)max((int64_t)0, min((int64_t)AT_KEYS, pos - (int64_t)a.r.window + 1 - t0));
+            }
+#pragma unroll
+            for (int i = 0; i < AT_KEYS; ++i) {
+              const bool in = i >= b && i < e && (i < s_end || i >= w_from);
+              if (!in) x[i] = 0xff800000u;
+            }
+          }
+        }
+        float mx[8];   // eight chains: one of 128 would cost its latency 128 times
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+#pragma unroll
+        for (int i = 16; i < AT_KEYS; i += 2)
+          mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
+        raise(fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
+                             fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))) * scale));
+        const float sub = below();
+        const uint64_t scale2 = pair(scale, scale), sub2 = pair(-sub, -sub);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights(i, x + 32 * i, [&](uint64_t s2) { return fma_pair(s2, scale2, sub2); });
       }
       const uint64_t all4 = add_pair(add_pair(sum[0], sum[1]), add_pair(sum[2], sum[3]));
       l += pair_lo(all4) + pair_hi(all4);

@@ -318,8 +318,11 @@ __device__ __forceinline__ float tanh_far(float z) {
 }
 // A product q.k's score in log2 under a cap.
 __device__ __forceinline__ float capped(const BiasArgs& b, float dot) {
-  const float z = dot * b.to_z, w = z * z;
-  return b.cap_log2 * (w <= 1.f ? z * tanh_ratio(w) : tanh_far(z));
+  // (both forms and a choice: a branch a product costs three times as much)
+  const float z = dot * b.to_z, w = z * z, near = z * tanh_ratio(fminf(w, 1.f)), far = tanh_far(z);
+  float t;
+  asm("{\n .reg .pred p;\n setp.le.f32 p, %1, 0f3F800000;\n selp.f32 %0, %2, %3, p;\n}" : "=f"(t) : "f"(w), "f"(near), "f"(far));
+  return b.cap_log2 * t;
 }
 // Scores in log2 of a warp's products: where all lie within |z| <= 1, without the far form.
 template <int N>
