@@ -31,12 +31,19 @@
 
 namespace ro {
 
-constexpr int AT_THREADS = 384, AT_ROWS = 128, AT_KEYS = 128;
-constexpr int AT_SOFTMAX = 256;     // threads 0 .. 255: softmax; then a warp each of products, loads, work
-// Registers: 168 a thread at launch (3 warps in each quarter of the SM); the
-// last warpgroup gives up what the softmax threads need, 2 x 216 + 72 = 3 x 168.
-#define AT_REGS_SOFTMAX 216
-#define AT_REGS_OTHERS 72
+constexpr int AT_ROWS = 128, AT_KEYS = 128;
+// SPLIT threads a row: 256 SPLIT of softmax, then a warp each of products, loads, work.
+template <int SPLIT>
+constexpr int AT_SOFTMAX = 256 * SPLIT;
+template <int SPLIT>
+constexpr int AT_THREADS = AT_SOFTMAX<SPLIT> + 128;
+// Registers: 168 (96) a thread at launch (3 or 5 warps in each quarter of the SM);
+// the last warpgroup gives up what the softmax threads need, 2 x 216 + 72 = 3 x 168
+// (4 x 104 + 64 = 5 x 96).
+template <int SPLIT>
+constexpr int AT_REGS_SOFTMAX = SPLIT == 1 ? 216 : 104;
+template <int SPLIT>
+constexpr int AT_REGS_OTHERS = SPLIT == 1 ? 72 : 64;
 constexpr uint32_t AT_TMEM_COLS = 512;
 // log2 of what a row's maximum may grow before O is rescaled; f16 weights, at
 // most 2^15, have to hold it beside the bits they are held higher by
@@ -88,6 +95,15 @@ template <int N>
 __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float ahead, bool both,
                                             bool voter, uint32_t (&x)[N]) {
   const uint64_t to_y = pair(scale_log2, scale_log2);
+  // Where no column that counts lies behind the row's slot, slope |ahead - i| is
+  // slope ahead - slope i, and its first part enters with the last product.
+  const bool line = !both || !__any_sync(0xffffffffu, ahead < (float)(N - 1));
+  const float off = line ? -slope * ahead : 0.f;
+  const uint64_t off2 = pair(off, off);
+  auto set = [&](int i, uint64_t y) {
+    x[i] = (uint32_t)y;
+    x[i + 1] = (uint32_t)(y >> 32);
+  };
   if (b.cap_log2 != 0.f) {
     float mx[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -103,9 +119,7 @@ __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2,
         uint64_t p = pair(term(TERMS), term(TERMS));
 #pragma unroll
         for (int k = TERMS - 1; k >= 0; --k) p = fma_pair(p, w, pair(term(k), term(k)));
-        const uint64_t y = mul_pair(mul_pair(v, to_y), p);
-        x[i] = (uint32_t)y;
-        x[i + 1] = (uint32_t)(y >> 32);
+        set(i, fma_pair(mul_pair(v, to_y), p, off2));
       }
     };
     if (!__any_sync(0xffffffffu, top > 0.5f)) {
@@ -114,29 +128,19 @@ __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2,
       near(std::integral_constant<int, TANH_TERMS>(), [](int k) { return tanh_term(k); });
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])));
+      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])) + off);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      const uint64_t y = mul_pair(pair_bits(x[i], x[i + 1]), to_y);
-      x[i] = (uint32_t)y;
-      x[i + 1] = (uint32_t)(y >> 32);
-    }
+    for (int i = 0; i < N; i += 2) set(i, fma_pair(pair_bits(x[i], x[i + 1]), to_y, off2));
   }
   if (b.slope) {
-    const uint64_t fall = pair(-slope, -slope), step = pair(-8.f, -8.f);
-    uint64_t d[4];             // distances of four pairs of columns, a chain each (whole numbers: exact to 2^24)
+    if (line) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = pair(ahead - 2 * i, ahead - 2 * i - 1);
+      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(fmaf(slope, (float)i, __uint_as_float(x[i])));
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      uint64_t v = d[(i / 2) & 3];
-      d[(i / 2) & 3] = add_pair(v, step);
-      if (both) v &= 0x7FFFFFFF7FFFFFFFull;
-      const uint64_t y = fma_pair(fall, v, pair_bits(x[i], x[i + 1]));
-      x[i] = (uint32_t)y;
-      x[i + 1] = (uint32_t)(y >> 32);
+      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(fmaf(-slope, fabsf(ahead - (float)i), __uint_as_float(x[i])));
     }
   }
 }
@@ -146,14 +150,16 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
   return lo >= 32 ? 0u : lo <= 0 ? below : below & ~((1u << lo) - 1u);
 }
 
-// B: biased (ro_cache_attend_biased).
-template <typename T, int DP, bool B>
-__global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
+// B: biased (ro_cache_attend_biased).  SPLIT 2: two threads a row, 64 columns of
+// a tile each, and a maximum of 0 for all rows: scores under a cap.
+template <typename T, int DP, bool B, int SPLIT>
+__global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
   using S = TileShape<DP>;
   using Tiles = std::conditional_t<B, BiasTiles<AT_KEYS>, SlotTiles<AT_KEYS>>;
   const AttendArgs& a = g.a;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 10 + 2 * AT_ITEMS + 1];
+  __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 10 + 2 * AT_ITEMS + 1 + 2];
+  __shared__ float s_pair[SPLIT == 1 ? 1 : 2 * AT_ROWS];   // from one of a row's threads to the other
   __shared__ TileItem<B> s_item[AT_ITEMS];
   __shared__ uint32_t s_tmem, s_gave_up;
   wait_predecessor();
@@ -164,7 +170,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
   // full / empty: queries, the ring, S, P, O, items
   const uint32_t b_q = step_smem(s_bar), b_qe = b_q + 8, b_full = b_qe + 8, b_empty = b_full + 8 * S::SLOTS,
                  b_s = b_empty + 8 * S::SLOTS, b_p = b_s + 16, b_o = b_p + 32, b_oe = b_o + 16, b_item = b_oe + 16,
-                 b_item_free = b_item + 8 * AT_ITEMS, b_want = b_item_free + 8 * AT_ITEMS;
+                 b_item_free = b_item + 8 * AT_ITEMS, b_want = b_item_free + 8 * AT_ITEMS,
+                 b_pair = b_want + 8;
   if (tid == 0) {
     s_gave_up = 0;
     bar_init(b_q, 1);
@@ -179,24 +186,26 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       bar_init(b_p + 16 * i, 4);       // P in two halves of 64 slots
       bar_init(b_p + 16 * i + 8, 4);
       bar_init(b_o + 8 * i, 1);
-      bar_init(b_oe + 8 * i, 4);
+      bar_init(b_oe + 8 * i, 4 * SPLIT);
+      bar_init(b_pair + 8 * i, 4 * SPLIT);
     }
     for (uint32_t i = 0; i < AT_ITEMS; ++i) {
       bar_init(b_item + 8 * i, 1);
-      bar_init(b_item_free + 8 * i, 10);   // 8 warps of softmax, loads, products
+      bar_init(b_item_free + 8 * i, 8 * SPLIT + 2);   // the warps of softmax, loads, products
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  if (warp == 8) tmem_alloc(step_smem(&s_tmem), AT_TMEM_COLS);
+  constexpr uint32_t WARP0 = AT_SOFTMAX<SPLIT> / 32;   // of products; loads and work after it
+  if (warp == WARP0) tmem_alloc(step_smem(&s_tmem), AT_TMEM_COLS);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tm = __shfl_sync(0xffffffffu, s_tmem, 0);
   const uint32_t tm_s = tm, tm_o = tm + 256;   // 128 columns for each row tile
 
-  if (warp >= AT_SOFTMAX / 32) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AT_REGS_OTHERS));
+  if (warp >= WARP0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AT_REGS_OTHERS<SPLIT>));
     // the k-th item, to a whole warp; released once its reader is done with it
     auto item = [&](uint32_t k) -> const TileItem<B>& {
       bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
@@ -206,7 +215,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       __syncwarp();
       if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
     };
-    if (warp == 10) {
+    if (warp == WARP0 + 2) {
       // ---- work ----
       // The first item by the CTA's number, the others as they are asked for;
       // items are in falling order of work where that is known.
@@ -284,7 +293,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         a.counter[0] = 0u;
         a.counter[1] = 0u;
       }
-    } else if (warp == 9) {
+    } else if (warp == WARP0 + 1) {
       // ---- loads ----
       const uint32_t boxes = AT_KEYS / g.box;
       uint32_t slot = 0, parity = 1, uses = 0, qi = 0;   // parity of the ring's round before
@@ -351,7 +360,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
         release(k);
       }
-    } else if (warp == 8) {
+    } else if (warp == WARP0) {
       // ---- products ----
       const uint32_t shape_s = mma_shape<T>(AT_KEYS, false), shape_o = mma_shape<T>(DP, true);
       const uint32_t one = elect_lane();
@@ -369,7 +378,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         const uint32_t va = v_lo + slot * (S::TILE_BYTES / 16);
 #pragma unroll
         for (uint32_t k = half * (AT_KEYS / 32); k < (half + 1) * (AT_KEYS / 32); ++k)
-          mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8, va + k * (2048 / 16), shape_o, add || k > 0);
+          // (P's halves lie where their own columns of S did: side by side, or 64 apart)
+          mma_ts(one, tm_o + w * 128, tm_s + w * 128 + k * 8 + (SPLIT == 2 ? half * 32 : 0), va + k * (2048 / 16), shape_o,
+                 add || k > 0);
       };
       uint32_t slot = 0, parity = 0, tiles = 0, qi = 0;   // place in the ring of the next tile used, its round's parity
       auto advance = [&] {
@@ -424,18 +435,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     __syncwarp();
     asm volatile("bar.sync 0;" ::: "memory");   // every product is read
     if (*(volatile uint32_t*)&s_gave_up) __nanosleep(1000000);   // copies and products in flight end by themselves
-    if (warp == 8) {
+    if (warp == WARP0) {
       tc_fence_after();
       tmem_free(tm, AT_TMEM_COLS);
     }
     return;
   }
   // ---- softmax: a thread a row ----
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AT_REGS_SOFTMAX));
-  const uint32_t w = warp >> 2, row = tid & 127;
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AT_REGS_SOFTMAX<SPLIT>));
+  const uint32_t w = (warp >> 2) & 1, row = tid & 127, h = SPLIT == 2 ? warp >> 3 : 0;   // row tile, row, half of the columns
   const uint32_t lanes = (warp & 3) << 21;                 // this warp's TMEM lanes
   const uint32_t ts = tm_s + w * 128 + lanes, to = tm_o + w * 128 + lanes;
   const float scale = a.r.scale_log2;
+  // the threads of row tile w meet (what one wrote to shared memory is seen by the others)
+  uint32_t meets = 0;
+  auto meet = [&] {
+    __syncwarp();
+    if (lane == 0) bar_arrive(b_pair + 8 * w);
+    bar_wait(b_pair + 8 * w, meets++ & 1, &s_gave_up, a.err);
+  };
   uint32_t tiles = 0, vslot = 1, vpar = 0, done = 0;       // tiles so far; the ring's place of V; items with slots so far
   for (uint32_t k = 0;; ++k) {
     bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
@@ -486,25 +504,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
     const bool sees_some = B ? see.some() : mine;
     // (rows that see nothing have no say in the others' maximum, and are set to nothing at the end)
     const bool voter = mine && sees_some;
-    // Scores under a cap of at most 2^80 need no running maximum where the weights
-    // have the exponents of 32 bits: no weight, sum or product leaves their range.
-    const bool held = B && std::is_same_v<T, __nv_bfloat16> && a.b.cap_log2 != 0.f && a.b.cap_log2 <= 80.f && !a.b.slope;
+    constexpr bool held = SPLIT == 2;
     __syncwarp();
     if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
-    const bool turned = B && (a.b.cap_log2 != 0.f || a.b.slope);
+    const bool turned = B && (SPLIT == 2 || a.b.cap_log2 != 0.f || a.b.slope);   // more than scaled
     float m = held ? 0.f : -INFINITY, l = 0.f;
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
       bool all = t < sinks_all || (t >= all_from && t < all_to);
-      const SlotTile st = slots.at(c0 + t);
       // biased: slots from the tile's first to the row's, the columns it sees
       float ahead = 0.f;
       int c_lo = 0, c_hi = 0, a_lo = 0, a_hi = 0;
-      bool zero = !all && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS);
       if constexpr (B) {
+        const SlotTile st = slots.at(c0 + t);
         all = !st.sink && st.t0 >= all_lo && st.t0 + AT_KEYS <= all_hi;
-        zero = !all && (st.lo != st.t0 || st.hi != st.t0 + AT_KEYS || holes);
         ahead = (float)(pos - (int64_t)st.t0);
         const int t0 = (int)st.t0, lo = (int)st.lo - t0, hi = (int)st.hi - t0;
         c_lo = max((int)see.c0 - t0, lo), c_hi = min((int)see.c1 - t0, hi);
@@ -512,23 +526,27 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       }
       // Values no row sees must not reach the product: zero them where the
       // tile is not whole (the products of both row tiles come after this).
-      if (w == 0 && zero) {
+      auto zero_values = [&](const SlotTile& st) {
+        if (w != 0 || (st.lo == st.t0 && st.hi == st.t0 + AT_KEYS && !holes)) return;
         bar_wait(b_full + 8 * vslot, vpar, &s_gave_up, a.err);
-        const uint32_t j = st.t0 + row;
+        // a thread a slot; two where there are two a row, each for the slots of its
+        // own columns (the products of the other half do not wait for it)
+        const uint32_t r = SPLIT == 2 ? 64 * h + (row & 63) : row, j = st.t0 + r;
+        constexpr uint32_t PIECES = S::BLOCKS * 8 / SPLIT;
+        const uint32_t first = SPLIT == 2 ? (row >> 6) * PIECES : 0;
         bool unseen = j < st.lo || j >= st.hi;
         if constexpr (B) unseen = unseen || !somebody_sees(q, a.r, a.b, holes, s_end, i0, i1, j);
         if (unseen) {
 #pragma unroll
-          for (uint32_t i = 0; i < S::BLOCKS; ++i)
-#pragma unroll
-            for (uint32_t z = 0; z < 8; ++z)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
-                                                                        i * S::BLOCK_BYTES + row * 128 + z * 16),
-                           "r"(0u)
-                           : "memory");
+          for (uint32_t i = 0; i < PIECES; ++i)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sm_ring + vslot * S::TILE_BYTES +
+                                                                      (first + i) / 8 * S::BLOCK_BYTES + r * 128 +
+                                                                      (first + i) % 8 * 16),
+                         "r"(0u)
+                         : "memory");
         }
         fence_async_smem();
-      }
+      };
       // The columns of [32 k, 32 k + 32) that a biased row sees.
       auto seen = [&](int k) {
         return bits_between(c_lo - 32 * k, c_hi - 32 * k) | bits_between(a_lo - 32 * k, a_hi - 32 * k);
@@ -555,7 +573,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
       };
       uint64_t sum[4] = {0, 0, 0, 0};   // pairs of 32-bit sums
-      // The weights of the i-th 32 columns, into TMEM.
+      // The weights of the i-th 32 columns, into TMEM (over the thread's own part of S).
       auto weights = [&](int i, const uint32_t* y32, auto argument) {
         uint32_t p[16];
 #pragma unroll
@@ -565,7 +583,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
           sum[z & 3] = add_pair(sum[z & 3], pair(e0, e1));
           p[z] = pack2<T>(e0, e1);   // rounded to the cache's type for the product; l sums what is not
         }
-        tc_st16(ts + i * 16, p);
+        tc_st16(ts + i * 16 + (SPLIT == 2 ? h * 32 : 0), p);
         if (i & 1) {   // the product of a half starts while the other's exponentials run
           tc_wait_st();
           tc_fence_before();
@@ -574,18 +592,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
         }
       };
       auto below = [&] { return (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>; };   // -inf: a row that has seen nothing yet
-      if (B && turned) {
-        uint32_t y[AT_KEYS];
+      if (turned) {
+        if (!all) zero_values(slots.at(c0 + t));
+        constexpr int COLS = AT_KEYS / SPLIT, PARTS = COLS / 32;
+        const int k0 = SPLIT == 2 ? 2 * (int)h : 0;   // this thread's columns, of 32
+        uint32_t y[COLS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, y + i * 32);
+        for (int i = 0; i < PARTS; ++i) tc_ld32(ts + (k0 + i) * 32, y + i * 32);
         tc_wait_ld(y);
-        bias_scores(a.b, scale, slope, ahead, a.b.until != nullptr, voter, y);
+        bias_scores(a.b, scale, slope, ahead - 32.f * k0, a.b.until != nullptr, voter, y);
         if (!all) {
-          uint32_t in[4];
+          uint32_t in[PARTS];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) in[k] = seen(k);
+          for (int k = 0; k < PARTS; ++k) in[k] = seen(k0 + k);
 #pragma unroll
-          for (int i = 0; i < AT_KEYS; ++i)
+          for (int i = 0; i < COLS; ++i)
             if (!(in[i / 32] >> (i % 32) & 1u)) y[i] = 0xff800000u;
         }
         if (!held) {
@@ -593,21 +614,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
 #pragma unroll
           for (int i = 0; i < 8; ++i) mx[i] = fmaxf(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1]));
 #pragma unroll
-          for (int i = 16; i < AT_KEYS; i += 2)
+          for (int i = 16; i < COLS; i += 2)
             mx[(i / 2) & 7] = fmaxf(fmaxf(mx[(i / 2) & 7], __uint_as_float(y[i])), __uint_as_float(y[i + 1]));
-          raise(fmaxf(m, fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
-                               fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])))));
+          const float top = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
+          raise(fmaxf(m, top));
         }
         const float sub = below();
         const uint64_t sub2 = pair(-sub, -sub);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) weights(i, y + 32 * i, [&](uint64_t s2) { return add_pair(s2, sub2); });
-      } else {
+        for (int i = 0; i < PARTS; ++i) weights(k0 + i, y + 32 * i, [&](uint64_t s2) { return held ? s2 : add_pair(s2, sub2); });
+      } else if constexpr (SPLIT == 1) {
         uint32_t x[AT_KEYS];
 #pragma unroll
         for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, x + i * 32);
         tc_wait_ld(x);
         if (!all) {
+          const SlotTile st = slots.at(c0 + t);
           if constexpr (B) {
             uint32_t in[4];
 #pragma unroll
@@ -630,6 +652,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
               if (!in) x[i] = 0xff800000u;
             }
           }
+          zero_values(st);
         }
         float mx[8];   // eight chains: one of 128 would cost its latency 128 times
 #pragma unroll
@@ -650,12 +673,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       if (vslot >= S::SLOTS) vslot -= S::SLOTS, vpar ^= 1;
     }   // (a wait that gave up ends the others at once)
     // ---- to the output, or to this run's partial result ----
-    uint32_t o[DP];
+    constexpr int OUT = DP / SPLIT;                        // this thread's columns of O
+    const uint32_t d0 = h * OUT;
+    if constexpr (SPLIT == 2) {                            // both halves' sums
+      float* const other = s_pair + w * AT_ROWS + row;
+      if (h == 1) *other = l;
+      meet();
+      if (h == 0) {
+        l += *other;
+        *other = l;
+      }
+      meet();
+      if (h == 1) l = *other;
+    }
+    uint32_t o[OUT];
     if (n > 0) {
       bar_wait(b_o + 8 * w, done & 1, &s_gave_up, a.err);
       tc_fence_after();
 #pragma unroll
-      for (int i = 0; i < DP / 32; ++i) tc_ld32(to + i * 32, o + i * 32);
+      for (int i = 0; i < OUT / 32; ++i) tc_ld32(to + d0 + i * 32, o + i * 32);
       tc_wait_ld(o);
       tc_fence_before();
       __syncwarp();
@@ -663,54 +699,55 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_tiles_kernel(const __gri
       ++done;
     } else {
 #pragma unroll
-      for (int i = 0; i < DP; ++i) o[i] = 0u;
+      for (int i = 0; i < OUT; ++i) o[i] = 0u;
     }
     if constexpr (B)
       if (!sees_some) {
         m = -INFINITY;
         l = 0.f;
 #pragma unroll
-        for (int i = 0; i < DP; ++i) o[i] = 0u;
+        for (int i = 0; i < OUT; ++i) o[i] = 0u;
       }
     const uint32_t prow = w * AT_ROWS + row;               // the row among the pair's 256
     constexpr uint32_t STEP = 2 * AT_ROWS;                 // rows of a run
     // four columns of a row together, rows next to one another: a warp's
     // accesses are whole lines
-    float4* part = (float4*)a.partial + (uint64_t)unit * a.max_chunks * (DP / 4) * STEP + prow;
+    float4* part = (float4*)a.partial + ((uint64_t)unit * a.max_chunks * (DP / 4) + d0 / 4) * STEP + prow;
     float2* ml = (float2*)(a.partial + (uint64_t)a.pairs * a.max_chunks * STEP * DP) +
                  (uint64_t)unit * a.max_chunks * STEP + prow;
     if (n_runs > 1) {   // joined by attend_join_kernel
       if (mine) {
 #pragma unroll
-        for (int i = 0; i < DP / 4; ++i)
+        for (int i = 0; i < OUT / 4; ++i)
           __stcg(part + ((uint64_t)run * (DP / 4) + i) * STEP,
                  make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
                              __uint_as_float(o[4 * i + 3])));
-        __stcg(ml + run * STEP, make_float2(m, l));
+        if (h == 0) __stcg(ml + run * STEP, make_float2(m, l));
       }
       continue;
     }
     if (!mine) continue;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    T* out = (T*)a.out + out_at;
-    uint32_t y[DP / 2];
+    T* out = (T*)a.out + out_at + d0;
+    const uint32_t left = a.c.head_dim > d0 ? a.c.head_dim - d0 : 0u;   // columns there are
+    uint32_t y[OUT / 2];
 #pragma unroll
-    for (int i = 0; i < DP / 2; ++i) y[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+    for (int i = 0; i < OUT / 2; ++i) y[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
     // Each row is its thread's: 32 bytes a store where rows are aligned to
     // them, half as many stores to as many lines.
     if (g.wide) {
 #pragma unroll
-      for (int i = 0; i < DP / 2; i += 8)
-        if ((uint32_t)i * 2 < a.c.head_dim)
+      for (int i = 0; i < OUT / 2; i += 8)
+        if ((uint32_t)i * 2 < left)
           asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 2 * i), "r"(y[i]), "r"(y[i + 1]),
                        "r"(y[i + 2]), "r"(y[i + 3]), "r"(y[i + 4]), "r"(y[i + 5]), "r"(y[i + 6]), "r"(y[i + 7])
                        : "memory");
     } else {
 #pragma unroll
-      for (int i = 0; i < DP / 2; i += 4)
-        if ((uint32_t)i * 2 < a.c.head_dim) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+      for (int i = 0; i < OUT / 2; i += 4)
+        if ((uint32_t)i * 2 < left) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
     }
-    if (a.lse) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
+    if (a.lse && h == 0) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
   }
   __syncwarp();
   tc_fence_before();
@@ -770,8 +807,19 @@ size_t attend_tiles_partial(const AttendArgs& a) {
 template <typename T, int DP>
 static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
-  launch_k(L, K_ATTEND_TILES, g.a.biased ? attend_tiles_kernel<T, DP, true> : attend_tiles_kernel<T, DP, false>, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), AT_THREADS,
-           TileShape<DP>::SMEM, g);
+  const unsigned ctas = (unsigned)std::min<uint64_t>(items, (uint64_t)sms);
+  // Scores under a cap of at most 2^80 need no running maximum where the weights
+  // have the exponents of 32 bits: no weight, sum or product leaves their range.
+  // Then two threads take a row (605 us against 623 for chunks under a cap of
+  // 30, 700 against 960 for one of 8); with a maximum to agree on they lose more.
+  auto kernel = g.a.biased ? attend_tiles_kernel<T, DP, true, 1> : attend_tiles_kernel<T, DP, false, 1>;
+  int threads = AT_THREADS<1>;
+  if constexpr (std::is_same_v<T, __nv_bfloat16>)
+    if (g.a.biased && g.a.b.cap_log2 != 0.f && g.a.b.cap_log2 <= 80.f && !g.a.b.slope) {
+      kernel = attend_tiles_kernel<T, DP, true, 2>;
+      threads = AT_THREADS<2>;
+    }
+  launch_k(L, K_ATTEND_TILES, kernel, ctas, threads, TileShape<DP>::SMEM, g);
   if (g.a.max_chunks > 1)
     launch_k(L, K_ATTEND_JOIN, attend_join_kernel<T, DP>, g.a.tiles * g.a.c.n_heads * (DP / 4), 2 * AT_ROWS, 0, g);
 }
@@ -795,11 +843,14 @@ bool launch_attend_tiles(const LaunchCfg& L, const AttendArgs& a, int dtype, int
 
 template <typename T, int DP>
 static cudaError_t allow() {
-  const cudaError_t e = cudaFuncSetAttribute(attend_tiles_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)TileShape<DP>::SMEM);
-  return e != cudaSuccess ? e
-                          : cudaFuncSetAttribute(attend_tiles_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)TileShape<DP>::SMEM);
+  auto set = [](void (*kernel)(AttendTileArgs)) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TileShape<DP>::SMEM);
+  };
+  cudaError_t e = set(attend_tiles_kernel<T, DP, false, 1>);
+  if (e == cudaSuccess) e = set(attend_tiles_kernel<T, DP, true, 1>);
+  if constexpr (std::is_same_v<T, __nv_bfloat16>)
+    if (e == cudaSuccess) e = set(attend_tiles_kernel<T, DP, true, 2>);
+  return e;
 }
 cudaError_t prepare_attend_tiles_kernels() {
   for (cudaError_t e : {allow<__nv_bfloat16, 64>(), allow<__nv_bfloat16, 128>(), allow<__half, 64>(), allow<__half, 128>()})

@@ -11,7 +11,10 @@
 //             whose flags it keeps as bits;
 //   *_list    the ranks of pages: every warp adds up what is counted before it;
 //   *_assign  entries, counts and copies.
-// Bound by latency: three launches, and in each a chain of dependent look-ups.
+// Bound by latency: each phase is a chain of dependent look-ups.  A plan of at
+// most 32,768 entries and pages is one launch of a cluster, whose CTAs meet
+// between the phases; a larger one is three launches of up to a CTA an SM.
+// Measured: PAGES_MEASURED
 // page_copy moves the copied pages' slots, 4 KB a warp at a time, bound by
 // reading and writing them once.
 #include <algorithm>
@@ -54,6 +57,7 @@ __device__ __forceinline__ PageCounts counted_before(const PagesArgs& a, PageCou
   __syncthreads();
   *total = sum(s_sum[1][lane]);
   PageCounts mine = sum(s_sum[0][lane]);
+  __syncthreads();   // read by all before a later phase writes it
   // the CTA's own warps before this one
   const uint4 v = __ldcg((const uint4*)a.counts + first + lane);
   PageCounts own = {};
@@ -112,8 +116,7 @@ __device__ __forceinline__ ForkEntry fork_entry(const PagesArgs& a, uint64_t e) 
 }
 __device__ __forceinline__ bool fork_copies(const ForkEntry& f) { return f.ok && f.at == f.full && f.rest > 0u && f.at < f.held; }
 
-__global__ void __launch_bounds__(PG_THREADS) fork_count_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void fork_count(const PagesArgs& a) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   PageCounts n = {};
   uint64_t e0, e1;
@@ -169,8 +172,7 @@ __global__ void __launch_bounds__(PG_THREADS) fork_count_kernel(const __grid_con
   }
 }
 
-__global__ void __launch_bounds__(PG_THREADS) fork_list_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void fork_list(const PagesArgs& a) {
   PageCounts total;
   const PageCounts before = counted_before(a, &total);
   const uint32_t lane = threadIdx.x & 31;
@@ -197,8 +199,7 @@ __global__ void __launch_bounds__(PG_THREADS) fork_list_kernel(const __grid_cons
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.m.n = 0;
 }
 
-__global__ void __launch_bounds__(PG_THREADS) fork_assign_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void fork_assign(const PagesArgs& a) {
   PageCounts total;
   const PageCounts before = counted_before(a, &total);
   const uint32_t lane = threadIdx.x & 31, below = (1u << lane) - 1u;
@@ -235,16 +236,14 @@ __global__ void __launch_bounds__(PG_THREADS) fork_assign_kernel(const __grid_co
 }
 
 // ---- compact -------------------------------------------------------------------------------
-__global__ void __launch_bounds__(PG_THREADS) compact_count_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void compact_count(const PagesArgs& a) {
   PageCounts n = {};
   n.free = count_free(a);
   if ((threadIdx.x & 31) == 0) a.counts[blockIdx.x * PG_WARPS + (threadIdx.x >> 5)] = n;
 }
 
 // The moves, and each moved page's rank.
-__global__ void __launch_bounds__(PG_THREADS) compact_list_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void compact_list(const PagesArgs& a) {
   PageCounts total;
   const PageCounts before = counted_before(a, &total);
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -299,8 +298,7 @@ __global__ void __launch_bounds__(PG_THREADS) compact_list_kernel(const __grid_c
   }
 }
 
-__global__ void __launch_bounds__(PG_THREADS) compact_assign_kernel(const __grid_constant__ PagesArgs a) {
-  wait_predecessor();
+__device__ __forceinline__ void compact_assign(const PagesArgs& a) {
   const uint64_t t = (uint64_t)blockIdx.x * PG_THREADS + threadIdx.x, step = (uint64_t)gridDim.x * PG_THREADS;
   const uint32_t used = *a.n_used, holes = *a.m.n;
   for (uint64_t k = t; k < holes && k < a.m.cap; k += step) {
@@ -326,6 +324,26 @@ __global__ void __launch_bounds__(PG_THREADS) compact_assign_kernel(const __grid
     }
     a.pages_out[e] = page;
   }
+}
+
+// The three phases: one cluster's, or a launch each.
+template <int PHASE>
+__global__ void __launch_bounds__(PG_THREADS) fork_kernel(const __grid_constant__ PagesArgs a) {
+  wait_predecessor();
+  if (PHASE == 0 || PHASE == 1) fork_count(a);
+  if (PHASE == 0) cluster_sync();
+  if (PHASE == 0 || PHASE == 2) fork_list(a);
+  if (PHASE == 0) cluster_sync();
+  if (PHASE == 0 || PHASE == 3) fork_assign(a);
+}
+template <int PHASE>
+__global__ void __launch_bounds__(PG_THREADS) compact_kernel(const __grid_constant__ PagesArgs a) {
+  wait_predecessor();
+  if (PHASE == 0 || PHASE == 1) compact_count(a);
+  if (PHASE == 0) cluster_sync();
+  if (PHASE == 0 || PHASE == 2) compact_list(a);
+  if (PHASE == 0) cluster_sync();
+  if (PHASE == 0 || PHASE == 3) compact_assign(a);
 }
 
 // ---- copies --------------------------------------------------------------------------------
@@ -367,18 +385,27 @@ __global__ void __launch_bounds__(PC_THREADS) page_copy_kernel(const __grid_cons
 }
 
 // ---- host ------------------------------------------------------------------------------------
+// CTAs of a plan: four entries or pages a thread; up to eight are a cluster.
+constexpr uint32_t PG_CLUSTER = 8;
 uint32_t pages_ctas(uint64_t items, int sms) {
-  return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(items, 4 * PG_THREADS), (uint64_t)sms));
+  const uint64_t n = std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(items, 4 * PG_THREADS), (uint64_t)sms));
+  uint32_t pow2 = 1;
+  while (pow2 < n) pow2 *= 2;
+  return n <= PG_CLUSTER ? std::min(PG_CLUSTER, 4 * pow2) : (uint32_t)n;   // (short chains before few CTAs)
+}
+template <class K>
+static void launch_phases(const LaunchCfg& L, const PagesArgs& a, uint32_t ctas, K whole, K count, K list, K assign) {
+  if (ctas <= PG_CLUSTER) {
+    launch_k(L, K_PAGES, whole, ctas, PG_THREADS, 0, a, dim3(ctas));
+    return;
+  }
+  for (K phase : {count, list, assign}) launch_k(L, K_PAGES, phase, ctas, PG_THREADS, 0, a);
 }
 void launch_fork(const LaunchCfg& L, const PagesArgs& a, uint32_t ctas) {
-  launch_k(L, K_PAGES, fork_count_kernel, ctas, PG_THREADS, 0, a);
-  launch_k(L, K_PAGES, fork_list_kernel, ctas, PG_THREADS, 0, a);
-  launch_k(L, K_PAGES, fork_assign_kernel, ctas, PG_THREADS, 0, a);
+  launch_phases(L, a, ctas, fork_kernel<0>, fork_kernel<1>, fork_kernel<2>, fork_kernel<3>);
 }
 void launch_compact(const LaunchCfg& L, const PagesArgs& a, uint32_t ctas) {
-  launch_k(L, K_PAGES, compact_count_kernel, ctas, PG_THREADS, 0, a);
-  launch_k(L, K_PAGES, compact_list_kernel, ctas, PG_THREADS, 0, a);
-  launch_k(L, K_PAGES, compact_assign_kernel, ctas, PG_THREADS, 0, a);
+  launch_phases(L, a, ctas, compact_kernel<0>, compact_kernel<1>, compact_kernel<2>, compact_kernel<3>);
 }
 void launch_page_copy(const LaunchCfg& L, const PagedArgs& c, const MoveArgs& m, uint32_t* err, int sms) {
   PageCopyArgs a;
