@@ -132,25 +132,42 @@ __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_
 template <>
 __device__ __forceinline__ __nv_bfloat16 minus_infinity<__nv_bfloat16>() { return __ushort_as_bfloat16(0xFF80); }
 
-// Sorts the first n of v, a power of two, by one CTA: falling or rising.
-// (Exchanges over at most 32 places stay within a warp's 64 items.)
+// Sorts the first n of v, a power of two of at most two a thread, by one CTA:
+// falling or rising.  Exchanges over at most 32 places stay within a warp's 64
+// items, in registers.
 __device__ __forceinline__ void sort_items(unsigned long long* v, uint32_t n, bool falling) {
   const uint32_t t = threadIdx.x;
+  const bool have = t < n / 2, idle = (t & ~31u) >= n / 2;   // (a whole warp without items only meets the others)
+  __syncthreads();
+  unsigned long long x[2] = {0, 0};
+  if (have) x[0] = v[2 * t], x[1] = v[2 * t + 1];
   for (uint32_t size = 2; size <= n; size *= 2)
     for (uint32_t step = size / 2; step > 0; step /= 2) {
-      if (step >= 32 || size == 2)
+      unsigned long long y[2];                 // the items at step's distance
+      if (step >= 64) {
+        __syncthreads();                       // read by all before it is written again
+        if (have) v[2 * t] = x[0], v[2 * t + 1] = x[1];
         __syncthreads();
-      else
-        __syncwarp();
-      if (t < n / 2) {
-        const uint32_t i = 2 * t - (t & (step - 1)), j = i + step;
-        const unsigned long long a = v[i], b = v[j];
-        if ((a < b) == (((i & size) == 0) == falling) && a != b) {
-          v[i] = b;
-          v[j] = a;
-        }
+        y[0] = have ? v[(2 * t) ^ step] : 0;
+        y[1] = have ? v[(2 * t + 1) ^ step] : 0;
+      } else if (idle) {
+        continue;
+      } else if (step >= 2) {
+        y[0] = __shfl_xor_sync(0xffffffffu, x[0], step / 2);
+        y[1] = __shfl_xor_sync(0xffffffffu, x[1], step / 2);
+      } else {
+        y[0] = x[1];
+        y[1] = x[0];
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < 2; ++j) {
+        const uint32_t i = 2 * t + j;
+        const bool larger = ((i & step) == 0) == (((i & size) == 0) == falling);
+        x[j] = (x[j] > y[j]) == larger ? x[j] : y[j];
       }
     }
+  __syncthreads();
+  if (have) v[2 * t] = x[0], v[2 * t + 1] = x[1];
   __syncthreads();
 }
 __device__ const float EXP_HI[32] = {RO_EXP_HI}, EXP_LO[32] = {RO_EXP_LO};
@@ -845,7 +862,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
     // The border's bin, by weights in 32 bits: `bins` of equal width, whole
     // numbers that add up to about 2^31.
-    const float per_bin = (float)SM_BINS / span;
+    // (the threads' smallest maximum lies about half-way to the least logit)
+    const float per_bin = (float)SM_BINS / fminf(2.f * span, fmaxf(45.f * T_, 1e-30f));
     auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_BINS - 1)); };
     uint32_t border = SM_BINS;
     if (top < INFINITY) {
@@ -1056,7 +1074,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_many_kernel(const __grid
 }
 // The queued rows, in turn.
 template <typename T>
-__global__ void __launch_bounds__(SM_THREADS) sample_queue_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(SM_THREADS, 2) sample_queue_kernel(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ SampleShared s;
   wait_predecessor();
