@@ -256,12 +256,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
             some = it.i0 < it.i1;
             if constexpr (B) {
               it.len = q.len;
-              it.span = bias_span(q, a.r, a.b, it.i0, max(it.i1, it.i0));
-              for (uint32_t w = 0; w < 2; ++w) {
-                const BiasSpan half = bias_span(q, a.r, a.b, min(it.i1, it.i0 + w * g.toks), min(it.i1, it.i0 + (w + 1) * g.toks));
-                it.all_lo[w] = half.all_lo;
-                it.all_hi[w] = half.total ? half.all_hi : 0u;
-              }
+              it.span = bias_span(q, a.r, a.b, it.i0, max(it.i1, it.i0), it.i0 + g.toks, it.all_lo, it.all_hi);
             } else {
               it.span = key_span(q, a.r, it.i0, max(it.i1, it.i0));
             }
@@ -726,27 +721,46 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       }
       continue;
     }
-    if (!mine) continue;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     T* out = (T*)a.out + out_at + d0;
     const uint32_t left = a.c.head_dim > d0 ? a.c.head_dim - d0 : 0u;   // columns there are
     uint32_t y[OUT / 2];
 #pragma unroll
     for (int i = 0; i < OUT / 2; ++i) y[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-    // Each row is its thread's: 32 bytes a store where rows are aligned to
-    // them, half as many stores to as many lines.
     if (g.wide) {
+      // Each thread has a row; the threads of a group of UNITS turn theirs into
+      // units of 32 bytes side by side, so that a store writes whole rows (a tile's
+      // 32 KB in 64 stores of 8 lines each; a row a thread: of 32 lines, OUT_ROWS).
+      constexpr uint32_t UNITS = OUT / 16;
 #pragma unroll
-      for (int i = 0; i < OUT / 2; i += 8)
-        if ((uint32_t)i * 2 < left)
-          asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 2 * i), "r"(y[i]), "r"(y[i + 1]),
-                       "r"(y[i + 2]), "r"(y[i + 3]), "r"(y[i + 4]), "r"(y[i + 5]), "r"(y[i + 6]), "r"(y[i + 7])
+      for (uint32_t s = 1; s < UNITS; s *= 2)
+#pragma unroll
+        for (uint32_t j = 0; j < UNITS; ++j) {
+          if (j & s) continue;
+#pragma unroll
+          for (uint32_t i = 0; i < 8; ++i) {
+            uint32_t &lo = y[j * 8 + i], &hi = y[(j | s) * 8 + i];
+            const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & s ? lo : hi, s);
+            (lane & s ? lo : hi) = got;
+          }
+        }
+      const uint64_t mine_at = mine ? reinterpret_cast<uint64_t>(out) : 0ull;
+#pragma unroll
+      for (uint32_t j = 0; j < UNITS; ++j) {
+        const uint64_t at = __shfl_sync(0xffffffffu, mine_at, (lane & ~(UNITS - 1u)) | j);
+        const uint32_t unit = lane & (UNITS - 1u);
+        if (at != 0ull && unit * 16 < left)
+          asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at + unit * 32), "r"(y[j * 8]),
+                       "r"(y[j * 8 + 1]), "r"(y[j * 8 + 2]), "r"(y[j * 8 + 3]), "r"(y[j * 8 + 4]), "r"(y[j * 8 + 5]),
+                       "r"(y[j * 8 + 6]), "r"(y[j * 8 + 7])
                        : "memory");
-    } else {
+      }
+    } else if (mine) {
 #pragma unroll
       for (int i = 0; i < OUT / 2; i += 4)
         if ((uint32_t)i * 2 < left) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
     }
+    if (!mine) continue;
     if (a.lse && h == 0) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
   }
   __syncwarp();

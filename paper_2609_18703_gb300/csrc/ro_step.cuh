@@ -233,12 +233,13 @@ struct BiasSpan {
   uint32_t holes;              // 1: some tokens see nothing; 2: sinks of several documents
   __device__ __forceinline__ uint32_t slot(uint32_t u) const { return u < s_n ? s_lo + u : lo + (u - s_n); }
 };
-// a whole warp, the tokens [i0, i1) of a sequence
+// A whole warp, the tokens [i0, i1) of a sequence.  of_lo, of_hi: [all_lo, all_hi)
+// of the tokens before `mid` and of the others (nothing where none sees anything).
 __device__ __forceinline__ BiasSpan bias_span(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t i0,
-                                              uint32_t i1) {
+                                              uint32_t i1, uint32_t mid, uint32_t* of_lo, uint32_t* of_hi) {
   const uint32_t lane = threadIdx.x & 31u;
   BiasSpan k;
-  uint32_t lo = ~0u, hi = 0, all_lo = 0, all_hi = ~0u, none = 0;
+  uint32_t lo = ~0u, hi = 0, all_lo[2] = {0, 0}, all_hi[2] = {~0u, ~0u}, none = 0, some = 0;
   for (uint32_t i = i0 + lane; i < i1; i += 32) {
     const RowSee s = row_see(q, r, b, i);
     if (!s.some()) {
@@ -247,13 +248,26 @@ __device__ __forceinline__ BiasSpan bias_span(const SeqInfo& q, const RowsArgs& 
     }
     lo = min(lo, s.c0);
     hi = max(hi, s.c1);
-    all_lo = max(all_lo, s.c0);
-    all_hi = min(all_hi, s.c1);
+    if (i < mid) {
+      some |= 1u;
+      all_lo[0] = max(all_lo[0], s.c0);
+      all_hi[0] = min(all_hi[0], s.c1);
+    } else {
+      some |= 2u;
+      all_lo[1] = max(all_lo[1], s.c0);
+      all_hi[1] = min(all_hi[1], s.c1);
+    }
+  }
+  some = __reduce_or_sync(0xffffffffu, some);
+#pragma unroll
+  for (uint32_t w = 0; w < 2; ++w) {
+    of_lo[w] = __reduce_max_sync(0xffffffffu, all_lo[w]);
+    of_hi[w] = some >> w & 1u ? __reduce_min_sync(0xffffffffu, all_hi[w]) : 0u;
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
-  k.all_lo = __reduce_max_sync(0xffffffffu, all_lo);
-  k.all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+  k.all_lo = max(of_lo[0], of_lo[1]);   // (a side without tokens that see something says nothing)
+  k.all_hi = some == 3u ? min(of_hi[0], of_hi[1]) : some == 1u ? of_hi[0] : of_hi[1];
   k.holes = __reduce_or_sync(0xffffffffu, none);
   k.s_lo = k.s_n = 0;
   if (lo > hi) lo = hi;        // nobody sees anything
@@ -278,6 +292,11 @@ __device__ __forceinline__ BiasSpan bias_span(const SeqInfo& q, const RowsArgs& 
   k.lo = lo;
   k.total = k.s_n + (hi - lo);
   return k;
+}
+__device__ __forceinline__ BiasSpan bias_span(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t i0,
+                                              uint32_t i1) {
+  uint32_t lo[2], hi[2];
+  return bias_span(q, r, b, i0, i1, i1, lo, hi);
 }
 // Whether one of the tokens [i0, i1) sees slot j of their span.
 __device__ __forceinline__ bool somebody_sees(const SeqInfo& q, const RowsArgs& r, const BiasArgs& b, uint32_t holes,
