@@ -15,6 +15,8 @@
 // mma.sync bounds it, at about an eighth of what the tensor-core tiles reach
 // (chunks of 2,048 tokens over up to 16,384 slots: 205 TFLOP/s against 1,550);
 // it also takes scales of 0 or less, whose softmax has its maximum elsewhere.
+// Biased (ro_cache_attend_biased): scores are capped, fall with distance and are
+// masked row by row before the maximum; slots nobody sees are loaded as zeros.
 #include <algorithm>
 
 #include "ro_step.cuh"

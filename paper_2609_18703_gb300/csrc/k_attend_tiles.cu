@@ -25,6 +25,14 @@
 // 64,000 slots 307 us, 1.74 PFLOP/s.  A pair of products takes 2,050 cycles at the
 // tensor cores' rate; a pair's cycle takes about 2,800, of which its softmax
 // is 1,400 (the maxima 500, the exponentials 900, 512 of them the XU's).
+//
+// Biased (ro_cache_attend_biased): what the rows see comes as two ranges of slots
+// each, columns as bit masks.  Scores that are only masked take the same path (75
+// us for frames of 243 tokens behind a window of 4,096, 0.84 PFLOP/s).  A cap adds
+// a tanh to each product: a polynomial where a warp's products allow it (z = x /
+// cap within 1/2 or 1), else that and 1 - 2 / (1 + e^2z): the same chunks under a
+// cap of 30 take 590 to 620 us, 1.08 PFLOP/s, bound by the multiply-adds (eight
+// for two products) beside the exponentials; a distance bias, two more, 570 us.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -87,18 +95,18 @@ constexpr uint32_t AT_ITEMS = 2;
 // which runs dry could do.
 constexpr uint32_t AT_AHEAD = 8;
 
-// Scores in log2 of N of a row's products, in pairs: under a cap, and falling with
-// the distance: `ahead` slots from the first column to the row's; `both`: columns
-// behind it count too.  voter: the row's products may be believed (others may hold
+// Scores in log2 of N of a row's products and `less` below, in pairs: under a cap,
+// and falling with the distance: `ahead` slots from the first column to the row's;
+// `both`: columns behind it count too.  voter: the row's products may be believed (others may hold
 // anything, and would decide which form the whole warp takes).
 template <int N>
-__device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float ahead, bool both,
-                                            bool voter, uint32_t (&x)[N]) {
+__device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float less, float ahead,
+                                            bool both, bool voter, uint32_t (&x)[N]) {
   const uint64_t to_y = pair(scale_log2, scale_log2);
   // Where no column that counts lies behind the row's slot, slope |ahead - i| is
   // slope ahead - slope i, and its first part enters with the last product.
   const bool line = !both || !__any_sync(0xffffffffu, ahead < (float)(N - 1));
-  const float off = line ? -slope * ahead : 0.f;
+  const float off = (line ? -slope * ahead : 0.f) - less;
   const uint64_t off2 = pair(off, off);
   auto set = [&](int i, uint64_t y) {
     x[i] = (uint32_t)y;
@@ -151,7 +159,7 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
 }
 
 // B: biased (ro_cache_attend_biased).  SPLIT 2: two threads a row, 64 columns of
-// a tile each, and a maximum of 0 for all rows: scores under a cap.
+// a tile each, and no running maximum: scores under a cap.
 template <typename T, int DP, bool B, int SPLIT>
 __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(const __grid_constant__ AttendTileArgs g) {
   using S = TileShape<DP>;
@@ -499,11 +507,13 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     const bool sees_some = B ? see.some() : mine;
     // (rows that see nothing have no say in the others' maximum, and are set to nothing at the end)
     const bool voter = mine && sees_some;
+    // SPLIT 2: the same for every row, 2^40 below what the cap lets weights be
     constexpr bool held = SPLIT == 2;
+    const float base = fmaxf(a.b.cap_log2 - 40.f, 0.f);
     __syncwarp();
     if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
     const bool turned = B && (SPLIT == 2 || a.b.cap_log2 != 0.f || a.b.slope);   // more than scaled
-    float m = held ? 0.f : -INFINITY, l = 0.f;
+    float m = held ? base : -INFINITY, l = 0.f;
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
@@ -595,7 +605,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) tc_ld32(ts + (k0 + i) * 32, y + i * 32);
         tc_wait_ld(y);
-        bias_scores(a.b, scale, slope, ahead - 32.f * k0, a.b.until != nullptr, voter, y);
+        bias_scores(a.b, scale, slope, held ? base : 0.f, ahead - 32.f * k0, a.b.until != nullptr, voter, y);
         if (!all) {
           uint32_t in[PARTS];
 #pragma unroll
@@ -730,7 +740,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     if (g.wide) {
       // Each thread has a row; the threads of a group of UNITS turn theirs into
       // units of 32 bytes side by side, so that a store writes whole rows (a tile's
-      // 32 KB in 64 stores of 8 lines each; a row a thread: of 32 lines, OUT_ROWS).
+      // 32 KB in 64 stores of 8 lines each, not 32: documents of 128 tokens 60 -> 51 us).
       constexpr uint32_t UNITS = OUT / 16;
 #pragma unroll
       for (uint32_t s = 1; s < UNITS; s *= 2)
@@ -822,14 +832,16 @@ template <typename T, int DP>
 static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
   const unsigned ctas = (unsigned)std::min<uint64_t>(items, (uint64_t)sms);
-  // Scores under a cap of at most 2^80 need no running maximum where the weights
-  // have the exponents of 32 bits: no weight, sum or product leaves their range.
-  // Then two threads take a row (605 us against 623 for chunks under a cap of
-  // 30, 700 against 960 for one of 8); with a maximum to agree on they lose more.
+  // Scores under a cap of at most 2^73 need no running maximum where the weights
+  // have the exponents of 32 bits: with 2^(cap - 40) (or 1) for all rows they lie
+  // between 2^-106 and 2^40, so sums of 2^20 values up to 2^67 stay in range, and
+  // so do values down to 2^-20 where every score lies at -cap.  Then two threads
+  // take a row (605 us against 623 for chunks under a cap of 30, 700 against 960
+  // for one of 8); with a maximum to agree on they lose more.
   auto kernel = g.a.biased ? attend_tiles_kernel<T, DP, true, 1> : attend_tiles_kernel<T, DP, false, 1>;
   int threads = AT_THREADS<1>;
   if constexpr (std::is_same_v<T, __nv_bfloat16>)
-    if (g.a.biased && g.a.b.cap_log2 != 0.f && g.a.b.cap_log2 <= 80.f && !g.a.b.slope) {
+    if (g.a.biased && g.a.b.cap_log2 != 0.f && g.a.b.cap_log2 <= 73.f && !g.a.b.slope) {
       kernel = attend_tiles_kernel<T, DP, true, 2>;
       threads = AT_THREADS<2>;
     }

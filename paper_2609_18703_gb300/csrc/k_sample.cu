@@ -22,6 +22,13 @@
 // memory.  Many rows take a CTA each, which reads its row from memory once and
 // what it needs of it again from L2; the wide ones among them are left to a
 // second kernel of clusters.
+//
+// Measured: one row of 32,000 32-bit logits, top-k and top-p: 13.4 us; 256 rows of
+// 131,072 bf16 logits: 18 us to draw the largest (the logits' bytes: 10), 34 with
+// top-k 50 and top-p; 130 us with settings of their own, among them some 17 wide
+// rows, whose exact sums take 100 instructions a token (23 us for 12 rows of them
+// without settings, 77 for 12 with top-p 0.9).  Bound by latency: meetings of a
+// cluster, sorts, and the chains of the exact weights.
 #include <algorithm>
 
 #include "fixed_exp.h"

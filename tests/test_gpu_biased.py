@@ -374,3 +374,16 @@ def test_refusals(ctx):
     assert torch.equal(case.out, before)
     ok(ctx, status())
     ok(ctx, ro.ro_ctx_sync(ctx))
+
+
+@pytest.mark.parametrize("cap", [5.0, 30.0, 50.0, 75.0])
+@pytest.mark.parametrize("size", [2.0 ** 60, 2.0 ** 30, 2.0 ** -30])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_values_of_any_size_under_a_cap(ctx, cap, size, sign):
+    """Scores near the cap on either side, values far from 1."""
+    c = Cache([400, 90], 2, 64, 32, BF16, 8)
+    c.v[:] = (c.v.double() * size).to(BF16)
+    case = Case(c, [90, 60], 4, cap=cap, scale=0.125)
+    case.q[:] = case.q.abs() * 4
+    c.k[:] = (c.k.abs() + 2) * sign      # products far beyond the cap
+    case.check(ctx)

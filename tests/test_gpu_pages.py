@@ -271,7 +271,7 @@ def run_compact(ctx, lists, refs, pool, page, in_place=False):
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("n,used,page,layers", [(1, 0, 4, 1), (1, 1, 4, 1), (2, 1, 4, 1), (31, 17, 3, 1), (32, 32, 16, 1),
                                                 (33, 1, 16, 2), (64, 0, 8, 1), (1000, 640, 4, 2), (20_000, 9_001, 1, 1),
-                                                (5000, 4999, 2, 1)])
+                                                (5000, 4999, 2, 1), (70_001, 30_000, 1, 1)])
 def test_compact(ctx, n, used, page, layers, in_place):
     g = np.random.default_rng(n + used)
     held = g.permutation(n)[:used].tolist()

@@ -304,3 +304,36 @@ def test_sums_next_to_a_border(ctx):
         for q in (p, np.nextafter(np.float32(p), np.float32(0)), np.nextafter(np.float32(p), np.float32(1))):
             check(ctx, x, torch.tensor([0.999]), top_p=float(q), top_k=1024)
             check(ctx, x.expand(n, V)[:2], torch.tensor([0.2, 0.999]), top_p=float(q))
+
+
+def test_many_rows_some_of_them_wide_in_a_graph(ctx):
+    """Rows that few candidates decide and rows left to the second kernel, captured and replayed."""
+    side = torch.cuda.Stream()
+    c2 = ro.ro_ctx_create(0, side, 1)
+    try:
+        n, V = 320, 40_000
+        x, u = rows(n, V, BF16, 31)
+        dev, du = x.cuda(), u.cuda()
+        p = torch.where(torch.arange(n) % 7 == 0, 0.97, 1.0)
+        k = torch.where(torch.arange(n) % 7 == 0, 0, torch.where(torch.arange(n) % 11 == 0, 0, 40))
+        token, logp, kept = check(ctx, x, u, top_p=p, top_k=k)
+        how = ro.ro_sampling(None, k.int().cuda(), p.float().cuda())
+        out, count = (torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2))
+        share = torch.zeros(n, device="cuda")
+        torch.cuda.synchronize()
+        ok(c2, ro.ro_sample(c2, dev, how, du, out, share, count))
+        ok(c2, ro.ro_ctx_sync(c2))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            ok(c2, ro.ro_sample(c2, dev, how, du, out, share, count))
+        for _ in range(3):
+            for z in (out, share, count):
+                z.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, token) and torch.equal(share, logp) and torch.equal(count, kept)
+        ok(c2, ro.ro_ctx_sync(c2))
+    finally:
+        ro.ro_ctx_destroy(c2)
