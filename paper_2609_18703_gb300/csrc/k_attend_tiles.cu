@@ -30,7 +30,7 @@
 // each, columns as bit masks.  Scores that are only masked take the same path (75
 // us for frames of 243 tokens behind a window of 4,096, 0.84 PFLOP/s).  A cap adds
 // a tanh to each product: a polynomial where a warp's products allow it (z = x /
-// cap within 1/2 or 1), else that and 1 - 2 / (1 + e^2z): the same chunks under a
+// cap within 0.33 or 1), else that and 1 - 2 / (1 + e^2z): the same chunks under a
 // cap of 30 take 590 to 620 us, 1.08 PFLOP/s, bound by the multiply-adds (eight
 // for two products) beside the exponentials; a distance bias, two more, 570 us.
 #include <algorithm>
@@ -130,7 +130,7 @@ __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2,
         set(i, fma_pair(mul_pair(v, to_y), p, off2));
       }
     };
-    if (!__any_sync(0xffffffffu, top > 0.5f)) {
+    if (!__any_sync(0xffffffffu, top > 0.33f)) {
       near(std::integral_constant<int, TANH_SHORT_TERMS>(), [](int k) { return tanh_short_term(k); });
     } else if (!__any_sync(0xffffffffu, top > 1.f)) {
       near(std::integral_constant<int, TANH_TERMS>(), [](int k) { return tanh_term(k); });

@@ -312,9 +312,9 @@ __device__ __forceinline__ bool somebody_sees(const SeqInfo& q, const RowsArgs& 
 }
 
 // tanh(z) within 2^-22 of its value: z times a polynomial of z^2 fitted to
-// tanh(z) / z for |z| <= 1 (3.7e-9 off) or, shorter, for |z| <= 1/2 (1.3e-8
+// tanh(z) / z for |z| <= 1 (3.7e-9 off) or, shorter, for |z| <= 0.33 (2.2e-8
 // off), and 1 - 2 / (1 + e^2z) beyond, where nothing cancels.
-constexpr int TANH_TERMS = 7, TANH_SHORT_TERMS = 4;
+constexpr int TANH_TERMS = 7, TANH_SHORT_TERMS = 3;
 __device__ __forceinline__ constexpr float tanh_term(int i) {
   constexpr float c[TANH_TERMS + 1] = {1.f, -0.3333328366279602f, 0.13332240283489227f, -0.05387570336461067f,
                                        0.02147844433784485f, -0.007937350310385227f, 0.002296661725267768f,
@@ -322,8 +322,7 @@ __device__ __forceinline__ constexpr float tanh_term(int i) {
   return c[i];
 }
 __device__ __forceinline__ constexpr float tanh_short_term(int i) {
-  constexpr float c[TANH_SHORT_TERMS + 1] = {1.f, -0.33333075046539307f, 0.13324907422065735f, -0.052994247525930405f,
-                                             0.017151307314634323f};
+  constexpr float c[TANH_SHORT_TERMS + 1] = {1.f, -0.33332693576812744f, 0.13303536176681519f, -0.04949129372835159f};
   return c[i];
 }
 __device__ __forceinline__ float tanh_ratio(float w) {   // tanh(z) / z of w = z^2 <= 1
