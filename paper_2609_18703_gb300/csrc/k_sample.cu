@@ -23,11 +23,11 @@
 // what it needs of it again from L2; the wide ones among them are left to a
 // second kernel of clusters.
 //
-// Measured: one row of 32,000 32-bit logits, top-k and top-p: 13.4 us; 256 rows of
-// 131,072 bf16 logits: 18 us to draw the largest (the logits' bytes: 10), 34 with
-// top-k 50 and top-p; 130 us with settings of their own, among them some 17 wide
-// rows, whose exact sums take 100 instructions a token (23 us for 12 rows of them
-// without settings, 77 for 12 with top-p 0.9).  Bound by latency: meetings of a
+// Measured: one row of 32,000 32-bit logits, top-k and top-p: 13.7 us; 256 rows of
+// 131,072 bf16 logits: 16 us to draw the largest (the logits' bytes: 10), 32 with
+// top-k 50 and top-p; 100 us with settings of their own, among them some 17 wide
+// rows, whose exact sums take 100 instructions a token (24 us for 12 rows of them
+// without settings, 76 for 12 with top-p 0.9).  Bound by latency: meetings of a
 // cluster, sorts, and the chains of the exact weights.
 #include <algorithm>
 
@@ -185,13 +185,19 @@ struct Threshold {
 };
 
 // Candidates held, two a thread; tokens they are meant to hold where top-k does
-// not say, and at most.
-constexpr uint32_t SM_LIST = 2 * SM_THREADS, SM_WANT = 512, SM_WANT_MOST = 704;
+// not say (with min-p, for top-p alone), and at most.
+constexpr uint32_t SM_LIST = 2 * SM_THREADS, SM_WANT_MIN = 512, SM_WANT = 256, SM_WANT_MOST = 704;
+// Maxima of a thread at most, each over every so-many-th of its blocks: the parts
+// that hold candidates are read again.  (Of a row's own CTA eight: 256 rows of
+// 131,072, top-p at 0.4, 147 us with two, 105 with eight.  Of a cluster's two,
+// whose threads have a few blocks in shared memory: one row of 32,000 13.5 against 14.7.)
+constexpr uint32_t SM_PARTS = 8;
 static_assert(2 * SM_LIST <= SM_BINS, "candidates and their weights lie where the bins do");
 constexpr uint32_t SM_COARSE = SM_THREADS;   // bins of the threads' maxima
 // What a sum of weights in 32 bits may be off, relative to itself: a weight's
-// argument, below 64, by three roundings, 2^-17; its exponential by 2^-22; a
-// thread's terms, at most 800 in two levels of sums of at most 200, by 2^-24 a sum.
+// argument, below 64, by three roundings, 2^-17; its exponential by 2^-22; the at
+// most 220 sums that it goes into, by 2^-24 each; where a sum is scaled to a larger
+// logit, at most 25 times, the factors by 2^-22 and 2^-24 each: 2^-15.1.
 constexpr float SM_SLACK = 1.f / (1 << 15);
 enum SampleWay : uint32_t { WAY_DONE, WAY_MASS, WAY_WIDE };
 constexpr uint32_t QUEUE_WIDE = 0x80000000u;   // beside a queued row: WAY_WIDE
@@ -215,7 +221,7 @@ struct __align__(16) SampleShared {
     uint64_t at, ties;                     // weight and tokens on the threshold before it
   } run;
   float rough, warp_rough[SM_WARPS];       // sums of weights in 32 bits
-  uint8_t flags[SM_WARPS][64];             // halves of a warp's threads that hold a candidate
+  uint8_t flags[SM_WARPS][32 * SM_PARTS];  // parts of a warp's threads that hold a candidate
   float temperature, top_p, min_p, u;
   uint32_t top_k, valid;
   double reach;                            // how far below the largest logit min-p reaches
@@ -226,7 +232,7 @@ struct __align__(16) SampleShared {
 // not by its candidates.
 template <typename T, bool WIDE>
 __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared& s, uint4* slice, uint32_t row, bool known_wide) {
-  constexpr uint32_t E = Logits<T>::E;
+  constexpr uint32_t E = Logits<T>::E, PARTS = WIDE ? 2 : SM_PARTS;
   // the low bits of a 16-bit logit's key follow from its sign
   constexpr int LOW = std::is_same_v<T, float> ? 0 : std::is_same_v<T, __half> ? 11 : 16;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -266,8 +272,32 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     s.reach = s.min_p > 0.f ? (double)s.temperature * log((double)s.min_p) : 0.0;
   }
   s.coarse[tid] = 0;
-  // ---- the slice, and its largest logit: of every second block of a thread's, two maxima ----
-  float my_top[2] = {-INFINITY, -INFINITY};
+  // ---- the slice, its largest logits, and where top-p will ask for it the sum of
+  // the weights in 32 bits, relative to the largest logit that the thread has met
+  // (a cluster, whose slices lie in shared memory, sums when the largest is known:
+  // this pass is then 0.6 us shorter for the rows that need no sum) ----
+  float my_top[PARTS];
+#pragma unroll
+  for (uint32_t h = 0; h < PARTS; ++h) my_top[h] = -INFINITY;
+  float met = -INFINITY, met_sum = 0.f;
+  const float per_unit = fminf(1.44269504f / (a.temperature ? a.temperature[row] : 1.f), 3.0e38f);
+  const uint32_t k_asked = a.top_k ? a.top_k[row] : 0u;
+  const bool rough_asked = !WIDE && a.top_p && a.top_p[row] < 1.f && (k_asked == 0u || k_asked >= a.vocab);
+  auto meet = [&](float largest) {
+    if (largest > met) {
+      met_sum *= ex2((met - largest) * per_unit);
+      met = largest;
+    }
+  };
+  auto add_met = [&](const uint4& v) {
+    float part[2] = {0.f, 0.f};
+#pragma unroll
+    for (uint32_t k = 0; k < E; ++k) {
+      const float z = (met - Logits<T>::at(v, k)) * per_unit;
+      part[k & 1] += z < 64.f ? ex2(-z) : 0.f;   // (a NaN is not below)
+    }
+    met_sum += part[0] + part[1];
+  };
   uint4 none;
   {
     __align__(16) T e[E];
@@ -287,7 +317,15 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     for (uint32_t q = 0; q < AHEAD; ++q) {
       const uint32_t j = i + q * SM_THREADS;
       if (a.staged && j >= in0 && j < in1) slice[j] = v[q];
-      my_top[q & 1] = fmaxf(my_top[q & 1], Logits<T>::largest(v[q]));
+      my_top[q % PARTS] = fmaxf(my_top[q % PARTS], Logits<T>::largest(v[q]));
+    }
+    if (rough_asked) {
+      float largest = my_top[0];
+#pragma unroll
+      for (uint32_t h = 1; h < PARTS; ++h) largest = fmaxf(largest, my_top[h]);
+      meet(largest);
+#pragma unroll
+      for (uint32_t q = 0; q < AHEAD; ++q) add_met(v[q]);
     }
   }
 #pragma unroll
@@ -303,14 +341,24 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       slice[i] = v;
     else
       s.edge[b0 + i == 0 ? 0 : 1] = v;
-    my_top[i / SM_THREADS & 1] = fmaxf(my_top[i / SM_THREADS & 1], Logits<T>::largest(v));
+    const float largest = Logits<T>::largest(v);
+#pragma unroll
+    for (uint32_t q = 0; q < PARTS; ++q)
+      if (q == i / SM_THREADS % PARTS) my_top[q] = fmaxf(my_top[q], largest);
+    if (rough_asked) {
+      meet(largest);
+      add_met(v);
+    }
   }
   {
-    uint32_t low = ~0u;
+    float largest = -INFINITY, smallest = INFINITY;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (my_top[h] > -INFINITY) low = min(low, logit_key(my_top[h]));
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, logit_key(fmaxf(my_top[0], my_top[1])));
+    for (uint32_t h = 0; h < PARTS; ++h) {
+      largest = fmaxf(largest, my_top[h]);
+      if (my_top[h] > -INFINITY) smallest = fminf(smallest, my_top[h]);
+    }
+    uint32_t low = largest > -INFINITY ? logit_key(smallest) : ~0u;
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, logit_key(largest));
     low = __reduce_min_sync(0xffffffffu, low);
     if (lane == 0) {
       s.warp_count[warp] = hi;
@@ -347,14 +395,17 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   if (T_ == 0.f || top_k == 1u || top_p == 0.f) {   // the first of the largest
     uint32_t place = ~0u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (my_top[h] == top)
-        for (uint32_t i = tid + h * SM_THREADS; i < n && place == ~0u; i += 2 * SM_THREADS) {
+    for (uint32_t h = 0; h < PARTS; ++h)
+      if (my_top[h] == top) {
+        uint32_t first = ~0u;
+        for (uint32_t i = tid + h * SM_THREADS; i < n && first == ~0u; i += PARTS * SM_THREADS) {
           const uint4 v = block(i);
 #pragma unroll
           for (uint32_t k = E; k-- > 0;)
-            if (Logits<T>::at(v, k) == top) place = (b0 + i) * E + k - off;
+            if (Logits<T>::at(v, k) == top) first = (b0 + i) * E + k - off;
         }
+        place = min(place, first);
+      }
     if (place != ~0u) atomicMin(&s.place, place);
     sync();
     if (rank == 0) {
@@ -427,7 +478,18 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       for (uint32_t q = 0; q < 4; ++q) use(v[q]);
     }
   };
-  // a thread's 32-bit sums, of the CTA: in s.rough once the CTA has met
+  // a thread's 32-bit sum: the CTA's is in s.rough once the CTA has met
+  auto rough_of = [&](float sum) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) s.warp_rough[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+      sum = 0.f;
+      for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
+      s.rough = sum;
+    }
+  };
   auto rough_sum = [&](float above) {
     float sum = 0.f;
     each_block([&](const uint4& v) {
@@ -439,15 +501,14 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       }
       sum += part[0] + part[1];
     });
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) s.warp_rough[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-      sum = 0.f;
-      for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
-      s.rough = sum;
-    }
+    rough_of(sum);
+  };
+  // of all, from what was met
+  auto rough_met = [&] {
+    if constexpr (WIDE)
+      rough_sum(-INFINITY);
+    else
+      rough_of(met < top ? met_sum * ex2((met - top) * per_unit) : met_sum);
   };
   auto rough_total = [&]() -> float {
     if (nc == 1) return s.rough;
@@ -519,18 +580,17 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
 
   // ---- few candidates ----
-  const uint32_t most = min(SM_WANT_MOST, nc * SM_THREADS * 3 / 2);   // of the threads' maxima
   uint32_t way = WAY_WIDE;
   if ((by_k || by_p || by_min) && top < INFINITY && !known_wide) {
-    const uint32_t want = by_k && top_k <= most ? top_k : min(SM_WANT, most);
-    const bool all_of_k = by_k && top_k <= most;   // the candidates hold the first top_k
+    const bool all_of_k = by_k && top_k <= SM_WANT_MOST;   // the candidates hold the first top_k
+    const uint32_t want = all_of_k ? top_k : by_min ? SM_WANT_MIN : SM_WANT;
     const float per_bin = (float)SM_COARSE / span;
     auto bin_of = [&](float y) { return (uint32_t)fminf((top - y) * per_bin, (float)(SM_COARSE - 1)); };
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (uint32_t h = 0; h < PARTS; ++h)
       if (my_top[h] > -INFINITY) atomicAdd(&s.coarse[bin_of(my_top[h])], 1u);
     // the sum that top-p is a share of, first in 32 bits
-    if (by_p && !all_of_k && !by_k) rough_sum(-INFINITY);
+    if (by_p && !by_k) rough_met();
     if (tid == 0) s.cut = SM_COARSE;
     sync();
     // the bin at which `want` maxima are reached is the last that is listed
@@ -549,14 +609,18 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     const float reach = (float)(cut + 1), limit = with_min ? key_logit(th.key) : -INFINITY;
     const bool far = cut >= SM_COARSE - 1;
     auto candidate = [&](float y) { return y > limit && (far || (top - y) * per_bin < reach); };
-    // A warp goes through the blocks of those of its threads' halves whose maximum is one, several at a time.
+    // A warp goes through the blocks of those of its threads' parts whose maximum is one, several at a time.
     uint8_t* flags = s.flags[warp];
-    const uint32_t flag0 = __ballot_sync(0xffffffffu, candidate(my_top[0])), flag1 = __ballot_sync(0xffffffffu, candidate(my_top[1]));
-    const uint32_t below = (1u << lane) - 1u;
-    if (flag0 >> lane & 1u) flags[__popc(flag0 & below)] = (uint8_t)lane;
-    if (flag1 >> lane & 1u) flags[__popc(flag0) + __popc(flag1 & below)] = (uint8_t)(lane | 32u);
+    uint32_t flagged = 0;
+#pragma unroll
+    for (uint32_t h = 0; h < PARTS; ++h) {
+      const bool flag = candidate(my_top[h]);
+      const uint32_t all = __ballot_sync(0xffffffffu, flag);
+      if (flag) flags[flagged + __popc(all & ((1u << lane) - 1u))] = (uint8_t)(lane | h << 5);
+      flagged += __popc(all);
+    }
     __syncwarp();
-    const uint32_t runs = (n + 2 * SM_THREADS - 1) / (2 * SM_THREADS), visits = (__popc(flag0) + __popc(flag1)) * runs;
+    const uint32_t runs = (n + PARTS * SM_THREADS - 1) / (PARTS * SM_THREADS), visits = flagged * runs;
     for (uint32_t x0 = 0; x0 < visits; x0 += 4 * 32) {
       uint4 v[4];
       uint32_t at[4];
@@ -564,7 +628,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       for (uint32_t q = 0; q < 4; ++q) {
         const uint32_t visit = x0 + q * 32 + lane, f = visit / runs;
         at[q] = n;
-        if (visit < visits) at[q] = warp * 32 + (flags[f] & 31u) + (flags[f] >> 5) * SM_THREADS + (visit - f * runs) * 2 * SM_THREADS;
+        if (visit < visits)
+          at[q] = warp * 32 + (flags[f] & 31u) + ((flags[f] >> 5) + (visit - f * runs) * PARTS) * SM_THREADS;
         v[q] = at[q] < n ? block(at[q]) : none;
       }
 #pragma unroll
@@ -574,7 +639,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
           if (const float y = Logits<T>::at(v[q], k); candidate(y)) enlist(y, (b0 + at[q]) * E + k - off);
     }
     sync();
-    if (by_p && !all_of_k && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
+    if (by_p && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
     // ---- the first CTA's ----
     const uint32_t listed = rank == 0 ? s.listed : 0;
     uint32_t stay = 0;
