@@ -16,18 +16,18 @@
 // Other rows are wide: top-k's border is found by passes over the bits of the
 // logits' keys (which order alike), top-p's by a histogram of weights in 32 bits
 // that names the border's bin, an exact pass that sums what lies above the bin,
-// and a sort of the bin itself.
+// and a sort of the bin itself, whose kept tokens' weights complete the sums.
 //
 // Few rows are split over clusters of CTAs, which hold their slices in shared
 // memory.  Many rows take a CTA each, which reads its row from memory once and
 // what it needs of it again from L2; the wide ones among them are left to a
 // second kernel of clusters.
 //
-// Measured: one row of 32,000 32-bit logits, top-k and top-p: 13.7 us; 256 rows of
-// 131,072 bf16 logits: 16 us to draw the largest (the logits' bytes: 10), 32 with
-// top-k 50 and top-p; 100 us with settings of their own, among them some 17 wide
+// Measured: one row of 32,000 32-bit logits, top-k and top-p: 14.4 us; 256 rows of
+// 131,072 bf16 logits: 16 us to draw the largest (the logits' bytes: 10), 30 with
+// top-k 50 and top-p; 94 us with settings of their own, among them some 17 wide
 // rows, whose exact sums take 100 instructions a token (24 us for 12 rows of them
-// without settings, 76 for 12 with top-p 0.9).  Bound by latency: meetings of a
+// without settings, 57 for 12 with top-p 0.9).  Bound by latency: meetings of a
 // cluster, sorts, and the chains of the exact weights.
 #include <algorithm>
 
@@ -65,6 +65,19 @@ __device__ __forceinline__ void cluster_write(const unsigned long long* p, uint3
 }
 __device__ __forceinline__ void cluster_write(const uint32_t* p, uint32_t rank, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "r"(v) : "memory");
+}
+// v to an item of CTA `rank` of nc (its own if that is one)
+__device__ __forceinline__ void cluster_add(uint32_t* p, uint32_t rank, uint32_t nc, uint32_t v) {
+  if (nc > 1)
+    cluster_take(p, rank, v);
+  else
+    atomicAdd(p, v);
+}
+__device__ __forceinline__ void cluster_add(unsigned long long* p, uint32_t rank, uint32_t nc, uint64_t v) {
+  if (nc > 1)
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(cluster_at(step_smem(p), rank)), "l"(v) : "memory");
+  else
+    atomicAdd(p, (unsigned long long)v);
 }
 template <class V>
 __device__ __forceinline__ V cluster_read(const V* p, uint32_t rank) {
@@ -206,7 +219,8 @@ struct __align__(16) SampleShared {
   unsigned long long mass[SM_BINS];
   uint32_t count[SM_BINS];
   unsigned long long warp_mass[SM_WARPS], warp_above[SM_WARPS];
-  uint32_t warp_ties[SM_WARPS], warp_count[SM_WARPS];
+  uint32_t warp_ties[SM_WARPS], warp_count[SM_WARPS], warp_above_count[SM_WARPS];
+  uint32_t border_ties[SM_WARPS];          // tokens on top-p's border in the warps' runs
   unsigned long long scan[SM_WARPS];
   unsigned long long found_left;
   uint32_t found;
@@ -533,15 +547,37 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   const float span = fmaxf(fminf(top - key_logit(least), 45.f * T_), 1e-30f);
   unsigned long long* list = s.mass;              // candidates: keys and ~indices
   unsigned long long* weights = s.mass + SM_LIST;
-  auto enlist = [&](float y, uint32_t index) {    // to the first CTA's list
-    const unsigned long long item = (unsigned long long)logit_key(y) << 32 | ~index;
-    if (nc > 1) {
-      const uint32_t at = cluster_take(&s.listed, 0, 1u);
-      if (at < SM_LIST) cluster_write(&s.mass[at], 0, item);
-    } else {
-      const uint32_t at = atomicAdd(&s.listed, 1u);
-      if (at < SM_LIST) s.mass[at] = item;
+  // To the CTA's list, by a whole warp: the logits whose bits are set in `hits`;
+  // index(b): of bit b's.
+  auto enlist = [&](uint32_t hits, auto&& index) {
+    if (!__any_sync(0xffffffffu, hits != 0u)) return;
+    const uint32_t mine = __popc(hits), inc = warp_incl_scan(mine);
+    uint32_t at = 0;
+    if (lane == 31) at = atomicAdd(&s.listed, inc);
+    at = __shfl_sync(0xffffffffu, at, 31) + inc - mine;
+    for (; hits != 0u; hits &= hits - 1u, ++at) {
+      const uint32_t i = index((uint32_t)__ffs(hits) - 1u);
+      const T y = a.staged ? ((const T*)slice)[i + off - b0 * E] : x[i];
+      if (at < SM_LIST) list[at] = (unsigned long long)logit_key((float)y) << 32 | ~i;
     }
+  };
+  // The first CTA, when all have met: everyone's list behind its own, and how many are
+  // listed.  (Placed from afar, on one counter, a row's thousand took 17,000 cycles more.)
+  auto all_listed = [&]() -> uint32_t {
+    if (nc == 1) return s.listed;
+    const uint32_t end = warp_incl_scan(lane < nc ? cluster_read(&s.listed, lane) : 0u), all = __shfl_sync(0xffffffffu, end, 31);
+    if (all > SM_LIST) return all;
+    for (uint32_t i0 = __shfl_sync(0xffffffffu, end, 0); i0 < all; i0 += SM_THREADS) {
+      const uint32_t i = i0 + tid;
+      uint32_t r = 0, before = 0;
+      for (uint32_t q = 0; q < nc; ++q) {
+        const uint32_t x = __shfl_sync(0xffffffffu, end, q);
+        if (x <= i) r = q + 1, before = x;
+      }
+      if (i < all) list[i] = cluster_read(&list[i - before], r);
+    }
+    __syncthreads();
+    return all;
   };
   // The first CTA: sorts what is listed; the weights of this thread's two items
   // and of those ahead of them; returns all their weight.
@@ -632,19 +668,37 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
           at[q] = warp * 32 + (flags[f] & 31u) + ((flags[f] >> 5) + (visit - f * runs) * PARTS) * SM_THREADS;
         v[q] = at[q] < n ? block(at[q]) : none;
       }
+      uint32_t hits = 0;
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q)
 #pragma unroll
-        for (uint32_t k = 0; k < E; ++k)
-          if (const float y = Logits<T>::at(v[q], k); candidate(y)) enlist(y, (b0 + at[q]) * E + k - off);
+        for (uint32_t k = 0; k < E; ++k) hits |= candidate(Logits<T>::at(v[q], k)) ? 1u << (q * E + k) : 0u;
+      static_assert(4 * E <= 32, "a bit a logit");
+      enlist(hits, [&](uint32_t b) {
+        const uint32_t q = b / E, i = q < 2u ? (q == 0u ? at[0] : at[1]) : (q == 2u ? at[2] : at[3]);
+        return (b0 + i) * E + b % E - off;
+      });
     }
     sync();
     if (by_p && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
     // ---- the first CTA's ----
-    const uint32_t listed = rank == 0 ? s.listed : 0;
+    const uint32_t listed = rank == 0 ? all_listed() : 0;
     uint32_t stay = 0;
     if (rank == 0) {
-      if (listed > 0 && listed <= SM_LIST) {
+      // Where the listed ones' weights add up to less than top-p's share, more tokens stay: nothing to sort.
+      bool short_of = false;
+      if (by_p && !by_k && !by_min && cut != SM_COARSE && listed <= SM_LIST) {
+        float sum = 0.f;
+        for (uint32_t i = tid; i < listed; i += SM_THREADS) sum += rough_weight(key_logit((uint32_t)(list[i] >> 32)));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) s.warp_rough[warp] = sum;
+        __syncthreads();
+        sum = 0.f;
+        for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
+        short_of = sum * (1.f + SM_SLACK) < rough_total() * top_p * (1.f - SM_SLACK);
+      }
+      if (listed > 0 && listed <= SM_LIST && !short_of) {
         const uint64_t list_mass = sort_list(listed);
         uint32_t by_limit = listed;                  // min-p's
         if (by_min) {
@@ -842,16 +896,16 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   struct Sums {
     uint64_t mass, above, before, ties_before;   // of all; of the bins above the border's; before this warp:
                                                  // weight above the threshold, tokens on it
-    uint64_t ties, count;                        // on it, above it, in all
+    uint64_t ties, count, above_count;           // on it, above it, in the bins above the border's
     uint64_t own;                                // this warp's weight above it
     uint32_t own_ties;
   };
-  // extra(y, index, in): whether its weight counts as `above`
+  // extra(v, in, index): those of a block whose weight counts as `above`, as bits
   auto sums = [&](auto weighed, auto&& extra) -> Sums {
     constexpr bool W = decltype(weighed)::value;
     const float limit = key_logit(th.key);
     uint64_t m = 0, up = 0;
-    uint32_t on = 0, above = 0;
+    uint32_t on = 0, above = 0, up_count = 0;
     for (uint32_t i = i0; i < i1; i += 32) {
       const bool have = i + lane < i1;
       const uint4 v = have ? block(i + lane) : make_uint4(0, 0, 0, 0);
@@ -868,22 +922,26 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       if constexpr (W) {
         weigh(y, in, w);
         m += total_of(w);
+        const uint32_t over = extra(v, in, (b0 + i + lane) * E - off);
 #pragma unroll
         for (uint32_t k = 0; k < E; ++k)
-          if (extra(y[k], (b0 + i + lane) * E + k - off, in[k])) {
+          if (over >> k & 1u) {
             more.hi += w[k].hi;
             more.lo += w[k].lo;
           }
         up += whole(more, bits);
+        up_count += __popc(over);
       }
     }
     m = warp_sum64(m);
     up = warp_sum64(up);
     on = __reduce_add_sync(0xffffffffu, on);
     above = __reduce_add_sync(0xffffffffu, above);
+    up_count = __reduce_add_sync(0xffffffffu, up_count);
     if (lane == 0) {
       s.warp_mass[warp] = m;
       s.warp_above[warp] = up;
+      s.warp_above_count[warp] = up_count;
       s.warp_ties[warp] = on;
       s.warp_count[warp] = above;
     }
@@ -897,6 +955,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       const uint64_t wu = nc > 1 ? cluster_read(&s.warp_above[w], r) : s.warp_above[w];
       const uint32_t wt = nc > 1 ? cluster_read(&s.warp_ties[w], r) : s.warp_ties[w];
       const uint32_t wc = nc > 1 ? cluster_read(&s.warp_count[w], r) : s.warp_count[w];
+      t.above_count += nc > 1 ? cluster_read(&s.warp_above_count[w], r) : s.warp_above_count[w];
       t.mass += wm;
       t.above += wu;
       t.ties += wt;
@@ -910,12 +969,13 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     t.above = warp_sum64(t.above);
     t.ties = warp_sum64(t.ties);
     t.count = warp_sum64(t.count);
+    t.above_count = warp_sum64(t.above_count);
     t.before = warp_sum64(t.before);
     t.ties_before = warp_sum64(t.ties_before);
     sync();   // read by all before it is written again
     return t;
   };
-  auto nothing = [](float, uint32_t, bool) { return false; };
+  auto nothing = [](const uint4&, const bool (&)[E], uint32_t) { return 0u; };
   auto cut_to_k = [&] {
     if (by_k && sums(std::false_type(), nothing).count > top_k) {
       uint64_t left;
@@ -925,6 +985,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
 
   cut_to_k();
+  Sums t = {};
+  bool summed = false;     // t is of what passes th
   if (by_p) {
     const Threshold cut = th;
     if (by_min) {          // top-p's sum is over the first top_k, whatever min-p says
@@ -940,8 +1002,10 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     uint32_t border = SM_BINS;
     if (top < INFINITY) {
       const float limit = key_logit(th.key);
-      rough_sum(limit);
+      // (of all tokens, the sum is known where candidates were looked for)
+      if (th.key != KEY_NONE || by_k || known_wide) rough_sum(limit);
       for (uint32_t i = tid; i < SM_BINS; i += SM_THREADS) s.count[i] = 0;
+      if (tid < SM_WARPS) s.border_ties[tid] = 0;
       if (tid == 0) {
         s.found = SM_BINS;
         s.listed = 0;
@@ -960,7 +1024,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       if (rank == 0) {   // the first CTA's alone: a bin of each of the others is a load from its shared memory
         constexpr uint32_t EACH = SM_BINS / SM_THREADS;
         static_assert(EACH == 4, "four bins a thread");
-        uint64_t mine[EACH] = {0, 0, 0, 0};
+        uint64_t mine[EACH] = {}, sum = 0;
         for (uint32_t q = 0; q < nc; ++q) {
           uint4 v;
           const uint32_t at = step_smem(&s.count[tid * EACH]);
@@ -970,7 +1034,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
                        : "memory");
           mine[0] += v.x; mine[1] += v.y; mine[2] += v.z; mine[3] += v.w;
         }
-        const uint64_t sum = mine[0] + mine[1] + mine[2] + mine[3];
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) sum += mine[j];
         const uint64_t inc = warp_incl_scan(sum);
         if (lane == 31) s.scan[warp] = inc;
         __syncthreads();
@@ -994,11 +1059,19 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       border = s.cut;
     }
     // exactly: all of it, what lies above the bin, and the bin's tokens
-    const Sums t = sums(std::true_type(), [&](float y, uint32_t index, bool in) {
-      if (!in || border == SM_BINS) return false;
-      const uint32_t b = bin_of(y);
-      if (b == border) enlist(y, index);
-      return b < border;
+    // (bin_of(y) against the border, without its conversion)
+    const float border_lo = (float)border, border_hi = border < SM_BINS - 1 ? border_lo + 1.f : INFINITY;
+    t = sums(std::true_type(), [&](const uint4& v, const bool (&in)[E], uint32_t index) {
+      uint32_t over = 0, hits = 0;
+      if (border == SM_BINS) return over;
+#pragma unroll
+      for (uint32_t k = 0; k < E; ++k) {
+        const float b = (top - Logits<T>::at(v, k)) * per_bin;
+        over |= in[k] && b < border_lo ? 1u << k : 0u;
+        hits |= in[k] && b >= border_lo && b < border_hi ? 1u << k : 0u;
+      }
+      enlist(hits, [&](uint32_t b) { return index + b; });
+      return over;
     });
     const uint64_t want = scaled(t.mass + tie * th.ties, top_p, true);
     if (want > t.mass) {
@@ -1006,7 +1079,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     } else {
       if (rank == 0) {
         Threshold found = {0, 0};
-        const uint32_t listed = s.listed;
+        const uint32_t listed = all_listed();
         if (border != SM_BINS && want > t.above && listed > 0 && listed <= SM_LIST) {
           const uint64_t all = sort_list(listed);
           if (want <= t.above + all) {
@@ -1015,6 +1088,26 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
             const uint32_t on = (2 * tid < n_in && (uint32_t)(list[2 * tid] >> 32) == key) +
                                 (2 * tid + 1 < n_in && (uint32_t)(list[2 * tid + 1] >> 32) == key);
             found = {key, (uint32_t)__syncthreads_count(on >= 1) + (uint32_t)__syncthreads_count(on >= 2)};
+            // What stays of the bin, to the sums of what lies above it, by the warps whose runs it is in.
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {
+              const unsigned long long item = 2 * tid + j < listed ? list[2 * tid + j] : 0;
+              const bool tied = (uint32_t)(item >> 32) == key;
+              if (2 * tid + j >= listed || (!tied && 2 * tid + j >= n_in)) continue;
+              const uint32_t b = (~(uint32_t)item + off) / E, r = b / a.blocks;
+              const uint32_t len = min(n_blocks, (r + 1) * a.blocks) - r * a.blocks;
+              const uint32_t w = (b - r * a.blocks) / ((len + SM_WARPS - 1) / SM_WARPS);
+              if (tied)
+                cluster_add(&s.border_ties[w], r, nc, 1u);
+              else
+                cluster_add(&s.warp_above[w], r, nc, own[j]);
+            }
+            if (tid < nc) {
+              if (nc > 1)
+                cluster_write(&s.cut, tid, n_in - found.ties);
+              else
+                s.cut = n_in - found.ties;
+            }
           }
         }
         if (tid < nc) {
@@ -1030,6 +1123,25 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       const Threshold found = s.border;
       if (found.ties != 0u) {
         th = found;
+        summed = true;
+        t.mass = t.before = t.ties_before = 0;
+        for (uint32_t q = lane; q < nc * SM_WARPS; q += 32) {
+          const uint32_t r = q / SM_WARPS, w = q % SM_WARPS;
+          const uint64_t wm = nc > 1 ? cluster_read(&s.warp_above[w], r) : s.warp_above[w];
+          const uint32_t wt = nc > 1 ? cluster_read(&s.border_ties[w], r) : s.border_ties[w];
+          t.mass += wm;
+          if (q < rank * SM_WARPS + warp) {
+            t.before += wm;
+            t.ties_before += wt;
+          }
+        }
+        t.mass = warp_sum64(t.mass);
+        t.before = warp_sum64(t.before);
+        t.ties_before = warp_sum64(t.ties_before);
+        t.own = s.warp_above[warp];
+        t.own_ties = s.border_ties[warp];
+        t.ties = found.ties;
+        t.count = t.above_count + s.cut;
       } else {             // too many tokens in the bin, or 32 bits named a wrong one
         uint64_t left;
         const uint32_t key = select(std::true_type(), want, &left);
@@ -1038,11 +1150,14 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         th.ties = (uint32_t)min((left + w - 1) / w, (uint64_t)0xFFFFFFFFu);
       }
     }
-    if (cut.key > th.key || (cut.key == th.key && cut.ties < th.ties)) th = cut;
+    if (cut.key > th.key || (cut.key == th.key && cut.ties < th.ties)) {
+      th = cut;
+      summed = false;
+    }
   }
 
   // ---- the token ----
-  const Sums t = sums(std::true_type(), nothing);
+  if (!summed) t = sums(std::true_type(), nothing);
   const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
   const uint64_t ties = min((uint64_t)th.ties, t.ties);
   const uint64_t total = t.mass + tie * ties;
@@ -1144,16 +1259,28 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_many_kernel(const __grid
     a.queue[atomicAdd(a.counter, 1u)] = row | (way == WAY_WIDE ? QUEUE_WIDE : 0u);
   if (a.cluster > 1) cluster_sync();
 }
-// The queued rows, in turn.
+// The queued rows: a cluster takes one, then whichever is next.  (A CTA an SM:
+// the exact sums spill at 64 registers, 109 against 100 us for 256 rows of which
+// 17 are queued; where all are, two a SM would be the faster.)
 template <typename T>
-__global__ void __launch_bounds__(SM_THREADS, 2) sample_queue_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(SM_THREADS) sample_queue_kernel(const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   __shared__ SampleShared s;
   wait_predecessor();
-  const uint32_t nc = a.cluster, rows = *(volatile uint32_t*)a.counter;
-  for (uint32_t i = blockIdx.x / nc; i < rows; i += gridDim.x / nc) {
+  const uint32_t nc = a.cluster, rows = *(volatile uint32_t*)a.counter, tid = threadIdx.x;
+  if (rows == 0u) return;
+  for (uint32_t i = blockIdx.x / nc; i < rows; i = s.row) {
+    uint32_t next = 0;
+    if (blockIdx.x % nc == 0 && tid < 32) {   // (asked for early: the answer takes a while)
+      if (tid == 0) next = gridDim.x / nc + atomicAdd(a.counter + 2, 1u);
+    }
     const uint32_t row = a.queue[i];
     sample_row<T, true>(a, s, (uint4*)smem_raw, row & ~QUEUE_WIDE, (row & QUEUE_WIDE) != 0u);
+    if (blockIdx.x % nc == 0 && tid < 32) {
+      next = __shfl_sync(0xffffffffu, next, 0);
+      if (nc == 1 && tid == 0) s.row = next;
+      if (nc > 1 && tid < nc) cluster_write(&s.row, tid, next);
+    }
     if (nc > 1)
       cluster_sync();
     else
@@ -1161,9 +1288,10 @@ __global__ void __launch_bounds__(SM_THREADS, 2) sample_queue_kernel(const __gri
   }
   // the last CTA to leave sets the count back for the next call
   __syncthreads();
-  if (threadIdx.x == 0 && ticket(a.counter + 1) == gridDim.x - 1) {
+  if (tid == 0 && ticket(a.counter + 1) == gridDim.x - 1) {
     a.counter[0] = 0u;
     a.counter[1] = 0u;
+    a.counter[2] = 0u;
   }
 }
 

@@ -257,7 +257,7 @@ struct SampleArgs {
   uint32_t cluster, blocks;  // CTAs of a row, 16-byte blocks of a slice
   uint32_t staged;           // slices are held in shared memory
   uint32_t* queue;           // [rows], where wide ones are queued
-  uint32_t* counter;         // of the queue, and a ticket: zero between calls
+  uint32_t* counter;         // of the queue's rows, a ticket, rows taken: zero between calls
   uint32_t* err;
 };
 // whether wide rows are queued for a second kernel (a.queue and a.counter are then given)

@@ -638,7 +638,7 @@ ro_status ro_sample(ro_ctx* ctx, int32_t dtype, const void* d_logits, uint64_t r
     void* p = nullptr;
     RO_TRY(c.scratch(SS_ROWS, n_rows * sizeof(uint32_t), &p));
     a.queue = (uint32_t*)p;
-    RO_TRY(c.scratch(SS_COUNTER, 2 * sizeof(uint32_t), &p));
+    RO_TRY(c.scratch(SS_COUNTER, 3 * sizeof(uint32_t), &p));
     a.counter = (uint32_t*)p;
   }
   launch_sample(c.launch(), a, dtype, c.sms());
