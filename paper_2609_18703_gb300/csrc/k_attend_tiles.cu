@@ -31,8 +31,8 @@
 // us for frames of 243 tokens behind a window of 4,096, 0.84 PFLOP/s).  A cap adds
 // a tanh to each product: a polynomial where a warp's products allow it (z = x /
 // cap within 0.33 or 1), else that and 1 - 2 / (1 + e^2z): the same chunks under a
-// cap of 30 take 590 to 620 us, 1.08 PFLOP/s, bound by the multiply-adds (eight
-// for two products) beside the exponentials; a distance bias, two more, 570 us.
+// cap of 30 take 575 to 590 us, 1.1 PFLOP/s, bound by the multiply-adds (seven
+// for two products) beside the exponentials.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
