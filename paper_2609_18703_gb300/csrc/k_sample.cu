@@ -228,6 +228,7 @@ struct __align__(16) SampleShared {
   uint32_t place;                          // of the largest logit, the first of equal ones
   uint32_t coarse[SM_COARSE];              // the threads' maxima, counted by distance from the largest
   uint32_t cut, listed, way, row;
+  uint32_t counts[SM_MAX_CLUSTER];         // what each CTA has listed
   Threshold border;
   uint4 edge[2];                           // a row's first and last block, where it does not fill them
   struct {
@@ -388,10 +389,9 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       s.least = least;
     }
     cluster_sync();
-    for (uint32_t r = 0; r < nc; ++r) {
-      best = max(best, cluster_read(&s.best, r));
-      least = min(least, cluster_read(&s.least, r));
-    }
+    // (a lane each of the others': one after the other costs a round trip each)
+    best = __reduce_max_sync(0xffffffffu, lane < nc ? cluster_read(&s.best, lane) : 0u);
+    least = __reduce_min_sync(0xffffffffu, lane < nc ? cluster_read(&s.least, lane) : ~0u);
   } else {
     __syncthreads();   // read by all before they are written again
   }
@@ -526,8 +526,9 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
   auto rough_total = [&]() -> float {
     if (nc == 1) return s.rough;
+    const float part = lane < nc ? __uint_as_float(cluster_read((const uint32_t*)&s.rough, lane)) : 0.f;
     float sum = 0.f;
-    for (uint32_t r = 0; r < nc; ++r) sum += __uint_as_float(cluster_read((const uint32_t*)&s.rough, r));
+    for (uint32_t r = 0; r < nc; ++r) sum += __shfl_sync(0xffffffffu, part, r);
     return sum;
   };
   auto with_log = [&](uint32_t token, float y, uint64_t total, uint32_t kept) {
@@ -563,9 +564,10 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
   // The first CTA, when all have met: everyone's list behind its own, and how many are
   // listed.  (Placed from afar, on one counter, a row's thousand took 17,000 cycles more.)
-  auto all_listed = [&]() -> uint32_t {
+  auto all_listed = [&](bool counted) -> uint32_t {   // counted: s.counts is written
     if (nc == 1) return s.listed;
-    const uint32_t end = warp_incl_scan(lane < nc ? cluster_read(&s.listed, lane) : 0u), all = __shfl_sync(0xffffffffu, end, 31);
+    const uint32_t theirs = lane >= nc ? 0u : counted ? s.counts[lane] : cluster_read(&s.listed, lane);
+    const uint32_t end = warp_incl_scan(theirs), all = __shfl_sync(0xffffffffu, end, 31);
     if (all > SM_LIST) return all;
     for (uint32_t i0 = __shfl_sync(0xffffffffu, end, 0); i0 < all; i0 += SM_THREADS) {
       const uint32_t i = i0 + tid;
@@ -631,7 +633,15 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     sync();
     // the bin at which `want` maxima are reached is the last that is listed
     uint32_t mine = 0;
-    for (uint32_t r = 0; r < nc; ++r) mine += nc > 1 ? cluster_read(&s.coarse[tid], r) : s.coarse[tid];
+    if (nc > 1) {
+      uint32_t v[SM_MAX_CLUSTER];
+#pragma unroll
+      for (uint32_t r = 0; r < SM_MAX_CLUSTER; ++r) v[r] = r < nc ? cluster_read(&s.coarse[tid], r) : 0u;
+#pragma unroll
+      for (uint32_t r = 0; r < SM_MAX_CLUSTER; ++r) mine += v[r];
+    } else {
+      mine = s.coarse[tid];
+    }
     const uint32_t inc = warp_incl_scan(mine);
     if (lane == 31) s.warp_count[warp] = inc;
     __syncthreads();
@@ -679,10 +689,14 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         return (b0 + i) * E + b % E - off;
       });
     }
+    if (nc > 1) {
+      __syncthreads();
+      if (tid == 0) cluster_write(&s.counts[rank], 0, s.listed);
+    }
     sync();
     if (by_p && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
     // ---- the first CTA's ----
-    const uint32_t listed = rank == 0 ? all_listed() : 0;
+    const uint32_t listed = rank == 0 ? all_listed(true) : 0;
     uint32_t stay = 0;
     if (rank == 0) {
       // Where the listed ones' weights add up to less than top-p's share, more tokens stay: nothing to sort.
@@ -1025,14 +1039,22 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         constexpr uint32_t EACH = SM_BINS / SM_THREADS;
         static_assert(EACH == 4, "four bins a thread");
         uint64_t mine[EACH] = {}, sum = 0;
-        for (uint32_t q = 0; q < nc; ++q) {
-          uint4 v;
-          const uint32_t at = step_smem(&s.count[tid * EACH]);
-          asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
-                       : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                       : "r"(nc > 1 ? cluster_at(at, q) : at)
-                       : "memory");
-          mine[0] += v.x; mine[1] += v.y; mine[2] += v.z; mine[3] += v.w;
+        for (uint32_t q0 = 0; q0 < nc; q0 += 4) {   // several at a time
+          uint4 v[4];
+#pragma unroll
+          for (uint32_t q = 0; q < 4; ++q) {
+            v[q] = make_uint4(0, 0, 0, 0);
+            const uint32_t at = step_smem(&s.count[tid * EACH]);
+            if (q0 + q < nc)
+              asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
+                           : "=r"(v[q].x), "=r"(v[q].y), "=r"(v[q].z), "=r"(v[q].w)
+                           : "r"(nc > 1 ? cluster_at(at, q0 + q) : at)
+                           : "memory");
+          }
+#pragma unroll
+          for (uint32_t q = 0; q < 4; ++q) {
+            mine[0] += v[q].x; mine[1] += v[q].y; mine[2] += v[q].z; mine[3] += v[q].w;
+          }
         }
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) sum += mine[j];
@@ -1079,7 +1101,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     } else {
       if (rank == 0) {
         Threshold found = {0, 0};
-        const uint32_t listed = all_listed();
+        const uint32_t listed = all_listed(false);
         if (border != SM_BINS && want > t.above && listed > 0 && listed <= SM_LIST) {
           const uint64_t all = sort_list(listed);
           if (want <= t.above + all) {
