@@ -236,7 +236,8 @@ ro_status ro_cache_attend_biased(ro_ctx* ctx, const ro_cache* cache, const uint6
  * Pages of a cache that several sequences share.  d_refs counts for every pool
  * page how many entries of page lists name it (and whatever else holds it); a
  * page with 0 is free.  Shared pages are full ones: a page that a sequence still
- * writes is its own.
+ * writes is its own.  Outputs share no memory with inputs or one another but
+ * where it is said (RO_E_INVAL).
  */
 /* Copies of pages: d_n[0] of them (at most cap), copy i the first d_slots[i]
  * slots of pool page d_from[i] to page d_to[i]. */
@@ -335,7 +336,8 @@ ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* move
  *              sum over those that stay (-inf where none).
  *   d_kept     uint32[n_rows] out or NULL: how many stay (drawing the largest: 1).
  * Weights are about 2^-40 exact and their sums are exact: tokens do not depend
- * on how the work is split.  vocab is at most 393,216.  Recorded: RO_E_INVAL for
+ * on how the work is split.  vocab is at most 393,216.  Outputs share no memory
+ * with inputs or one another (RO_E_INVAL).  Recorded: RO_E_INVAL for
  * a row whose settings or u are out of range or NaN (RO_NO_TOKEN there).
  */
 #define RO_NO_TOKEN 0xFFFFFFFFu

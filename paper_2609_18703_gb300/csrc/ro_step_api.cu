@@ -2,6 +2,7 @@
 // choice of kernel by sizes, types and alignment, workspaces and launches.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "ro_step.h"
 
@@ -160,6 +161,20 @@ ro_status check_moves(StepCall& c, const char* fn, const ro_moves* m, uint64_t l
 bool touch(const void* p, uint64_t p_bytes, const void* q, uint64_t q_bytes) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return p_bytes && q_bytes && a < b + q_bytes && b < a + p_bytes;
+}
+// Whether an output shares bytes with an input or with another output.
+struct Bytes {
+  const void* p;
+  uint64_t n;
+};
+bool clash(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins) {
+  for (const Bytes* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Bytes& i : ins)
+      if (touch(o->p, o->n, i.p, i.n)) return true;
+    for (const Bytes* q = outs.begin(); q != o; ++q)
+      if (touch(o->p, o->n, q->p, q->n)) return true;
+  }
+  return false;
 }
 // Flags, ranks and counts of a plan over the pool's pages.
 ro_status plan_scratch(StepCall& c, uint64_t items, PagesArgs* a, uint32_t* ctas) {
@@ -531,6 +546,13 @@ ro_status ro_cache_fork(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_le
     return c.refuse(RO_E_INVAL, "%s: counts change in place or in another array", fn);
   if (touch(d_len, (uint64_t)cache->n_seqs * 4, d_len_out, n_children * 4) || touch(cache->d_pages, 4, d_dst_pages, n_dst * 4))
     return c.refuse(RO_E_INVAL, "%s: the continuations' lengths and pages go to arrays of their own", fn);
+  const uint64_t room = moves->cap * 4, starts = ((uint64_t)cache->n_seqs + 1) * 8;
+  if (clash({{d_dst_pages, n_dst * 4}, {d_len_out, n_children * 4}, {d_refs_out, d_refs_out == d_refs ? 0 : pool},
+             {moves->d_from, room}, {moves->d_to, room}, {moves->d_slots, room}, {moves->d_n, 4}},
+            {{d_len, (uint64_t)cache->n_seqs * 4}, {d_child_base, starts}, {d_child_parent, n_children * 4},
+             {d_dst_base, n_children ? (n_children + 1) * 8 : 0}, {d_dst_seq, n_dst * 4}, {d_refs, pool},
+             {cache->d_page_base, starts}, {cache->d_pages, 4}}))
+    return c.refuse(RO_E_INVAL, "%s: outputs share memory with inputs or one another", fn);
   RO_TRY(c.begin());
   a.c = paged(cache);
   a.refs = d_refs;
@@ -570,6 +592,11 @@ ro_status ro_cache_compact(ro_ctx* ctx, const ro_cache* cache, uint32_t* d_pages
     return c.refuse(RO_E_INVAL, "%s: counts change in place or in another array", fn);
   if (d_pages_out != cache->d_pages && touch(cache->d_pages, n_list * 4, d_pages_out, n_list * 4))
     return c.refuse(RO_E_INVAL, "%s: lists change in place or in another array", fn);
+  const uint64_t room = moves->cap * 4;
+  if (clash({{d_pages_out, d_pages_out == cache->d_pages ? 0 : n_list * 4}, {d_refs_out, d_refs_out == d_refs ? 0 : pool},
+             {d_n_used, 4}, {moves->d_from, room}, {moves->d_to, room}, {moves->d_slots, room}, {moves->d_n, 4}},
+            {{d_refs, pool}, {cache->d_page_base, ((uint64_t)cache->n_seqs + 1) * 8}, {cache->d_pages, 4}}))
+    return c.refuse(RO_E_INVAL, "%s: outputs share memory with inputs or one another", fn);
   RO_TRY(c.begin());
   a.c = paged(cache);
   a.refs = d_refs;
@@ -617,6 +644,12 @@ ro_status ro_sample(ro_ctx* ctx, int32_t dtype, const void* d_logits, uint64_t r
                         how ? (const void*)how->d_top_p : nullptr, how ? (const void*)how->d_min_p : nullptr})
     if (!aligned(p, 4)) return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
   if (n_rows == 0) return RO_OK;
+  const uint64_t each = n_rows * 4, elem = dtype == RO_F32 ? 4 : 2;
+  const ro_sampling neutral = {}, &set = how ? *how : neutral;
+  if (clash({{d_token, each}, {d_logp, d_logp ? each : 0}, {d_kept, d_kept ? each : 0}},
+            {{d_logits, ((n_rows - 1) * row_stride + vocab) * elem}, {d_u, each}, {set.d_temperature, set.d_temperature ? each : 0},
+             {set.d_top_k, set.d_top_k ? each : 0}, {set.d_top_p, set.d_top_p ? each : 0}, {set.d_min_p, set.d_min_p ? each : 0}}))
+    return c.refuse(RO_E_INVAL, "%s: outputs share memory with inputs or one another", fn);
   RO_TRY(c.begin());
   SampleArgs a = {};
   a.x = d_logits;

@@ -406,3 +406,38 @@ def test_refusals(ctx):
     ok(ctx, ro.ro_ctx_sync(ctx))
     ok(ctx, status())
     ok(ctx, ro.ro_ctx_sync(ctx))
+
+
+def test_outputs_that_share_memory_are_refused(ctx):
+    """An output on an input or on another output, in part or in whole, where the header does not allow it."""
+    pool = Pool(8, 1, 16, 32)
+    base, pages, refs = i64([0, 2]), i32([1, 3]), i32([0, 1, 0, 1, 0, 0, 0, 0])
+    cache = pool.caches(base, pages)[0]
+    t, n = moves_of(8)
+    moves = ro.ro_moves(*t, n)
+    free = torch.zeros(64, dtype=torch.int32, device="cuda")
+    good = dict(cache=cache, d_len=i32([20]), d_child_base=i64([0, 1]), d_child_parent=i32([0]), d_dst_base=i64([0, 2]),
+                d_dst_seq=i32([0, 0]), d_dst_pages=free[:2], d_len_out=free[8:9], d_refs=refs, d_refs_out=free[16:24], moves=moves)
+
+    def fork(**change):
+        return ro.ro_cache_fork(ctx, *{**good, **change}.values())
+
+    for bad in (dict(d_dst_pages=good["d_dst_seq"]), dict(d_len_out=good["d_child_parent"]), dict(d_dst_pages=free[17:19]),
+                dict(d_len_out=free[1:2]), dict(d_dst_pages=t[1][:2]), dict(d_refs_out=t[0]), dict(d_len_out=n),
+                dict(d_dst_pages=refs[:2]), dict(moves=ro.ro_moves(t[0], t[0], t[2], n)),
+                dict(moves=ro.ro_moves(t[0], t[1], t[2], t[2][:1])), dict(moves=ro.ro_moves(t[0], refs, t[2], n))):
+        assert fork(**bad) == ro.RO_E_INVAL, bad
+    used = free[32:33]
+
+    def compact(out=free[:2], counts=free[16:24], used=used, m=moves):
+        return ro.ro_cache_compact(ctx, cache, out, refs, counts, used, m)
+
+    for bad in (dict(out=free[16:18]), dict(out=refs[:2]), dict(counts=t[2]), dict(used=n), dict(used=refs[:1]),
+                dict(used=free[1:2]), dict(m=ro.ro_moves(t[0], t[1], t[1], n))):
+        assert compact(**bad) == ro.RO_E_INVAL, bad
+    ok(ctx, ro.ro_ctx_sync(ctx))
+    assert not free.any() and refs.tolist() == [0, 1, 0, 1, 0, 0, 0, 0]
+    ok(ctx, fork())
+    ok(ctx, compact())
+    ok(ctx, fork(d_refs=free[16:24].copy_(refs), d_refs_out=free[16:24]))   # in place
+    ok(ctx, ro.ro_ctx_sync(ctx))

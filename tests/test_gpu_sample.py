@@ -337,3 +337,17 @@ def test_many_rows_some_of_them_wide_in_a_graph(ctx):
         ok(c2, ro.ro_ctx_sync(c2))
     finally:
         ro.ro_ctx_destroy(c2)
+
+
+def test_outputs_that_share_memory_are_refused(ctx):
+    x, u = rows(3, 100, F32, 1)
+    dev, du = x.cuda(), u.cuda()
+    ints, floats = torch.zeros(16, dtype=torch.int32, device="cuda"), torch.ones(16, device="cuda")
+    how = ro.ro_sampling(floats[:3], ints[8:11], floats[3:6])
+    for token, logp, kept in ((ints[8:11], None, None), (ints[10:13], None, None), (ints[:3], None, ints[2:5]),
+                              (ints[:3], floats[2:5], None), (ints[:3], du, None), (ints[:3], dev[1, :3], None),
+                              (ints[:3], dev.view(-1)[297:], None), (ints[:3], None, ints[6:9])):
+        assert ro.ro_sample(ctx, dev, how, du, token, logp, kept) == ro.RO_E_INVAL
+    ok(ctx, ro.ro_ctx_sync(ctx))
+    ok(ctx, ro.ro_sample(ctx, dev, how, du, ints[:3], floats[6:9], ints[3:6]))
+    ok(ctx, ro.ro_ctx_sync(ctx))
