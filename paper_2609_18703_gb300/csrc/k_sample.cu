@@ -23,11 +23,11 @@
 // what it needs of it again from L2; the wide ones among them are left to a
 // second kernel of clusters.
 //
-// Measured: one row of 32,000 32-bit logits, top-k and top-p: 14.4 us; 256 rows of
+// Measured: one row of 32,000 32-bit logits, top-k and top-p: 14.2 us; 256 rows of
 // 131,072 bf16 logits: 16 us to draw the largest (the logits' bytes: 10), 30 with
-// top-k 50 and top-p; 94 us with settings of their own, among them some 17 wide
+// top-k 50 and top-p; 90 us with settings of their own, among them some 17 wide
 // rows, whose exact sums take 100 instructions a token (24 us for 12 rows of them
-// without settings, 57 for 12 with top-p 0.9).  Bound by latency: meetings of a
+// without settings, 55 for 12 with top-p 0.9).  Bound by latency: meetings of a
 // cluster, sorts, and the chains of the exact weights.
 #include <algorithm>
 
@@ -998,15 +998,12 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     }
   };
 
+  const Threshold cut = th;                 // min-p's
+  if (by_p) th = {KEY_NONE, 0};             // (top-p's sum is over the first top_k, whatever min-p says)
   cut_to_k();
   Sums t = {};
   bool summed = false;     // t is of what passes th
   if (by_p) {
-    const Threshold cut = th;
-    if (by_min) {          // top-p's sum is over the first top_k, whatever min-p says
-      th = {KEY_NONE, 0};
-      cut_to_k();
-    }
     const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
     // The border's bin, by weights in 32 bits: `bins` of equal width, whole
     // numbers that add up to about 2^31.
