@@ -351,3 +351,18 @@ def test_outputs_that_share_memory_are_refused(ctx):
     ok(ctx, ro.ro_ctx_sync(ctx))
     ok(ctx, ro.ro_sample(ctx, dev, how, du, ints[:3], floats[6:9], ints[3:6]))
     ok(ctx, ro.ro_ctx_sync(ctx))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n", [3, 80])
+@pytest.mark.parametrize("spread", [0.2, 1.5])
+def test_wide_rows_of_all_settings(ctx, dtype, n, spread):
+    """Rows that keep thousands of tokens, few of them and more than are worked on at a time: nuclei within top-k, cut
+    shorter by min-p or not, borders between equal logits; calls one after the other."""
+    V = 40_001
+    for seed in (n, n + 1):
+        x, u = rows(n, V, dtype, seed, spread)
+        x[::7, 5000:9000] = x[::7, 4999:5000]      # borders among equal ones
+        g = np.random.default_rng(seed)
+        check(ctx, x, u, temperature=g.choice([0.7, 1.0, 2.0], n), top_k=g.choice([0, 0, 1500, 20_000, V - 1], n),
+              top_p=g.choice([0.3, 0.9, 0.999, 1.0], n), min_p=g.choice([0.0, 0.0, 1e-4, 0.02], n))
