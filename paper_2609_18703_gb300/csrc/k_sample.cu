@@ -42,6 +42,7 @@ constexpr uint32_t SM_WARPS = SM_THREADS / 32, SM_BINS = 2048, SM_MAX_CLUSTER = 
 constexpr uint32_t SM_SLICE = 80 * 1024;
 constexpr uint32_t NO_TOKEN = 0xFFFFFFFFu;
 constexpr uint32_t KEY_NONE = 0x007FFFFFu;   // of -inf
+constexpr uint32_t KEY_MINUS_ZERO = 0x7FFFFFFFu;
 
 // larger logit, larger key; -0 as 0
 __device__ __forceinline__ uint32_t logit_key(float x) {
@@ -542,6 +543,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   if (s.min_p > 0.f) {   // w >= min_p; the smallest such float
     const float least_x = __double2float_ru((double)top + s.reach);
     th.key = max(KEY_NONE, logit_key(least_x) - 1u);
+    // (as a number -0 is 0, which has to lie above the threshold; no logit has its key)
+    if (th.key == KEY_MINUS_ZERO) th.key = KEY_MINUS_ZERO - 1u;
   }
   const bool by_k = top_k != 0u && top_k < a.vocab, by_p = top_p < 1.f, by_min = s.min_p > 0.f;
   // (as far as weights go: beyond 45 T they are below 2^-64)
@@ -1181,6 +1184,10 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   const uint64_t ties = min((uint64_t)th.ties, t.ties);
   const uint64_t total = t.mass + tie * ties;
   const uint64_t goal = scaled(total, s.u, false);   // the first running sum above it
+  if (total == 0) {   // (the largest logit stays in every row: nothing has to be left unwritten all the same)
+    if (rank == 0 && tid == 0) finish(NO_TOKEN, -INFINITY, 0);
+    return WAY_DONE;
+  }
   uint64_t ties_before = t.ties_before;
   uint64_t at = t.before + tie * min(ties, ties_before);
   const uint64_t mine = t.own + tie * (min(ties, ties_before + t.own_ties) - min(ties, ties_before));
