@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
       nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
       const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
       f[z] = exp2f(m[z] - top);
-      sub[z] = top - WEIGHT_UP<T>;
+      sub[z] = weight_base<T>(top);
       m[z] = nm[z];
       l[z] *= f[z];
     }

@@ -191,7 +191,7 @@ struct FewRows {
       nm[z] = fmaxf(nm[z], __shfl_xor_sync(0xffffffffu, nm[z], 2));
       const float top = nm[z] == -INFINITY ? 0.f : nm[z];   // a row that has seen nothing yet
       f[z] = ex2(m[z] - top);
-      sub[z] = top - WEIGHT_UP<T>;
+      sub[z] = weight_base<T>(top);
     }
     if (__any_sync(0xffffffffu, nm[0] > m[0] || nm[1] > m[1])) {
 #pragma unroll

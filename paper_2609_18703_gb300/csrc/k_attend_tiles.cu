@@ -561,7 +561,9 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       // (Rows that are no token's have no say: theirs may hold whatever an
       // earlier kernel left, and would decide how the others are rounded.)
       auto raise = [&](float mn) {
-        if (!__any_sync(0xffffffffu, voter && mn > m + AT_SLACK<T>)) return;
+        bool moves = mn > m + AT_SLACK<T>;
+        if constexpr (B) moves = mn - m > AT_SLACK<T>;   // (scores past 2^24, where the sum would be rounded)
+        if (!__any_sync(0xffffffffu, voter && moves)) return;
         const float f = mn == -INFINITY ? 1.f : ex2(m - mn);
         m = mn;
         l *= f;
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
           if (lane == 0) bar_arrive(b_p + 16 * w + (i / 2) * 8);
         }
       };
-      auto below = [&] { return (m == -INFINITY ? 0.f : m) - WEIGHT_UP<T, AT_SLACK<T>>; };   // -inf: a row that has seen nothing yet
+      auto below = [&] { return weight_base<T, AT_SLACK<T>>(m == -INFINITY ? 0.f : m); };   // -inf: a row that has seen nothing yet
       if (turned) {
         if (!all) zero_values(slots.at(c0 + t));
         constexpr int COLS = AT_KEYS / SPLIT, PARTS = COLS / 32;

@@ -82,6 +82,15 @@ template <typename T, int SLACK = 0>
 constexpr int WEIGHT_UP = 0;
 template <int SLACK>
 constexpr int WEIGHT_UP<__half, SLACK> = 15 - SLACK;
+// What is taken off a row's scores (in log2) before the exponential: its maximum,
+// less what weights are held higher by.  Past 2^24 the difference is rounded up,
+// or its rounding would lift weights out of f16's range.
+template <typename T, int SLACK = 0>
+__device__ __forceinline__ float weight_base(float top) {
+  constexpr float up = WEIGHT_UP<T, SLACK>;
+  const float base = top - up;
+  return up != 0.f && top - base > up + 0.5f ? __fsub_ru(top, up) : base;
+}
 // ln sum_j exp(..) of a row from its maximum (in log2) and its sum
 template <typename T, int SLACK = 0>
 __device__ __forceinline__ float row_lse(float m, float l) {
