@@ -204,8 +204,9 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
  * distance, or are masked by documents and prefixes.  With a = the slot of a
  * new token t and x_j = scale * q.k_j:
  *   cap > 0:   x_j becomes cap * tanh(x_j / cap);
- *   d_slope:   then slope[query head] * |a - j| is taken off (finite slopes;
- *              distances count slots);
+ *   d_slope:   then slope[query head] * |a - j| is taken off (finite slopes of
+ *              either sign; distances count slots; what passes 32 bits' range
+ *              counts as infinite);
  *   d_first:   t sees no slot before d_first[t], the first one of its
  *              document; sinks are the `sinks` slots from there on.  A token
  *              whose d_first lies behind its own slot sees nothing (tokens

@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(AR_THREADS) attend_rows_kernel(const __grid_co
         row_a[z] = q.first + i;
         if constexpr (BIASED) {
           see[z] = row_see(q, a.r, a.b, i);
-          slope[z] = a.b.slope ? a.b.slope[kh * G + g] * LOG2E : 0.f;
+          slope[z] = slope_log2(a.b, kh * G + g);
         }
       }
     }

@@ -93,7 +93,7 @@ struct FewRows {
         row_a[z] = q.first + i;
         if constexpr (B) {
           see[z] = row_see(q, a.r, a.b, i);
-          if (a.b.slope) slope[z] = a.b.slope[h] * LOG2E;
+          slope[z] = slope_log2(a.b, h);
         }
       }
     }

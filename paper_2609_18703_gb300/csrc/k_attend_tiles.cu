@@ -102,12 +102,7 @@ constexpr uint32_t AT_AHEAD = 8;
 template <int N>
 __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2, float slope, float less, float ahead,
                                             bool both, bool voter, uint32_t (&x)[N]) {
-  const uint64_t to_y = pair(scale_log2, scale_log2);
-  // Where no column that counts lies behind the row's slot, slope |ahead - i| is
-  // slope ahead - slope i, and its first part enters with the last product.
-  const bool line = !both || !__any_sync(0xffffffffu, ahead < (float)(N - 1));
-  const float off = (line ? -slope * ahead : 0.f) - less;
-  const uint64_t off2 = pair(off, off);
+  const uint64_t to_y = pair(scale_log2, scale_log2), off2 = pair(-less, -less);
   auto set = [&](int i, uint64_t y) {
     x[i] = (uint32_t)y;
     x[i + 1] = (uint32_t)(y >> 32);
@@ -136,16 +131,26 @@ __device__ __forceinline__ void bias_scores(const BiasArgs& b, float scale_log2,
       near(std::integral_constant<int, TANH_TERMS>(), [](int k) { return tanh_term(k); });
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])) + off);
+      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(capped(b, __uint_as_float(x[i])) - less);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < N; i += 2) set(i, fma_pair(pair_bits(x[i], x[i + 1]), to_y, off2));
   }
   if (b.slope) {
-    if (line) {
+    // The distance first, then one rounding of the whole: slope (ahead - i) as
+    // slope ahead - slope i would round a near slot's score at a far one's size.
+    if (!both || !__any_sync(0xffffffffu, ahead < (float)(N - 1))) {   // no column that counts lies behind the row's slot
+      const uint64_t fall = pair(-slope, -slope), step = pair(-8.f, -8.f);
+      uint64_t d[4];   // of every fourth pair of columns
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = __float_as_uint(fmaf(slope, (float)i, __uint_as_float(x[i])));
+      for (int k = 0; k < 4; ++k) d[k] = pair(ahead - (float)(2 * k), ahead - (float)(2 * k + 1));
+#pragma unroll
+      for (int i = 0; i < N; i += 2) {
+        uint64_t& at = d[(i / 2) & 3];
+        set(i, fma_pair(fall, at, pair_bits(x[i], x[i + 1])));
+        if (i + 8 < N) at = add_pair(at, step);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] = __float_as_uint(fmaf(-slope, fabsf(ahead - (float)i), __uint_as_float(x[i])));
@@ -487,7 +492,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       s_end = it.span.s_lo + it.span.s_n;
       if (mine) {
         see = row_see(q, a.r, a.b, tok);
-        if (a.b.slope) slope = a.b.slope[head] * LOG2E;
+        slope = slope_log2(a.b, head);
       }
     } else {
       const int64_t a_lo = it.first + j0, a_hi = it.first + (live ? j1 : j0 + 1) - 1;

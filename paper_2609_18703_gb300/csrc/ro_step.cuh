@@ -211,6 +211,11 @@ __device__ __forceinline__ bool sees(const RowsArgs& r, int64_t a, uint32_t j) {
 }
 
 // ---- biased attention: what a token sees, and its scores ---------------------------------
+// A query head's slope in log2, finite: a row's own slot is 0 slots away.
+__device__ __forceinline__ float slope_log2(const BiasArgs& b, uint32_t head) {
+  constexpr float most = 3.402823466e38f;
+  return b.slope ? fminf(fmaxf(b.slope[head] * LOG2E, -most), most) : 0.f;
+}
 // A token sees the slots [a0, a1) (its document's first ones, behind a window)
 // and [c0, c1).  Its own slot is one of the latter unless it sees nothing.
 struct RowSee {
