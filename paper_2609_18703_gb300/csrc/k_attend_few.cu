@@ -147,8 +147,17 @@ struct FewRows {
     if constexpr (B) {
       const bool all = whole && st.t0 >= ks.all_lo && st.t0 + KEYS <= ks.all_hi;
       float(&flat)[KEYS / 2] = reinterpret_cast<float(&)[KEYS / 2]>(s);
+      uint32_t in = ~0u;   // bits of the products that their rows see
+      if (!all) {
+        in = 0u;
+#pragma unroll
+        for (int i = 0; i < KEYS / 2; ++i) {
+          const uint32_t j = st.t0 + (i / 4) * 8 + (lane & 3) * 2 + (i & 1);
+          in |= j >= st.lo && j < st.hi && see[(i >> 1) & 1].sees(j) ? 1u << i : 0u;
+        }
+      }
       if (a.b.cap_log2 != 0.f) {
-        cap_scores(a.b, flat);
+        cap_scores(a.b, in, flat);
       } else {
 #pragma unroll
         for (int i = 0; i < KEYS / 2; ++i) flat[i] *= a.r.scale_log2;
@@ -164,8 +173,7 @@ struct FewRows {
       for (int x = 0; x < KEYS / 8; ++x)
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
-          const uint32_t j = st.t0 + x * 8 + (lane & 3) * 2 + (z & 1);
-          if (!all && (j < st.lo || j >= st.hi || !see[z >> 1].sees(j))) s[x][z] = -INFINITY;
+          if (!(in >> (4 * x + z) & 1u)) s[x][z] = -INFINITY;
           nm[z >> 1] = fmaxf(nm[z >> 1], s[x][z]);
         }
     } else {

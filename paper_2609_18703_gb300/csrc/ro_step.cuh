@@ -356,12 +356,15 @@ __device__ __forceinline__ float capped(const BiasArgs& b, float dot) {
   asm("{\n .reg .pred p;\n setp.le.f32 p, %1, 0f3F800000;\n selp.f32 %0, %2, %3, p;\n}" : "=f"(t) : "f"(w), "f"(near), "f"(far));
   return b.cap_log2 * t;
 }
-// Scores in log2 of a warp's products: where all lie within |z| <= 1, without the far form.
+// Scores in log2 of a warp's products: where all that count lie within |z| <= 1,
+// without the far form.  in: bits of those that their rows see.  (The forms differ
+// in a score's last bits: what nobody sees has no say in them.)
 template <int N>
-__device__ __forceinline__ void cap_scores(const BiasArgs& b, float (&x)[N]) {
+__device__ __forceinline__ void cap_scores(const BiasArgs& b, uint32_t in, float (&x)[N]) {
+  static_assert(N <= 32, "a bit a product");
   float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
+  for (int i = 0; i < N; ++i) top = fmaxf(top, in >> i & 1u ? fabsf(x[i]) : 0.f);
   if (__any_sync(0xffffffffu, top * fabsf(b.to_z) > 1.f)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = capped(b, x[i]);
