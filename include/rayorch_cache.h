@@ -327,7 +327,8 @@ ro_status ro_cache_copy(ro_ctx* ctx, const ro_cache* cache, const ro_moves* move
  * The token drawn is the first of those that stay, by index, whose running sum
  * of w passes u times the sum over all of them.  temperature 0 draws the
  * largest logit, the first of equal ones.  A logit that is -inf or NaN is never
- * drawn and does not count.
+ * drawn and does not count; differences of logits past 32 bits' range are
+ * infinite.
  *   d_logits   [n_rows][vocab] of `dtype` (bf16, f16 or f32), row_stride
  *              elements from row to row, any alignment to the element.
  *   how        settings of each row, NULL (also in it): the neutral ones.

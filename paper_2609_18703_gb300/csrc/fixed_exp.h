@@ -84,16 +84,28 @@ RO_HD float bits_float(int32_t i) {
 }
 
 struct ExpScale {
-  float hi, lo;   // log2(e) / T in two floats
+  float hi, lo;   // log2(e) / (up T) in two floats
+  // a power of two that keeps them, and what they multiply, normal numbers: 1 for
+  // temperatures from 2^-64 to 2^64
+  float up = 1.f;
 };
+RO_HD ExpScale exp_scale(float T) {
+  ExpScale c;
+  c.up = T < 0x1p-64f ? 0x1p64f : T > 0x1p64f ? 0x1p-64f : 1.f;
+  const float t = RO_MUL(T, c.up);
+  c.hi = 1.44269502162933349609f / t;   // the quotient, and its remainder's
+  c.lo = RO_ADD(RO_FMA(-c.hi, t, 1.44269502162933349609f), 1.92596299112661746887e-8f) / t;
+  return c;
+}
 struct Pair32 {
   float hi, lo;
 };
 // z, x <= top, neither a NaN; its higher part is 64 or more (or NaN) for weights of 0.
 RO_HD Pair32 exp_argument(float top, float x, ExpScale c) {
-  const float d = x == top ? 0.f : RO_ADD(top, -x);
-  const float v = RO_ADD(d, -top);               // what d's rounding lost, exactly:
-  const float lost = x == top ? 0.f : RO_ADD(RO_ADD(top, -RO_ADD(d, -v)), RO_ADD(-x, -v));
+  const float apart = x == top ? 0.f : RO_ADD(top, -x);
+  const float v = RO_ADD(apart, -top);           // what its rounding lost, exactly:
+  const float rest = x == top ? 0.f : RO_ADD(RO_ADD(top, -RO_ADD(apart, -v)), RO_ADD(-x, -v));
+  const float d = RO_MUL(apart, c.up), lost = RO_MUL(rest, c.up);
   Pair32 z;
   z.hi = d == 0.f ? 0.f : RO_MUL(d, c.hi);
   z.lo = d == 0.f ? 0.f : RO_FMA(lost, c.hi, RO_FMA(d, c.lo, RO_FMA(d, c.hi, -z.hi)));

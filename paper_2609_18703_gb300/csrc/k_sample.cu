@@ -432,9 +432,11 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   }
 
   // ---- weights ----
-  // log2(e) / T in two floats: the quotient, and its remainder's
-  const float c = 1.44269502162933349609f / T_;
-  const ExpScale scale = {c, c < 3.0e38f ? (fmaf(-c, T_, 1.44269502162933349609f) + 1.92596299112661746887e-8f) / T_ : 0.f};
+  const ExpScale scale = exp_scale(T_);
+  // Of weights in 32 bits.  Below T = 5e-39 it is too small a factor: they are then
+  // bounds of the weights, and decide nothing.
+  const float rough_scale = fminf(1.44269504f / T_, 3.0e38f);
+  const bool rough_holds = rough_scale < 3.0e38f;
   const float my_hi = EXP_HI[lane], my_lo = EXP_LO[lane];   // the table, an entry a lane
   // Bits of a weight behind the point: as many as keep the sum below 2^63, where
   // it is known roughly, and so few that none is lost (many light tokens together count).
@@ -480,7 +482,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
   // in 32 bits, of a logit that is no NaN
   auto rough_weight = [&](float y) -> float {
-    const float z = (top - y) * scale.hi;
+    const float z = (top - y) * rough_scale;
     return z < 64.f ? ex2(-z) : 0.f;
   };
   auto key_of = [&](float y) -> uint32_t { return y == y ? logit_key(y) : KEY_NONE; };   // (a NaN is never drawn)
@@ -713,7 +715,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         __syncthreads();
         sum = 0.f;
         for (uint32_t w = 0; w < SM_WARPS; ++w) sum += s.warp_rough[w];
-        short_of = sum * (1.f + SM_SLACK) < rough_total() * top_p * (1.f - SM_SLACK);
+        short_of = !rough_holds || sum * (1.f + SM_SLACK) < rough_total() * top_p * (1.f - SM_SLACK);
       }
       if (listed > 0 && listed <= SM_LIST && !short_of) {
         const uint64_t list_mass = sort_list(listed);
@@ -739,7 +741,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
           }
           stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), first)));
           way = WAY_DONE;
-        } else if (!by_k) {
+        } else if (!by_k && rough_holds) {
           const float rough = rough_total() * top_p * (float)(1ull << bits);
           const uint32_t lo = max(1u, count_below((uint64_t)(rough * (1.f - SM_SLACK)), listed));
           const uint32_t hi = max(1u, count_below((uint64_t)(rough * (1.f + SM_SLACK)) + 2, listed));
