@@ -238,7 +238,8 @@ ro_status ro_cache_attend_biased(ro_ctx* ctx, const ro_cache* cache, const uint6
  * page how many entries of page lists name it (and whatever else holds it); a
  * page with 0 is free.  Shared pages are full ones: a page that a sequence still
  * writes is its own.  Outputs share no memory with inputs or one another but
- * where it is said (RO_E_INVAL).
+ * where it is said (RO_E_INVAL; recorded where they lie behind the first entry of
+ * a page list whose length only the GPU knows).
  */
 /* Copies of pages: d_n[0] of them (at most cap), copy i the first d_slots[i]
  * slots of pool page d_from[i] to page d_to[i]. */

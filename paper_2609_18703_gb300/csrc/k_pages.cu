@@ -90,6 +90,19 @@ __device__ __forceinline__ uint32_t count_free(const PagesArgs& a) {
   return n;
 }
 
+// An output that shares memory with the page list, whose length the host does not know.
+__device__ __forceinline__ void record_shared(const PagesArgs& a, uint64_t n, const void* p, uint64_t count) {
+  const char *list = (const char*)a.c.pages, *out = (const char*)p;
+  if (out < list + n * 4 && list < out + count * 4) record(a.err, ERR_INVAL);
+}
+__device__ __forceinline__ void record_shared_moves(const PagesArgs& a, uint64_t n) {
+  record_shared(a, n, a.m.from, a.m.cap);
+  record_shared(a, n, a.m.to, a.m.cap);
+  record_shared(a, n, a.m.slots, a.m.cap);
+  record_shared(a, n, a.m.n, 1);
+  record_shared(a, n, a.refs_out, a.c.n_pages);
+}
+
 // ---- fork --------------------------------------------------------------------------------
 // An entry of the new lists: where it lies in its continuation, what the parent holds.
 struct ForkEntry {
@@ -199,7 +212,12 @@ __device__ __forceinline__ void fork_list(const PagesArgs& a) {
       record(a.err, ERR_INVAL);
     }
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.m.n = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *a.m.n = 0;
+    record_shared_moves(a, n);
+    record_shared(a, n, a.dst_pages, a.n_dst);
+    record_shared(a, n, a.len_out, a.n_children);
+  }
 }
 
 __device__ __forceinline__ void fork_assign(const PagesArgs& a) {
@@ -311,7 +329,12 @@ __device__ __forceinline__ void compact_assign(const PagesArgs& a) {
     a.refs_out[from] = 0;
   }
   const uint64_t n = a.c.page_base[a.c.n_seqs];
-  if (n > a.n_list && t == 0) record(a.err, ERR_CAPACITY);
+  if (t == 0) {
+    if (n > a.n_list) record(a.err, ERR_CAPACITY);
+    record_shared_moves(a, n);
+    record_shared(a, n, a.n_used, 1);
+    if (a.pages_out != a.c.pages) record_shared(a, n, a.pages_out, a.n_list);
+  }
   for (uint64_t e = t; e < n && e < a.n_list; e += step) {
     uint32_t page = a.c.pages[e];
     if (page >= a.c.n_pages) {

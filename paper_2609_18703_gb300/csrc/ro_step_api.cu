@@ -162,7 +162,8 @@ bool touch(const void* p, uint64_t p_bytes, const void* q, uint64_t q_bytes) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return p_bytes && q_bytes && a < b + q_bytes && b < a + p_bytes;
 }
-// Whether an output shares bytes with an input or with another output.
+// Whether an output shares bytes with an input or with another output.  (An input
+// that changes in place is its output.)
 struct Bytes {
   const void* p;
   uint64_t n;
@@ -547,11 +548,12 @@ ro_status ro_cache_fork(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_le
   if (touch(d_len, (uint64_t)cache->n_seqs * 4, d_len_out, n_children * 4) || touch(cache->d_pages, 4, d_dst_pages, n_dst * 4))
     return c.refuse(RO_E_INVAL, "%s: the continuations' lengths and pages go to arrays of their own", fn);
   const uint64_t room = moves->cap * 4, starts = ((uint64_t)cache->n_seqs + 1) * 8;
-  if (clash({{d_dst_pages, n_dst * 4}, {d_len_out, n_children * 4}, {d_refs_out, d_refs_out == d_refs ? 0 : pool},
+  // (of the page list only the GPU knows the length: the kernel looks at the rest)
+  if (clash({{d_dst_pages, n_dst * 4}, {d_len_out, n_children * 4}, {d_refs_out, pool},
              {moves->d_from, room}, {moves->d_to, room}, {moves->d_slots, room}, {moves->d_n, 4}},
             {{d_len, (uint64_t)cache->n_seqs * 4}, {d_child_base, starts}, {d_child_parent, n_children * 4},
-             {d_dst_base, n_children ? (n_children + 1) * 8 : 0}, {d_dst_seq, n_dst * 4}, {d_refs, pool},
-             {cache->d_page_base, starts}, {cache->d_pages, 4}}))
+             {d_dst_base, n_children ? (n_children + 1) * 8 : 0}, {d_dst_seq, n_dst * 4},
+             {d_refs, d_refs == d_refs_out ? 0 : pool}, {cache->d_page_base, starts}, {cache->d_pages, 4}}))
     return c.refuse(RO_E_INVAL, "%s: outputs share memory with inputs or one another", fn);
   RO_TRY(c.begin());
   a.c = paged(cache);
@@ -590,12 +592,13 @@ ro_status ro_cache_compact(ro_ctx* ctx, const ro_cache* cache, uint32_t* d_pages
   const uint64_t pool = (uint64_t)cache->n_pages * sizeof(uint32_t);
   if (d_refs_out != d_refs && touch(d_refs, pool, d_refs_out, pool))
     return c.refuse(RO_E_INVAL, "%s: counts change in place or in another array", fn);
-  if (d_pages_out != cache->d_pages && touch(cache->d_pages, n_list * 4, d_pages_out, n_list * 4))
-    return c.refuse(RO_E_INVAL, "%s: lists change in place or in another array", fn);
+  // (of a list that does not change in place only the GPU knows the length: the kernel looks at the rest)
+  const bool in_place = n_list && d_pages_out == cache->d_pages;
   const uint64_t room = moves->cap * 4;
-  if (clash({{d_pages_out, d_pages_out == cache->d_pages ? 0 : n_list * 4}, {d_refs_out, d_refs_out == d_refs ? 0 : pool},
+  if (clash({{d_pages_out, n_list * 4}, {d_refs_out, pool},
              {d_n_used, 4}, {moves->d_from, room}, {moves->d_to, room}, {moves->d_slots, room}, {moves->d_n, 4}},
-            {{d_refs, pool}, {cache->d_page_base, ((uint64_t)cache->n_seqs + 1) * 8}, {cache->d_pages, 4}}))
+            {{d_refs, d_refs == d_refs_out ? 0 : pool}, {cache->d_page_base, ((uint64_t)cache->n_seqs + 1) * 8},
+             {cache->d_pages, in_place ? 0ull : 4ull}}))
     return c.refuse(RO_E_INVAL, "%s: outputs share memory with inputs or one another", fn);
   RO_TRY(c.begin());
   a.c = paged(cache);
