@@ -217,7 +217,7 @@ ro_status ro_cache_evict(ro_ctx* ctx, const ro_cache* cache, const uint32_t* d_l
  * window == 0, j > a - window, or j < first + sinks.  Everything else is
  * ro_cache_attend's: arguments, outputs, empty rows (out 0, lse -inf), unseen
  * slots never used, equal bits for equal calls.
- * cap must be 0 or finite, at least 1e-6, with scale / cap at most 1e30.
+ * cap must be 0 or from 1e-6 to 1e30, with |scale / cap| 0 or from 1e-37 to 1e30.
  */
 typedef struct {
   float cap;                    /* 0: none */

@@ -199,8 +199,11 @@ ro_status attend(const char* fn, StepCall& c, const ro_cache* cache, const uint6
   if (!aligned(d_out, 16) || out_tok % 8 || out_head % 8)
     return c.refuse(RO_E_INVAL, "%s: the output wants a 16-byte pointer and strides of 8 elements", fn);
   if (bias) {
-    if (!(bias->cap == 0.f || (bias->cap >= 1e-6f && std::isfinite(bias->cap) && std::fabs(scale / bias->cap) <= 1e30f)))
-      return c.refuse(RO_E_INVAL, "%s: cap must be 0 or finite, at least 1e-6, and scale / cap at most 1e30", fn);
+    // (the cap in log2 and scale / cap are normal numbers then, or 0)
+    const float ratio = std::fabs(scale / bias->cap);
+    if (!(bias->cap == 0.f ||
+          (bias->cap >= 1e-6f && bias->cap <= 1e30f && (scale == 0.f || (ratio >= 1e-37f && ratio <= 1e30f)))))
+      return c.refuse(RO_E_INVAL, "%s: cap must be 0 or from 1e-6 to 1e30, and scale / cap 0 or from 1e-37 to 1e30", fn);
     if (!aligned(bias->d_slope, 4) || !aligned(bias->d_first, 4) || !aligned(bias->d_until, 4))
       return c.refuse(RO_E_INVAL, "%s: a pointer off its type's alignment", fn);
   }
