@@ -83,6 +83,7 @@ struct TileItem {
   uint32_t c0, n;            // the run's slot tiles
   uint32_t run, n_runs;
   uint32_t last;             // no work: the end
+  uint32_t again;            // SPLIT 2: for the second time; the first time's place, from 1 on
 };
 // A pair of row tiles for the join: its first token, its tokens, its runs.
 struct JoinItem {
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
   __shared__ uint64_t s_bar[2 + 2 * S::SLOTS + 10 + 2 * AT_ITEMS + 1 + 2];
   __shared__ float s_pair[SPLIT == 1 ? 1 : 2 * AT_ROWS];   // from one of a row's threads to the other
   __shared__ TileItem<B> s_item[AT_ITEMS];
-  __shared__ uint32_t s_tmem, s_gave_up;
+  __shared__ uint32_t s_tmem, s_gave_up, s_doubt[AT_ITEMS];
   wait_predecessor();
   const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t G = a.r.group;
@@ -220,6 +221,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     for (uint32_t i = 0; i < AT_ITEMS; ++i) {
       bar_init(b_item + 8 * i, 1);
       bar_init(b_item_free + 8 * i, 8 * SPLIT + 2);   // the warps of softmax, loads, products
+      s_doubt[i] = 0;
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -249,6 +251,31 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       // items are in falling order of work where that is known.
       const uint32_t items = a.tiles * a.c.n_heads * a.max_chunks;
       uint32_t k = 0;
+      // hands the k-th item over, and comes back when the next one is wanted
+      auto hand_over = [&](const TileItem<B>& it) {
+        const uint32_t slot = k % AT_ITEMS;
+        if (k >= AT_ITEMS) bar_wait_idle(b_item_free + 8 * slot, (k / AT_ITEMS - 1) & 1, &s_gave_up, a.err);
+        __syncwarp();
+        if (lane == 0) s_item[slot] = it;
+        __syncwarp();
+        if (lane == 0) bar_arrive(b_item + 8 * slot);
+        if (!it.last) bar_wait_idle(b_want, k & 1, &s_gave_up, a.err);
+        ++k;
+      };
+      // SPLIT 2: the p-th item once its output is written, and it free: handed over
+      // again if it is to be computed for a second time
+      auto look_back = [&](uint32_t p) {
+        const uint32_t slot = p % AT_ITEMS;
+        bar_wait(b_item_free + 8 * slot, (p / AT_ITEMS) & 1, &s_gave_up, a.err);
+        const uint32_t doubt = *(volatile uint32_t*)&s_doubt[slot];
+        TileItem<B> it = s_item[slot];
+        __syncwarp();
+        if (doubt == 0u || has_given_up(&s_gave_up)) return;
+        if (lane == 0) s_doubt[slot] = 0u;
+        it.again = 1 + slot;
+        hand_over(it);
+      };
+      uint32_t looked = 0;       // items whose first time is known to do, or handed over again
       for (uint32_t id = blockIdx.x;;) {
         TileItem<B> it = {};
         it.last = id >= items;
@@ -299,13 +326,10 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
         if (!it.last && a.max_chunks > 1 && it.run == 0 && lane == 0)   // for the join of the runs
           ((JoinItem*)a.join)[it.unit] = {it.tok0 + it.i0, some ? it.i1 - it.i0 : 0u, some ? it.n_runs : 0u};
         if (some) {
-          const uint32_t slot = k % AT_ITEMS;
-          if (k >= AT_ITEMS) bar_wait_idle(b_item_free + 8 * slot, (k / AT_ITEMS - 1) & 1, &s_gave_up, a.err);
-          if (lane == 0) s_item[slot] = it;
-          __syncwarp();
-          if (lane == 0) bar_arrive(b_item + 8 * slot);
-          if (!it.last) bar_wait_idle(b_want, k & 1, &s_gave_up, a.err);
-          ++k;
+          // (all items before the end; else those whose places are to be taken)
+          if constexpr (SPLIT == 2)
+            for (; looked < k && (it.last || looked + AT_ITEMS <= k) && !has_given_up(&s_gave_up); ++looked) look_back(looked);
+          hand_over(it);
         }
         if (it.last || has_given_up(&s_gave_up)) break;
         if (lane == 0) id = gridDim.x + atomicAdd(a.counter, 1u);
@@ -478,11 +502,13 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     bar_wait(b_pair + 8 * w, meets++ & 1, &s_gave_up, a.err);
   };
   uint32_t tiles = 0, vslot = 1, vpar = 0, done = 0;       // tiles so far; the ring's place of V; items with slots so far
+  uint32_t sums = 0;                                       // SPLIT 2: of the last two items' weights, in log2, 16 bits a place
+  static_assert(AT_ITEMS == 2, "a sum a place");
   for (uint32_t k = 0;; ++k) {
     bar_wait(b_item + 8 * (k % AT_ITEMS), (k / AT_ITEMS) & 1, &s_gave_up, a.err);
     const TileItem<B>& it = s_item[k % AT_ITEMS];
     if (it.last || has_given_up(&s_gave_up)) break;
-    const uint32_t n = it.n, c0 = it.c0, i1 = it.i1, n_runs = it.n_runs;
+    const uint32_t n = it.n, c0 = it.c0, i0 = it.i0, i1 = it.i1;
     const Tiles slots(it.span, g.box);
     const uint32_t j0 = it.i0 + w * g.toks, j1 = min(i1, j0 + g.toks);   // the row tile's tokens
     const bool live = j0 < i1;
@@ -521,19 +547,34 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       all_from = all_from > c0 ? all_from - c0 : 0;
       all_to = all_to > c0 ? all_to - c0 : 0;
     }
-    const uint64_t out_at = (it.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
-    const uint64_t lse_at = (it.tok0 + tok) * a.n_q_heads + head;
-    const uint32_t unit = it.unit, run = it.run, i0 = it.i0;
+    // where its results go; SPLIT 2, short of registers, looks it up at the end and
+    // frees the item then
+    uint64_t out_at, lse_at;
+    uint32_t unit, run, n_runs;
+    auto place = [&] {
+      out_at = (it.tok0 + tok) * a.out_tok + (uint64_t)head * a.out_head;
+      lse_at = (it.tok0 + tok) * a.n_q_heads + head;
+      unit = it.unit, run = it.run, n_runs = it.n_runs;
+    };
+    auto release = [&] {
+      __syncwarp();
+      if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
+    };
     const bool sees_some = B ? see.some() : mine;
     // (rows that see nothing have no say in the others' maximum, and are set to nothing at the end)
     const bool voter = mine && sees_some;
-    // SPLIT 2: the same for every row, 2^40 below what the cap lets weights be
+    // SPLIT 2: the same for every row, so low that small values keep their bits:
+    // weights are 1 (2^-17 under the largest cap) or more.  Sums that leave 32 bits
+    // show; the item is then computed again, each row relative to what its weights
+    // added up to (or to the cap).
     constexpr bool held = SPLIT == 2;
-    const float base = fmaxf(a.b.cap_log2 - 40.f, 0.f);
-    __syncwarp();
-    if (lane == 0) bar_arrive(b_item_free + 8 * (k % AT_ITEMS));
+    if constexpr (SPLIT == 1) {
+      place();
+      release();
+    }
     const bool turned = B && (SPLIT == 2 || a.b.cap_log2 != 0.f || a.b.slope);   // more than scaled
-    float m = held ? base : -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f;
+    if constexpr (held) m = it.again == 0u ? fmaxf(-a.b.cap_log2, -56.f) : (float)(int16_t)(sums >> 16 * (it.again - 1));
     for (uint32_t t = 0; t < n; ++t, ++tiles) {
       bar_wait(b_s + 8 * w, tiles & 1, &s_gave_up, a.err);
       tc_fence_after();
@@ -627,7 +668,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) tc_ld32(ts + (k0 + i) * 32, y + i * 32);
         tc_wait_ld(y);
-        bias_scores(a.b, scale, slope, held ? base : 0.f, ahead - 32.f * k0, a.b.until != nullptr, voter, all,
+        bias_scores(a.b, scale, slope, held ? m : 0.f, ahead - 32.f * k0, a.b.until != nullptr, voter, all,
                     [&](int k) { return seen(k0 + k); }, y);
         if (!all) {
           uint32_t in[PARTS];
@@ -729,6 +770,18 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
 #pragma unroll
       for (int i = 0; i < OUT; ++i) o[i] = 0u;
     }
+    if constexpr (SPLIT == 2) place();
+    uint32_t sum_at = 0;                                   // SPLIT 2: the weights' sum, a power of two
+    if constexpr (held) {
+      const bool number = l > 0.f && l < 0x1p126f;
+      sum_at = number ? __float_as_uint(l) >> 23 : 127u;
+      const int sum = number ? (int)m + (int)sum_at - 127 : (int)a.b.cap_log2;
+      sums = k % AT_ITEMS == 0 ? (sums & 0xFFFF0000u) | (sum & 0xFFFF) : (sums & 0xFFFFu) | (uint32_t)sum << 16;
+    }
+    // whether a row's results are no numbers, which a second time may make of them
+    auto doubt = [&](bool number) {
+      if (__any_sync(0xffffffffu, voter && !number && it.again == 0u) && lane == 0) s_doubt[k % AT_ITEMS] = 1u;
+    };
     if constexpr (B)
       if (!sees_some) {
         m = -INFINITY;
@@ -744,6 +797,19 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     float2* ml = (float2*)(a.partial + (uint64_t)a.pairs * a.max_chunks * STEP * DP) +
                  (uint64_t)unit * a.max_chunks * STEP + prow;
     if (n_runs > 1) {   // joined by attend_join_kernel
+      if constexpr (held) {   // relative to the weights' sum, as runs with a maximum are
+        const float f = __uint_as_float((254u - sum_at) << 23);
+        m = l > 0.f ? m + (float)((int)sum_at - 127) : -INFINITY;
+        l *= f;
+        float none = l * 0.f;
+#pragma unroll
+        for (int i = 0; i < OUT; ++i) {
+          const float x = __uint_as_float(o[i]) * f;
+          o[i] = __float_as_uint(x);
+          none = fmaf(x, 0.f, none);
+        }
+        doubt(none == 0.f);
+      }
       if (mine) {
 #pragma unroll
         for (int i = 0; i < OUT / 4; ++i)
@@ -752,6 +818,7 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
                              __uint_as_float(o[4 * i + 3])));
         if (h == 0) __stcg(ml + run * STEP, make_float2(m, l));
       }
+      if constexpr (SPLIT == 2) release();
       continue;
     }
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
@@ -760,6 +827,12 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
     uint32_t y[OUT / 2];
 #pragma unroll
     for (int i = 0; i < OUT / 2; ++i) y[i] = pack2<T>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+    if constexpr (held) {
+      __nv_bfloat162 none = __float2bfloat162_rn(l * 0.f);
+#pragma unroll
+      for (int i = 0; i < OUT / 2; ++i) none = __hfma2(*reinterpret_cast<__nv_bfloat162*>(&y[i]), __float2bfloat162_rn(0.f), none);
+      doubt(__low2float(none) == 0.f && __high2float(none) == 0.f);
+    }
     if (g.wide) {
       // Each thread has a row; the threads of a group of UNITS turn theirs into
       // units of 32 bytes side by side, so that a store writes whole rows (a tile's
@@ -793,8 +866,8 @@ __global__ void __launch_bounds__(AT_THREADS<SPLIT>, 1) attend_tiles_kernel(cons
       for (int i = 0; i < OUT / 2; i += 4)
         if ((uint32_t)i * 2 < left) *(uint4*)(out + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
     }
-    if (!mine) continue;
-    if (a.lse && h == 0) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
+    if (mine && a.lse && h == 0) a.lse[lse_at] = row_lse<T, AT_SLACK<T>>(m, l);
+    if constexpr (SPLIT == 2) release();
   }
   __syncwarp();
   tc_fence_before();
@@ -855,12 +928,13 @@ template <typename T, int DP>
 static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   const uint64_t items = (uint64_t)g.a.tiles * g.a.c.n_heads * g.a.max_chunks;
   const unsigned ctas = (unsigned)std::min<uint64_t>(items, (uint64_t)sms);
-  // Scores under a cap of at most 2^73 need no running maximum where the weights
-  // have the exponents of 32 bits: with 2^(cap - 40) (or 1) for all rows they lie
-  // between 2^-106 and 2^40, so sums of 2^20 values up to 2^67 stay in range, and
-  // so do values down to 2^-20 where every score lies at -cap.  Then two threads
-  // take a row (605 us against 623 for chunks under a cap of 30, 700 against 960
-  // for one of 8); with a maximum to agree on they lose more.
+  // Scores under a cap of at most 73 in log2 (50.6) need no running maximum where
+  // the weights have the exponents of 32 bits: with 2^-cap (or 2^-56) for all rows
+  // they lie between 2^-17 and 2^129.  Then two threads take a row (chunks under a cap
+  // of 2, 8, 30 or 50: 1,120, 677, 579 and 579 us against 1,540, 952, 634 and 634); with a
+  // maximum to agree on they lose more.  Pairs of row tiles whose sums such weights
+  // take out of range, by scores beyond 40 or values beyond 2^30 or so, are computed
+  // twice.
   auto kernel = g.a.biased ? attend_tiles_kernel<T, DP, true, 1> : attend_tiles_kernel<T, DP, false, 1>;
   int threads = AT_THREADS<1>;
   if constexpr (std::is_same_v<T, __nv_bfloat16>)
