@@ -6,8 +6,9 @@
 //   first few equal to it.  The token is the first kept one, by index, whose
 //   running sum of weights passes u times the sum of all kept.
 //
-// Weights and sums are 64-bit fixed point (fixed_exp.h), so no sum depends on
-// its order and tokens do not depend on how a row is split.
+// Weights are 64-bit fixed point (fixed_exp.h), the same wherever they are computed,
+// and their sums whole numbers of up to 69 bits, so no sum depends on its order and
+// tokens do not depend on how a row is split.
 //
 // Where the settings leave few tokens, those are found without a threshold being
 // known: among the threads' largest logits the want-th largest has at least `want`
@@ -94,20 +95,29 @@ __device__ __forceinline__ V cluster_read(const V* p, uint32_t rank) {
     return (V)v;
   }
 }
-// x * f as a whole number, rounded down or up; 0 <= f < 1, x < 2^63.  (f is a
+// A row's sum of weights: of up to 2^19, each at most 2^50.  (A warp's run of a
+// row's slice, at most 2^13 tokens, adds up to 64 bits.)
+using Sum = unsigned __int128;
+__device__ __forceinline__ float sum_float(Sum x) { return fmaf((float)(uint64_t)(x >> 64), 0x1p64f, (float)(uint64_t)x); }
+// x * f as a whole number, rounded down or up; 0 <= f < 1, x < 2^70.  (f is a
 // whole number of at most 24 bits over a power of two.)
-__device__ __forceinline__ uint64_t scaled(uint64_t x, float f, bool up) {
+__device__ __forceinline__ Sum scaled(Sum x, float f, bool up) {
   if (f == 0.f || x == 0) return 0;
   int e;
   const uint64_t m = (uint64_t)(frexpf(f, &e) * 16777216.f);   // f = m 2^(e - 24)
   const int shift = 24 - e;                                      // at least 24
   if (shift >= 96) return up ? 1 : 0;
-  const unsigned __int128 y = (unsigned __int128)x * m;
-  return (uint64_t)((y + (up ? ((unsigned __int128)1 << shift) - 1 : 0)) >> shift);
+  return (x * m + (up ? ((Sum)1 << shift) - 1 : 0)) >> shift;
 }
 __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+__device__ __forceinline__ Sum warp_sum(Sum v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1)
+    v += (Sum)__shfl_xor_sync(0xffffffffu, (uint32_t)(v >> 64), d) << 64 | __shfl_xor_sync(0xffffffffu, (uint64_t)v, d);
   return v;
 }
 
@@ -222,8 +232,9 @@ struct __align__(16) SampleShared {
   unsigned long long warp_mass[SM_WARPS], warp_above[SM_WARPS];
   uint32_t warp_ties[SM_WARPS], warp_count[SM_WARPS], warp_above_count[SM_WARPS];
   uint32_t border_ties[SM_WARPS];          // tokens on top-p's border in the warps' runs
-  unsigned long long scan[SM_WARPS];
-  unsigned long long found_left;
+  unsigned long long scan[SM_WARPS], scan_high[SM_WARPS];
+  Sum left;                                // of what is wanted, on the border found
+  unsigned long long list_sum;             // of the listed ones' weights, as far as they count
   uint32_t found;
   uint32_t best, least;                    // keys of the largest logit, and of the threads' smallest maximum
   uint32_t place;                          // of the largest logit, the first of equal ones
@@ -234,7 +245,8 @@ struct __align__(16) SampleShared {
   uint4 edge[2];                           // a row's first and last block, where it does not fill them
   struct {
     uint32_t first, last;
-    uint64_t at, ties;                     // weight and tokens on the threshold before it
+    uint64_t ties;                         // tokens on the threshold and weight before it
+    Sum at;
   } run;
   float rough, warp_rough[SM_WARPS];       // sums of weights in 32 bits
   uint8_t flags[SM_WARPS][32 * SM_PARTS];  // parts of a warp's threads that hold a candidate
@@ -438,10 +450,9 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   const float rough_scale = fminf(1.44269504f / T_, 3.0e38f);
   const bool rough_holds = rough_scale < 3.0e38f;
   const float my_hi = EXP_HI[lane], my_lo = EXP_LO[lane];   // the table, an entry a lane
-  // Bits of a weight behind the point: as many as keep the sum below 2^63, where
-  // it is known roughly, and so few that none is lost (many light tokens together count).
-  uint32_t bits = WEIGHT_BITS;
-  auto bits_for = [&](float sum) { bits = min(WEIGHT_BITS, 61u - (uint32_t)ilogbf(fmaxf(sum, 1.f))); };
+  // Every weight has the same bits behind the point, whatever the row's sum and
+  // whoever takes it, so a draw does not depend on how the row is split.
+  constexpr float ONE = (float)(1ull << WEIGHT_BITS);
   // Of a whole warp's logits, some a lane; 0 where !in.  (Up to four together:
   // one after another each would wait for its chain of some 60 instructions.)
   auto weigh = [&](auto& y, auto& in, auto& w) {
@@ -457,7 +468,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       if (!__any_sync(0xffffffffu, some)) continue;
 #pragma unroll
       for (int k = 0; k < G; ++k) {
-        const Weight v = exp_weight(exp_argument(top, in[g + k] ? y[g + k] : top, scale), (float)(1ull << bits), [&](uint32_t j) {
+        const Weight v = exp_weight(exp_argument(top, in[g + k] ? y[g + k] : top, scale), ONE, [&](uint32_t j) {
           return Pair32{__shfl_sync(0xffffffffu, my_hi, j), __shfl_sync(0xffffffffu, my_lo, j)};
         });
         if (in[g + k]) w[g + k] = v;
@@ -469,7 +480,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     const bool ins[1] = {in};
     Weight w[1];
     weigh(ys, ins, w);
-    return whole(w[0], bits);
+    return whole(w[0], WEIGHT_BITS);
   };
   auto total_of = [&](const auto& w) -> uint64_t {   // of a few
     Weight m = {0, 0};
@@ -478,7 +489,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       m.hi += w[k].hi;
       m.lo += w[k].lo;
     }
-    return whole(m, bits);
+    return whole(m, WEIGHT_BITS);
   };
   // in 32 bits, of a logit that is no NaN
   auto rough_weight = [&](float y) -> float {
@@ -534,10 +545,11 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     for (uint32_t r = 0; r < nc; ++r) sum += __shfl_sync(0xffffffffu, part, r);
     return sum;
   };
-  auto with_log = [&](uint32_t token, float y, uint64_t total, uint32_t kept) {
+  auto with_log = [&](uint32_t token, float y, Sum total, uint32_t kept) {
     const Pair32 z = exp_argument(top, y, scale);
     const double less = ((double)z.hi + (double)z.lo) * 0.69314718055994530942;
-    finish(token, -(float)(less + log((double)total * (1.0 / (double)(1ull << bits)))), kept);
+    const double sum = (double)(uint32_t)(total >> 64) * 0x1p64 + (double)(uint64_t)total;
+    finish(token, -(float)(less + log(sum * (1.0 / (double)(1ull << WEIGHT_BITS)))), kept);
   };
 
   // ---- thresholds ----
@@ -600,7 +612,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     weigh(ys, ins, w);
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
-      own[j] = whole(w[j], bits);
+      own[j] = whole(w[j], WEIGHT_BITS);
       if (ins[j]) weights[2 * tid + j] = own[j];
     }
     const uint64_t sum = own[0] + own[1];
@@ -699,7 +711,6 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       if (tid == 0) cluster_write(&s.counts[rank], 0, s.listed);
     }
     sync();
-    if (by_p && !by_k) bits_for(rough_total());   // (the listed ones' sum is below 2^60 anyway)
     // ---- the first CTA's ----
     const uint32_t listed = rank == 0 ? all_listed(true) : 0;
     uint32_t stay = 0;
@@ -735,14 +746,14 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         } else if (all_of_k || (cut == SM_COARSE && !with_min)) {   // the sum is the listed ones'
           uint64_t sum = list_mass;
           if (first < listed) {
-            if (tid == first / 2) s.found_left = ahead[first & 1];
+            if (tid == first / 2) s.list_sum = ahead[first & 1];
             __syncthreads();
-            sum = s.found_left;
+            sum = s.list_sum;
           }
-          stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), first)));
+          stay = min(stay, max(1u, count_below((uint64_t)scaled(sum, top_p, true), first)));
           way = WAY_DONE;
         } else if (!by_k && rough_holds) {
-          const float rough = rough_total() * top_p * (float)(1ull << bits);
+          const float rough = fminf(rough_total() * top_p * ONE, 0x1p62f);   // (more than the listed ones' sum)
           const uint32_t lo = max(1u, count_below((uint64_t)(rough * (1.f - SM_SLACK)), listed));
           const uint32_t hi = max(1u, count_below((uint64_t)(rough * (1.f + SM_SLACK)) + 2, listed));
           if (!whole && hi == listed) {              // tokens that are not listed may stay
@@ -766,7 +777,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     way = s.way;
     if (way == WAY_DONE || (WIDE && way == WAY_MASS)) {
       if (way == WAY_MASS) {   // the border lies within what 32 bits may be off
-        uint64_t sum = 0;
+        uint64_t mine = 0;
         for (uint32_t i = warp * 32; i < n; i += SM_THREADS) {
           const bool have = i + lane < n;
           const uint4 v = have ? block(i + lane) : make_uint4(0, 0, 0, 0);
@@ -779,23 +790,24 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
             in[k] = have && y[k] > -INFINITY;
           }
           weigh(y, in, w);
-          sum += total_of(w);
+          mine += total_of(w);
         }
-        sum = warp_sum64(sum);
-        if (lane == 0) s.warp_mass[warp] = sum;
+        mine = warp_sum64(mine);
+        if (lane == 0) s.warp_mass[warp] = mine;
         sync();
-        sum = 0;
+        Sum sum = 0;
         for (uint32_t q = lane; q < nc * SM_WARPS; q += 32)
           sum += nc > 1 ? cluster_read(&s.warp_mass[q % SM_WARPS], q / SM_WARPS) : s.warp_mass[q % SM_WARPS];
-        sum = warp_sum64(sum);
-        if (rank == 0) stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), listed)));
+        sum = scaled(warp_sum(sum), top_p, true);
+        const uint64_t share = sum >> 62 != 0 ? 1ull << 62 : (uint64_t)sum;   // (that is more than the listed ones' sum)
+        if (rank == 0) stay = min(stay, max(1u, count_below(share, listed)));
         sync();
       }
       if (rank == 0) {
         // the sum of those that stay, then where it passes the goal, by index
-        if (2 * tid < stay && stay <= 2 * tid + 2) s.found_left = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
+        if (2 * tid < stay && stay <= 2 * tid + 2) s.list_sum = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
         __syncthreads();
-        const uint64_t total = s.found_left, goal = scaled(total, s.u, false);
+        const uint64_t total = s.list_sum, goal = (uint64_t)scaled(total, s.u, false);
         uint32_t size = 2;
         while (size < stay) size *= 2;
         // indices rise, and each remembers its candidate
@@ -834,12 +846,12 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     return way;
   } else {
   // ---- wide rows ----
-  bits_for((float)a.vocab);
   const uint32_t rounds = (n + SM_THREADS - 1) / SM_THREADS;
   // Finds the key where the tokens above `th`, largest first, reach `want` (in
   // tokens or in weight), which they do: leaves the key and what is still wanted of it.
-  auto select = [&](auto by_mass, uint64_t want, uint64_t* left) -> uint32_t {
+  auto select = [&](auto by_mass, Sum want, Sum* left) -> uint32_t {
     constexpr bool MASS = decltype(by_mass)::value;
+    constexpr int HIGH = 38;   // a bin's weight in two parts: 2^12 of 2^38 a token at most
     uint32_t prefix = 0, mask = 0;
 #pragma unroll 1
     for (int pass = 0; pass < (LOW == 0 ? 3 : 2); ++pass) {
@@ -862,7 +874,10 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
           const bool in = i < n && key > th.key && (key & mask) == prefix;
           if constexpr (MASS) {
             const uint64_t w = weight(y, in);
-            if (in && w) atomicAdd(&s.mass[(key >> shift) & (bins - 1)], (unsigned long long)w);
+            if (in && w) {
+              atomicAdd(&s.mass[(key >> shift) & (bins - 1)], (unsigned long long)w & ((1ull << HIGH) - 1));
+              atomicAdd(&s.count[(key >> shift) & (bins - 1)], (uint32_t)(w >> HIGH));
+            }
           } else {
             if (in) atomicAdd(&s.count[(key >> shift) & (bins - 1)], 1u);
           }
@@ -871,39 +886,50 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       sync();
       // a thread sums its bins over the cluster, largest keys first
       const uint32_t each = max(1u, bins / SM_THREADS);
-      uint64_t mine[SM_BINS / SM_THREADS], sum = 0;
+      uint64_t low[SM_BINS / SM_THREADS], low_sum = 0;
+      uint32_t high[SM_BINS / SM_THREADS], high_sum = 0;   // (tokens, where those count)
 #pragma unroll
       for (uint32_t j = 0; j < SM_BINS / SM_THREADS; ++j) {
-        mine[j] = 0;
+        low[j] = 0;
+        high[j] = 0;
         const uint32_t d = tid * each + j;
         if (j < each && d < bins) {
           const uint32_t bin = bins - 1 - d;
           for (uint32_t q = 0; q < nc; ++q) {
-            if constexpr (MASS)
-              mine[j] += nc > 1 ? cluster_read(&s.mass[bin], q) : s.mass[bin];
-            else
-              mine[j] += nc > 1 ? cluster_read(&s.count[bin], q) : s.count[bin];
+            if constexpr (MASS) low[j] += nc > 1 ? cluster_read(&s.mass[bin], q) : s.mass[bin];
+            high[j] += nc > 1 ? cluster_read(&s.count[bin], q) : s.count[bin];
           }
         }
-        sum += mine[j];
+        low_sum += low[j];
+        high_sum += high[j];
       }
-      const uint64_t inc = warp_incl_scan(sum);
-      if (lane == 31) s.scan[warp] = inc;
+      const uint64_t low_inc = warp_incl_scan(low_sum);
+      const uint32_t high_inc = warp_incl_scan(high_sum);
+      if (lane == 31) {
+        s.scan[warp] = low_inc;
+        s.scan_high[warp] = high_inc;
+      }
       __syncthreads();
-      uint64_t before = inc - sum;
-      for (uint32_t q = 0; q < warp; ++q) before += s.scan[q];
+      uint64_t low_before = low_inc - low_sum, high_before = high_inc - high_sum;
+      for (uint32_t q = 0; q < warp; ++q) {
+        low_before += s.scan[q];
+        high_before += s.scan_high[q];
+      }
+      auto both = [&](uint64_t h, uint64_t l) -> Sum { return MASS ? ((Sum)h << HIGH) + l : (Sum)h; };
+      Sum before = both(high_before, low_before);
 #pragma unroll
       for (uint32_t j = 0; j < SM_BINS / SM_THREADS; ++j) {
-        if (before < want && before + mine[j] >= want) {
+        const Sum upto = before + both(high[j], low[j]);
+        if (before < want && upto >= want) {
           s.found = bins - 1 - (tid * each + j);
-          s.found_left = want - before;
+          s.left = want - before;
         }
-        before += mine[j];
+        before = upto;
       }
       sync();   // every CTA has read the others' bins
       prefix |= s.found << shift;
       mask |= (bins - 1) << shift;
-      want = s.found_left;
+      want = s.left;
       __syncthreads();
     }
     prefix |= (prefix & 0x80000000u) ? 0u : (1u << LOW) - 1u;   // a negative logit's low bits are ones
@@ -913,8 +939,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   // Sums of what passes the threshold: over this warp's run of the slice, then over all before it.
   const uint32_t per = (n + SM_WARPS - 1) / SM_WARPS, i0 = min(n, warp * per), i1 = min(n, i0 + per);
   struct Sums {
-    uint64_t mass, above, before, ties_before;   // of all; of the bins above the border's; before this warp:
-                                                 // weight above the threshold, tokens on it
+    Sum mass, above, before;                     // of all; of the bins above the border's; before this warp:
+    uint64_t ties_before;                        // weight above the threshold, tokens on it
     uint64_t ties, count, above_count;           // on it, above it, in the bins above the border's
     uint64_t own;                                // this warp's weight above it
     uint32_t own_ties;
@@ -948,7 +974,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
             more.hi += w[k].hi;
             more.lo += w[k].lo;
           }
-        up += whole(more, bits);
+        up += whole(more, WEIGHT_BITS);
         up_count += __popc(over);
       }
     }
@@ -984,12 +1010,12 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         t.ties_before += wt;
       }
     }
-    t.mass = warp_sum64(t.mass);
-    t.above = warp_sum64(t.above);
+    t.mass = warp_sum(t.mass);
+    t.above = warp_sum(t.above);
     t.ties = warp_sum64(t.ties);
     t.count = warp_sum64(t.count);
     t.above_count = warp_sum64(t.above_count);
-    t.before = warp_sum64(t.before);
+    t.before = warp_sum(t.before);
     t.ties_before = warp_sum64(t.ties_before);
     sync();   // read by all before it is written again
     return t;
@@ -997,7 +1023,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   auto nothing = [](const uint4&, const bool (&)[E], uint32_t) { return 0u; };
   auto cut_to_k = [&] {
     if (by_k && sums(std::false_type(), nothing).count > top_k) {
-      uint64_t left;
+      Sum left;
       th.key = select(std::false_type(), top_k, &left);
       th.ties = (uint32_t)left;
     }
@@ -1028,7 +1054,6 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       }
       sync();
       const float sum_f = rough_total(), unit = 2147483648.f / sum_f;
-      if (th.ties == 0u) bits_for(sum_f);
       each_block([&](const uint4& v) {
 #pragma unroll
         for (uint32_t k = 0; k < E; ++k) {
@@ -1068,7 +1093,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
           if (q < warp) before += s.scan[q];
           all += s.scan[q];
         }
-        const float ties_f = (float)(tie * th.ties) / (float)(1ull << bits) * unit;
+        const float ties_f = (float)tie * (float)th.ties / ONE * unit;
         const uint64_t want = max((uint64_t)1, (uint64_t)(((float)all + ties_f) * top_p));
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) {
@@ -1097,9 +1122,16 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
       enlist(hits, [&](uint32_t b) { return index + b; });
       return over;
     });
-    const uint64_t want = scaled(t.mass + tie * th.ties, top_p, true);
+    const Sum want = scaled(t.mass + (Sum)tie * th.ties, top_p, true);
+    // how many tokens of weight w, at least 1, it takes to reach x
+    auto reach = [](Sum x, uint64_t w) -> uint32_t {
+      uint32_t n = (uint32_t)(sum_float(x) / (float)w);   // one off at most
+      while ((Sum)w * n < x) ++n;
+      while (n > 0u && (Sum)w * (n - 1u) >= x) --n;
+      return n;
+    };
     if (want > t.mass) {
-      th.ties = (uint32_t)min((want - t.mass + tie - 1) / tie, (uint64_t)th.ties);
+      th.ties = min(reach(want - t.mass, tie), th.ties);
     } else {
       if (rank == 0) {
         Threshold found = {0, 0};
@@ -1107,7 +1139,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         if (border != SM_BINS && want > t.above && listed > 0 && listed <= SM_LIST) {
           const uint64_t all = sort_list(listed);
           if (want <= t.above + all) {
-            const uint32_t n_in = count_below(want - t.above, listed);   // at least 1
+            const uint32_t n_in = count_below((uint64_t)(want - t.above), listed);   // at least 1
             const uint32_t key = (uint32_t)(list[n_in - 1] >> 32);
             const uint32_t on = (2 * tid < n_in && (uint32_t)(list[2 * tid] >> 32) == key) +
                                 (2 * tid + 1 < n_in && (uint32_t)(list[2 * tid + 1] >> 32) == key);
@@ -1159,19 +1191,18 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
             t.ties_before += wt;
           }
         }
-        t.mass = warp_sum64(t.mass);
-        t.before = warp_sum64(t.before);
+        t.mass = warp_sum(t.mass);
+        t.before = warp_sum(t.before);
         t.ties_before = warp_sum64(t.ties_before);
         t.own = s.warp_above[warp];
         t.own_ties = s.border_ties[warp];
         t.ties = found.ties;
         t.count = t.above_count + s.cut;
       } else {             // too many tokens in the bin, or 32 bits named a wrong one
-        uint64_t left;
+        Sum left;
         const uint32_t key = select(std::true_type(), want, &left);
-        const uint64_t w = weight(key_logit(key), true);
         th.key = key;
-        th.ties = (uint32_t)min((left + w - 1) / w, (uint64_t)0xFFFFFFFFu);
+        th.ties = reach(left, weight(key_logit(key), true));
       }
     }
     if (cut.key > th.key || (cut.key == th.key && cut.ties < th.ties)) {
@@ -1184,18 +1215,18 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   if (!summed) t = sums(std::true_type(), nothing);
   const uint64_t tie = weight(key_logit(th.key), th.ties != 0u);
   const uint64_t ties = min((uint64_t)th.ties, t.ties);
-  const uint64_t total = t.mass + tie * ties;
-  const uint64_t goal = scaled(total, s.u, false);   // the first running sum above it
+  const Sum total = t.mass + (Sum)tie * ties;
+  const Sum goal = scaled(total, s.u, false);   // the first running sum above it
   if (total == 0) {   // (the largest logit stays in every row: nothing has to be left unwritten all the same)
     if (rank == 0 && tid == 0) finish(NO_TOKEN, -INFINITY, 0);
     return WAY_DONE;
   }
   uint64_t ties_before = t.ties_before;
-  uint64_t at = t.before + tie * min(ties, ties_before);
-  const uint64_t mine = t.own + tie * (min(ties, ties_before + t.own_ties) - min(ties, ties_before));
+  Sum at = t.before + (Sum)tie * min(ties, ties_before);
+  const Sum mine = t.own + (Sum)tie * (min(ties, ties_before + t.own_ties) - min(ties, ties_before));
   // The warp whose run has it shares the run with the CTA's other warps.
   const bool has = goal >= at && goal < at + mine;
-  if (has && lane == 0) s.run = {i0, i1, at, ties_before};
+  if (has && lane == 0) s.run = {i0, i1, ties_before, at};
   if (!__syncthreads_or(has)) return WAY_DONE;
   const uint32_t r1 = s.run.last, part = (r1 - s.run.first + SM_WARPS - 1) / SM_WARPS;
   const uint32_t j0 = min(r1, s.run.first + warp * part), j1 = min(r1, j0 + part);
@@ -1242,11 +1273,11 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     const uint64_t sum = total_of(w) + tie * (min(ties, rank_on + on) - min(ties, rank_on));
     const uint64_t inc = warp_incl_scan(sum), all = __shfl_sync(0xffffffffu, inc, 31);
     if (goal < at + all) {
-      uint64_t upto = at + inc - sum;
+      Sum upto = at + (inc - sum);
       bool done = !(goal >= upto && goal < upto + sum);
 #pragma unroll
       for (uint32_t k = 0; k < E; ++k) {
-        uint64_t wk = whole(w[k], bits);
+        uint64_t wk = whole(w[k], WEIGHT_BITS);
         if (i + lane < j1 && y[k] == limit) {
           if (rank_on < ties) wk = tie;
           ++rank_on;
