@@ -132,6 +132,7 @@ ro_status ro_cache_append(ro_ctx* ctx, const ro_cache* cache, const uint64_t* d_
 
 /* ------------------------------------------------------------------------
  * ro_cache_attend — attention of new tokens over the cache that holds them.
+ * scale is finite, times log2 e too.
  * n_q_heads is a multiple of the cache's heads; query head g reads cache head
  * g / (n_q_heads / n_heads).  A new token at slot a sees the slots j <= a with
  * window == 0, j > a - window, or j < sinks (a sliding window that counts the

@@ -11,6 +11,7 @@ using namespace ro;
 namespace {
 
 constexpr uint32_t MAX_HEADS = 65535;
+constexpr float LOG2_E = 1.44269504088896340736f;
 constexpr uint64_t MAX_GRID = 0x7FFFFFFFull;
 // Runs whose partial results a call keeps: 1,024 of attend_tiles' 133 KB,
 // 16,384 of attend_few's 8 KB (about 136 MB either way, and the workspace's
@@ -107,7 +108,7 @@ ro_status check_rows(StepCall& c, const char* fn, const ro_cache* k, const uint6
     return c.refuse(RO_E_INVAL, "%s: query heads must be a multiple of the cache's", fn);
   if (!aligned(q, 16) || q_tok % 8 || q_head % 8)
     return c.refuse(RO_E_INVAL, "%s: q wants a 16-byte pointer and strides of 8 elements", fn);
-  if (!std::isfinite(scale)) return c.refuse(RO_E_INVAL, "%s: scale must be finite", fn);
+  if (!std::isfinite(scale * LOG2_E)) return c.refuse(RO_E_INVAL, "%s: scale must be finite, times log2 e too", fn);
   return RO_OK;
 }
 
@@ -145,7 +146,7 @@ RowsArgs rows_of(const uint64_t* tok_base, const uint32_t* len, uint64_t n_token
   // slots are below 2^31: a wider window sees everything
   r.window = window < 0x80000000u ? window : 0u;
   r.sinks = std::min(sinks, 0x7FFFFFFFu);
-  r.scale_log2 = scale * 1.44269504088896340736f;
+  r.scale_log2 = scale * LOG2_E;
   return r;
 }
 
@@ -222,7 +223,7 @@ ro_status attend(const char* fn, StepCall& c, const ro_cache* cache, const uint6
   a.err = c.err();
   if (bias) {
     a.biased = 1;
-    a.b.cap_log2 = bias->cap * 1.44269504088896340736f;
+    a.b.cap_log2 = bias->cap * LOG2_E;
     a.b.to_z = bias->cap != 0.f ? scale / bias->cap : 0.f;
     a.b.slope = bias->d_slope;
     a.b.first = bias->d_first;
