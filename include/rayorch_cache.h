@@ -48,7 +48,8 @@
  * to the output's type; attention rounds the softmax weights of a tile to the
  * cache's type for the matrix product with the values (f16 weights are held
  * higher by a power of two for it: none above 2^-36 of its row's largest is
- * lost).
+ * lost); products scale * q.k without a cap stay below 2^22 in size over f16
+ * caches, 2^28 over bf16 ones.
  * Tensors are [tokens][heads][head_dim] with an element stride of 1 in the
  * last dimension and token and head strides in elements.  Where not said
  * otherwise the cache operators want 16-byte aligned pointers and strides that
