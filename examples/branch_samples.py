@@ -7,8 +7,7 @@ that ended give their pages back, and the pool is closed up when it got sparse:
 
   ro_expand_noalloc       sequences -> pages, sequences -> tokens, prompts -> samples
   ro_cache_append         rotary by position, keys and values into the pages
-  ro_cache_attend_biased  prompts' tokens see their document alone, samples all
-                          that is theirs
+  ro_cache_attend_biased  attention over what a sequence holds, capped scores
   ro_cache_fork           prompts -> samples; later samples -> those that go on
   ro_sample               each sample's next token, with settings of its own
   ro_cache_compact        the pages in use move together
