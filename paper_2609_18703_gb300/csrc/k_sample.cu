@@ -101,13 +101,14 @@ using Sum = unsigned __int128;
 __device__ __forceinline__ float sum_float(Sum x) { return fmaf((float)(uint64_t)(x >> 64), 0x1p64f, (float)(uint64_t)x); }
 // x * f as a whole number, rounded down or up; 0 <= f < 1, x < 2^70.  (f is a
 // whole number of at most 24 bits over a power of two.)
-__device__ __forceinline__ Sum scaled(Sum x, float f, bool up) {
+template <class X>
+__device__ __forceinline__ X scaled(X x, float f, bool up) {
   if (f == 0.f || x == 0) return 0;
   int e;
   const uint64_t m = (uint64_t)(frexpf(f, &e) * 16777216.f);   // f = m 2^(e - 24)
   const int shift = 24 - e;                                      // at least 24
   if (shift >= 96) return up ? 1 : 0;
-  return (x * m + (up ? ((Sum)1 << shift) - 1 : 0)) >> shift;
+  return (X)(((Sum)x * m + (up ? ((Sum)1 << shift) - 1 : 0)) >> shift);
 }
 __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
 #pragma unroll
@@ -445,10 +446,9 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
 
   // ---- weights ----
   const ExpScale scale = exp_scale(T_);
-  // Of weights in 32 bits.  Below T = 5e-39 it is too small a factor: they are then
-  // bounds of the weights, and decide nothing.
-  const float rough_scale = fminf(1.44269504f / T_, 3.0e38f);
-  const bool rough_holds = rough_scale < 3.0e38f;
+  // Weights in 32 bits have one factor.  Below T = 5e-39 it is too small: they are
+  // then bounds of the weights, and decide nothing.
+  const bool rough_holds = per_unit < 3.0e38f;
   const float my_hi = EXP_HI[lane], my_lo = EXP_LO[lane];   // the table, an entry a lane
   // Every weight has the same bits behind the point, whatever the row's sum and
   // whoever takes it, so a draw does not depend on how the row is split.
@@ -493,7 +493,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
   };
   // in 32 bits, of a logit that is no NaN
   auto rough_weight = [&](float y) -> float {
-    const float z = (top - y) * rough_scale;
+    const float z = (top - y) * per_unit;
     return z < 64.f ? ex2(-z) : 0.f;
   };
   auto key_of = [&](float y) -> uint32_t { return y == y ? logit_key(y) : KEY_NONE; };   // (a NaN is never drawn)
@@ -545,11 +545,10 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
     for (uint32_t r = 0; r < nc; ++r) sum += __shfl_sync(0xffffffffu, part, r);
     return sum;
   };
-  auto with_log = [&](uint32_t token, float y, Sum total, uint32_t kept) {
+  auto with_log = [&](uint32_t token, float y, double total, uint32_t kept) {
     const Pair32 z = exp_argument(top, y, scale);
     const double less = ((double)z.hi + (double)z.lo) * 0.69314718055994530942;
-    const double sum = (double)(uint32_t)(total >> 64) * 0x1p64 + (double)(uint64_t)total;
-    finish(token, -(float)(less + log(sum * (1.0 / (double)(1ull << WEIGHT_BITS)))), kept);
+    finish(token, -(float)(less + log(total * (1.0 / (double)(1ull << WEIGHT_BITS)))), kept);
   };
 
   // ---- thresholds ----
@@ -750,7 +749,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
             __syncthreads();
             sum = s.list_sum;
           }
-          stay = min(stay, max(1u, count_below((uint64_t)scaled(sum, top_p, true), first)));
+          stay = min(stay, max(1u, count_below(scaled(sum, top_p, true), first)));
           way = WAY_DONE;
         } else if (!by_k && rough_holds) {
           const float rough = fminf(rough_total() * top_p * ONE, 0x1p62f);   // (more than the listed ones' sum)
@@ -807,7 +806,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         // the sum of those that stay, then where it passes the goal, by index
         if (2 * tid < stay && stay <= 2 * tid + 2) s.list_sum = ahead[(stay - 1) & 1] + own[(stay - 1) & 1];
         __syncthreads();
-        const uint64_t total = s.list_sum, goal = (uint64_t)scaled(total, s.u, false);
+        const uint64_t total = s.list_sum, goal = scaled(total, s.u, false);
         uint32_t size = 2;
         while (size < stay) size *= 2;
         // indices rise, and each remembers its candidate
@@ -834,7 +833,7 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         for (uint32_t j = 0; j < 2; ++j) {
           if (goal >= at && goal < at + w2[j]) {
             const unsigned long long o = order[2 * tid + j];
-            with_log((uint32_t)(o >> 32), key_logit((uint32_t)(list[(uint32_t)o] >> 32)), total, stay);
+            with_log((uint32_t)(o >> 32), key_logit((uint32_t)(list[(uint32_t)o] >> 32)), (double)total, stay);
           }
           at += w2[j];
         }
@@ -1285,7 +1284,8 @@ __device__ __forceinline__ uint32_t sample_row(const SampleArgs& a, SampleShared
         upto += wk;
         if (!done && goal < upto) {
           done = true;
-          with_log((b0 + i + lane) * E + k - off, y[k], total, (uint32_t)(t.count + ties));
+          with_log((b0 + i + lane) * E + k - off, y[k],
+                   (double)(uint32_t)(total >> 64) * 0x1p64 + (double)(uint64_t)total, (uint32_t)(t.count + ties));
         }
       }
       break;
