@@ -31,8 +31,9 @@
 // us for frames of 243 tokens behind a window of 4,096, 0.84 PFLOP/s).  A cap adds
 // a tanh to each product: a polynomial where a warp's products allow it (z = x /
 // cap within 0.33 or 1), else that and 1 - 2 / (1 + e^2z): the same chunks under a
-// cap of 30 take 575 to 590 us, 1.1 PFLOP/s, bound by the multiply-adds (seven
-// for two products) beside the exponentials.
+// cap of 30 take 580 to 590 us, 1.1 PFLOP/s.  No unit is full there (tensor cores 49
+// %, issue 54 %, FMA 26 %, XU 24 %): a thread loads its columns, finds their form,
+// then takes all their polynomials and only then their exponentials.
 #include <algorithm>
 
 #include "ro_tcgen05.cuh"
@@ -931,10 +932,11 @@ static void launch_tiles(const LaunchCfg& L, const AttendTileArgs& g, int sms) {
   // Scores under a cap of at most 73 in log2 (50.6) need no running maximum where
   // the weights have the exponents of 32 bits: with 2^-cap (or 2^-56) for all rows
   // they lie between 2^-17 and 2^129.  Then two threads take a row (chunks under a cap
-  // of 2, 8, 30 or 50: 1,120, 677, 579 and 579 us against 1,540, 952, 634 and 634); with a
-  // maximum to agree on they lose more.  Pairs of row tiles whose sums such weights
-  // take out of range, by scores beyond 40 or values beyond 2^30 or so, are computed
-  // twice.
+  // of 2, 8, 30 or 50: 1,159, 681, 581 and 580 us against 1,568, 959, 650 and 650 of one
+  // thread a row; of 52, past the limit, 651); with a maximum to agree on they lose
+  // more.  Pairs of row tiles whose sums such weights take out of range, by scores
+  // beyond 40 or values beyond 2^30 or so, are computed twice (values of 2^100: 1,155
+  // us for 590).
   auto kernel = g.a.biased ? attend_tiles_kernel<T, DP, true, 1> : attend_tiles_kernel<T, DP, false, 1>;
   int threads = AT_THREADS<1>;
   if constexpr (std::is_same_v<T, __nv_bfloat16>)

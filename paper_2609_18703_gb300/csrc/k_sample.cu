@@ -24,7 +24,7 @@
 // what it needs of it again from L2; the wide ones among them are left to a
 // second kernel of clusters.
 //
-// Measured: one row of 32,000 32-bit logits, top-k and top-p: 14.2 us; 256 rows of
+// Measured: one row of 32,000 32-bit logits, top-k and top-p: 14.9 us; 256 rows of
 // 131,072 bf16 logits: 16 us to draw the largest (the logits' bytes: 10), 30 with
 // top-k 50 and top-p; 90 us with settings of their own, among them some 17 wide
 // rows, whose exact sums take 100 instructions a token (24 us for 12 rows of them
